@@ -263,6 +263,56 @@ rtl_status rtl_sparse_lora_linear_fp8(const void* X, const void* Wq, const float
                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point (MXFP4): every 32 values along the contraction share a power of two,
+ * and each value is an E2M1 code (sign, 0 .5 1 1.5 2 3 4 6).
+ *   codes    two to a byte, the even index in the low half: row r of an [rows, cols] matrix is cols / 2
+ *            bytes at r * ldq. Row strides of codes count BYTES. cols % 32 == 0.
+ *   scales   the biased exponent (E8M0: 2^(byte - 127), 0xFF = NaN) of block b = col / 32 of row r is byte
+ *            [b / 8][r][b % 8] of an array [ceil(cols / 256)][rows][8]: records of eight per row, the rows
+ *            of 256 columns one run. Bytes of blocks behind cols are written as 0 and read as if they were.
+ *
+ * rtl_quantize_mxfp4 - bf16 [rows, cols] to codes and scales: exponent floor(log2 max|x|) - 2 over the
+ *   block, at least -127; code = the value nearest to x / 2^exponent, ties to the even code, at most 6 in
+ *   magnitude. A block of zeros has scale byte 0. A block with a NaN or an infinity has scale byte 0xFF
+ *   and codes 0: all of it reads as NaN.
+ *   X        bf16 (ld), 16-byte aligned, ld % 8 == 0.
+ *   Q, S     nullable together: blocks along the rows of X. Q [rows, cols / 2] bytes (ldq), S as above;
+ *            cols % 32 == 0.
+ *   Qt, St   nullable together: blocks down the columns, the result transposed: codes and scales of the
+ *            [cols, R] matrix X^T, R = rows rounded up to a multiple of 32, zeros behind rows. Qt [cols, R / 2] bytes
+ *            (ldqt); cols % 8 == 0. One read of X serves both: an X that is contracted along both of its axes
+ *            (a training step's gradient, weight or activation) then is the left or right operand of
+ *            rtl_mxfp4_packed_linear in either.
+ *   Q, Qt 16-byte aligned, ldq, ldqt % 16 == 0; S, St 8-byte aligned.
+ *
+ * rtl_dequantize_mxfp4 - the values of codes and scales as bf16 (exact up to the range of bf16).
+ *   Q, ldq, S as above, cols % 32 == 0; X [rows, cols] bf16 (ld), 16-byte aligned, ld % 8 == 0.
+ *
+ * rtl_mxfp4_packed_linear - Y = Xq Wq^T (+ b) on codes, on the microscaled matrix instruction, fp32
+ *   accumulation, bf16 output.
+ *   Xq [M, K / 2] bytes (ldx), Xs its scales; Wq [N, K / 2] bytes (ldw), Ws its scales; K % 32 == 0; codes 16-byte
+ *   aligned with strides % 16 == 0, scales 8-byte aligned; bias NULL or bf16 [N]; Y [M, N] bf16 (ldy).
+ *   workspace  rtl_mxfp4_packed_linear_workspace(M, N, K) bytes (may be 0), all of it optional, as for rtl_dense_linear.
+ * rtl_mxfp4_linear - the same from a bf16 activation, quantised in the call as rtl_quantize_mxfp4 does.
+ *   X [M, K] bf16 (ldx), 16-byte aligned, ldx % 8 == 0, K % 32 == 0.
+ *   workspace  rtl_mxfp4_linear_workspace(M, N, K) bytes, 256-byte aligned. Same bits as the two calls it stands for,
+ *   on workspaces of the queried sizes.
+ * ------------------------------------------------------------------------------------------- */
+rtl_status rtl_quantize_mxfp4(const void* X, int64_t rows, int64_t cols, int64_t ld,
+                              void* Q, int64_t ldq, void* S, void* Qt, int64_t ldqt, void* St, void* stream);
+rtl_status rtl_dequantize_mxfp4(const void* Q, int64_t ldq, const void* S, int64_t rows, int64_t cols,
+                                void* X, int64_t ld, void* stream);
+size_t rtl_mxfp4_packed_linear_workspace(int64_t M, int64_t N, int64_t K);
+rtl_status rtl_mxfp4_packed_linear(const void* Xq, const void* Xs, const void* Wq, const void* Ws,
+                                   const void* bias, void* Y, int64_t M, int64_t N, int64_t K,
+                                   int64_t ldx, int64_t ldw, int64_t ldy,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+size_t rtl_mxfp4_linear_workspace(int64_t M, int64_t N, int64_t K);
+rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const void* bias, void* Y,
+                            int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw, int64_t ldy,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * rtl_diag_matrix_rate - diagnostic, not a step of the method: measures the issue rate of the matrix
  * instruction the linears are built on with nothing else running (operands in registers), so that a
  * benchmark can quote the tile loops against a ceiling measured on the device at hand.

@@ -22,6 +22,8 @@ SYMBOLS = ["rtl_sparsify_pack_workspace", "rtl_sparsify_pack", "rtl_packed_linea
            "rtl_quantize_fp8", "rtl_sparsify_pack_fp8_workspace", "rtl_sparsify_pack_fp8",
            "rtl_sparse_linear_fp8_workspace", "rtl_sparse_linear_fp8",
            "rtl_sparse_lora_linear_fp8_workspace", "rtl_sparse_lora_linear_fp8",
+           "rtl_quantize_mxfp4", "rtl_dequantize_mxfp4", "rtl_mxfp4_packed_linear_workspace", "rtl_mxfp4_packed_linear",
+           "rtl_mxfp4_linear_workspace", "rtl_mxfp4_linear",
            "rtl_diag_matrix_rate", "rtl_diag_fill_rate", "rtl_diag_pack_sweep", "rtl_diag_tile_plan", "rtl_init", "rtl_status_str", "rtl_version"]
 
 _lib = None
@@ -84,6 +86,18 @@ def lib():
         L.rtl_sparse_lora_linear_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i64, i64,
                                                  i64, ci, fl, vp, sz, vp]
         L.rtl_sparse_lora_linear_fp8.restype = ci
+        L.rtl_quantize_mxfp4.argtypes = [vp, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp]
+        L.rtl_quantize_mxfp4.restype = ci
+        L.rtl_dequantize_mxfp4.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp]
+        L.rtl_dequantize_mxfp4.restype = ci
+        L.rtl_mxfp4_packed_linear_workspace.argtypes = [i64, i64, i64]
+        L.rtl_mxfp4_packed_linear_workspace.restype = sz
+        L.rtl_mxfp4_packed_linear.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, sz, vp]
+        L.rtl_mxfp4_packed_linear.restype = ci
+        L.rtl_mxfp4_linear_workspace.argtypes = [i64, i64, i64]
+        L.rtl_mxfp4_linear_workspace.restype = sz
+        L.rtl_mxfp4_linear.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, sz, vp]
+        L.rtl_mxfp4_linear.restype = ci
         L.rtl_diag_pack_sweep.argtypes = [vp, i64, i64, i64, ci, fl, vp, sz, vp]
         L.rtl_diag_pack_sweep.restype = ci
         L.rtl_diag_tile_plan.argtypes = [i64, i64, ci, C.POINTER(C.c_int64)]
@@ -323,6 +337,146 @@ def sparse_lora_linear_fp8(X, Wq, x_scale, LA, LB, bias=None, comp=COMP_GROUP, e
                                       X.stride(0), Wq.stride(0), LA.stride(0), LB.stride(0), Y.stride(0), comp, eps,
                                       _p(ws), ws.numel(), _stream())
     _check(st, "rtl_sparse_lora_linear_fp8")
+    return Y
+
+
+# ---- microscaled 4-bit floating point (MXFP4): uint8 tensors, two codes to a byte -----------------
+
+def _on_current(*ts):
+    """Device tensors of the current device only: the launch goes to its current stream."""
+    _need_cuda(*ts)
+    cur = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.device.index != cur:
+            raise ValueError("tensor on %s, current device is cuda:%d" % (t.device, cur))
+
+
+def _matrix(t, dtype, name, dim=2):
+    if t.dtype != dtype or t.dim() != dim or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError("%s: %s tensor of %d dimensions with contiguous rows expected" % (name, dtype, dim))
+
+
+def _vector(t, n, name, dtype=torch.bfloat16):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+        raise ValueError("%s: contiguous %s tensor of %d expected" % (name, dtype, n))
+
+
+def _ld(t):
+    """Row stride; torch leaves any value there for a single row."""
+    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _given(out, shape, dtype, like, name="out"):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _matrix(out, dtype, name, len(shape))
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError("%s: shape %s expected" % (name, tuple(shape)))
+    return out
+
+
+def mxfp4_scales_shape(rows, cols):
+    """Shape of the scale bytes of a [rows, cols] matrix: byte of block b = col // 32 of row r at [b // 8, r, b % 8]."""
+    return ((cols + 255) // 256, rows, 8)
+
+
+def _scales(S, rows, cols, name):
+    if S.dtype != torch.uint8 or tuple(S.shape) != mxfp4_scales_shape(rows, cols) or not S.is_contiguous():
+        raise ValueError("%s: contiguous uint8 tensor of shape %s expected" % (name, mxfp4_scales_shape(rows, cols)))
+
+
+def quantize_mxfp4(X, along="cols", out=None):
+    """rtl_quantize_mxfp4: bf16 [rows, cols] -> codes and scales, blocks of 32 along its rows ("cols": (Q [rows, cols/2], S)),
+    down its columns ("rows": (Qt [cols, R/2], St) of X^T, R = rows rounded up to a multiple of 32) or both in one pass
+    ((Q, S, Qt, St)). uint8 tensors; S has mxfp4_scales_shape."""
+    if along not in ("cols", "rows", "both"):
+        raise ValueError("along: 'cols', 'rows' or 'both'")
+    _on_current(X)
+    _matrix(X, torch.bfloat16, "X")
+    rows, cols = X.shape
+    pad = (rows + 31) // 32 * 32
+    shapes = []
+    if along != "rows":
+        shapes += [(rows, cols // 2), mxfp4_scales_shape(rows, cols)]
+    if along != "cols":
+        shapes += [(cols, pad // 2), mxfp4_scales_shape(cols, pad)]
+    if out is None:
+        out = tuple(torch.empty(s, dtype=torch.uint8, device=X.device) for s in shapes)
+    else:
+        _on_current(*out)
+        if len(out) != len(shapes):
+            raise ValueError("out: %d tensors expected" % len(shapes))
+        for i in range(0, len(out), 2):
+            _given(out[i], shapes[i], torch.uint8, X)
+            if tuple(out[i + 1].shape) != shapes[i + 1] or out[i + 1].dtype != torch.uint8 or not out[i + 1].is_contiguous():
+                raise ValueError("out: contiguous uint8 scales of shape %s expected" % (shapes[i + 1],))
+    a = [None, 0, None]
+    b = [None, 0, None]
+    if along != "rows":
+        a = [_p(out[0]), _ld(out[0]), _p(out[1])]
+    if along != "cols":
+        b = [_p(out[-2]), _ld(out[-2]), _p(out[-1])]
+    _check(lib().rtl_quantize_mxfp4(_p(X), rows, cols, _ld(X), *a, *b, _stream()), "rtl_quantize_mxfp4")
+    return out
+
+
+def dequantize_mxfp4(Q, S, out=None):
+    """rtl_dequantize_mxfp4: codes [rows, cols/2] and scales -> bf16 [rows, cols]."""
+    _on_current(Q, S, out)
+    _matrix(Q, torch.uint8, "Q")
+    rows, cols = Q.shape[0], Q.shape[1] * 2
+    _scales(S, rows, cols, "S")
+    X = _given(out, (rows, cols), torch.bfloat16, Q)
+    _check(lib().rtl_dequantize_mxfp4(_p(Q), _ld(Q), _p(S), rows, cols, _p(X), _ld(X), _stream()), "rtl_dequantize_mxfp4")
+    return X
+
+
+def mxfp4_packed_linear_workspace(M, N, K):
+    return int(lib().rtl_mxfp4_packed_linear_workspace(M, N, K))
+
+
+def mxfp4_packed_linear(Xq, Xs, Wq, Ws, bias=None, out=None, ws=None):
+    """rtl_mxfp4_packed_linear: Y = Xq Wq^T (+ bias) on codes and scales of quantize_mxfp4, bf16 [M,N]."""
+    _on_current(Xq, Xs, Wq, Ws, bias, out, ws)
+    _matrix(Xq, torch.uint8, "Xq")
+    _matrix(Wq, torch.uint8, "Wq")
+    M, N, K = Xq.shape[0], Wq.shape[0], Wq.shape[1] * 2
+    if Xq.shape[1] * 2 != K:
+        raise ValueError("Xq and Wq differ in K")
+    _scales(Xs, M, K, "Xs")
+    _scales(Ws, N, K, "Ws")
+    _vector(bias, N, "bias")
+    Y = _given(out, (M, N), torch.bfloat16, Wq)
+    L = lib()
+    if ws is None:
+        ws = _ws(L.rtl_mxfp4_packed_linear_workspace(M, N, K), Wq.device)
+    st = L.rtl_mxfp4_packed_linear(_p(Xq), _p(Xs), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, _ld(Xq), _ld(Wq), _ld(Y),
+                                   _p(ws), ws.numel(), _stream())
+    _check(st, "rtl_mxfp4_packed_linear")
+    return Y
+
+
+def mxfp4_linear_workspace(M, N, K):
+    return int(lib().rtl_mxfp4_linear_workspace(M, N, K))
+
+
+def mxfp4_linear(X, Wq, Ws, bias=None, out=None, ws=None):
+    """rtl_mxfp4_linear: Y = mxfp4(X) Wq^T (+ bias), X bf16 [M,K] quantised in the call, bf16 [M,N]."""
+    _on_current(X, Wq, Ws, bias, out, ws)
+    _matrix(X, torch.bfloat16, "X")
+    _matrix(Wq, torch.uint8, "Wq")
+    M, K = X.shape
+    N = Wq.shape[0]
+    if Wq.shape[1] * 2 != K:
+        raise ValueError("X and Wq differ in K")
+    _scales(Ws, N, K, "Ws")
+    _vector(bias, N, "bias")
+    Y = _given(out, (M, N), torch.bfloat16, X)
+    L = lib()
+    if ws is None:
+        ws = _ws(L.rtl_mxfp4_linear_workspace(M, N, K), X.device)
+    st = L.rtl_mxfp4_linear(_p(X), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, _ld(X), _ld(Wq), _ld(Y), _p(ws), ws.numel(), _stream())
+    _check(st, "rtl_mxfp4_linear")
     return Y
 
 

@@ -39,7 +39,7 @@ rtl_status device_ready(void** scratch_out = nullptr) {
                 d.state = -1;
             } else {
                 if (rtl::prepare_pack_kernels() != hipSuccess || rtl::prepare_gemm_kernels() != hipSuccess ||
-                    rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
+                    rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_mx_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
                     return RTL_ERR_HIP;
                 void* ptr = nullptr;
                 if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return RTL_ERR_HIP;
@@ -551,6 +551,113 @@ rtl_status rtl_dense_linear(const void* X, const void* W, const void* bias, void
     g.M = M; g.N = N; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldy;
     hipError_t e = rtl::launch_gemm(false, g, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// ---- microscaled 4-bit floating point ---------------------------------------------------------
+static bool too_large(int64_t v) { return v < 0 || v > ((int64_t)1 << 30); }
+// Bytes of the scales of a [rows, cols] matrix.
+static size_t mx_scale_bytes(int64_t rows, int64_t cols) { return (size_t)((cols + 255) / 256) * (size_t)rows * 8; }
+
+rtl_status rtl_quantize_mxfp4(const void* X, int64_t rows, int64_t cols, int64_t ld, void* Q, int64_t ldq, void* S, void* Qt, int64_t ldqt,
+                              void* St, void* stream) {
+    const bool along = Q || S, down = Qt || St;
+    if (too_large(rows) || too_large(cols) || ld < cols || cols % (along ? 32 : 8) != 0) return RTL_ERR_SHAPE;
+    if (along && ldq < cols / 2) return RTL_ERR_SHAPE;
+    if (down && ldqt < (rows + 31) / 32 * 16) return RTL_ERR_SHAPE;
+    if (((rows + 31) / 32) * ((cols + 127) / 128) >= ((int64_t)1 << 31)) return RTL_ERR_SHAPE;      // workgroups
+    if (rows == 0 || cols == 0) return RTL_OK;
+    if (!X || (!along && !down) || (along && (!Q || !S)) || (down && (!Qt || !St))) return RTL_ERR_NULL;
+    if (ld % 8 != 0 || !aligned(X, 16)) return RTL_ERR_ALIGN;
+    if (along && (ldq % 16 != 0 || !aligned(Q, 16) || !aligned(S, 8))) return RTL_ERR_ALIGN;
+    if (down && (ldqt % 16 != 0 || !aligned(Qt, 16) || !aligned(St, 8))) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    const hipError_t e = rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), rows, cols, ld, static_cast<uint8_t*>(Q), ldq,
+                                                    static_cast<uint8_t*>(S), static_cast<uint8_t*>(Qt), ldqt, static_cast<uint8_t*>(St),
+                                                    static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+rtl_status rtl_dequantize_mxfp4(const void* Q, int64_t ldq, const void* S, int64_t rows, int64_t cols, void* X, int64_t ld, void* stream) {
+    if (too_large(rows) || too_large(cols) || cols % 32 != 0 || ldq < cols / 2 || ld < cols) return RTL_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return RTL_OK;
+    if (!Q || !S || !X) return RTL_ERR_NULL;
+    if (ldq % 16 != 0 || ld % 8 != 0 || !aligned(Q, 16) || !aligned(S, 8) || !aligned(X, 16)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    const hipError_t e = rtl::launch_dequantize_mxfp4(static_cast<const uint8_t*>(Q), ldq, static_cast<const uint8_t*>(S), rows, cols,
+                                                      static_cast<uint16_t*>(X), ld, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// Sizes and pointers of a product with a 4-bit weight; a_extent, a_granule: row extent and stride granule of the left operand.
+static rtl_status check_mx(const void* A, const void* Wq, const void* Ws, const void* bias, const void* Y, int64_t M, int64_t N, int64_t K,
+                           int64_t lda, int64_t ldw, int64_t ldy, int64_t a_extent, int64_t a_granule) {
+    if (too_large(M) || too_large(N) || K <= 0 || too_large(K) || K % 32 != 0 || lda < a_extent || ldw < K / 2 || ldy < N)
+        return RTL_ERR_SHAPE;
+    if (lda > ((int64_t)1 << 22) || ldw > ((int64_t)1 << 22)) return RTL_ERR_SHAPE;      // 32-bit offsets inside a tile
+    if (((M + 255) / 256) * ((N + 127) / 128) >= ((int64_t)1 << 31)) return RTL_ERR_SHAPE;
+    if (M == 0 || N == 0) return RTL_OK;
+    if (!A || !Wq || !Ws || !Y) return RTL_ERR_NULL;
+    if (lda % a_granule != 0 || ldw % 16 != 0 || !aligned(A, 16) || !aligned(Wq, 16) || !aligned(Ws, 8) || !aligned(Y, 2) ||
+        (bias && !aligned(bias, 2)))
+        return RTL_ERR_ALIGN;
+    return RTL_OK;
+}
+
+static rtl_status mx_product(const uint8_t* Xq, const uint8_t* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
+                             int64_t K, int64_t ldx, int64_t ldw, int64_t ldy, uint8_t* workspace, size_t used, size_t bytes, hipStream_t s) {
+    rtl::GemmArgs g{};
+    give_partials(g, workspace, used, bytes, (size_t)RTL_STATIC_SCRATCH_BYTES);
+    g.fp4 = true;
+    g.A = Xq;
+    g.a_scale = Xs;
+    g.a_scale_rows = M;
+    g.W = Wq;
+    g.w_scale = static_cast<const uint8_t*>(Ws);
+    g.w_scale_rows = N;
+    g.bias = static_cast<const uint16_t*>(bias);
+    g.Y = static_cast<uint16_t*>(Y);
+    g.M = M; g.N = N; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldy;
+    return rtl::launch_gemm(false, g, s) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+size_t rtl_mxfp4_packed_linear_workspace(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0) return 0;
+    return rtl::gemm_partial_bytes(false, false, M, N, K, (size_t)RTL_STATIC_SCRATCH_BYTES, true);
+}
+
+rtl_status rtl_mxfp4_packed_linear(const void* Xq, const void* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
+                                   int64_t K, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    const rtl_status st = check_mx(Xq, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K / 2, 16);
+    if (st != RTL_OK || M == 0 || N == 0) return st;
+    if (!Xs) return RTL_ERR_NULL;
+    if (!aligned(Xs, 8)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    return mx_product(static_cast<const uint8_t*>(Xq), static_cast<const uint8_t*>(Xs), Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy,
+                      static_cast<uint8_t*>(workspace), 0, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+// rtl_mxfp4_linear workspace: [codes of X, dense rows | their scales | partial planes]
+static size_t mx_codes_bytes(int64_t M, int64_t K) { return round_up((size_t)M * (size_t)(K / 2), 256); }
+static size_t mx_ws(int64_t M, int64_t K) { return mx_codes_bytes(M, K) + round_up(mx_scale_bytes(M, K), 256); }
+size_t rtl_mxfp4_linear_workspace(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0) return 0;
+    return mx_ws(M, K) + rtl_mxfp4_packed_linear_workspace(M, N, K);
+}
+
+rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N, int64_t K, int64_t ldx,
+                            int64_t ldw, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    const rtl_status st = check_mx(X, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K, 8);
+    if (st != RTL_OK || M == 0 || N == 0) return st;
+    const size_t need = mx_ws(M, K);
+    if (!workspace || workspace_bytes < need) return RTL_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    uint8_t* scales = base + mx_codes_bytes(M, K);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), M, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
+        return RTL_ERR_HIP;
+    return mx_product(base, scales, Wq, Ws, bias, Y, M, N, K, K / 2, ldw, ldy, base, need, workspace_bytes, s);
 }
 
 }  // extern "C"

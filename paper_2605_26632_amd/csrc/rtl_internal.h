@@ -87,12 +87,19 @@ struct GemmArgs {
     size_t partial_bytes;
     int64_t part_pitch;     // filled in by launch_gemm
     int k_splits;
+    // fp4 (dense only): A and W hold two E2M1 codes to a byte, lda and ldw count bytes, K is a multiple of 32 and the scale bytes
+    // are records of 8 per row and 256-k block, the rows of a block contiguous: record of row r in block b at (b * rows + r) * 8
+    bool fp4;
+    const uint8_t* a_scale; // rows: a_scale_rows
+    const uint8_t* w_scale;
+    int64_t a_scale_rows, w_scale_rows;
 };
 // Bytes of partial planes launch_gemm would use of `room` bytes.
-size_t gemm_partial_bytes(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t room);
+size_t gemm_partial_bytes(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t room, bool fp4 = false);
 // The form launch_gemm picks with `room` bytes of planes (host arithmetic, for the tests): out = {index of the small tile
 // shape or -1, parts of the contraction (1: not split over workgroups), rows of the part tile}.
 void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t room, int out[3]);
+void mx_choice(int64_t M, int64_t N, int64_t K, size_t room, int out[3]);       // the same for 4-bit operands
 // One-time set-up per device (rtl_init, or the first entry-point call): raises the dynamic-LDS limit
 // of every tile-loop kernel and makes the runtime load both code objects, so that later launches
 // are plain kernel nodes (HIP-graph capture needs no warm-up call).
@@ -128,6 +135,14 @@ hipError_t launch_sparsify_down(const uint16_t* X, int64_t M, int64_t K, int64_t
 // (nullable) receives scale[0] * mul[0].
 hipError_t launch_tensor_scale(const float* rowsums, int64_t M, float eps, float* scale, hipStream_t stream,
                                const float* mul = nullptr, float* fused = nullptr);
+
+// ---- microscaled 4-bit codes (mx.hip) ---------------------------------------------------------
+// Codes and scale records as in the header. (Q, S) and (Qt, St) are each optional, not both absent.
+hipError_t prepare_mx_kernels();
+hipError_t launch_quantize_mxfp4(const uint16_t* X, int64_t rows, int64_t cols, int64_t ld, uint8_t* Q, int64_t ldq, uint8_t* S, uint8_t* Qt,
+                                 int64_t ldqt, uint8_t* St, hipStream_t stream);
+hipError_t launch_dequantize_mxfp4(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64_t rows, int64_t cols, uint16_t* X, int64_t ld,
+                                   hipStream_t stream);
 
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------
 // Issue-rate probe: `blocks` workgroups of four waves, each wave issuing 4 * iters matrix

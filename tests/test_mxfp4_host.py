@@ -1,0 +1,70 @@
+"""Refusals of the microscaled 4-bit entry points, all before any launch."""
+import pytest
+import torch
+
+from paper_2605_26632_amd import binding as rtl
+
+FAKE = 0x10000      # non-null, aligned, never dereferenced
+NULL, SHAPE, ALIGN, WORKSPACE = 1, 2, 3, 4
+
+
+def call(f, defaults, **kw):
+    assert set(kw) <= set(defaults)
+    return f(*dict(defaults, **kw).values())
+
+
+def test_quantize_refusals():
+    d = dict(X=FAKE, rows=4, cols=64, ld=64, Q=FAKE, ldq=32, S=FAKE, Qt=FAKE, ldqt=16, St=FAKE, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_quantize_mxfp4, d, **kw)
+    assert f(cols=40, ld=64) == SHAPE and f(cols=44, ld=64, Q=None, S=None) == SHAPE and f(ld=56) == SHAPE
+    assert f(rows=-1) == SHAPE and f(cols=-32) == SHAPE and f(rows=(1 << 30) + 1, ldqt=1 << 40) == SHAPE
+    assert f(ldq=16) == SHAPE and f(rows=33, ldqt=16) == SHAPE
+    assert f(X=None) == NULL and f(Q=None) == NULL and f(S=None) == NULL and f(Qt=None) == NULL and f(St=None) == NULL
+    assert f(Q=None, S=None, Qt=None, St=None) == NULL
+    assert f(X=FAKE + 8) == ALIGN and f(ld=68) == ALIGN and f(Q=FAKE + 8) == ALIGN and f(ldq=40) == ALIGN and f(S=FAKE + 4) == ALIGN
+    assert f(Qt=FAKE + 8) == ALIGN and f(ldqt=24) == ALIGN and f(St=FAKE + 4) == ALIGN
+    assert f(rows=0) == 0 and f(cols=0) == 0
+
+
+def test_dequantize_refusals():
+    d = dict(Q=FAKE, ldq=32, S=FAKE, rows=4, cols=64, X=FAKE, ld=64, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_dequantize_mxfp4, d, **kw)
+    assert f(cols=48) == SHAPE and f(ldq=16) == SHAPE and f(ld=56) == SHAPE and f(rows=-1) == SHAPE
+    assert f(Q=None) == NULL and f(S=None) == NULL and f(X=None) == NULL
+    assert f(Q=FAKE + 8) == ALIGN and f(S=FAKE + 4) == ALIGN and f(X=FAKE + 8) == ALIGN and f(ldq=40) == ALIGN and f(ld=68) == ALIGN
+    assert f(rows=0) == 0 and f(cols=0) == 0
+
+
+def test_packed_linear_refusals():
+    d = dict(Xq=FAKE, Xs=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, M=4, N=8, K=64, ldx=32, ldw=32, ldy=8, ws=None, wsb=0, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_mxfp4_packed_linear, d, **kw)
+    assert f(K=48) == SHAPE and f(K=0) == SHAPE and f(ldx=16) == SHAPE and f(ldw=16) == SHAPE and f(ldy=7) == SHAPE and f(M=-1) == SHAPE
+    assert f(ldx=(1 << 22) + 16) == SHAPE and f(M=(1 << 30) + 1) == SHAPE and f(M=1 << 30, N=1 << 30, ldy=1 << 30) == SHAPE
+    for p in ("Xq", "Xs", "Wq", "Ws", "Y"):
+        assert f(**{p: None}) == NULL
+    assert f(Xq=FAKE + 8) == ALIGN and f(Xs=FAKE + 4) == ALIGN and f(Wq=FAKE + 8) == ALIGN and f(Ws=FAKE + 4) == ALIGN
+    assert f(Y=FAKE + 1) == ALIGN and f(bias=FAKE + 1) == ALIGN and f(ldx=40) == ALIGN and f(ldw=40) == ALIGN
+    assert f(M=0) == 0 and f(N=0) == 0
+    assert rtl.mxfp4_packed_linear_workspace(0, 8, 64) == 0
+
+
+def test_linear_refusals():
+    d = dict(X=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, M=4, N=8, K=64, ldx=64, ldw=32, ldy=8, ws=FAKE, wsb=1 << 20, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_mxfp4_linear, d, **kw)
+    assert f(K=48) == SHAPE and f(ldx=56) == SHAPE and f(ldw=16) == SHAPE and f(ldy=7) == SHAPE and f(ldx=(1 << 22) + 8) == SHAPE
+    for p in ("X", "Wq", "Ws", "Y"):
+        assert f(**{p: None}) == NULL
+    assert f(X=FAKE + 8) == ALIGN and f(ldx=68) == ALIGN and f(ws=FAKE + 128) == ALIGN
+    need = rtl.mxfp4_linear_workspace(4, 8, 64)
+    assert need > 0 and f(wsb=255) == WORKSPACE and f(ws=None) == WORKSPACE
+    assert f(M=0) == 0 and f(N=0) == 0
+
+
+def test_binding_refuses_host_tensors_and_wrong_arguments():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        rtl.quantize_mxfp4(x)
+    with pytest.raises(ValueError):
+        rtl.quantize_mxfp4(x, along="depth")
+    with pytest.raises(ValueError):
+        rtl.mxfp4_linear(x, x, x)
