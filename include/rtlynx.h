@@ -313,6 +313,51 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
                             void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Linears grouped by expert: the rows of one activation divided over E weights,
+ *     Y[o_e .. o_{e+1}) = X[o_e .. o_{e+1}) W_e^T (+ b_e),   e = 0 .. E - 1,
+ * their gradients, and the same with 4-bit weights.
+ *
+ *   offsets  device int32 [E + 1], ascending: rows o_e up to o_{e+1} belong to expert e; experts may have no rows.
+ *            Rows in front of o_0 and from o_E on belong to nobody: they are neither used nor written. (Offsets are read by the
+ *            kernels alone. Whatever they hold, nothing outside of the tensors is touched: they are cut to [0, T], and an
+ *            expert that would end before it begins has no rows. What overlapping experts write is unspecified.)
+ *   T        rows of the activation, E experts, 0 <= E <= 65536. T == 0, E == 0, N == 0 or K == 0 as for the other linears; a weight
+ *            gradient is written for T == 0 too (zeros).
+ *   X [T, K] bf16 (ldx), W [E, N, K] bf16 (ldw between rows, stride_w between experts, both in elements, stride_w % 8 == 0; stride_w of
+ *            0: one weight for all), bias NULL or bf16 [E, N], Y [T, N] bf16 (ldy).
+ *
+ * rtl_grouped_linear       K % 64 == 0; alignment as for rtl_dense_linear. T, E, N must leave fewer than 2^24 workgroups (RTL_ERR_SHAPE).
+ * rtl_grouped_linear_dgrad dX[o_e .. o_{e+1}) = dY[o_e .. o_{e+1}) W_e, bf16 [T, K] (lddx). N % 8 == 0, K % 8 == 0; dY [T, N] (lddy), W and
+ *            dX 16-byte aligned with strides % 8 == 0.
+ * rtl_grouped_linear_wgrad dW_e = dY_e^T X_e and, with dbias, db_e = the sum of the rows of dY_e, both of type dw_type
+ *            (RTL_BF16 or RTL_F32): dW [E, N, K] (lddw, stride_dw >= (N - 1) lddw + K), dbias NULL or [E, N]. Every element is written, zeros for an expert
+ *            without rows. Sizes and alignment as for dgrad. fp32 sums in a fixed order; a row of dY or X enters its own expert's
+ *            gradient only, whatever it holds.
+ *   workspace  rtl_grouped_linear_wgrad_workspace(T, E, N, K) bytes (may be 0), all of it optional, 256-byte aligned.
+ * rtl_grouped_mxfp4_linear the forward product with the weights as MXFP4 codes and X quantised in the call: Wq [E, N, K / 2] bytes (ldw, stride_w
+ *            in bytes, % 16 == 0), Ws the scales of the [E * N, K] matrix of all experts' rows (what rtl_quantize_mxfp4 makes of it in one call).
+ *            K % 32 == 0; X as for rtl_mxfp4_linear.
+ *   workspace  rtl_grouped_mxfp4_linear_workspace(T, E, N, K) bytes, 256-byte aligned.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { RTL_BF16 = 0, RTL_F32 = 1 } rtl_dtype;
+rtl_status rtl_grouped_linear(const void* X, const int32_t* offsets, const void* W, const void* bias, void* Y,
+                              int64_t T, int64_t E, int64_t N, int64_t K,
+                              int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, void* stream);
+rtl_status rtl_grouped_linear_dgrad(const void* dY, const int32_t* offsets, const void* W, void* dX,
+                                    int64_t T, int64_t E, int64_t N, int64_t K,
+                                    int64_t lddy, int64_t ldw, int64_t stride_w, int64_t lddx, void* stream);
+size_t rtl_grouped_linear_wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K);
+rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t* offsets, void* dW, void* dbias, rtl_dtype dw_type,
+                                    int64_t T, int64_t E, int64_t N, int64_t K,
+                                    int64_t lddy, int64_t ldx, int64_t lddw, int64_t stride_dw,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+size_t rtl_grouped_mxfp4_linear_workspace(int64_t T, int64_t E, int64_t N, int64_t K);
+rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const void* Wq, const void* Ws, const void* bias, void* Y,
+                                    int64_t T, int64_t E, int64_t N, int64_t K,
+                                    int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * rtl_diag_matrix_rate - diagnostic, not a step of the method: measures the issue rate of the matrix
  * instruction the linears are built on with nothing else running (operands in registers), so that a
  * benchmark can quote the tile loops against a ceiling measured on the device at hand.

@@ -24,6 +24,8 @@ SYMBOLS = ["rtl_sparsify_pack_workspace", "rtl_sparsify_pack", "rtl_packed_linea
            "rtl_sparse_lora_linear_fp8_workspace", "rtl_sparse_lora_linear_fp8",
            "rtl_quantize_mxfp4", "rtl_dequantize_mxfp4", "rtl_mxfp4_packed_linear_workspace", "rtl_mxfp4_packed_linear",
            "rtl_mxfp4_linear_workspace", "rtl_mxfp4_linear",
+           "rtl_grouped_linear", "rtl_grouped_linear_dgrad", "rtl_grouped_linear_wgrad_workspace", "rtl_grouped_linear_wgrad",
+           "rtl_grouped_mxfp4_linear_workspace", "rtl_grouped_mxfp4_linear",
            "rtl_diag_matrix_rate", "rtl_diag_fill_rate", "rtl_diag_pack_sweep", "rtl_diag_tile_plan", "rtl_init", "rtl_status_str", "rtl_version"]
 
 _lib = None
@@ -98,6 +100,18 @@ def lib():
         L.rtl_mxfp4_linear_workspace.restype = sz
         L.rtl_mxfp4_linear.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, sz, vp]
         L.rtl_mxfp4_linear.restype = ci
+        L.rtl_grouped_linear.argtypes = [vp, vp, vp, vp, vp] + [i64] * 8 + [vp]
+        L.rtl_grouped_linear.restype = ci
+        L.rtl_grouped_linear_dgrad.argtypes = [vp, vp, vp, vp] + [i64] * 8 + [vp]
+        L.rtl_grouped_linear_dgrad.restype = ci
+        L.rtl_grouped_linear_wgrad_workspace.argtypes = [i64] * 4
+        L.rtl_grouped_linear_wgrad_workspace.restype = sz
+        L.rtl_grouped_linear_wgrad.argtypes = [vp, vp, vp, vp, vp, ci] + [i64] * 8 + [vp, sz, vp]
+        L.rtl_grouped_linear_wgrad.restype = ci
+        L.rtl_grouped_mxfp4_linear_workspace.argtypes = [i64] * 4
+        L.rtl_grouped_mxfp4_linear_workspace.restype = sz
+        L.rtl_grouped_mxfp4_linear.argtypes = [vp] * 6 + [i64] * 8 + [vp, sz, vp]
+        L.rtl_grouped_mxfp4_linear.restype = ci
         L.rtl_diag_pack_sweep.argtypes = [vp, i64, i64, i64, ci, fl, vp, sz, vp]
         L.rtl_diag_pack_sweep.restype = ci
         L.rtl_diag_tile_plan.argtypes = [i64, i64, ci, C.POINTER(C.c_int64)]
@@ -477,6 +491,120 @@ def mxfp4_linear(X, Wq, Ws, bias=None, out=None, ws=None):
         ws = _ws(L.rtl_mxfp4_linear_workspace(M, N, K), X.device)
     st = L.rtl_mxfp4_linear(_p(X), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, _ld(X), _ld(Wq), _ld(Y), _p(ws), ws.numel(), _stream())
     _check(st, "rtl_mxfp4_linear")
+    return Y
+
+
+# ---- linears grouped by expert: rows offsets[e] .. offsets[e + 1] of the activation belong to weight e ------------
+
+def _experts(offsets, W, dtype, name):
+    """(experts, rows, row length, row stride, expert stride) of a stack of weights, after checking it and the offsets."""
+    _matrix(W, dtype, name, 3)
+    E, N, K = W.shape
+    if offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,) or not offsets.is_contiguous():
+        raise ValueError("offsets: contiguous int32 tensor of %d expected" % (E + 1))
+    return E, N, K, _ld(W), W.stride(0) if E > 1 else 0
+
+
+def _group_bias(bias, E, N):
+    if bias is not None and (bias.dtype != torch.bfloat16 or tuple(bias.shape) != (E, N) or not bias.is_contiguous()):
+        raise ValueError("bias: contiguous bf16 tensor of shape (%d, %d) expected" % (E, N))
+
+
+def _group_out(out, shape, like):
+    """Rows of no expert are left alone: zeros in a new tensor."""
+    if out is None:
+        return torch.zeros(shape, dtype=torch.bfloat16, device=like.device)
+    return _given(out, shape, torch.bfloat16, like)
+
+
+def grouped_linear(X, offsets, W, bias=None, out=None):
+    """rtl_grouped_linear: Y[rows of e] = X[rows of e] W[e]^T (+ bias[e]); X bf16 [T,K], offsets int32 [E+1] on the device,
+    W bf16 [E,N,K], bias [E,N]; bf16 [T,N]. Rows of no expert keep what `out` held (zeros without `out`)."""
+    _on_current(X, offsets, W, bias, out)
+    _matrix(X, torch.bfloat16, "X")
+    E, N, K, ldw, stride = _experts(offsets, W, torch.bfloat16, "W")
+    T = X.shape[0]
+    if X.shape[1] != K:
+        raise ValueError("X and W differ in K")
+    _group_bias(bias, E, N)
+    Y = _group_out(out, (T, N), X)
+    st = lib().rtl_grouped_linear(_p(X), _p(offsets), _p(W), _p(bias), _p(Y), T, E, N, K, _ld(X), ldw, stride, _ld(Y), _stream())
+    _check(st, "rtl_grouped_linear")
+    return Y
+
+
+def grouped_linear_dgrad(dY, offsets, W, out=None):
+    """rtl_grouped_linear_dgrad: dX[rows of e] = dY[rows of e] W[e]; bf16 [T,K]."""
+    _on_current(dY, offsets, W, out)
+    _matrix(dY, torch.bfloat16, "dY")
+    E, N, K, ldw, stride = _experts(offsets, W, torch.bfloat16, "W")
+    T = dY.shape[0]
+    if dY.shape[1] != N:
+        raise ValueError("dY and W differ in N")
+    dX = _group_out(out, (T, K), dY)
+    st = lib().rtl_grouped_linear_dgrad(_p(dY), _p(offsets), _p(W), _p(dX), T, E, N, K, _ld(dY), ldw, stride, _ld(dX), _stream())
+    _check(st, "rtl_grouped_linear_dgrad")
+    return dX
+
+
+def grouped_linear_wgrad_workspace(T, E, N, K):
+    return int(lib().rtl_grouped_linear_wgrad_workspace(T, E, N, K))
+
+
+def grouped_linear_wgrad(dY, X, offsets, with_bias=False, dtype=torch.bfloat16, out=None, ws=None):
+    """rtl_grouped_linear_wgrad: (dW [E,N,K], db [E,N] or None), dW[e] = dY[rows of e]^T X[rows of e], db[e] the sum of the rows of
+    dY, in bf16 or float32. `out`: the two tensors (the second None without a bias); they then settle with_bias and dtype."""
+    _on_current(dY, X, offsets, ws)
+    _matrix(dY, torch.bfloat16, "dY")
+    _matrix(X, torch.bfloat16, "X")
+    T, N = dY.shape
+    K, E = X.shape[1], offsets.shape[0] - 1
+    if X.shape[0] != T:
+        raise ValueError("dY and X differ in rows")
+    if out is None:
+        dW = torch.empty((E, N, K), dtype=dtype, device=dY.device)
+        db = torch.empty((E, N), dtype=dtype, device=dY.device) if with_bias else None
+    else:
+        dW, db = out
+        dtype = dW.dtype
+        _on_current(dW, db)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("gradients in bf16 or float32")
+    if E < 0 or tuple(_experts(offsets, dW, dtype, "dW")[:3]) != (E, N, K):
+        raise ValueError("dW: shape %s expected" % ((E, N, K),))
+    if db is not None and (db.dtype != dtype or tuple(db.shape) != (E, N) or not db.is_contiguous()):
+        raise ValueError("db: contiguous %s tensor of shape %s expected" % (dtype, (E, N)))
+    L = lib()
+    if ws is None:
+        ws = _ws(L.rtl_grouped_linear_wgrad_workspace(T, E, N, K), dY.device)
+    st = L.rtl_grouped_linear_wgrad(_p(dY), _p(X), _p(offsets), _p(dW), _p(db), 1 if dtype == torch.float32 else 0, T, E, N, K,
+                                    _ld(dY), _ld(X), _ld(dW), dW.stride(0) if E > 1 else 0, _p(ws), ws.numel(), _stream())
+    _check(st, "rtl_grouped_linear_wgrad")
+    return dW, db
+
+
+def grouped_mxfp4_linear_workspace(T, E, N, K):
+    return int(lib().rtl_grouped_mxfp4_linear_workspace(T, E, N, K))
+
+
+def grouped_mxfp4_linear(X, offsets, Wq, Ws, bias=None, out=None, ws=None):
+    """rtl_grouped_mxfp4_linear: grouped_linear with X quantised in the call and 4-bit weights: Wq uint8 [E,N,K/2], Ws the scales of
+    the [E*N, K] matrix of all rows (what quantize_mxfp4(W.view(E * N, K)) returns); bf16 [T,N]."""
+    _on_current(X, offsets, Wq, Ws, bias, out, ws)
+    _matrix(X, torch.bfloat16, "X")
+    E, N, half, ldw, stride = _experts(offsets, Wq, torch.uint8, "Wq")
+    T, K = X.shape
+    if half * 2 != K:
+        raise ValueError("X and Wq differ in K")
+    _scales(Ws, E * N, K, "Ws")
+    _group_bias(bias, E, N)
+    Y = _group_out(out, (T, N), X)
+    L = lib()
+    if ws is None:
+        ws = _ws(L.rtl_grouped_mxfp4_linear_workspace(T, E, N, K), X.device)
+    st = L.rtl_grouped_mxfp4_linear(_p(X), _p(offsets), _p(Wq), _p(Ws), _p(bias), _p(Y), T, E, N, K, _ld(X), ldw, stride, _ld(Y),
+                                    _p(ws), ws.numel(), _stream())
+    _check(st, "rtl_grouped_mxfp4_linear")
     return Y
 
 

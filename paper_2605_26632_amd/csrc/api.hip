@@ -2,6 +2,7 @@
 // error paths can be exercised on a host without a GPU.
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include "rtl_internal.h"
 
@@ -39,7 +40,8 @@ rtl_status device_ready(void** scratch_out = nullptr) {
                 d.state = -1;
             } else {
                 if (rtl::prepare_pack_kernels() != hipSuccess || rtl::prepare_gemm_kernels() != hipSuccess ||
-                    rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_mx_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
+                    rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_mx_kernels() != hipSuccess ||
+                    rtl::prepare_grouped_kernels() != hipSuccess || rtl::prepare_grouped_grad_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
                     return RTL_ERR_HIP;
                 void* ptr = nullptr;
                 if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return RTL_ERR_HIP;
@@ -658,6 +660,137 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
     if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), M, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
         return RTL_ERR_HIP;
     return mx_product(base, scales, Wq, Ws, bias, Y, M, N, K, K / 2, ldw, ldy, base, need, workspace_bytes, s);
+}
+
+// ---- linears grouped by expert -----------------------------------------------------------------
+static const int64_t kMaxExperts = 65536;
+// Sizes that every grouped call shares; strides in the units of their operand, `extent` of them to a row of the weight.
+static bool bad_group_sizes(int64_t T, int64_t E, int64_t N, int64_t K) {
+    return too_large(T) || too_large(N) || K < 0 || too_large(K) || E < 0 || E > kMaxExperts;
+}
+static bool bad_strides(std::initializer_list<int64_t> lds) {
+    for (int64_t ld : lds)
+        if (ld > ((int64_t)1 << 22)) return true;          // 32-bit offsets inside a tile
+    return false;
+}
+
+static rtl_status check_grouped(const void* X, const int32_t* offsets, const void* W, const void* bias, const void* Y, int64_t T, int64_t E, int64_t N,
+                                int64_t K, int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, bool fp4) {
+    const int64_t wide = fp4 ? K / 2 : K, granule = fp4 ? 16 : 8;
+    if (bad_group_sizes(T, E, N, K) || K == 0 || K % (fp4 ? 32 : 64) != 0 || ldx < K || ldw < wide || ldy < N || stride_w < 0) return RTL_ERR_SHAPE;
+    if (bad_strides({ldx, ldw})) return RTL_ERR_SHAPE;
+    if (T == 0 || E == 0 || N == 0) return RTL_OK;
+    if (rtl::grouped_grid(T, E, N, fp4) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (!X || !offsets || !W || !Y) return RTL_ERR_NULL;
+    if (ldx % 8 != 0 || ldw % granule != 0 || stride_w % granule != 0 || !aligned(X, 16) || !aligned(offsets, 4) || !aligned(W, 16) || !aligned(Y, 2) ||
+        (bias && !aligned(bias, 2)))
+        return RTL_ERR_ALIGN;
+    return RTL_OK;
+}
+
+rtl_status rtl_grouped_linear(const void* X, const int32_t* offsets, const void* W, const void* bias, void* Y, int64_t T, int64_t E, int64_t N, int64_t K,
+                              int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, void* stream) {
+    const rtl_status st = check_grouped(X, offsets, W, bias, Y, T, E, N, K, ldx, ldw, stride_w, ldy, false);
+    if (st != RTL_OK || T == 0 || E == 0 || N == 0) return st;
+    RTL_REQUIRE_DEVICE();
+    rtl::GemmArgs g{};
+    g.A = X;
+    g.W = W;
+    g.bias = static_cast<const uint16_t*>(bias);
+    g.Y = static_cast<uint16_t*>(Y);
+    g.M = T; g.N = N; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldy;
+    return rtl::launch_grouped(g, rtl::GroupArgs{offsets, (int)E, stride_w}, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// rtl_grouped_mxfp4_linear workspace: [codes of X | their scales]
+size_t rtl_grouped_mxfp4_linear_workspace(int64_t T, int64_t E, int64_t N, int64_t K) {
+    if (T <= 0 || E <= 0 || N <= 0 || K <= 0) return 0;
+    return mx_ws(T, K);
+}
+
+rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t T, int64_t E,
+                                    int64_t N, int64_t K, int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+    const rtl_status st = check_grouped(X, offsets, Wq, bias, Y, T, E, N, K, ldx, ldw, stride_w, ldy, true);
+    if (st != RTL_OK || T == 0 || E == 0 || N == 0) return st;
+    if (!Ws) return RTL_ERR_NULL;
+    if (!aligned(Ws, 8)) return RTL_ERR_ALIGN;
+    const size_t need = mx_ws(T, K);
+    if (!workspace || workspace_bytes < need) return RTL_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rtl::GemmArgs g{};
+    g.fp4 = true;
+    g.A = base;
+    g.lda = K / 2;
+    uint8_t* scales = base + mx_codes_bytes(T, K);
+    g.a_scale = scales;
+    g.a_scale_rows = T;
+    g.W = Wq;
+    g.w_scale = static_cast<const uint8_t*>(Ws);
+    g.w_scale_rows = E * N;
+    g.bias = static_cast<const uint16_t*>(bias);
+    g.Y = static_cast<uint16_t*>(Y);
+    g.M = T; g.N = N; g.K = K; g.ldw = ldw; g.ldy = ldy;
+    if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), T, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
+        return RTL_ERR_HIP;
+    return rtl::launch_grouped(g, rtl::GroupArgs{offsets, (int)E, stride_w}, s) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+rtl_status rtl_grouped_linear_dgrad(const void* dY, const int32_t* offsets, const void* W, void* dX, int64_t T, int64_t E, int64_t N, int64_t K,
+                                    int64_t lddy, int64_t ldw, int64_t stride_w, int64_t lddx, void* stream) {
+    if (bad_group_sizes(T, E, N, K) || N % 8 != 0 || K % 8 != 0 || lddy < N || ldw < K || lddx < K || stride_w < 0) return RTL_ERR_SHAPE;
+    if (bad_strides({lddy, ldw, lddx})) return RTL_ERR_SHAPE;
+    if (T == 0 || E == 0 || K == 0) return RTL_OK;
+    if (N == 0) return RTL_ERR_SHAPE;                      // no gradient to speak of, and nothing that would write dX
+    if (rtl::dgrad_grid(T, E, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (!dY || !offsets || !W || !dX) return RTL_ERR_NULL;
+    if (lddy % 8 != 0 || ldw % 8 != 0 || lddx % 8 != 0 || stride_w % 8 != 0 || !aligned(dY, 16) || !aligned(offsets, 4) || !aligned(W, 16) ||
+        !aligned(dX, 16))
+        return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    rtl::GroupedGradArgs g{};
+    g.offsets = offsets;
+    g.experts = (int)E;
+    g.dY = static_cast<const uint16_t*>(dY);
+    g.W = static_cast<const uint16_t*>(W);
+    g.out = dX;
+    g.T = T; g.N = N; g.K = K; g.lddy = lddy; g.ldw = ldw; g.w_stride = stride_w; g.ldo = lddx;
+    return rtl::launch_grouped_dgrad(g, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+size_t rtl_grouped_linear_wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K) {
+    (void)T; (void)E; (void)N; (void)K;
+    return 0;
+}
+
+rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t* offsets, void* dW, void* dbias, rtl_dtype dw_type, int64_t T, int64_t E,
+                                    int64_t N, int64_t K, int64_t lddy, int64_t ldx, int64_t lddw, int64_t stride_dw, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+    (void)workspace; (void)workspace_bytes;
+    if (dw_type != RTL_BF16 && dw_type != RTL_F32) return RTL_ERR_ARG;
+    if (bad_group_sizes(T, E, N, K) || N % 8 != 0 || K % 8 != 0 || lddy < N || ldx < K || lddw < K) return RTL_ERR_SHAPE;
+    if (bad_strides({lddy, ldx, lddw})) return RTL_ERR_SHAPE;
+    if (E == 0 || N == 0 || K == 0) return RTL_OK;
+    if (E > 1 && stride_dw < (N - 1) * lddw + K) return RTL_ERR_SHAPE;       // experts' gradients must not overlap
+    if (rtl::wgrad_grid(E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (!offsets || !dW || (T > 0 && (!dY || !X))) return RTL_ERR_NULL;
+    if (lddy % 8 != 0 || ldx % 8 != 0 || lddw % 8 != 0 || stride_dw % 8 != 0 || !aligned(dY, 16) || !aligned(X, 16) || !aligned(offsets, 4) ||
+        !aligned(dW, 16) || (dbias && !aligned(dbias, dw_type == RTL_F32 ? 4 : 2)))
+        return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    rtl::GroupedGradArgs g{};
+    g.offsets = offsets;
+    g.experts = (int)E;
+    g.dY = static_cast<const uint16_t*>(dY);
+    g.X = static_cast<const uint16_t*>(X);
+    g.out = dW;
+    g.bias_out = dbias;
+    g.f32 = dw_type == RTL_F32;
+    g.T = T; g.N = N; g.K = K; g.lddy = lddy; g.ldx = ldx; g.ldo = lddw; g.o_stride = stride_dw;
+    return rtl::launch_grouped_wgrad(g, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
 }  // extern "C"

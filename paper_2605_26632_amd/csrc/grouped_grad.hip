@@ -1,0 +1,461 @@
+// Gradients of the linears grouped by expert, bf16 operands, fp32 accumulation (v_mfma_f32_16x16x32_bf16):
+//
+//   input  : dX[rows of e] = dY[rows of e] W[e]              contraction over N: dY is contiguous along it, W is not
+//   weight : dW[e] = dY[rows of e]^T X[rows of e]            contraction over the expert's rows: neither operand is contiguous along it
+//   bias   : db[e] = sum of the rows of dY
+//
+// The matrix instruction wants eight values along the contraction from each lane. An operand that is not contiguous along it is staged as it
+// lies in memory (64 rows of the contraction, BM or BN columns) and transposed on the way out of LDS: ds_read_b64_tr_b16 hands lane i of
+// 16 lanes the i-th column of the 4 x 16 block that the sixteen addressed (lane l points at row l / 4, columns 4 (l % 4) ..; measured), so two of them
+// make a fragment.
+// One tile loop for both: a stage is 64 of the contraction, travels to LDS by direct loads through a ring, and is worked off in two
+// halves of 32; the fragments of a half are read behind the matrix instructions of the half before it.
+// A contraction that is no multiple of 64 takes its last, partial block first: there the places behind its end are filled with zeros instead
+// of loaded (on both sides: what lies in memory behind an expert's rows may be NaN), at no cost to the loop.
+#include "groups.h"
+
+namespace rtl {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+struct GradSmem {
+    static constexpr int kA = BM * 128, kB = BN * 128, kStage = kA + kB, kRing = STAGES * kStage;
+    static constexpr int kEpiRow = (BN / WAVES_N) * 2 + 16;
+    static constexpr int kEpi = WAVES_M * WAVES_N * (BM / WAVES_M) * kEpiRow;
+    static constexpr int kTotal = kRing > kEpi ? kRing : kEpi;
+    static_assert(kTotal <= 160 * 1024, "LDS budget of a CU");
+};
+
+// Tiles of an operand staged as it lies in memory: rows of W columns, in chunks of 32 bytes. A wave's transposing read is served 32 lanes at a
+// time, which are eight rows (0 .. 3 and 8 .. 11 of a run of 16, or the same plus 4) of one 32-byte column chunk: the chunk is XORed with a
+// number that differs for all eight, so that they meet 64 different banks.
+__device__ __forceinline__ int row_key(int row) { return (row & 3) | ((row >> 3) & 1) << 2; }
+
+struct GradArgs {
+    const uint16_t* A;       // A_COL: A(c, i) at A[c * lda + i], else at A[i * lda + c]
+    const uint16_t* B;       // B(c, j) at B[c * ldb + j]
+    void* C;                 // C(i, j) = sum over c of A(c, i) B(c, j), at C[i * ldc + j], bf16 or fp32
+    int64_t lda, ldb, ldc;
+    int64_t m, n, depth;     // extents of i, j (both from the tile's own matrix) and c
+};
+
+template <bool A_COL, bool F32, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+__device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, const int64_t n0) {
+    using L = GradSmem<BM, BN, WAVES_M, WAVES_N, STAGES>;
+    constexpr int NW = WAVES_M * WAVES_N, WTM = BM / WAVES_M, WTN = BN / WAVES_N, TM = WTM / 16, TN = WTN / 16;
+    static_assert(!A_COL || BM % 128 == 0, "eight 32-byte chunks to a row");
+    static_assert(BN % 128 == 0, "eight 32-byte chunks to a row");
+    static_assert((!A_COL || BM == 128 || NW == 8) && (BN == 128 || NW == 8) && NW % 4 == 0, "order of a wave's requests (col_unit)");
+    constexpr int A_PER_W = L::kA / 1024 / NW, B_PER_W = L::kB / 1024 / NW, LOADS = A_PER_W + B_PER_W;
+    static_assert(L::kA % (1024 * NW) == 0 && L::kB % (1024 * NW) == 0, "tile loads must divide over the waves");
+
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+    const int64_t rows_a = a.m - m0, cols_b = a.n - n0;
+    const int KT = (int)((a.depth + 63) / 64), tail = (int)(a.depth % 64);
+
+    // ---- global -> LDS: a lane's chunks; beyond the matrix's edge it repeats the last one (only outputs that are not stored see it) ----
+    const int64_t step_a = A_COL ? 64 * a.lda * 2 : 128, step_b = 64 * a.ldb * 2;
+    const uint8_t* base_a = reinterpret_cast<const uint8_t*>(a.A + (A_COL ? m0 : m0 * a.lda));
+    const uint8_t* base_b = reinterpret_cast<const uint8_t*>(a.B + n0);
+    // block b > 0 is block b - 1 of memory when the last one is not full and comes first
+    if (tail) {
+        base_a -= step_a;
+        base_b -= step_b;
+    }
+    base_a = reinterpret_cast<const uint8_t*>(uniform64(base_a));
+    base_b = reinterpret_cast<const uint8_t*>(uniform64(base_b));
+    using wA = std::integral_constant<int, BM>;
+    using wB = std::integral_constant<int, BN>;
+    // An operand staged as it lies in memory: a request fills 1 KiB of consecutive rows (512 / width of them). A wave takes requests whose rows
+    // have one and the same key in every lane, so that one register of lane offsets serves them all and the rows between them are scalar.
+    auto col_unit = [&](auto width, int s) {               // request s of this wave, counted in 1 KiB pieces of the tile
+        constexpr int W = decltype(width)::value;
+        if constexpr (W == 256) return (wave & 1) | (s & 1) << 1 | (wave >> 1 & 1) << 2 | (s >> 1) << 3 | (wave >> 2) << 4;   // 2 rows each
+        else return wave + s * NW;                                                                                  // 4 rows each
+    };
+    uint32_t oa, ob;
+    int a_row = 0;                                         // row-major A: the lane's row of request 0; oa its chunk in the row
+    auto row_unit = [&](int s) { return (wave & 1) | s << 1 | (wave >> 1) * (2 * A_PER_W); };      // 8 rows each, one chunk order
+    auto col_offset = [&](auto width, int64_t ld, int64_t valid) {
+        constexpr int W = decltype(width)::value, CH = W / 8;
+        const int row = col_unit(width, 0) * (512 / W) + lane / CH, c = (lane % CH) ^ (row_key(row) << 1);
+        return (uint32_t)(lane / CH * ld * 2 + min((int64_t)c * 8, valid - 8) * 2);
+    };
+    if constexpr (A_COL) {
+        oa = col_offset(wA{}, a.lda, rows_a);
+    } else {
+        int c;
+        unswz8(row_unit(0) * 64 + lane, a_row, c);
+        oa = c * 16;
+    }
+    ob = col_offset(wB{}, a.ldb, cols_b);
+    auto gload_one = [&](int kt, int buf, auto n_tag) {
+        constexpr int n = decltype(n_tag)::value;
+        const uint32_t base = lds0 + buf * L::kStage;
+        if constexpr (n < A_PER_W && A_COL) {
+            const int u = col_unit(wA{}, n);
+            lds_dma16_so(base_a + kt * step_a + u * (512 / BM) * a.lda * 2, oa, base + u * 1024);
+        } else if constexpr (n < A_PER_W) {
+            // (formed anew for each request: as four registers the offsets did not fit beside the fragments)
+            int row = a_row;
+            asm volatile("" : "+v"(row));
+            row = min(row + 16 * n, (int)rows_a - 1);
+            lds_dma16_so(base_a + kt * step_a, (uint32_t)row * (uint32_t)(a.lda * 2) + oa, base + row_unit(n) * 1024);
+        } else if constexpr (n < LOADS) {
+            const int u = col_unit(wB{}, n - A_PER_W);
+            lds_dma16_so(base_b + kt * step_b + u * (512 / BN) * a.ldb * 2, ob, base + L::kA + u * 1024);
+        }
+    };
+    auto gload = [&](int kt, int buf) { static_for<LOADS>([&](auto n) { gload_one(kt, buf, n); }); };
+    auto gload_tail = [&]() {                                          // stage 0 when it is the partial block
+        static_for<LOADS>([&](auto n_tag) {
+            constexpr int n = decltype(n_tag)::value;
+            int at;
+            bool in;
+            if constexpr (n < A_PER_W && !A_COL) {
+                in = (int)oa / 2 < tail;
+                at = row_unit(n) * 1024;
+            } else if constexpr (n < A_PER_W && A_COL) {
+                const int u = col_unit(wA{}, n);
+                in = u * (512 / BM) + lane / (BM / 8) < tail;
+                at = u * 1024;
+            } else {
+                const int u = col_unit(wB{}, n - A_PER_W);
+                in = u * (512 / BN) + lane / (BN / 8) < tail;
+                at = L::kA + u * 1024;
+            }
+            if (in) gload_one(KT, 0, n_tag);
+            else *reinterpret_cast<uint4*>(smem + at + lane * 16) = make_uint4(0, 0, 0, 0);
+        });
+    };
+
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // ---- fragments: two sets, one per half of a stage ----------------------------------------------------
+    const int li = lane & 15, kb = lane >> 4;
+    struct Frags {
+        Frag8 a[TM], b[TN];
+    } f[2];
+    // Column block q of a tile staged as it lies in memory: (q ^ key) * 32 is lane_key ^ (q * 32) with everything else in the lane's address
+    // a multiple of 256 or below 32, so that one exclusive or with a constant leads from block to block.
+    typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
+    const int tr_row = 8 * kb + (li >> 2), tr_lane = (row_key(tr_row) << 5) + (li & 3) * 8;
+    uint32_t tr_a = lds0 + tr_row * (BM * 2) + tr_lane + wm * TM * 32, tr_b = lds0 + L::kA + tr_row * (BN * 2) + tr_lane + wn * TN * 32;
+    static_assert(TM == 8 || !A_COL || (TM == 4 && BM == 128), "column blocks of a wave: an aligned run of at most eight");
+    static_assert(TN == 8 || TN == 4 || TN == 2, "likewise");
+    if constexpr (TM < 8) tr_a = lds0 + tr_row * (BM * 2) + (tr_lane ^ (wm * TM * 32 & 255)) + (wm * TM * 32 & ~255);
+    if constexpr (TN < 8) tr_b = lds0 + L::kA + tr_row * (BN * 2) + (tr_lane ^ (wn * TN * 32 & 255)) + (wn * TN * 32 & ~255);
+    auto tr_frag = [&](uint32_t at, auto width, auto half) {
+        constexpr int W = decltype(width)::value * 2, H = decltype(half)::value;
+        typedef __attribute__((address_space(3))) bf16x4* lds4;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4)((lds_ptr)(uintptr_t)at + 32 * H * W));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds4)((lds_ptr)(uintptr_t)at + 32 * H * W + 4 * W));
+        return bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    auto read_item = [&](int buf, auto half_tag, auto e_tag) {         // tr_a and tr_b point into buffer buf already
+        constexpr int H = decltype(half_tag)::value, e = decltype(e_tag)::value;
+        if constexpr (e < TM && A_COL) {
+            f[H].a[e].v = tr_frag(tr_a ^ (e * 32), wA{}, half_tag);
+        } else if constexpr (e < TM) {
+            f[H].a[e].u = *reinterpret_cast<const uint4*>(smem + buf * L::kStage + swz8(wm * WTM + e * 16 + li, 4 * H + kb));
+        } else {
+            f[H].b[e - TM].v = tr_frag(tr_b ^ ((e - TM) * 32), wB{}, half_tag);
+        }
+    };
+    constexpr int NMMA = TM * TN, ITEMS = TM + TN;
+    // Matrix work of half H; behind it the fragments of the other half (of buffer rbuf) and LO <= n < HI of the requests of stage kt_load.
+    auto half = [&](auto h_tag, auto read_tag, int rbuf, auto lo_tag, auto hi_tag, int kt_load, int buf) {
+        constexpr int H = decltype(h_tag)::value, LO = decltype(lo_tag)::value, CNT = decltype(hi_tag)::value - LO;
+        constexpr int RPM = (ITEMS + NMMA - 1) / NMMA, LPM = (CNT + NMMA - 1) / NMMA;
+        asm volatile("" : "+v"(tr_b));                  // one register, not an address per column block kept through the loop
+        if constexpr (A_COL) asm volatile("" : "+v"(tr_a));
+        static_for<NMMA>([&](auto n_tag) {
+            constexpr int n = decltype(n_tag)::value, i = n % TM, j = n / TM;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[H].a[i].v, f[H].b[j].v, acc[i][j], 0, 0, 0);
+            if constexpr (decltype(read_tag)::value) {
+                constexpr int r0 = n * RPM < ITEMS ? n * RPM : ITEMS, r1 = (n + 1) * RPM < ITEMS ? (n + 1) * RPM : ITEMS;
+                static_for<r1 - r0>([&](auto e) { read_item(rbuf, std::integral_constant<int, 1 - H>{}, std::integral_constant<int, r0 + decltype(e)::value>{}); });
+            }
+            constexpr int g0 = n * LPM < CNT ? n * LPM : CNT, g1 = (n + 1) * LPM < CNT ? (n + 1) * LPM : CNT;
+            static_for<g1 - g0>([&](auto e) { gload_one(kt_load, buf, std::integral_constant<int, LO + g0 + decltype(e)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    if (KT > 0) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            if (s < KT) {
+                if (s == 0 && tail) gload_tail();
+                else gload(s, s);
+            }
+        if (KT >= STAGES) wait_vmcnt_lgkm0<(STAGES - 1) * LOADS>();
+        else wait_vmcnt_lgkm0<0>();
+        barrier();
+        static_for<ITEMS>([&](auto e) { read_item(0, std::integral_constant<int, 0>{}, e); });
+        wait_vmcnt_lgkm0<63>();
+        // Inside stage kt: first half of its matrix work, the reads of its second half, (ring of three and more) the rest of the requests of
+        // stage kt + STAGES - 1 | own reads done, stage kt + 1 landed | barrier | second half, the first reads of stage kt + 1 and the
+        // requests of stage kt + STAGES into the buffer that nobody reads any more.
+        constexpr int SPLIT = STAGES == 2 ? LOADS : (LOADS + 1) / 2;
+        using c0 = std::integral_constant<int, 0>;
+        using c1 = std::integral_constant<int, 1>;
+        using cS = std::integral_constant<int, SPLIT>;
+        using cL = std::integral_constant<int, LOADS>;
+        using T = std::true_type;
+        using F = std::false_type;
+        int cur = 0;
+        auto stage_step = [&](int kt, auto load_a, auto load_b, auto has_next, auto pending) {
+            const int nxt = cur + 1 == STAGES ? 0 : cur + 1, prv = cur == 0 ? STAGES - 1 : cur - 1;
+            using a_lo = std::conditional_t<decltype(load_a)::value, cS, c0>;
+            using a_hi = std::conditional_t<decltype(load_a)::value, cL, c0>;
+            using b_hi = std::conditional_t<decltype(load_b)::value, cS, c0>;
+            half(c0{}, T{}, cur, a_lo{}, a_hi{}, kt + STAGES - 1, prv);
+            wait_vmcnt_lgkm0<decltype(pending)::value * LOADS>();
+            barrier();
+            tr_a += (nxt - cur) * L::kStage;
+            tr_b += (nxt - cur) * L::kStage;
+            half(c1{}, has_next, nxt, c0{}, b_hi{}, kt + STAGES, cur);
+            cur = nxt;
+        };
+        using P = std::integral_constant<int, STAGES - 2>;
+        static_assert(STAGES == 2 || STAGES == 3 || STAGES == 4, "ring depth");
+        int kt = 0;
+        if constexpr (STAGES == 2) {
+            for (; kt < KT - 2; ++kt) stage_step(kt, F{}, T{}, T{}, P{});
+            // (the last stage reads fragments that nobody uses: a step of its own without them came out of the compiler with spills)
+            for (; kt < KT; ++kt) stage_step(kt, F{}, F{}, T{}, P{});
+        } else {
+          if (KT > STAGES) {
+            stage_step(kt, F{}, T{}, T{}, P{});
+            for (kt = 1; kt < KT - STAGES; ++kt) stage_step(kt, T{}, T{}, T{}, P{});
+            stage_step(kt, T{}, F{}, T{}, P{});
+            ++kt;
+          }
+          if constexpr (STAGES >= 4) {
+            if (kt == KT - 4) { stage_step(kt, F{}, F{}, T{}, std::integral_constant<int, 2>{}); ++kt; }
+          }
+          if (kt == KT - 3) { stage_step(kt, F{}, F{}, T{}, std::integral_constant<int, 1>{}); ++kt; }
+          if (kt == KT - 2) { stage_step(kt, F{}, F{}, T{}, std::integral_constant<int, 0>{}); ++kt; }
+          stage_step(kt, F{}, F{}, F{}, std::integral_constant<int, 0>{});
+        }
+    }
+
+    // ---- store: register r of a block is row 4 kb + r, column li -----------------------------------------
+    if constexpr (F32) {
+        float* C = static_cast<float*>(a.C);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int64_t col = n0 + wn * WTN + j * 16 + li;
+            if (col >= a.n) continue;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t row = m0 + wm * WTM + i * 16 + 4 * kb + r;
+                    if (row < a.m) C[row * a.ldc + col] = acc[i][j][r];
+                }
+        }
+    } else {
+        // (the lane's numbers formed again: kept through the loop they cost registers there)
+        int lane = threadIdx.x;
+        asm volatile("" : "+v"(lane));
+        lane &= 63;
+        const int li = lane & 15, kb = lane >> 4;
+        // through LDS, so that rows leave in 16-byte pieces; two lanes of neighbouring columns first trade halves, so that each writes two
+        // columns of one row
+        wait_vmcnt_lgkm0<0>();
+        barrier();                                   // the ring is free
+        uint8_t* ep = smem + wave * (WTM * L::kEpiRow);
+        const bool odd = lane & 1;
+        const uint32_t sel = odd ? 0x03020706u : 0x05040100u;
+        uint8_t* const ep_lane = ep + (4 * kb + (odd ? 2 : 0)) * L::kEpiRow + (li & ~1) * 2;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const f32x2 pv = {acc[i][j][r], acc[i][j][r + 2]};
+                    const uint32_t own = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2));      // RNE
+                    const uint32_t partner = (uint32_t)__builtin_amdgcn_mov_dpp((int)own, 0xB1, 0xF, 0xF, true);
+                    *reinterpret_cast<uint32_t*>(ep_lane + (i * 16 + r) * L::kEpiRow + j * 32) = __builtin_amdgcn_perm(partner, own, sel);
+                }
+        uint16_t* C = static_cast<uint16_t*>(a.C);
+        constexpr int CPR = WTN / 8, CHUNKS = WTM * CPR;
+#pragma unroll
+        for (int q0 = 0; q0 < CHUNKS; q0 += 64) {
+            const int q = q0 + lane, rl = q / CPR, c = q % CPR;
+            const int64_t row = m0 + wm * WTM + rl, col = n0 + wn * WTN + c * 8;
+            if (q < CHUNKS && row < a.m && col < a.n)
+                *reinterpret_cast<uint4*>(C + row * a.ldc + col) = *reinterpret_cast<const uint4*>(ep + rl * L::kEpiRow + c * 16);
+        }
+    }
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void dgrad_kernel(const GroupedGradArgs a) {
+    GroupTile t;
+    const int tiles_n = (int)((a.K + BN - 1) / BN);
+    if (!group_tile(a.offsets, a.experts, (int)a.T, BM, tiles_n, t)) return;
+    GradArgs g;
+    g.A = a.dY + t.begin * a.lddy;
+    g.lda = a.lddy;
+    g.B = a.W + t.expert * a.w_stride;
+    g.ldb = a.ldw;
+    g.C = static_cast<uint16_t*>(a.out) + t.begin * a.ldo;
+    g.ldc = a.ldo;
+    g.m = t.rows;
+    g.n = a.K;
+    g.depth = a.N;
+    int pm, pn;
+    tile_walk<8>(t.tile, (t.rows + BM - 1) / BM, tiles_n, pm, pn);
+    grad_tile<false, false, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
+}
+
+template <bool F32, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const GroupedGradArgs a) {
+    const int tiles_m = (int)((a.N + BM - 1) / BM), tiles_n = (int)((a.K + BN - 1) / BN), tiles = tiles_m * tiles_n;
+    const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8;
+    const int t = xcd_share_start((int)gridDim.x, xcd) + local;
+    const int e = t / tiles;
+    const RowRange r = expert_rows(a.offsets, e, (int)a.T);
+    GradArgs g;
+    g.A = a.dY + r.begin * a.lddy;
+    g.lda = a.lddy;
+    g.B = a.X + r.begin * a.ldx;
+    g.ldb = a.ldx;
+    if constexpr (F32) g.C = static_cast<float*>(a.out) + e * a.o_stride;
+    else g.C = static_cast<uint16_t*>(a.out) + e * a.o_stride;
+    g.ldc = a.ldo;
+    g.m = a.N;
+    g.n = a.K;
+    g.depth = r.end - r.begin;
+    int pm, pn;
+    tile_walk<8>(t % tiles, tiles_m, tiles_n, pm, pn);
+    grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
+}
+
+// Bias gradient: a workgroup adds up 64 columns of an expert's rows, 32 rows at a time, then its 32 partial sums in a fixed order.
+__global__ __launch_bounds__(256) void bgrad_kernel(const GroupedGradArgs a) {
+    __shared__ float part[32][65];
+    const int64_t blocks = (a.N + 63) / 64;
+    const int e = (int)(blockIdx.x / blocks);
+    const int64_t col = blockIdx.x % blocks * 64 + threadIdx.x % 8 * 8;
+    const RowRange r = expert_rows(a.offsets, e, (int)a.T);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (col < a.N)
+        for (int row = r.begin + threadIdx.x / 8; row < r.end; row += 32) {
+            const uint4 v = *reinterpret_cast<const uint4*>(a.dY + row * a.lddy + col);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[2 * i] += __uint_as_float(w[i] << 16);
+                sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x / 8][threadIdx.x % 8 * 8 + i] = sum[i];
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
+    const int64_t c = blockIdx.x % blocks * 64 + threadIdx.x;
+    if (c >= a.N) return;
+    if (a.f32) static_cast<float*>(a.bias_out)[e * a.N + c] = s;
+    else static_cast<uint16_t*>(a.bias_out)[e * a.N + c] = (uint16_t)f32_to_bf16_rne(s);
+}
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+struct Grad {
+    using L = GradSmem<BM, BN, WAVES_M, WAVES_N, STAGES>;
+    static int64_t dgrad_grid(int64_t T, int64_t E, int64_t K) { return group_grid(T, E, K, BM, BN); }
+    static int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) { return E * ((N + BM - 1) / BM) * ((K + BN - 1) / BN); }
+    static constexpr dim3 block() { return dim3(WAVES_M * WAVES_N * 64); }
+    static hipError_t limit(const void* k) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, L::kTotal); }
+    static hipError_t prepare_dgrad() { return limit(reinterpret_cast<const void*>(dgrad_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>)); }
+    static hipError_t prepare_wgrad() {
+        const hipError_t e = limit(reinterpret_cast<const void*>(wgrad_kernel<false, BM, BN, WAVES_M, WAVES_N, STAGES>));
+        return e != hipSuccess ? e : limit(reinterpret_cast<const void*>(wgrad_kernel<true, BM, BN, WAVES_M, WAVES_N, STAGES>));
+    }
+    static hipError_t dgrad(const GroupedGradArgs& a, hipStream_t stream) {
+        hipLaunchKernelGGL((dgrad_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>), dim3((unsigned)dgrad_grid(a.T, a.experts, a.K)), block(),
+                           L::kTotal, stream, a);
+        return hipGetLastError();
+    }
+    static hipError_t wgrad(const GroupedGradArgs& a, hipStream_t stream) {
+        const dim3 grid((unsigned)wgrad_grid(a.experts, a.N, a.K));
+        if (a.f32) hipLaunchKernelGGL((wgrad_kernel<true, BM, BN, WAVES_M, WAVES_N, STAGES>), grid, block(), L::kTotal, stream, a);
+        else hipLaunchKernelGGL((wgrad_kernel<false, BM, BN, WAVES_M, WAVES_N, STAGES>), grid, block(), L::kTotal, stream, a);
+        return hipGetLastError();
+    }
+};
+
+template <class Op>
+auto with_dgrad(int shape, Op op) {
+    switch (shape) {
+        case 0: return op(Grad<64, 128, 1, 4, 4>{});
+        case 1: return op(Grad<128, 128, 2, 2, 2>{});
+        default: return op(Grad<256, 256, 2, 4, 2>{});
+    }
+}
+template <class Op>
+auto with_wgrad(int shape, Op op) {
+    if (shape == 0) return op(Grad<128, 128, 2, 2, 2>{});
+    return op(Grad<256, 256, 2, 4, 2>{});
+}
+
+}  // namespace
+
+static int dgrad_shape(int64_t T, int64_t E) {
+    const int64_t rows = T / E;
+    return rows <= 64 ? 0 : rows <= 160 ? 1 : 2;
+}
+static int wgrad_shape(int64_t E, int64_t N, int64_t K) { return E * ((N + 255) / 256) * ((K + 255) / 256) < 192 ? 0 : 1; }
+
+int64_t dgrad_grid(int64_t T, int64_t E, int64_t K) {
+    return with_dgrad(dgrad_shape(T, E), [&](auto k) { return decltype(k)::dgrad_grid(T, E, K); });
+}
+int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) {
+    return with_wgrad(wgrad_shape(E, N, K), [&](auto k) { return decltype(k)::wgrad_grid(E, N, K); });
+}
+
+hipError_t prepare_grouped_grad_kernels() {
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_dgrad(i, [](auto k) { return decltype(k)::prepare_dgrad(); });
+    for (int i = 0; i < 2 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
+    hipFuncAttributes attr;
+    if (e == hipSuccess) e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(bgrad_kernel));
+    return e;
+}
+
+hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream) {
+    return with_dgrad(dgrad_shape(a.T, a.experts), [&](auto k) { return decltype(k)::dgrad(a, stream); });
+}
+
+hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, hipStream_t stream) {
+    const hipError_t e = with_wgrad(wgrad_shape(a.experts, a.N, a.K), [&](auto k) { return decltype(k)::wgrad(a, stream); });
+    if (e != hipSuccess || !a.bias_out) return e;
+    hipLaunchKernelGGL(bgrad_kernel, dim3((unsigned)(a.experts * ((a.N + 63) / 64))), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace rtl

@@ -144,6 +144,35 @@ hipError_t launch_quantize_mxfp4(const uint16_t* X, int64_t rows, int64_t cols, 
 hipError_t launch_dequantize_mxfp4(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64_t rows, int64_t cols, uint16_t* X, int64_t ld,
                                    hipStream_t stream);
 
+// ---- linears grouped by expert (grouped.hip, grouped_grad.hip) ----------------------------------
+struct GroupArgs {
+    const int* offsets;     // [experts + 1]: rows offsets[e] .. offsets[e + 1] belong to expert e
+    int experts;
+    int64_t w_stride;       // elements (4-bit: bytes) between the experts' weights
+};
+constexpr int64_t kMaxGroupGrid = (int64_t)1 << 24;
+// Workgroups of a launch over the experts' tiles: an upper bound, the offsets are on the device.
+int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn);
+hipError_t prepare_grouped_kernels();
+// a: M the rows of X, W and the bias of expert 0 (bias [experts, N]); 4-bit: w_scale_rows = experts * N.
+// Workgroups of the launch (the calls refuse kMaxGroupGrid and more).
+int64_t grouped_grid(int64_t T, int64_t E, int64_t N, bool fp4);
+hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
+struct GroupedGradArgs {
+    const int* offsets;
+    int experts;
+    const uint16_t *dY, *W, *X;
+    void* out;              // dgrad: dX bf16; wgrad: dW of expert 0, fp32 with f32 set, else bf16
+    void* bias_out;         // wgrad: nullable, [experts, N], the type of out
+    bool f32;
+    int64_t T, N, K, lddy, ldw, w_stride, ldx, ldo, o_stride;
+};
+hipError_t prepare_grouped_grad_kernels();
+int64_t dgrad_grid(int64_t T, int64_t E, int64_t K);
+int64_t wgrad_grid(int64_t E, int64_t N, int64_t K);
+hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream);
+hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, hipStream_t stream);
+
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------
 // Issue-rate probe: `blocks` workgroups of four waves, each wave issuing 4 * iters matrix
 // instructions (kind 0: dense 32x32x16 bf16, kind 1: structured-sparse 32x32x32 bf16) on register

@@ -1,0 +1,230 @@
+"""Linears grouped by expert and their gradients on the GPU against plain products in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import mx_ref as ref
+from paper_2605_26632_amd import binding as rtl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def bf16(gen, *shape, std=1.0):
+    return (torch.randn(*shape, generator=gen, device=DEV) * std).to(torch.bfloat16)
+
+
+def generator(seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    return gen
+
+
+def offsets_of(counts, front=0):
+    return torch.tensor([front + sum(counts[:e]) for e in range(len(counts) + 1)], dtype=torch.int32, device=DEV)
+
+
+def split(rng, T, E, empty):
+    """T rows over E experts, some of them without."""
+    w = rng.random(E) ** 2 * (rng.random(E) >= empty)
+    w[rng.integers(E)] += 0.1
+    return rng.multinomial(T, w / w.sum()).tolist()
+
+
+def strided(t, pad=8, fill=float("nan")):
+    """The same matrix or stack of matrices with rows further apart, NaN between them."""
+    wide = torch.full((*t.shape[:-1], t.shape[-1] + 2 * pad), fill, dtype=t.dtype, device=DEV)
+    wide[..., pad:-pad] = t
+    return wide[..., pad:-pad]
+
+
+# T, E, N, K, share of empty experts: from one row to several tiles an expert, every tile shape, more experts than one wave has lanes
+SIZES = [(1, 1, 40, 64, 0.0), (1, 5, 24, 128, 0.0), (7, 3, 264, 192, 0.3), (70, 70, 64, 64, 0.5), (90, 2, 136, 320, 0.0), (300, 130, 72, 128, 0.3),
+         (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0)]
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", SIZES)
+@pytest.mark.parametrize("bias", [False, True])
+def test_forward(T, E, N, K, empty, bias):
+    """Any split of the rows; strided operands with NaN between their rows; rows of nobody hold NaN, are not used and stay as they were."""
+    gen, rng = generator(T + E + N + K), np.random.default_rng(T * E)
+    counts, front, behind = split(rng, T, E, empty), 3, 5
+    off = offsets_of(counts, front)
+    X = torch.full((front + T + behind, K), float("nan"), dtype=torch.bfloat16, device=DEV)
+    X[front:front + T] = bf16(gen, T, K)
+    n = N - 3                                                   # no multiple of anything
+    W, b = strided(bf16(gen, E, n, K)), bf16(gen, E, n) if bias else None
+    for pitch in (n + 4, (n + 23) // 8 * 8):                      # element and 16-byte stores
+        full = torch.full((front + T + behind, pitch), 3.0, dtype=torch.bfloat16, device=DEV)
+        Y = rtl.grouped_linear(strided(X), off, W, bias=b, out=full[:, :n])
+        assert (full[:, n:] == 3.0).all() and (full[:front] == 3.0).all() and (full[front + T:] == 3.0).all()
+        o = off.tolist()
+        for e in range(E):
+            if counts[e]:
+                ref.check_product(Y[o[e]:o[e + 1]], ref.values(X[o[e]:o[e + 1]]), ref.values(W[e]), None if b is None else ref.values(b[e]))
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", SIZES)
+def test_input_gradient(T, E, N, K, empty):
+    gen, rng = generator(T + E + N + K + 1), np.random.default_rng(T * E + 1)
+    counts, front, behind = split(rng, T, E, empty), 2, 4
+    off = offsets_of(counts, front)
+    dY = torch.full((front + T + behind, N), float("nan"), dtype=torch.bfloat16, device=DEV)
+    dY[front:front + T] = bf16(gen, T, N)
+    k = K - 24                                                    # no multiple of a tile or a 64-wide stage
+    W = strided(bf16(gen, E, N, k))
+    full = torch.full((front + T + behind, k + 16), 3.0, dtype=torch.bfloat16, device=DEV)
+    dX = rtl.grouped_linear_dgrad(strided(dY), off, W, out=full[:, :k])
+    assert (full[:, k:] == 3.0).all() and (full[:front] == 3.0).all() and (full[front + T:] == 3.0).all()
+    o = off.tolist()
+    for e in range(E):
+        if counts[e]:
+            ref.check_product(dX[o[e]:o[e + 1]], ref.values(dY[o[e]:o[e + 1]]), ref.values(W[e]).T)
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", SIZES + [(700, 2, 1040, 3080, 0.0), (200, 40, 520, 640, 0.5)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_weight_and_bias_gradient(T, E, N, K, empty, dtype):
+    """Every element is written; NaN in the rows of nobody and between the rows stays out; an expert's NaN reaches its own gradient only."""
+    gen, rng = generator(T + E + N + K + 2), np.random.default_rng(T * E + 2)
+    counts, front, behind = split(rng, T, E, empty), 70, 90
+    off = offsets_of(counts, front)
+    dY = torch.full((front + T + behind, N), float("nan"), dtype=torch.bfloat16, device=DEV)
+    X = torch.full((front + T + behind, K), float("nan"), dtype=torch.bfloat16, device=DEV)
+    dY[front:front + T], X[front:front + T] = bf16(gen, T, N), bf16(gen, T, K)
+    sick = None
+    if E > 2 and sum(c > 0 for c in counts) > 1:
+        sick = next(e for e in range(E) if counts[e])
+        X[off[sick], 0] = float("nan")
+        dY[off[sick], 1] = float("inf")
+    full = torch.full((E + 1, N, K + 8), 3.0, dtype=dtype, device=DEV)
+    db = torch.full((E, N), 3.0, dtype=dtype, device=DEV)
+    dW, _ = rtl.grouped_linear_wgrad(strided(dY), strided(X), off, out=(full[:E, :, :K], db))
+    assert (full[E:] == 3.0).all() and (full[..., K:] == 3.0).all()
+    o = off.tolist()
+    for e in range(E):
+        if e == sick:
+            assert torch.isnan(dW[e, :, 0]).all() and not torch.isfinite(db[e, 1])
+            continue
+        g, x = ref.values(dY[o[e]:o[e + 1]]), ref.values(X[o[e]:o[e + 1]])
+        if counts[e] == 0:
+            assert (dW[e] == 0).all() and (db[e] == 0).all()
+            continue
+        ref.check_product(dW[e], g.T, x.T, dtype=dtype)
+        ref.check_product(db[e:e + 1], np.ones((1, counts[e])), g.T, dtype=dtype)
+    again = rtl.grouped_linear_wgrad(dY, X, off, with_bias=True, dtype=dtype)
+    keep = [e for e in range(E) if e != sick]
+    assert torch.equal(again[0][keep], dW[keep]) and torch.equal(again[1][keep], db[keep])      # the same bits every time
+
+
+def test_gradients_against_differences():
+    """Small integers, so that everything is exact: moving X, W or b by a step changes sum(Y * G) by the step times the gradient."""
+    rng = np.random.default_rng(7)
+    T, E, N, K = 40, 3, 32, 64
+    counts = [11, 0, 29]
+    off = offsets_of(counts)
+    ints = lambda *s: torch.from_numpy(rng.integers(-1, 2, s)).to(DEV).to(torch.bfloat16)
+    X, W, b, G = ints(T, K), ints(E, N, K), ints(E, N), ints(T, N)
+    loss = lambda x, w, c: (rtl.grouped_linear(x, off, w, bias=c).double() * G.double()).sum().item()
+    dX = rtl.grouped_linear_dgrad(G, off, W)
+    dW, db = rtl.grouped_linear_wgrad(G, X, off, with_bias=True, dtype=torch.float32)
+    for _ in range(8):
+        sx, sw, sb = ints(T, K), ints(E, N, K), ints(E, N)
+        assert loss(X + sx, W, b) - loss(X, W, b) == (dX.double() * sx.double()).sum().item()
+        assert loss(X, W + sw, b) - loss(X, W, b) == (dW.double() * sw.double()).sum().item()
+        assert loss(X, W, b + sb) - loss(X, W, b) == (db.double() * sb.double()).sum().item()
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", SIZES + [(64, 32, 300, 992, 0.3), (2000, 3, 700, 544, 0.0)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_mxfp4_forward(T, E, N, K, empty, bias):
+    gen, rng = generator(T + E + N + K + 3), np.random.default_rng(T * E + 3)
+    counts, front, behind = split(rng, T, E, empty), 1, 2
+    off = offsets_of(counts, front)
+    X = bf16(gen, front + T + behind, K)
+    X[front + T:] = float("nan")
+    n = N - 3
+    wc, wb = ref.random_codes(rng, E * n, K)
+    wq, ws = ref.on_device(wc, wb)
+    stack = torch.full((E, n, K // 2 + 16), 0x77, dtype=torch.uint8, device=DEV)
+    stack[..., :K // 2] = wq.reshape(E, n, K // 2)
+    b = bf16(gen, E, n) if bias else None
+    full = torch.full((front + T + behind, n + 5), 3.0, dtype=torch.bfloat16, device=DEV)
+    Y = rtl.grouped_mxfp4_linear(X, off, stack[..., :K // 2], ws, bias=b, out=full[:, :n])
+    assert (full[:, n:] == 3.0).all() and (full[:front] == 3.0).all() and (full[front + T:] == 3.0).all()
+    w = ref.decode(wc, wb).reshape(E, n, K)
+    o = off.tolist()
+    for e in range(E):
+        if counts[e]:
+            ref.check_product(Y[o[e]:o[e + 1]], ref.decode(*ref.quantize(ref.values(X[o[e]:o[e + 1]]))), w[e], None if b is None else ref.values(b[e]))
+
+
+def test_one_weight_for_all_experts():
+    """A broadcast weight: forward and input gradient use it; its weight gradient has to be a stack of its own."""
+    gen = generator(4)
+    off = offsets_of([9, 30, 1])
+    X, W, G = bf16(gen, 40, 128), bf16(gen, 1, 72, 128), bf16(gen, 40, 72)
+    wide = W.expand(3, 72, 128)
+    ref.check_product(rtl.grouped_linear(X, off, wide), ref.values(X), ref.values(W[0]))
+    ref.check_product(rtl.grouped_linear_dgrad(G, off, wide), ref.values(G), ref.values(W[0]).T)
+    with pytest.raises(rtl.RtlError):
+        rtl.grouped_linear_wgrad(G, X, off, out=(wide, None))
+
+
+@pytest.mark.parametrize("bad", [[0, 50, 20, 40], [-7, 10, 20, 90], [60, 40, 20, 0], [0, 2 ** 31 - 1, -2 ** 31, 40], [40, 40, 40, 40]])
+def test_offsets_that_are_no_offsets_touch_nothing_else(bad):
+    gen = generator(5)
+    T, E, N, K = 40, 3, 72, 64
+    off = torch.tensor(bad, dtype=torch.int64).to(torch.int32).to(DEV)
+    X, W, G = bf16(gen, T, K), bf16(gen, E, N, K), bf16(gen, T, N)
+    wq, ws = rtl.quantize_mxfp4(W.reshape(E * N, K))
+    for f, width in ((lambda o: rtl.grouped_linear(X, off, W, out=o), N), (lambda o: rtl.grouped_linear_dgrad(G, off, W, out=o), K),
+                     (lambda o: rtl.grouped_mxfp4_linear(X, off, wq.reshape(E, N, K // 2), ws, out=o), N)):
+        full = torch.full((T + 64, width + 64), 3.0, dtype=torch.bfloat16, device=DEV)
+        f(full[32:32 + T, 32:32 + width])
+        full[32:32 + T, 32:32 + width] = 3.0
+        assert (full == 3.0).all()
+    dW, db = rtl.grouped_linear_wgrad(G, X, off, with_bias=True)
+    assert torch.isfinite(dW).all() and torch.isfinite(db).all()
+
+
+def test_no_rows():
+    W = torch.randn(3, 16, 64, device=DEV).to(torch.bfloat16)
+    off = offsets_of([0, 0, 0])
+    X, G = (torch.empty(0, n, dtype=torch.bfloat16, device=DEV) for n in (64, 16))
+    assert rtl.grouped_linear(X, off, W).shape == (0, 16) and rtl.grouped_linear_dgrad(G, off, W).shape == (0, 64)
+    dW = torch.full_like(W, 5.0)
+    rtl.grouped_linear_wgrad(G, X, off, out=(dW, None))
+    assert (dW == 0).all()
+
+
+def test_training_step_captured_and_replayed():
+    """Forward and both gradients in one graph on another stream, the rows divided anew between the replays without a word to the host."""
+    rtl.init()
+    gen = generator(6)
+    T, E, N, K = 300, 5, 136, 192
+    X, W, G = bf16(gen, T, K), bf16(gen, E, N, K), bf16(gen, T, N)
+    b = bf16(gen, E, N)
+    off = offsets_of([60] * 5)
+    Y, dX = torch.zeros(T, N, dtype=torch.bfloat16, device=DEV), torch.zeros(T, K, dtype=torch.bfloat16, device=DEV)
+    dW, db = torch.zeros(E, N, K, device=DEV), torch.zeros(E, N, device=DEV)
+    wq, ws = rtl.quantize_mxfp4(W.reshape(E * N, K))
+    Yq = torch.zeros_like(Y)
+    room = torch.empty(rtl.grouped_mxfp4_linear_workspace(T, E, N, K), dtype=torch.uint8, device=DEV)
+    room_w = torch.empty(max(rtl.grouped_linear_wgrad_workspace(T, E, N, K), 256), dtype=torch.uint8, device=DEV)
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        rtl.grouped_linear(X, off, W, bias=b, out=Y)
+        rtl.grouped_mxfp4_linear(X, off, wq.reshape(E, N, K // 2), ws, bias=b, out=Yq, ws=room)
+        rtl.grouped_linear_dgrad(G, off, W, out=dX)
+        rtl.grouped_linear_wgrad(G, X, off, out=(dW, db), ws=room_w)
+    for counts in ([300, 0, 0, 0, 0], [1, 99, 0, 150, 50], [0, 0, 0, 0, 300], [60] * 5):
+        off.copy_(offsets_of(counts))
+        X.copy_(bf16(gen, T, K))
+        graph.replay()
+        want = (rtl.grouped_linear(X, off, W, bias=b), rtl.grouped_mxfp4_linear(X, off, wq.reshape(E, N, K // 2), ws, bias=b),
+                rtl.grouped_linear_dgrad(G, off, W), *rtl.grouped_linear_wgrad(G, X, off, with_bias=True, dtype=torch.float32))
+        torch.cuda.synchronize()
+        for got, w in zip((Y, Yq, dX, dW, db), want):
+            assert torch.equal(got, w)

@@ -1,0 +1,75 @@
+"""Refusals of the entry points of linears grouped by expert, all before any launch."""
+import pytest
+import torch
+
+from paper_2605_26632_amd import binding as rtl
+
+FAKE = 0x10000      # non-null, aligned, never dereferenced
+NULL, SHAPE, ALIGN, WORKSPACE, ARG = 1, 2, 3, 4, 5
+BIG = 1 << 30
+
+
+def caller(name, defaults):
+    def f(**kw):
+        assert set(kw) <= set(defaults)
+        return getattr(rtl.lib(), name)(*dict(defaults, **kw).values())
+    return f
+
+
+def check_common(f, pointers):
+    assert f(T=-1) == SHAPE and f(E=-1) == SHAPE and f(N=-8) == SHAPE and f(K=-64) == SHAPE
+    assert f(T=BIG + 1) == SHAPE and f(E=65537) == SHAPE
+    for p in pointers:
+        assert f(**{p: None}) == NULL
+        assert f(**{p: FAKE + 1}) == ALIGN
+
+
+def test_forward_refusals():
+    f = caller("rtl_grouped_linear", dict(X=FAKE, off=FAKE, W=FAKE, bias=None, Y=FAKE, T=16, E=2, N=24, K=64, ldx=64, ldw=64, sw=24 * 64, ldy=24,
+                                          stream=None))
+    check_common(f, ("X", "off", "W", "Y"))
+    assert f(K=32) == SHAPE and f(K=0) == SHAPE and f(ldx=56) == SHAPE and f(ldw=56) == SHAPE and f(ldy=23) == SHAPE and f(sw=-8) == SHAPE
+    assert f(ldx=(1 << 22) + 8) == SHAPE and f(ldw=(1 << 22) + 8) == SHAPE
+    assert f(T=BIG, N=BIG, ldy=BIG) == SHAPE                       # 2^24 workgroups and more
+    assert f(ldx=68) == ALIGN and f(ldw=68) == ALIGN and f(sw=24 * 64 + 4) == ALIGN and f(bias=FAKE + 1) == ALIGN
+    assert f(T=0) == 0 and f(E=0) == 0 and f(N=0) == 0
+
+
+def test_mxfp4_forward_refusals():
+    f = caller("rtl_grouped_mxfp4_linear", dict(X=FAKE, off=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, T=16, E=2, N=24, K=64, ldx=64, ldw=32,
+                                                sw=24 * 32, ldy=24, ws=FAKE, wsb=1 << 20, stream=None))
+    check_common(f, ("X", "off", "Wq", "Ws", "Y"))
+    assert f(K=48) == SHAPE and f(ldw=16) == SHAPE and f(ldx=56) == SHAPE
+    assert f(ldw=40) == ALIGN and f(sw=24 * 32 + 8) == ALIGN and f(ws=FAKE + 64) == ALIGN
+    assert f(ws=None) == WORKSPACE and f(wsb=511) == WORKSPACE and f(wsb=rtl.grouped_mxfp4_linear_workspace(16, 2, 24, 64) - 1) == WORKSPACE
+    assert f(T=0) == 0 and f(E=0) == 0 and f(N=0) == 0
+
+
+def test_input_gradient_refusals():
+    f = caller("rtl_grouped_linear_dgrad", dict(dY=FAKE, off=FAKE, W=FAKE, dX=FAKE, T=16, E=2, N=24, K=64, lddy=24, ldw=64, sw=24 * 64, lddx=64,
+                                                stream=None))
+    check_common(f, ("dY", "off", "W", "dX"))
+    assert f(N=20) == SHAPE and f(K=60) == SHAPE and f(lddy=16) == SHAPE and f(ldw=56) == SHAPE and f(lddx=56) == SHAPE and f(N=0) == SHAPE
+    assert f(lddy=28) == ALIGN and f(lddx=68) == ALIGN and f(dX=FAKE + 8) == ALIGN
+    assert f(T=0) == 0 and f(E=0) == 0 and f(K=0) == 0
+
+
+def test_weight_gradient_refusals():
+    f = caller("rtl_grouped_linear_wgrad", dict(dY=FAKE, X=FAKE, off=FAKE, dW=FAKE, db=None, type=0, T=16, E=2, N=24, K=64, lddy=24, ldx=64, lddw=64,
+                                                sdw=24 * 64, ws=None, wsb=0, stream=None))
+    check_common(f, ("dY", "X", "off", "dW"))
+    assert f(type=2) == ARG and f(type=-1) == ARG
+    assert f(N=20) == SHAPE and f(K=60) == SHAPE and f(lddw=56) == SHAPE
+    assert f(sdw=23 * 64 + 56) == SHAPE and f(sdw=0) == SHAPE          # the experts' gradients would overlap
+    assert f(lddw=68, sdw=24 * 72) == ALIGN and f(dW=FAKE + 8) == ALIGN and f(db=FAKE + 1) == ALIGN and f(db=FAKE + 2, type=1) == ALIGN
+    assert f(E=0) == 0 and f(N=0) == 0 and f(K=0) == 0
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    w = torch.zeros(2, 8, 64, dtype=torch.bfloat16)
+    off = torch.zeros(3, dtype=torch.int32)
+    for f in (lambda: rtl.grouped_linear(x, off, w), lambda: rtl.grouped_linear_dgrad(x, off, w), lambda: rtl.grouped_linear_wgrad(x, x, off),
+              lambda: rtl.grouped_mxfp4_linear(x, off, w, w)):
+        with pytest.raises(ValueError):
+            f()
