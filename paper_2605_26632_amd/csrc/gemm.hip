@@ -232,7 +232,7 @@ static double simulate_schedule(int64_t nb, int64_t nt, double cb, double ct) {
     return worst;
 }
 
-static TilePlan make_plan(int64_t M, int64_t N, bool dense, bool fp4) {
+static TilePlan make_plan(int64_t M, int64_t N, bool dense) {
     const double c256 = dense ? 64 : 51, c192 = dense ? 56 : 43, c128 = 0.64 * c256;
     const int64_t tm = (M + 255) / 256;
     const int64_t n256 = (N + 255) / 256, n192 = (N + 191) / 192, n128 = (N + kTailBN - 1) / kTailBN;
@@ -240,9 +240,9 @@ static TilePlan make_plan(int64_t M, int64_t N, bool dense, bool fp4) {
         // very large grids: many rounds, the last one no longer matters; pick the cheaper uniform shape
         // by rounds x bytes per stage and skip the simulation (it is linear in the number of tiles)
         const double r256 = (double)((tm * n256 + 255) / 256) * c256, r192 = (double)((tm * n192 + 255) / 256) * c192;
-        return r192 < r256 || fp4 ? TilePlan{true, M, (int)(tm * n192), 0, r192} : TilePlan{false, M, (int)(tm * n256), 0, r256};
+        return r192 < r256 ? TilePlan{true, M, (int)(tm * n192), 0, r192} : TilePlan{false, M, (int)(tm * n256), 0, r256};
     }
-    double best_cost = fp4 ? 1e300 : simulate_schedule(tm * n256, 0, c256, c128);
+    double best_cost = simulate_schedule(tm * n256, 0, c256, c128);
     TilePlan best{false, M, (int)(tm * n256), 0, best_cost};
     auto consider = [&](bool use_192, int64_t p) {
         if (p < 0 || p > tm) return;
@@ -256,7 +256,7 @@ static TilePlan make_plan(int64_t M, int64_t N, bool dense, bool fp4) {
     };
     consider(true, tm);
     // body sizes that fill whole rounds of the chip, and a few panels around them
-    for (int use_192 = fp4; use_192 < 2; ++use_192) {
+    for (int use_192 = 0; use_192 < 2; ++use_192) {
         const int64_t tn = use_192 ? n192 : n256;
         const int64_t rounds = tm * tn / 256;
         for (int64_t r = rounds; r >= rounds - 1 && r >= 0; --r)
@@ -266,15 +266,15 @@ static TilePlan make_plan(int64_t M, int64_t N, bool dense, bool fp4) {
 }
 
 // Plans are cached per (M, N, kind): the simulation costs tens of microseconds on the host.
-static TilePlan plan_for(int64_t M, int64_t N, bool dense, bool fp4 = false) {
-    struct Entry { int64_t M, N; bool dense, fp4; TilePlan plan; };
+static TilePlan plan_for(int64_t M, int64_t N, bool dense) {
+    struct Entry { int64_t M, N; bool dense; TilePlan plan; };
     static std::mutex mu;
     static std::vector<Entry> cache;
     std::lock_guard<std::mutex> lock(mu);
     for (const Entry& e : cache)
-        if (e.M == M && e.N == N && e.dense == dense && e.fp4 == fp4) return e.plan;
-    const TilePlan p = make_plan(M, N, dense, fp4);
-    if (cache.size() < 4096) cache.push_back(Entry{M, N, dense, fp4, p});
+        if (e.M == M && e.N == N && e.dense == dense) return e.plan;
+    const TilePlan p = make_plan(M, N, dense);
+    if (cache.size() < 4096) cache.push_back(Entry{M, N, dense, p});
     return p;
 }
 
@@ -386,7 +386,7 @@ static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_
 size_t gemm_partial_bytes(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t room, bool fp4) {
     const int64_t blocks = k_blocks(K, fp8, fp4);
     if (blocks < 32 || ((M + 255) / 256) * ((N + 127) / 128) > 128) return 0;       // (the bound of the loop above at two splits)
-    const SplitChoice c = pick_split(plan_for(M, N, !sparse, fp4), M, N, blocks, !sparse, fp8, room);
+    const SplitChoice c = pick_split(plan_for(M, N, !sparse), M, N, blocks, !sparse, fp8, room);
     return c.k_splits > 1 ? (size_t)c.k_splits * (size_t)M * (size_t)part_pitch(N) * 4 : 0;
 }
 
@@ -398,7 +398,7 @@ void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t 
 }
 
 void mx_choice(int64_t M, int64_t N, int64_t K, size_t room, int out[3]) {
-    const SplitChoice c = pick_split(plan_for(M, N, true, true), M, N, k_blocks(K, false, true), true, false, room);
+    const SplitChoice c = pick_split(plan_for(M, N, true), M, N, k_blocks(K, false, true), true, false, room);
     out[0] = c.k_splits > 1 ? -1 : c.shape;
     out[1] = c.k_splits;
     out[2] = c.part_256 ? 256 : 128;
@@ -459,6 +459,7 @@ hipError_t prepare_gemm_kernels() {
     run(Mixed<false, 192, 2, 4, 2>::prepare());
     run(Mixed<false, 256, 2, 4, 2>::prepare());
     run(Mixed<false, 192, 2, 4, 2, 0, false, true, true>::prepare());
+    run(Mixed<false, 256, 2, 4, 2, 0, false, true, true>::prepare());
     auto prep = [](auto k) { return decltype(k)::prepare(); };
     for (int i = 0; i < 6; ++i) {
         run(with_split<true, 0, false, false>(i, prep));
@@ -481,7 +482,7 @@ hipError_t prepare_gemm_kernels() {
 
 hipError_t launch_gemm(bool sparse, const GemmArgs& a_in, hipStream_t stream) {
     GemmArgs a = a_in;
-    const TilePlan plan = plan_for(a.M, a.N, !sparse, a.fp4);
+    const TilePlan plan = plan_for(a.M, a.N, !sparse);
     a.m_split = plan.m_split;
     a.body_tiles = plan.body_tiles;
     a.tail_tiles = plan.tail_tiles;
@@ -542,7 +543,10 @@ hipError_t launch_gemm(bool sparse, const GemmArgs& a_in, hipStream_t stream) {
         if (lora) return Mixed<true, 256, 2, 4, 3, 1>::launch(a, stream);
         return Mixed<true, 256, 2, 4, 3>::launch(a, stream);
     }
-    if (a.fp4) return Mixed<false, 192, 2, 4, 2, 0, false, true, true>::launch(a, stream);
+    if (a.fp4) {
+        if (plan.use_192) return Mixed<false, 192, 2, 4, 2, 0, false, true, true>::launch(a, stream);
+        return Mixed<false, 256, 2, 4, 2, 0, false, true, true>::launch(a, stream);
+    }
     // dense: stages of 64 k (whole-line requests on the row-major operands), body tiles with a ring of two
     if (plan.use_192) return Mixed<false, 192, 2, 4, 2>::launch(a, stream);
     return Mixed<false, 256, 2, 4, 2>::launch(a, stream);

@@ -311,7 +311,25 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
             base_b -= 128;
         }
     }
-    uint32_t oa[A_PER_W];
+    // FP4 256 x 256: scales and fragments leave no room for an offset per request. A wave takes requests of one chunk order (eight rows each, all
+    // even or all odd), so that they differ in the row only, and forms each offset anew from the lane's first row and its chunk.
+    constexpr bool LEAN = FP4 && BM == 256 && BN == 256 && NW == 8;
+    constexpr int OA = LEAN ? 2 : A_PER_W, OB = LEAN ? 2 : B_PER_W;
+    auto lean_unit = [&](int s) { return (wave & 1) | s << 1 | (wave >> 1) << 3; };
+    auto lean_offset = [&](uint32_t first_row, int s, int64_t rows, int64_t ld, uint32_t chunk) {
+        asm volatile("" : "+v"(first_row));
+        return min(first_row + 16 * s, (uint32_t)(rows - 1)) * (uint32_t)ld + chunk;
+    };
+    // Chunk of memory that is kept at chunk place c of a row. FP4: a lane feeds places kb and 4 + kb to its two matrix instructions, as the others
+    // do (neighbouring places would meet the same banks), but they hold neighbouring chunks, whose scale bytes are neighbours too.
+    auto chunk_at = [](int c) { return FP4 ? (c & 3) << 1 | c >> 2 : c; };
+    uint32_t oa[OA];
+    if constexpr (LEAN) {
+        int row, c;
+        unswz8(lean_unit(0) * 64 + lane, row, c);
+        oa[0] = row;
+        oa[1] = chunk_at(c) * 16;
+    } else
 #pragma unroll
     for (int s = 0; s < A_PER_W; ++s) {
         const int p = (wave * A_PER_W + s) * 64 + lane;
@@ -320,16 +338,17 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         const int64_t gr = min((int64_t)row, rows_a - 1);
         // (the k-major buffer is padded to whole tiles: rows past M hold unspecified bytes whose
         //  products only reach outputs that are never stored)
-        oa[s] = SPARSE ? (uint32_t)(row * 64 + c * 16) : (uint32_t)(gr * a.lda * ESZ + c * 16);
+        oa[s] = SPARSE ? (uint32_t)(row * 64 + c * 16) : (uint32_t)(gr * a.lda * ESZ + chunk_at(c) * 16);
     }
-    uint32_t ob[B_PER_W];
+    uint32_t ob[OB];
+    if constexpr (!LEAN)
 #pragma unroll
     for (int s = 0; s < B_PER_W; ++s) {
         const int p = wave * B_CH + min(s * 64 + lane, B_CH - 1);   // masked lanes of a half load: any valid chunk
         int row, c;
         unswz8(p, row, c);
         const int64_t gr = min((int64_t)row, rows_b - 1);
-        ob[s] = (uint32_t)(gr * a.ldw * ESZ + c * 16);
+        ob[s] = (uint32_t)(gr * a.ldw * ESZ + chunk_at(c) * 16);
     }
     const uint8_t* base_m = nullptr;
     uint32_t om = 0;
@@ -343,18 +362,24 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     // FP4: the scales' records, 8 bytes per row and 256-k block, the rows of a block contiguous. A load moves those of 32 rows, of A or of B.
     const uint8_t* base_s[M_PER_W ? M_PER_W : 1];
     int64_t stride_s[M_PER_W ? M_PER_W : 1];
-    uint32_t os[M_PER_W ? M_PER_W : 1];
+    uint32_t os[LEAN || !M_PER_W ? 1 : M_PER_W];
+    auto scale_rows = [&](int s) { return min(wave * M_PER_W + s, M_LOADS - 1) < BM / 32 ? rows_a : rows_b; };
+    // (beyond the edge: the last four bytes of the last record, for outputs that are never stored)
+    auto scale_offset = [&](uint32_t lane4, int s) {
+        const int unit = min(wave * M_PER_W + s, M_LOADS - 1);
+        return min((uint32_t)((unit < BM / 32 ? unit : unit - BM / 32) * 256) + lane4, (uint32_t)(min(scale_rows(s), (int64_t)256) * MREC - 4));
+    };
     if constexpr (FP4) {
 #pragma unroll
         for (int s = 0; s < M_PER_W; ++s) {
+            if constexpr (LEAN) os[0] = lane * 4;
             const int unit = min(wave * M_PER_W + s, M_LOADS - 1);
             const bool of_a = unit < BM / 32;
             stride_s[s] = (of_a ? a.a_scale_rows : a.w_scale_rows) * MREC;
             base_s[s] = of_a ? a.a_scale + m0 * MREC : a.w_scale + n0 * MREC;
             if constexpr (PART) base_s[s] += kblk0 * stride_s[s];
             if (tail_chunks != 0) base_s[s] -= stride_s[s];
-            const int row = (of_a ? unit : unit - BM / 32) * 32 + lane / 2;
-            os[s] = (uint32_t)(min((int64_t)row, (of_a ? rows_a : rows_b) - 1) * MREC + (lane & 1) * 4);
+            if constexpr (!LEAN) os[s] = scale_offset(lane * 4, s);
             base_s[s] = reinterpret_cast<const uint8_t*>(uniform64(base_s[s]));
         }
     }
@@ -375,7 +400,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     auto gload_one = [&](int kt, int stage, auto n_tag) {
         constexpr int n = decltype(n_tag)::value;
         const uint32_t base = lds0 + stage * L::kStage;
-        if constexpr (n < A_PER_W) {
+        if constexpr (LEAN && n < A_PER_W) {
+            lds_dma16_so(base_a + (int64_t)kt * 128, lean_offset(oa[0], n, rows_a, a.lda, oa[1]), base + lean_unit(n) * 1024);
+        } else if constexpr (LEAN && n < A_PER_W + B_PER_W) {
+            lds_dma16_so(base_b + (int64_t)kt * 128, lean_offset(oa[0], n - A_PER_W, rows_b, a.ldw, oa[1]),
+                         base + L::kABytes + L::kMetaBytes + lean_unit(n - A_PER_W) * 1024);
+        } else if constexpr (n < A_PER_W) {
             lds_dma16_so(base_a + (int64_t)(kt * WAVES_K + wk) * a_stride, oa[n], base + (wave * A_PER_W + n) * 1024);
         } else if constexpr (n < A_PER_W + B_PER_W) {
             constexpr int s = n - A_PER_W;
@@ -391,7 +421,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
                         base + L::kABytes + (wave * M_PER_W + s) * 256);
         } else if constexpr (FP4 && n < A_PER_W + B_PER_W + M_PER_W) {
             constexpr int s = n - A_PER_W - B_PER_W;
-            lds_dma4_so(base_s[s] + (int64_t)(kt * WAVES_K + wk) * stride_s[s], os[s],
+            uint32_t at;
+            if constexpr (LEAN && n >= 0) {
+                uint32_t lane4 = os[0];
+                asm volatile("" : "+v"(lane4));
+                at = scale_offset(lane4, s);
+            } else {
+                at = os[s];
+            }
+            lds_dma4_so(base_s[s] + (int64_t)(kt * WAVES_K + wk) * stride_s[s], at,
                         base + L::kABytes + min(wave * M_PER_W + s, M_LOADS - 1) * 256);
         }
     };
@@ -401,15 +439,19 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     auto gload_tail = [&]() {
         static_for<LOADS_PER_STAGE>([&](auto n_tag) {
             constexpr int n = decltype(n_tag)::value;
-            if constexpr (n < A_PER_W) {
+            if constexpr (LEAN && n < A_PER_W + B_PER_W) {
+                if ((int)oa[1] < tail_chunks * 16) gload_one(all_blocks, 0, n_tag);
+            } else if constexpr (LEAN && n >= 0) {
+                gload_one(all_blocks, 0, n_tag);
+            } else if constexpr (n < A_PER_W) {
                 int row, c;
                 unswz8((wave * A_PER_W + n) * 64 + lane, row, c);
-                if (c < tail_chunks) lds_dma16_so(base_a + (int64_t)all_blocks * 128, oa[n], lds0 + (wave * A_PER_W + n) * 1024);
+                if (chunk_at(c) < tail_chunks) lds_dma16_so(base_a + (int64_t)all_blocks * 128, oa[n], lds0 + (wave * A_PER_W + n) * 1024);
             } else if constexpr (n < A_PER_W + B_PER_W) {
                 constexpr int s = n - A_PER_W;
                 int row, c;
                 unswz8(wave * B_CH + min(s * 64 + lane, B_CH - 1), row, c);
-                if (c < tail_chunks && s * 64 + lane < B_CH)
+                if (chunk_at(c) < tail_chunks && s * 64 + lane < B_CH)
                     lds_dma16_so(base_b + (int64_t)all_blocks * 128, ob[s], lds0 + L::kABytes + L::kMetaBytes + (wave * B_CH + s * 64) * 16);
             } else {
                 constexpr int s = n - A_PER_W - B_PER_W;
@@ -495,18 +537,24 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     //      R0 row blocks. One set of fragments: the A registers of a row block are refilled for the next stage behind its last
     //      matrix instruction, the B registers behind theirs in the last row block (two sets would not fit beside
     //      256 x 256 accumulators) -----------------------------------------------------------------------------------
-    constexpr int R0 = TM >= 4 ? 2 : 1, ROW = 2 * TN, M1 = (TM - R0) * ROW;       // ROW: matrix instructions of a row block
-    Frag16 fa[SPARSE ? 1 : TM], fb[SPARSE ? 1 : TN];
-    // Chunk of a row that a lane feeds to its matrix instruction c: FP4 takes neighbours, so that the scale bytes of both lie together.
-    auto chunk_of = [&](int c) { return FP4 ? 2 * kb + c : 4 * c + kb; };
-    // FP4: scale bytes of this and the next stage, those of two row blocks (then column blocks) of the lane to a word.
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    constexpr int R0 = LEAN ? 4 : TM >= 4 ? 2 : 1, ROW = 2 * TN, M1 = (TM - R0) * ROW;       // ROW: matrix instructions of a row block
+    // LEAN: six sets of A registers for the eight row blocks. The barrier comes in the middle of the stage; until then the last two row blocks
+    // are read behind the first two, into their registers.
+    constexpr int A_SETS = LEAN ? 6 : TM;
+    auto a_set = [](int i) { return i < A_SETS ? i : i - A_SETS; };
+    Frag16 fa[SPARSE ? 1 : A_SETS], fb[SPARSE ? 1 : TN];
+    // FP4: scale bytes of this stage, those of two row blocks (then column blocks) of the lane to a word, and of the next one as they were
+    // read. (Put together at the end of the stage: right behind the reads it would wait for them each time.)
     constexpr int SC_RD = FP4 ? TM + TN : 0, SC_W = (SC_RD + 1) / 2;
-    u16x2 sc[SC_W ? SC_W : 1], sc_nxt[SC_W ? SC_W : 1];
+    uint32_t sc[SC_W ? SC_W : 1], sc_nxt[2 * SC_W ? 2 * SC_W : 1];
+    auto take_scales = [&](uint32_t mask) {
+#pragma unroll
+        for (int e = 0; e < SC_W; ++e) sc[e] = (sc_nxt[2 * e] | (2 * e + 1 < SC_RD ? sc_nxt[2 * e + 1] << 16 : 0u)) & mask;
+    };
     auto read_scale = [&](int stage, auto e_tag) {
         constexpr int e = decltype(e_tag)::value;
         const uint8_t* rec = stage_base(stage) + L::kABytes + 2 * kb;
-        sc_nxt[e / 2][e % 2] = *reinterpret_cast<const uint16_t*>(
+        sc_nxt[e] = *reinterpret_cast<const uint16_t*>(
             e < TM ? rec + (arow0 + e * S) * MREC : rec + (BM + brow0 + (e - TM) * S) * MREC);
     };
     // LDS read e of a stage: 0 .. 2 TM - 1 the two chunks of each row block, then the chunks of the columns in the order in
@@ -517,10 +565,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         const uint8_t* base = stage_base(stage);
         const uint8_t* bB = base + L::kABytes + L::kMetaBytes;
         if constexpr (e < A_RD)
-            fa[e / 2].u[e % 2] = *reinterpret_cast<const uint4*>(base + swz8(arow0 + e / 2 * S, chunk_of(e % 2)));
+            fa[a_set(e / 2)].u[e % 2] = *reinterpret_cast<const uint4*>(base + swz8(arow0 + e / 2 * S, 4 * (e % 2) + kb));
         else
             fb[(e - A_RD) % TN].u[(e - A_RD) / TN] =
-                *reinterpret_cast<const uint4*>(bB + swz8(brow0 + (e - A_RD) % TN * S, chunk_of((e - A_RD) / TN)));
+                *reinterpret_cast<const uint4*>(bB + swz8(brow0 + (e - A_RD) % TN * S, 4 * ((e - A_RD) / TN) + kb));
     };
     // Which of them go behind which of the M1 matrix instructions that follow the barrier: as soon as their registers are
     // free, evenly spread. (The last row block's two follow the first matrix instructions of the next stage.)
@@ -542,12 +590,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         }
         return t;
     }();
-    static_assert(SPARSE || kSlots.total == A_RD - 2 + B_RD, "every read has a slot");
+    static_assert(SPARSE || LEAN || kSlots.total == A_RD - 2 + B_RD, "every read has a slot");
     auto mma_row = [&](auto i_tag, auto n_tag) {             // matrix instruction n of row block i
         constexpr int i = decltype(i_tag)::value, n = decltype(n_tag)::value, j = n % TN, c = n / TN;
         if constexpr (FP4) {
-            acc[i][j] = fp4_mma<2 * (i % 2) + c, 2 * ((TM + j) % 2) + c>(fa[i].u[c], fb[j].u[c], acc[i][j], __builtin_bit_cast(int, sc[i / 2]),
-                                                                         __builtin_bit_cast(int, sc[(TM + j) / 2]));
+            acc[i][j] = fp4_mma<2 * (i % 2) + c, 2 * ((TM + j) % 2) + c>(fa[a_set(i)].u[c], fb[j].u[c], acc[i][j], (int)sc[i / 2], (int)sc[(TM + j) / 2]);
             return;
         }
         const bf16x16 x = fa[i].v, y = fb[j].v;
@@ -588,13 +635,14 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
 #pragma unroll
             for (int i = 0; i < TM * IXW; ++i) ix[i] = ix_nxt[i];
         } else {
-            static_for<A_RD - 2>([&](auto e) { read_row(0, e); });
+            static_for<A_RD - 2>([&](auto e) {
+                constexpr int i = decltype(e)::value / 2;
+                if constexpr (!LEAN || (i != 1 && i < A_SETS)) read_row(0, e);
+            });
             static_for<B_RD>([&](auto e) { read_row(0, std::integral_constant<int, A_RD + decltype(e)::value>{}); });
             if constexpr (FP4) {
                 static_for<SC_RD>([&](auto e) { read_scale(0, e); });
-                const uint16_t keep = !tail_first ? 0xFFFF : (2 * kb < tail_chunks ? 0xFF : 0) | (2 * kb + 1 < tail_chunks ? 0xFF00 : 0);
-#pragma unroll
-                for (int e = 0; e < SC_W; ++e) sc[e] = sc_nxt[e] & u16x2{keep, keep};
+                take_scales(!tail_first ? ~0u : (2 * kb < tail_chunks ? 0xFF00FFu : 0u) | (2 * kb + 1 < tail_chunks ? 0xFF00FF00u : 0u));
             }
         }
     }
@@ -630,7 +678,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         else static_for<R0 * ROW>([&](auto n) {
             constexpr int m = decltype(n)::value;
             mma_row(std::integral_constant<int, m / ROW>{}, std::integral_constant<int, m % ROW>{});
-            if constexpr (m < 2) read_row(cur, std::integral_constant<int, A_RD - 2 + m>{});
+            if constexpr (LEAN) {
+                constexpr int item = m < 2 ? 2 + m : m == 8 || m == 9 ? 12 + m - 8 : m == 16 || m == 17 ? 14 + m - 16 : -1;      // row blocks 1, 6, 7
+                if constexpr (item >= 0) read_row(cur, std::integral_constant<int, item>{});
+            } else if constexpr (m < 2) read_row(cur, std::integral_constant<int, A_RD - 2 + m>{});
             requests(n, std::integral_constant<int, R0 * ROW>{}, a_lo{}, a_hi{}, kt + STAGES - 1, prv);
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -640,17 +691,21 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         else static_for<M1>([&](auto n) {
             constexpr int m = decltype(n)::value;
             mma_row(std::integral_constant<int, R0 + m / ROW>{}, std::integral_constant<int, m % ROW>{});
-            if constexpr (HAS_NEXT)
+            if constexpr (HAS_NEXT && LEAN) {
+                // row blocks 2, 3 at once, 4, 5 and 0 behind the row blocks that had their registers, B behind the last one, scales between
+                constexpr int a = m < 4 ? 4 + m : m == 8 || m == 9 ? m : m == 16 || m == 17 ? 10 + m - 16 : m == 24 || m == 25 ? m - 24 : -1;
+                constexpr int q = m >= 4 && m < 8 ? m - 4 : m >= 10 && m < 16 ? m - 6 : m == 18 || m == 19 ? m - 8 : -1;
+                if constexpr (a >= 0) read_row(nxt, std::integral_constant<int, a>{});
+                if constexpr (m >= 24) read_row(nxt, std::integral_constant<int, A_RD + m - 24>{});
+                if constexpr (q >= 0) read_scale(nxt, std::integral_constant<int, q>{});
+            } else if constexpr (HAS_NEXT)
                 static_for<kSlots.count[m]>([&](auto e) { read_row(nxt, std::integral_constant<int, kSlots.item[m][decltype(e)::value]>{}); });
-            if constexpr (HAS_NEXT && FP4)
+            if constexpr (HAS_NEXT && FP4 && !LEAN)
                 static_for<(m + 1) * SC_RD / M1 - m * SC_RD / M1>([&](auto e) { read_scale(nxt, std::integral_constant<int, m * SC_RD / M1 + decltype(e)::value>{}); });
             requests(n, std::integral_constant<int, M1>{}, c0{}, b_hi{}, kt + STAGES, cur);
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (HAS_NEXT && FP4) {
-#pragma unroll
-            for (int e = 0; e < SC_W; ++e) sc[e] = sc_nxt[e];
-        }
+        if constexpr (HAS_NEXT && FP4) take_scales(~0u);
         if constexpr (HAS_NEXT && SPARSE) {
 #pragma unroll
             for (int i = 0; i < TM * IXW; ++i) ix[i] = ix_nxt[i];
@@ -660,7 +715,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     static_assert(STAGES == 2 || STAGES == 3 || STAGES == 4, "ring depth");
     using P = std::integral_constant<int, STAGES - 2>;
     int kt = 0;
-    if (WAVES_K == 1 || KT > 0) {
+    if constexpr (LEAN) {
+        // (the last stage reads fragments that nobody uses: as a step of its own, without them, it came out of the compiler with spills)
+        for (; kt < KT - 2; ++kt) stage_step(kt, F{}, T{}, T{}, P{});
+        for (; kt < KT; ++kt) stage_step(kt, F{}, F{}, T{}, P{});
+    } else if (WAVES_K == 1 || KT > 0) {
         if (KT > STAGES) {
             // stage 0 has no half-requested predecessor; from then on both halves carry requests
             stage_step(kt, F{}, T{}, T{}, P{});

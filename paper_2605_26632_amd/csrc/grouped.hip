@@ -5,21 +5,52 @@
 namespace rtl {
 namespace {
 
+// The problem of `rows` rows of an expert.
+template <bool FP4>
+__device__ __forceinline__ GemmArgs expert_problem(const GemmArgs& a, const GroupArgs& g, int expert, int begin, int rows) {
+    constexpr int ESZ = FP4 ? 1 : 2;
+    GemmArgs b = a;
+    b.M = rows;
+    b.A = static_cast<const uint8_t*>(a.A) + begin * a.lda * ESZ;
+    b.W = static_cast<const uint8_t*>(a.W) + expert * g.w_stride * ESZ;
+    b.Y = a.Y + begin * a.ldy;
+    if (a.bias) b.bias = a.bias + expert * a.N;
+    if constexpr (FP4) {
+        b.a_scale = a.a_scale + (int64_t)begin * 8;
+        b.w_scale = a.w_scale + expert * a.N * 8;
+    }
+    return b;
+}
+
+template <bool FP4>
+__global__ __launch_bounds__(512) void grouped_mixed_kernel(const GemmArgs a, const GroupArgs g) {
+    MixedTile t;
+    if (!group_tile_mixed(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), t)) return;
+    const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
+    if (t.tall) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4>(b, t.tile);
+    else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4>(b, t.tile);
+}
+
+template <bool FP4>
+struct GroupedMixed {
+    using L0 = Smem<false, 256, 256, 2, 2, 4, false, 1, FP4>;
+    using L1 = Smem<false, 128, 256, 3, 2, 4, false, 1, FP4>;
+    static constexpr int kLds = L0::kTotal > L1::kTotal ? L0::kTotal : L1::kTotal;
+    static int64_t grid(int64_t T, int64_t E, int64_t N) { return group_grid(T, E, N, 128, 256); }
+    static hipError_t prepare() {
+        return hipFuncSetAttribute(reinterpret_cast<const void*>(grouped_mixed_kernel<FP4>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    }
+    static hipError_t launch(const GemmArgs& a, const GroupArgs& g, hipStream_t stream) {
+        hipLaunchKernelGGL(grouped_mixed_kernel<FP4>, dim3((unsigned)grid(a.M, g.experts, a.N)), dim3(512), kLds, stream, a, g);
+        return hipGetLastError();
+    }
+};
+
 template <bool FP4, int BM, int BN, int WAVES_M, int WAVES_N, int WAVES_K, int STAGES>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * WAVES_K * 64) void grouped_kernel(const GemmArgs a, const GroupArgs g) {
     GroupTile t;
     if (!group_tile(g.offsets, g.experts, (int)a.M, BM, (int)((a.N + BN - 1) / BN), t)) return;
-    constexpr int ESZ = FP4 ? 1 : 2;
-    GemmArgs b = a;
-    b.M = t.rows;
-    b.A = static_cast<const uint8_t*>(a.A) + t.begin * a.lda * ESZ;
-    b.W = static_cast<const uint8_t*>(a.W) + t.expert * g.w_stride * ESZ;
-    b.Y = a.Y + t.begin * a.ldy;
-    if (a.bias) b.bias = a.bias + t.expert * a.N;
-    if constexpr (FP4) {
-        b.a_scale = a.a_scale + (int64_t)t.begin * 8;
-        b.w_scale = a.w_scale + t.expert * a.N * 8;
-    }
+    const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
     gemm_tile<false, BM, BN, WAVES_M, WAVES_N, STAGES, 0, false, WAVES_K, false, false, true, FP4>(b, t.tile);
 }
 
@@ -45,7 +76,7 @@ auto with_grouped(int shape, Op op) {
         case 0: return op(Grouped<FP4, 32, 32, 1, 1, 4, 4>{});
         case 1: return op(Grouped<FP4, 64, 64, 1, 2, 2, 4>{});
         case 2: return op(Grouped<FP4, 128, 128, 2, 2, 1, 3>{});
-        default: return op(Grouped<FP4, 256, FP4 ? 192 : 256, 2, 4, 1, 2>{});
+        default: return op(GroupedMixed<FP4>{});
     }
 }
 

@@ -310,32 +310,53 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
     }
 }
 
+__device__ __forceinline__ GradArgs dgrad_problem(const GroupedGradArgs& a, int expert, int begin, int rows) {
+    GradArgs g;
+    g.A = a.dY + begin * a.lddy;
+    g.lda = a.lddy;
+    g.B = a.W + expert * a.w_stride;
+    g.ldb = a.ldw;
+    g.C = static_cast<uint16_t*>(a.out) + begin * a.ldo;
+    g.ldc = a.ldo;
+    g.m = rows;
+    g.n = a.K;
+    g.depth = a.N;
+    return g;
+}
+
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void dgrad_kernel(const GroupedGradArgs a) {
     GroupTile t;
     const int tiles_n = (int)((a.K + BN - 1) / BN);
     if (!group_tile(a.offsets, a.experts, (int)a.T, BM, tiles_n, t)) return;
-    GradArgs g;
-    g.A = a.dY + t.begin * a.lddy;
-    g.lda = a.lddy;
-    g.B = a.W + t.expert * a.w_stride;
-    g.ldb = a.ldw;
-    g.C = static_cast<uint16_t*>(a.out) + t.begin * a.ldo;
-    g.ldc = a.ldo;
-    g.m = t.rows;
-    g.n = a.K;
-    g.depth = a.N;
     int pm, pn;
-    tile_walk<8>(t.tile, (t.rows + BM - 1) / BM, tiles_n, pm, pn);
-    grad_tile<false, false, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
+    tile_walk<16>(t.tile, (t.rows + BM - 1) / BM, tiles_n, pm, pn);
+    grad_tile<false, false, BM, BN, WAVES_M, WAVES_N, STAGES>(dgrad_problem(a, t.expert, t.begin, t.rows), (int64_t)pm * BM, (int64_t)pn * BN);
+}
+
+__global__ __launch_bounds__(512) void dgrad_mixed_kernel(const GroupedGradArgs a) {
+    MixedTile t;
+    const int tiles_n = (int)((a.K + 255) / 256);
+    if (!group_tile_mixed(a.offsets, a.experts, (int)a.T, tiles_n, t)) return;
+    const GradArgs g = dgrad_problem(a, t.expert, t.begin, t.rows);
+    int pm, pn;
+    if (t.tall) {
+        tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
+        grad_tile<false, false, 256, 256, 2, 4, 2>(g, (int64_t)pm * 256, (int64_t)pn * 256);
+    } else {
+        tile_walk<16>(t.tile, t.panels, tiles_n, pm, pn);
+        grad_tile<false, false, 128, 256, 2, 4, 3>(g, (int64_t)pm * 128, (int64_t)pn * 256);
+    }
 }
 
 template <bool F32, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const GroupedGradArgs a) {
-    const int tiles_m = (int)((a.N + BM - 1) / BM), tiles_n = (int)((a.K + BN - 1) / BN), tiles = tiles_m * tiles_n;
-    const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8;
-    const int t = xcd_share_start((int)gridDim.x, xcd) + local;
-    const int e = t / tiles;
+    // Every XCD takes an eighth of every expert's tiles (neighbours in the walk), so that uneven experts do not make uneven XCDs; which
+    // eighth turns with the expert, for experts of fewer than eight tiles.
+    const int tiles_m = (int)((a.N + BM - 1) / BM), tiles_n = (int)((a.K + BN - 1) / BN), tiles = tiles_m * tiles_n, per = (tiles + 7) / 8;
+    const int e = (int)blockIdx.x / 8 / per, share = ((int)blockIdx.x + e) % 8;
+    const int t = xcd_share_start(tiles, share) + (int)blockIdx.x / 8 % per;
+    if (t >= xcd_share_start(tiles, share + 1)) return;
     const RowRange r = expert_rows(a.offsets, e, (int)a.T);
     GradArgs g;
     g.A = a.dY + r.begin * a.lddy;
@@ -349,7 +370,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
     g.n = a.K;
     g.depth = r.end - r.begin;
     int pm, pn;
-    tile_walk<8>(t % tiles, tiles_m, tiles_n, pm, pn);
+    tile_walk<8>(t, tiles_m, tiles_n, pm, pn);
     grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
 }
 
@@ -362,13 +383,21 @@ __global__ __launch_bounds__(256) void bgrad_kernel(const GroupedGradArgs a) {
     const RowRange r = expert_rows(a.offsets, e, (int)a.T);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (col < a.N)
-        for (int row = r.begin + threadIdx.x / 8; row < r.end; row += 32) {
-            const uint4 v = *reinterpret_cast<const uint4*>(a.dY + row * a.lddy + col);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        for (int row = r.begin + threadIdx.x / 8; row < r.end; row += 32 * 8) {       // eight loads in flight
+            uint4 v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sum[2 * i] += __uint_as_float(w[i] << 16);
-                sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+            for (int u = 0; u < 8; ++u) {
+                v[u] = make_uint4(0, 0, 0, 0);
+                if (row + 32 * u < r.end) v[u] = *reinterpret_cast<const uint4*>(a.dY + (row + 32 * u) * a.lddy + col);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum[2 * i] += __uint_as_float(w[i] << 16);
+                    sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+                }
             }
         }
 #pragma unroll
@@ -388,7 +417,7 @@ template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 struct Grad {
     using L = GradSmem<BM, BN, WAVES_M, WAVES_N, STAGES>;
     static int64_t dgrad_grid(int64_t T, int64_t E, int64_t K) { return group_grid(T, E, K, BM, BN); }
-    static int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) { return E * ((N + BM - 1) / BM) * ((K + BN - 1) / BN); }
+    static int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) { return E * 8 * ((((N + BM - 1) / BM) * ((K + BN - 1) / BN) + 7) / 8); }
     static constexpr dim3 block() { return dim3(WAVES_M * WAVES_N * 64); }
     static hipError_t limit(const void* k) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, L::kTotal); }
     static hipError_t prepare_dgrad() { return limit(reinterpret_cast<const void*>(dgrad_kernel<BM, BN, WAVES_M, WAVES_N, STAGES>)); }
@@ -409,12 +438,26 @@ struct Grad {
     }
 };
 
+struct DgradMixed {
+    using L0 = GradSmem<256, 256, 2, 4, 2>;
+    using L1 = GradSmem<128, 256, 2, 4, 3>;
+    static constexpr int kLds = L0::kTotal > L1::kTotal ? L0::kTotal : L1::kTotal;
+    static int64_t dgrad_grid(int64_t T, int64_t E, int64_t K) { return group_grid(T, E, K, 128, 256); }
+    static hipError_t prepare_dgrad() {
+        return hipFuncSetAttribute(reinterpret_cast<const void*>(dgrad_mixed_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    }
+    static hipError_t dgrad(const GroupedGradArgs& a, hipStream_t stream) {
+        hipLaunchKernelGGL(dgrad_mixed_kernel, dim3((unsigned)dgrad_grid(a.T, a.experts, a.K)), dim3(512), kLds, stream, a);
+        return hipGetLastError();
+    }
+};
+
 template <class Op>
 auto with_dgrad(int shape, Op op) {
     switch (shape) {
         case 0: return op(Grad<64, 128, 1, 4, 4>{});
         case 1: return op(Grad<128, 128, 2, 2, 2>{});
-        default: return op(Grad<256, 256, 2, 4, 2>{});
+        default: return op(DgradMixed{});
     }
 }
 template <class Op>

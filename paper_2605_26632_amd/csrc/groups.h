@@ -65,5 +65,83 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
     return false;
 }
 
+// Two tile heights in one launch, for experts of many rows: as many 256-row panels as fill whole rounds of the chip, the rest of the rows in 128-row
+// ones. An expert's last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts,
+// 4096 columns: 576 tiles of 256 x 256, 2.25 rounds that cost 3).
+struct MixedTile {
+    bool tall;                           // 256 rows, else 128
+    int expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
+};
+constexpr int kUnits = 256;              // compute units
+constexpr float kHalfCost = 0.6f;        // time of a 128 x 256 tile in those of a 256 x 256 one
+
+__device__ __forceinline__ float mixed_rounds(int tall, int half) {      // rounds that `tall` tiles and then `half` tiles take
+    const int full = (tall + kUnits - 1) / kUnits, over = max(0, half - (full * kUnits - tall));
+    return (float)full + (float)((over + kUnits - 1) / kUnits) * kHalfCost;
+}
+
+__device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int T, int tiles_n, MixedTile& out) {
+    const int lane = threadIdx.x & 63, grid = (int)gridDim.x, most = grid / tiles_n;
+    auto lane_rows = [&](int e0) {
+        RowRange r{0, 0};
+        if (e0 + lane < E) r = expert_rows(offsets, e0 + lane, T);
+        return r;
+    };
+    auto scan = [&](int n) {             // inclusive
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int up = __shfl_up(n, d);
+            if (lane >= d) n += up;
+        }
+        return n;
+    };
+    // panels of all experts: full ones, and 128-row ones of what is left of each (sums cut to the grid's size: see group_tile)
+    RowRange r = lane_rows(0);
+    int full = 0, rest = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const RowRange x = e0 ? lane_rows(e0) : r;
+        const int n = x.end - x.begin;
+        full = min(full + __builtin_amdgcn_readlane(scan(n / 256), 63), most);
+        rest = min(rest + __builtin_amdgcn_readlane(scan((n % 256 + 127) / 128), 63), most);
+    }
+    int p = full;
+    float best = mixed_rounds(full * tiles_n, rest * tiles_n);
+    for (int k = full * tiles_n / kUnits, i = 0; i < 2 && k >= 0; ++i, --k) {
+        const int q = min(k * kUnits / tiles_n, full);
+        const float c = mixed_rounds(q * tiles_n, (2 * (full - q) + rest) * tiles_n);
+        if (c < best) {
+            best = c;
+            p = q;
+        }
+    }
+    const int nb = p * tiles_n, nt = (2 * (full - p) + rest) * tiles_n;
+    const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8, nb_x = nb / 8 + (xcd < nb % 8);
+    if (local >= xcd_share_start(nb + nt, xcd + 1) - xcd_share_start(nb + nt, xcd)) return false;
+    out.tall = local < nb_x;
+    const int t = out.tall ? xcd_share_start(nb, xcd) + local : xcd_share_start(nb + nt, xcd) - xcd_share_start(nb, xcd) + (local - nb_x);
+    const int panel = t / tiles_n;
+    int before = 0, full_before = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        if (e0) r = lane_rows(e0);
+        const int n = r.end - r.begin, f = n / 256, f_upto = scan(f);
+        const int taken = min(max(p - (full_before + f_upto - f), 0), f);         // tall panels of the lane's expert
+        const int count = out.tall ? taken : 2 * (f - taken) + (n % 256 + 127) / 128, upto = scan(count);
+        const uint64_t hit = __ballot(before + upto > panel);
+        if (hit) {
+            const int l = __builtin_ctzll(hit), cut = __builtin_amdgcn_readlane(taken, l) * 256;
+            const int begin = __builtin_amdgcn_readlane(r.begin, l), end = __builtin_amdgcn_readlane(r.end, l);
+            out.expert = e0 + l;
+            out.begin = out.tall ? begin : begin + cut;
+            out.rows = out.tall ? cut : end - begin - cut;
+            out.panels = __builtin_amdgcn_readlane(count, l);
+            out.tile = t - (before + __builtin_amdgcn_readlane(upto, l) - out.panels) * tiles_n;
+            return true;
+        }
+        before = min(before + __builtin_amdgcn_readlane(upto, 63), 1 << 28);
+        full_before = min(full_before + __builtin_amdgcn_readlane(f_upto, 63), 1 << 28);
+    }
+    return false;
+}
+
 }  // namespace
 }  // namespace rtl
