@@ -356,47 +356,62 @@ def sparse_lora_linear_fp8(X, Wq, x_scale, LA, LB, bias=None, comp=COMP_GROUP, e
 
 # ---- microscaled 4-bit floating point (MXFP4): uint8 tensors, two codes to a byte -----------------
 
-def _on_current(*ts):
-    """Device tensors of the current device only: the launch goes to its current stream."""
-    _need_cuda(*ts)
-    cur = torch.cuda.current_device()
+# These checks run on every call and a small product takes the GPU less time than they do: each property of a tensor is asked for once.
+
+def _here(*ts):
+    """Number of the current device, which has to hold all of the tensors: the launch goes to its current stream."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
     for t in ts:
-        if t is not None and t.device.index != cur:
-            raise ValueError("tensor on %s, current device is cuda:%d" % (t.device, cur))
+        if t is not None and (t.get_device() != dev or dev < 0):
+            raise ValueError("librtlynx takes tensors of the current device (%d) only, not of %s" % (dev, t.device))
+    return dev
 
 
-def _matrix(t, dtype, name, dim=2):
-    if t.dtype != dtype or t.dim() != dim or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError("%s: %s tensor of %d dimensions with contiguous rows expected" % (name, dtype, dim))
+def _matrix(t, dtype, name):
+    """(rows, columns, row stride). torch leaves any stride there for a single row."""
+    stride = t.stride()
+    if len(stride) != 2 or t.dtype is not dtype:
+        raise ValueError("%s: %s matrix expected" % (name, dtype))
+    rows, cols = t.shape
+    if stride[1] != 1 and cols > 1:
+        raise ValueError("%s: contiguous rows expected" % name)
+    return rows, cols, stride[0] if rows > 1 else cols
 
 
-def _vector(t, n, name, dtype=torch.bfloat16):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
-        raise ValueError("%s: contiguous %s tensor of %d expected" % (name, dtype, n))
+def _stack(t, dtype, name):
+    """(matrices, rows, columns, row stride, matrix stride)."""
+    stride = t.stride()
+    if len(stride) != 3 or t.dtype is not dtype:
+        raise ValueError("%s: stack of %s matrices expected" % (name, dtype))
+    n, rows, cols = t.shape
+    if stride[2] != 1 and cols > 1:
+        raise ValueError("%s: contiguous rows expected" % name)
+    return n, rows, cols, stride[1] if rows > 1 else cols, stride[0] if n > 1 else 0
 
 
-def _ld(t):
-    """Row stride; torch leaves any value there for a single row."""
-    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+def _whole(t, shape, dtype, name):
+    """A contiguous tensor of just this shape, or None."""
+    if t is not None and (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()):
+        raise ValueError("%s: contiguous %s tensor of shape %s expected" % (name, dtype, tuple(shape)))
 
 
-def _given(out, shape, dtype, like, name="out"):
+def _output(out, rows, cols, dtype, like, new=torch.empty):
+    """(out or a new tensor, its row stride)."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    _matrix(out, dtype, name, len(shape))
-    if tuple(out.shape) != tuple(shape):
-        raise ValueError("%s: shape %s expected" % (name, tuple(shape)))
-    return out
+        return new((rows, cols), dtype=dtype, device=like.device), cols
+    m, n, ld = _matrix(out, dtype, "out")
+    if m != rows or n != cols:
+        raise ValueError("out: shape (%d, %d) expected" % (rows, cols))
+    return out, ld
+
+
+def _on(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def mxfp4_scales_shape(rows, cols):
     """Shape of the scale bytes of a [rows, cols] matrix: byte of block b = col // 32 of row r at [b // 8, r, b % 8]."""
     return ((cols + 255) // 256, rows, 8)
-
-
-def _scales(S, rows, cols, name):
-    if S.dtype != torch.uint8 or tuple(S.shape) != mxfp4_scales_shape(rows, cols) or not S.is_contiguous():
-        raise ValueError("%s: contiguous uint8 tensor of shape %s expected" % (name, mxfp4_scales_shape(rows, cols)))
 
 
 def quantize_mxfp4(X, along="cols", out=None):
@@ -405,43 +420,34 @@ def quantize_mxfp4(X, along="cols", out=None):
     ((Q, S, Qt, St)). uint8 tensors; S has mxfp4_scales_shape."""
     if along not in ("cols", "rows", "both"):
         raise ValueError("along: 'cols', 'rows' or 'both'")
-    _on_current(X)
-    _matrix(X, torch.bfloat16, "X")
-    rows, cols = X.shape
-    pad = (rows + 31) // 32 * 32
-    shapes = []
+    dev = _here(X, *(out or ()))
+    rows, cols, ld = _matrix(X, torch.bfloat16, "X")
+    u8, pad = torch.uint8, (rows + 31) // 32 * 32
+    if out is not None and len(out) != (4 if along == "both" else 2):
+        raise ValueError("out: %d tensors expected" % (4 if along == "both" else 2))
+    q = s = qt = st = None
+    ldq = ldqt = 0
     if along != "rows":
-        shapes += [(rows, cols // 2), mxfp4_scales_shape(rows, cols)]
+        q, ldq = _output(out and out[0], rows, cols // 2, u8, X)
+        shape = mxfp4_scales_shape(rows, cols)
+        s = out[1] if out else torch.empty(shape, dtype=u8, device=X.device)
+        _whole(s, shape, u8, "out")
     if along != "cols":
-        shapes += [(cols, pad // 2), mxfp4_scales_shape(cols, pad)]
-    if out is None:
-        out = tuple(torch.empty(s, dtype=torch.uint8, device=X.device) for s in shapes)
-    else:
-        _on_current(*out)
-        if len(out) != len(shapes):
-            raise ValueError("out: %d tensors expected" % len(shapes))
-        for i in range(0, len(out), 2):
-            _given(out[i], shapes[i], torch.uint8, X)
-            if tuple(out[i + 1].shape) != shapes[i + 1] or out[i + 1].dtype != torch.uint8 or not out[i + 1].is_contiguous():
-                raise ValueError("out: contiguous uint8 scales of shape %s expected" % (shapes[i + 1],))
-    a = [None, 0, None]
-    b = [None, 0, None]
-    if along != "rows":
-        a = [_p(out[0]), _ld(out[0]), _p(out[1])]
-    if along != "cols":
-        b = [_p(out[-2]), _ld(out[-2]), _p(out[-1])]
-    _check(lib().rtl_quantize_mxfp4(_p(X), rows, cols, _ld(X), *a, *b, _stream()), "rtl_quantize_mxfp4")
-    return out
+        qt, ldqt = _output(out and out[-2], cols, pad // 2, u8, X)
+        shape = mxfp4_scales_shape(cols, pad)
+        st = out[-1] if out else torch.empty(shape, dtype=u8, device=X.device)
+        _whole(st, shape, u8, "out")
+    _check(lib().rtl_quantize_mxfp4(_p(X), rows, cols, ld, _p(q), ldq, _p(s), _p(qt), ldqt, _p(st), _on(dev)), "rtl_quantize_mxfp4")
+    return (q, s, qt, st) if along == "both" else (q, s) if along == "cols" else (qt, st)
 
 
 def dequantize_mxfp4(Q, S, out=None):
     """rtl_dequantize_mxfp4: codes [rows, cols/2] and scales -> bf16 [rows, cols]."""
-    _on_current(Q, S, out)
-    _matrix(Q, torch.uint8, "Q")
-    rows, cols = Q.shape[0], Q.shape[1] * 2
-    _scales(S, rows, cols, "S")
-    X = _given(out, (rows, cols), torch.bfloat16, Q)
-    _check(lib().rtl_dequantize_mxfp4(_p(Q), _ld(Q), _p(S), rows, cols, _p(X), _ld(X), _stream()), "rtl_dequantize_mxfp4")
+    dev = _here(Q, S, out)
+    rows, half, ldq = _matrix(Q, torch.uint8, "Q")
+    _whole(S, mxfp4_scales_shape(rows, half * 2), torch.uint8, "S")
+    X, ld = _output(out, rows, half * 2, torch.bfloat16, Q)
+    _check(lib().rtl_dequantize_mxfp4(_p(Q), ldq, _p(S), rows, half * 2, _p(X), ld, _on(dev)), "rtl_dequantize_mxfp4")
     return X
 
 
@@ -451,23 +457,26 @@ def mxfp4_packed_linear_workspace(M, N, K):
 
 def mxfp4_packed_linear(Xq, Xs, Wq, Ws, bias=None, out=None, ws=None):
     """rtl_mxfp4_packed_linear: Y = Xq Wq^T (+ bias) on codes and scales of quantize_mxfp4, bf16 [M,N]."""
-    _on_current(Xq, Xs, Wq, Ws, bias, out, ws)
-    _matrix(Xq, torch.uint8, "Xq")
-    _matrix(Wq, torch.uint8, "Wq")
-    M, N, K = Xq.shape[0], Wq.shape[0], Wq.shape[1] * 2
-    if Xq.shape[1] * 2 != K:
+    dev = _here(Xq, Xs, Wq, Ws, bias, out, ws)
+    M, half, ldx = _matrix(Xq, torch.uint8, "Xq")
+    N, half_w, ldw = _matrix(Wq, torch.uint8, "Wq")
+    K = half * 2
+    if half_w != half:
         raise ValueError("Xq and Wq differ in K")
-    _scales(Xs, M, K, "Xs")
-    _scales(Ws, N, K, "Ws")
-    _vector(bias, N, "bias")
-    Y = _given(out, (M, N), torch.bfloat16, Wq)
+    _whole(Xs, mxfp4_scales_shape(M, K), torch.uint8, "Xs")
+    _whole(Ws, mxfp4_scales_shape(N, K), torch.uint8, "Ws")
+    _whole(bias, (N,), torch.bfloat16, "bias")
+    Y, ldy = _output(out, M, N, torch.bfloat16, Wq)
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_mxfp4_packed_linear_workspace(M, N, K), Wq.device)
-    st = L.rtl_mxfp4_packed_linear(_p(Xq), _p(Xs), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, _ld(Xq), _ld(Wq), _ld(Y),
-                                   _p(ws), ws.numel(), _stream())
+    st = L.rtl_mxfp4_packed_linear(_p(Xq), _p(Xs), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, ldx, ldw, ldy, _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_mxfp4_packed_linear")
     return Y
+
+
+def _bytes(ws):
+    return ws.numel() * ws.element_size() if ws.is_contiguous() else 0
 
 
 def mxfp4_linear_workspace(M, N, K):
@@ -476,73 +485,51 @@ def mxfp4_linear_workspace(M, N, K):
 
 def mxfp4_linear(X, Wq, Ws, bias=None, out=None, ws=None):
     """rtl_mxfp4_linear: Y = mxfp4(X) Wq^T (+ bias), X bf16 [M,K] quantised in the call, bf16 [M,N]."""
-    _on_current(X, Wq, Ws, bias, out, ws)
-    _matrix(X, torch.bfloat16, "X")
-    _matrix(Wq, torch.uint8, "Wq")
-    M, K = X.shape
-    N = Wq.shape[0]
-    if Wq.shape[1] * 2 != K:
+    dev = _here(X, Wq, Ws, bias, out, ws)
+    M, K, ldx = _matrix(X, torch.bfloat16, "X")
+    N, half, ldw = _matrix(Wq, torch.uint8, "Wq")
+    if half * 2 != K:
         raise ValueError("X and Wq differ in K")
-    _scales(Ws, N, K, "Ws")
-    _vector(bias, N, "bias")
-    Y = _given(out, (M, N), torch.bfloat16, X)
+    _whole(Ws, mxfp4_scales_shape(N, K), torch.uint8, "Ws")
+    _whole(bias, (N,), torch.bfloat16, "bias")
+    Y, ldy = _output(out, M, N, torch.bfloat16, X)
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_mxfp4_linear_workspace(M, N, K), X.device)
-    st = L.rtl_mxfp4_linear(_p(X), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, _ld(X), _ld(Wq), _ld(Y), _p(ws), ws.numel(), _stream())
+    st = L.rtl_mxfp4_linear(_p(X), _p(Wq), _p(Ws), _p(bias), _p(Y), M, N, K, ldx, ldw, ldy, _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_mxfp4_linear")
     return Y
 
 
 # ---- linears grouped by expert: rows offsets[e] .. offsets[e + 1] of the activation belong to weight e ------------
-
-def _experts(offsets, W, dtype, name):
-    """(experts, rows, row length, row stride, expert stride) of a stack of weights, after checking it and the offsets."""
-    _matrix(W, dtype, name, 3)
-    E, N, K = W.shape
-    if offsets.dtype != torch.int32 or tuple(offsets.shape) != (E + 1,) or not offsets.is_contiguous():
-        raise ValueError("offsets: contiguous int32 tensor of %d expected" % (E + 1))
-    return E, N, K, _ld(W), W.stride(0) if E > 1 else 0
-
-
-def _group_bias(bias, E, N):
-    if bias is not None and (bias.dtype != torch.bfloat16 or tuple(bias.shape) != (E, N) or not bias.is_contiguous()):
-        raise ValueError("bias: contiguous bf16 tensor of shape (%d, %d) expected" % (E, N))
-
-
-def _group_out(out, shape, like):
-    """Rows of no expert are left alone: zeros in a new tensor."""
-    if out is None:
-        return torch.zeros(shape, dtype=torch.bfloat16, device=like.device)
-    return _given(out, shape, torch.bfloat16, like)
-
+# `out` of the row-wise results: rows of no expert keep what it held; without `out` they are zeros.
 
 def grouped_linear(X, offsets, W, bias=None, out=None):
     """rtl_grouped_linear: Y[rows of e] = X[rows of e] W[e]^T (+ bias[e]); X bf16 [T,K], offsets int32 [E+1] on the device,
-    W bf16 [E,N,K], bias [E,N]; bf16 [T,N]. Rows of no expert keep what `out` held (zeros without `out`)."""
-    _on_current(X, offsets, W, bias, out)
-    _matrix(X, torch.bfloat16, "X")
-    E, N, K, ldw, stride = _experts(offsets, W, torch.bfloat16, "W")
-    T = X.shape[0]
-    if X.shape[1] != K:
+    W bf16 [E,N,K], bias [E,N]; bf16 [T,N]."""
+    dev = _here(X, offsets, W, bias, out)
+    T, K, ldx = _matrix(X, torch.bfloat16, "X")
+    E, N, K_w, ldw, stride = _stack(W, torch.bfloat16, "W")
+    if K_w != K:
         raise ValueError("X and W differ in K")
-    _group_bias(bias, E, N)
-    Y = _group_out(out, (T, N), X)
-    st = lib().rtl_grouped_linear(_p(X), _p(offsets), _p(W), _p(bias), _p(Y), T, E, N, K, _ld(X), ldw, stride, _ld(Y), _stream())
+    _whole(offsets, (E + 1,), torch.int32, "offsets")
+    _whole(bias, (E, N), torch.bfloat16, "bias")
+    Y, ldy = _output(out, T, N, torch.bfloat16, X, torch.zeros)
+    st = lib().rtl_grouped_linear(_p(X), _p(offsets), _p(W), _p(bias), _p(Y), T, E, N, K, ldx, ldw, stride, ldy, _on(dev))
     _check(st, "rtl_grouped_linear")
     return Y
 
 
 def grouped_linear_dgrad(dY, offsets, W, out=None):
     """rtl_grouped_linear_dgrad: dX[rows of e] = dY[rows of e] W[e]; bf16 [T,K]."""
-    _on_current(dY, offsets, W, out)
-    _matrix(dY, torch.bfloat16, "dY")
-    E, N, K, ldw, stride = _experts(offsets, W, torch.bfloat16, "W")
-    T = dY.shape[0]
-    if dY.shape[1] != N:
+    dev = _here(dY, offsets, W, out)
+    T, N, lddy = _matrix(dY, torch.bfloat16, "dY")
+    E, N_w, K, ldw, stride = _stack(W, torch.bfloat16, "W")
+    if N_w != N:
         raise ValueError("dY and W differ in N")
-    dX = _group_out(out, (T, K), dY)
-    st = lib().rtl_grouped_linear_dgrad(_p(dY), _p(offsets), _p(W), _p(dX), T, E, N, K, _ld(dY), ldw, stride, _ld(dX), _stream())
+    _whole(offsets, (E + 1,), torch.int32, "offsets")
+    dX, ldx = _output(out, T, K, torch.bfloat16, dY, torch.zeros)
+    st = lib().rtl_grouped_linear_dgrad(_p(dY), _p(offsets), _p(W), _p(dX), T, E, N, K, lddy, ldw, stride, ldx, _on(dev))
     _check(st, "rtl_grouped_linear_dgrad")
     return dX
 
@@ -554,31 +541,31 @@ def grouped_linear_wgrad_workspace(T, E, N, K):
 def grouped_linear_wgrad(dY, X, offsets, with_bias=False, dtype=torch.bfloat16, out=None, ws=None):
     """rtl_grouped_linear_wgrad: (dW [E,N,K], db [E,N] or None), dW[e] = dY[rows of e]^T X[rows of e], db[e] the sum of the rows of
     dY, in bf16 or float32. `out`: the two tensors (the second None without a bias); they then settle with_bias and dtype."""
-    _on_current(dY, X, offsets, ws)
-    _matrix(dY, torch.bfloat16, "dY")
-    _matrix(X, torch.bfloat16, "X")
-    T, N = dY.shape
-    K, E = X.shape[1], offsets.shape[0] - 1
-    if X.shape[0] != T:
+    dW, db = out if out is not None else (None, None)
+    dev = _here(dY, X, offsets, dW, db, ws)
+    T, N, lddy = _matrix(dY, torch.bfloat16, "dY")
+    T_x, K, ldx = _matrix(X, torch.bfloat16, "X")
+    if T_x != T:
         raise ValueError("dY and X differ in rows")
+    E = offsets.numel() - 1
+    if E < 0:
+        raise ValueError("offsets: at least one number expected")
+    _whole(offsets, (E + 1,), torch.int32, "offsets")
     if out is None:
         dW = torch.empty((E, N, K), dtype=dtype, device=dY.device)
         db = torch.empty((E, N), dtype=dtype, device=dY.device) if with_bias else None
-    else:
-        dW, db = out
-        dtype = dW.dtype
-        _on_current(dW, db)
-    if dtype not in (torch.bfloat16, torch.float32):
+    dtype = dW.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("gradients in bf16 or float32")
-    if E < 0 or tuple(_experts(offsets, dW, dtype, "dW")[:3]) != (E, N, K):
-        raise ValueError("dW: shape %s expected" % ((E, N, K),))
-    if db is not None and (db.dtype != dtype or tuple(db.shape) != (E, N) or not db.is_contiguous()):
-        raise ValueError("db: contiguous %s tensor of shape %s expected" % (dtype, (E, N)))
+    e, n, k, lddw, stride = _stack(dW, dtype, "dW")
+    if e != E or n != N or k != K:
+        raise ValueError("dW: shape (%d, %d, %d) expected" % (E, N, K))
+    _whole(db, (E, N), dtype, "db")
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_grouped_linear_wgrad_workspace(T, E, N, K), dY.device)
-    st = L.rtl_grouped_linear_wgrad(_p(dY), _p(X), _p(offsets), _p(dW), _p(db), 1 if dtype == torch.float32 else 0, T, E, N, K,
-                                    _ld(dY), _ld(X), _ld(dW), dW.stride(0) if E > 1 else 0, _p(ws), ws.numel(), _stream())
+    st = L.rtl_grouped_linear_wgrad(_p(dY), _p(X), _p(offsets), _p(dW), _p(db), 1 if dtype is torch.float32 else 0, T, E, N, K,
+                                    lddy, ldx, lddw, stride, _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_grouped_linear_wgrad")
     return dW, db
 
@@ -590,20 +577,19 @@ def grouped_mxfp4_linear_workspace(T, E, N, K):
 def grouped_mxfp4_linear(X, offsets, Wq, Ws, bias=None, out=None, ws=None):
     """rtl_grouped_mxfp4_linear: grouped_linear with X quantised in the call and 4-bit weights: Wq uint8 [E,N,K/2], Ws the scales of
     the [E*N, K] matrix of all rows (what quantize_mxfp4(W.view(E * N, K)) returns); bf16 [T,N]."""
-    _on_current(X, offsets, Wq, Ws, bias, out, ws)
-    _matrix(X, torch.bfloat16, "X")
-    E, N, half, ldw, stride = _experts(offsets, Wq, torch.uint8, "Wq")
-    T, K = X.shape
+    dev = _here(X, offsets, Wq, Ws, bias, out, ws)
+    T, K, ldx = _matrix(X, torch.bfloat16, "X")
+    E, N, half, ldw, stride = _stack(Wq, torch.uint8, "Wq")
     if half * 2 != K:
         raise ValueError("X and Wq differ in K")
-    _scales(Ws, E * N, K, "Ws")
-    _group_bias(bias, E, N)
-    Y = _group_out(out, (T, N), X)
+    _whole(offsets, (E + 1,), torch.int32, "offsets")
+    _whole(Ws, mxfp4_scales_shape(E * N, K), torch.uint8, "Ws")
+    _whole(bias, (E, N), torch.bfloat16, "bias")
+    Y, ldy = _output(out, T, N, torch.bfloat16, X, torch.zeros)
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_grouped_mxfp4_linear_workspace(T, E, N, K), X.device)
-    st = L.rtl_grouped_mxfp4_linear(_p(X), _p(offsets), _p(Wq), _p(Ws), _p(bias), _p(Y), T, E, N, K, _ld(X), ldw, stride, _ld(Y),
-                                    _p(ws), ws.numel(), _stream())
+    st = L.rtl_grouped_mxfp4_linear(_p(X), _p(offsets), _p(Wq), _p(Ws), _p(bias), _p(Y), T, E, N, K, ldx, ldw, stride, ldy, _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_grouped_mxfp4_linear")
     return Y
 

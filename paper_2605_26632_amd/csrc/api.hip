@@ -41,7 +41,7 @@ rtl_status device_ready(void** scratch_out = nullptr) {
             } else {
                 if (rtl::prepare_pack_kernels() != hipSuccess || rtl::prepare_gemm_kernels() != hipSuccess ||
                     rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_mx_kernels() != hipSuccess ||
-                    rtl::prepare_grouped_kernels() != hipSuccess || rtl::prepare_grouped_grad_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
+                    rtl::prepare_grouped_kernels() != hipSuccess || rtl::prepare_few_rows_kernels() != hipSuccess || rtl::prepare_grouped_grad_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
                     return RTL_ERR_HIP;
                 void* ptr = nullptr;
                 if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return RTL_ERR_HIP;
@@ -605,7 +605,7 @@ static rtl_status check_mx(const void* A, const void* Wq, const void* Ws, const 
     return RTL_OK;
 }
 
-static rtl_status mx_product(const uint8_t* Xq, const uint8_t* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
+static rtl_status mx_product(const void* Xq, const uint8_t* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
                              int64_t K, int64_t ldx, int64_t ldw, int64_t ldy, uint8_t* workspace, size_t used, size_t bytes, hipStream_t s) {
     rtl::GemmArgs g{};
     give_partials(g, workspace, used, bytes, (size_t)RTL_STATIC_SCRATCH_BYTES);
@@ -619,7 +619,9 @@ static rtl_status mx_product(const uint8_t* Xq, const uint8_t* Xs, const void* W
     g.bias = static_cast<const uint16_t*>(bias);
     g.Y = static_cast<uint16_t*>(Y);
     g.M = M; g.N = N; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldy;
-    return rtl::launch_gemm(false, g, s) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+    // (Xs NULL: X is bf16 still, and few_rows_choice has said `quantise`)
+    const bool few = rtl::few_rows_choice(M, M, K, true) != rtl::FewRows::no;
+    return (few ? rtl::launch_few_rows(g, s) : rtl::launch_gemm(false, g, s)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
 size_t rtl_mxfp4_packed_linear_workspace(int64_t M, int64_t N, int64_t K) {
@@ -657,6 +659,8 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
     uint8_t* base = static_cast<uint8_t*>(workspace);
     uint8_t* scales = base + mx_codes_bytes(M, K);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (rtl::few_rows_choice(M, M, K, true) == rtl::FewRows::quantise)
+        return mx_product(X, nullptr, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, nullptr, 0, 0, s);
     if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), M, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
         return RTL_ERR_HIP;
     return mx_product(base, scales, Wq, Ws, bias, Y, M, N, K, K / 2, ldw, ldy, base, need, workspace_bytes, s);
@@ -680,7 +684,7 @@ static rtl_status check_grouped(const void* X, const int32_t* offsets, const voi
     if (bad_group_sizes(T, E, N, K) || K == 0 || K % (fp4 ? 32 : 64) != 0 || ldx < K || ldw < wide || ldy < N || stride_w < 0) return RTL_ERR_SHAPE;
     if (bad_strides({ldx, ldw})) return RTL_ERR_SHAPE;
     if (T == 0 || E == 0 || N == 0) return RTL_OK;
-    if (rtl::grouped_grid(T, E, N, fp4) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (rtl::grouped_grid(T, E, N, K, fp4) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
     if (!X || !offsets || !W || !Y) return RTL_ERR_NULL;
     if (ldx % 8 != 0 || ldw % granule != 0 || stride_w % granule != 0 || !aligned(X, 16) || !aligned(offsets, 4) || !aligned(W, 16) || !aligned(Y, 2) ||
         (bias && !aligned(bias, 2)))
@@ -723,19 +727,24 @@ rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const
     hipStream_t s = static_cast<hipStream_t>(stream);
     rtl::GemmArgs g{};
     g.fp4 = true;
-    g.A = base;
-    g.lda = K / 2;
-    uint8_t* scales = base + mx_codes_bytes(T, K);
-    g.a_scale = scales;
-    g.a_scale_rows = T;
     g.W = Wq;
     g.w_scale = static_cast<const uint8_t*>(Ws);
     g.w_scale_rows = E * N;
     g.bias = static_cast<const uint16_t*>(bias);
     g.Y = static_cast<uint16_t*>(Y);
     g.M = T; g.N = N; g.K = K; g.ldw = ldw; g.ldy = ldy;
-    if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), T, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
-        return RTL_ERR_HIP;
+    if (rtl::grouped_few_rows(T, E, K, true) == rtl::FewRows::quantise) {
+        g.A = X;
+        g.lda = ldx;
+    } else {
+        uint8_t* scales = base + mx_codes_bytes(T, K);
+        if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), T, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
+            return RTL_ERR_HIP;
+        g.A = base;
+        g.lda = K / 2;
+        g.a_scale = scales;
+        g.a_scale_rows = T;
+    }
     return rtl::launch_grouped(g, rtl::GroupArgs{offsets, (int)E, stride_w}, s) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 

@@ -91,7 +91,12 @@ static int grouped_shape(int64_t T, int64_t E) {
     return rows <= 24 ? 0 : rows <= 64 ? 1 : rows <= 160 ? 2 : 3;
 }
 
-int64_t grouped_grid(int64_t T, int64_t E, int64_t N, bool fp4) {
+FewRows grouped_few_rows(int64_t T, int64_t E, int64_t K, bool fp4) {
+    return T <= 8 * E ? few_rows_choice((T + E - 1) / E, T, K, fp4) : FewRows::no;
+}
+
+int64_t grouped_grid(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
+    if (grouped_few_rows(T, E, K, fp4) != FewRows::no) return few_rows_grid(E, N);
     auto grid = [&](auto k) { return decltype(k)::grid(T, E, N); };
     return fp4 ? with_grouped<true>(grouped_shape(T, E), grid) : with_grouped<false>(grouped_shape(T, E), grid);
 }
@@ -108,6 +113,7 @@ hipError_t prepare_grouped_kernels() {
 
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream) {
     auto go = [&](auto k) { return decltype(k)::launch(a, g, stream); };
+    if (grouped_few_rows(a.M, g.experts, a.K, a.fp4) != FewRows::no) return launch_grouped_few_rows(a, g, stream);
     const int shape = grouped_shape(a.M, g.experts);
     return a.fp4 ? with_grouped<true>(shape, go) : with_grouped<false>(shape, go);
 }

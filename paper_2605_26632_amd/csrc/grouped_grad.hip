@@ -2,7 +2,7 @@
 //
 //   input  : dX[rows of e] = dY[rows of e] W[e]              contraction over N: dY is contiguous along it, W is not
 //   weight : dW[e] = dY[rows of e]^T X[rows of e]            contraction over the expert's rows: neither operand is contiguous along it
-//   bias   : db[e] = sum of the rows of dY
+//   bias   : db[e] = sum of the rows of dY                   beside the weight gradient, by the tiles of its first columns
 //
 // The matrix instruction wants eight values along the contraction from each lane. An operand that is not contiguous along it is staged as it
 // lies in memory (64 rows of the contraction, BM or BN columns) and transposed on the way out of LDS: ds_read_b64_tr_b16 hands lane i of
@@ -39,6 +39,7 @@ struct GradArgs {
     const uint16_t* A;       // A_COL: A(c, i) at A[c * lda + i], else at A[i * lda + c]
     const uint16_t* B;       // B(c, j) at B[c * ldb + j]
     void* C;                 // C(i, j) = sum over c of A(c, i) B(c, j), at C[i * ldc + j], bf16 or fp32
+    void* row_sums;          // weight gradient, nullable: the sums over c of A(c, i) at [i], the type of C, by the tiles of j = 0
     int64_t lda, ldb, ldc;
     int64_t m, n, depth;     // extents of i, j (both from the tile's own matrix) and c
 };
@@ -174,6 +175,27 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
             f[H].b[e - TM].v = tr_frag(tr_b ^ ((e - TM) * 32), wB{}, half_tag);
         }
     };
+    // Sums of A (the bias gradient): A times a matrix of ones, the row blocks of a wave's row of tiles dealt over the waves that share them.
+    constexpr int SUMS = A_COL ? TM / WAVES_N : 0;
+    static_assert(!A_COL || TM % WAVES_N == 0, "row blocks divide over the waves");
+    const bool sum_rows = A_COL && a.row_sums && n0 == 0;
+    f32x4 sums[SUMS ? SUMS : 1];
+    sums[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (SUMS > 1)
+#pragma unroll
+        for (int u = 1; u < SUMS; ++u) sums[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add_rows = [&](auto h_tag) {
+        constexpr int H = decltype(h_tag)::value;
+        const bf16x8 one = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        static_for<(H < 2 ? WAVES_N : 0)>([&](auto w_tag) {
+            constexpr int w = decltype(w_tag)::value;
+            if (wn == w)
+                static_for<SUMS>([&](auto u) {
+                    constexpr int i = w * SUMS + decltype(u)::value;
+                    sums[decltype(u)::value] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[H].a[i].v, one, sums[decltype(u)::value], 0, 0, 0);
+                });
+        });
+    };
     constexpr int NMMA = TM * TN, ITEMS = TM + TN;
     // Matrix work of half H; behind it the fragments of the other half (of buffer rbuf) and LO <= n < HI of the requests of stage kt_load.
     auto half = [&](auto h_tag, auto read_tag, int rbuf, auto lo_tag, auto hi_tag, int kt_load, int buf) {
@@ -192,6 +214,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
             static_for<g1 - g0>([&](auto e) { gload_one(kt_load, buf, std::integral_constant<int, LO + g0 + decltype(e)::value>{}); });
             __builtin_amdgcn_sched_barrier(0);
         });
+        if constexpr (A_COL)
+            if (sum_rows) add_rows(h_tag);
     };
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -259,19 +283,41 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
     }
 
     // ---- store: register r of a block is row 4 kb + r, column li -----------------------------------------
-    if constexpr (F32) {
-        float* C = static_cast<float*>(a.C);
+    if constexpr (A_COL) {
+        if (sum_rows && li == 0) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t col = n0 + wn * WTN + j * 16 + li;
-            if (col >= a.n) continue;
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int u = 0; u < SUMS; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int64_t row = m0 + wm * WTM + i * 16 + 4 * kb + r;
-                    if (row < a.m) C[row * a.ldc + col] = acc[i][j][r];
+                    const int64_t row = m0 + wm * WTM + (wn * SUMS + u) * 16 + 4 * kb + r;
+                    if (row >= a.m) continue;
+                    if constexpr (F32) static_cast<float*>(a.row_sums)[row] = sums[u][r];
+                    else static_cast<uint16_t*>(a.row_sums)[row] = (uint16_t)f32_to_bf16_rne(sums[u][r]);
                 }
+        }
+    }
+    if constexpr (F32) {
+        // row block by row block through LDS, so that rows leave in whole lines
+        wait_vmcnt_lgkm0<0>();
+        barrier();                                   // the ring is free
+        constexpr int ROWB = WTN * 4 + 16, CPR = WTN / 4;
+        static_assert(NW * 16 * ROWB <= L::kTotal, "row blocks fit in the ring");
+        uint8_t* ep = smem + wave * (16 * ROWB);
+        float* C = static_cast<float*>(a.C);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) *reinterpret_cast<float*>(ep + (4 * kb + r) * ROWB + (j * 16 + li) * 4) = acc[i][j][r];
+            // (LDS operations of a wave complete in order)
+#pragma unroll
+            for (int q0 = 0; q0 < 16 * CPR; q0 += 64) {
+                const int rl = (q0 + lane) / CPR, c = (q0 + lane) % CPR;
+                const int64_t row = m0 + wm * WTM + i * 16 + rl, col = n0 + wn * WTN + c * 4;
+                const float4 v = *reinterpret_cast<const float4*>(ep + rl * ROWB + c * 16);
+                if (row < a.m && col < a.n) *reinterpret_cast<float4*>(C + row * a.ldc + col) = v;
+            }
         }
     } else {
         // (the lane's numbers formed again: kept through the loop they cost registers there)
@@ -369,48 +415,11 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
     g.m = a.N;
     g.n = a.K;
     g.depth = r.end - r.begin;
+    if constexpr (F32) g.row_sums = a.bias_out ? static_cast<float*>(a.bias_out) + e * a.N : nullptr;
+    else g.row_sums = a.bias_out ? static_cast<uint16_t*>(a.bias_out) + e * a.N : nullptr;
     int pm, pn;
     tile_walk<8>(t, tiles_m, tiles_n, pm, pn);
     grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
-}
-
-// Bias gradient: a workgroup adds up 64 columns of an expert's rows, 32 rows at a time, then its 32 partial sums in a fixed order.
-__global__ __launch_bounds__(256) void bgrad_kernel(const GroupedGradArgs a) {
-    __shared__ float part[32][65];
-    const int64_t blocks = (a.N + 63) / 64;
-    const int e = (int)(blockIdx.x / blocks);
-    const int64_t col = blockIdx.x % blocks * 64 + threadIdx.x % 8 * 8;
-    const RowRange r = expert_rows(a.offsets, e, (int)a.T);
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (col < a.N)
-        for (int row = r.begin + threadIdx.x / 8; row < r.end; row += 32 * 8) {       // eight loads in flight
-            uint4 v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                v[u] = make_uint4(0, 0, 0, 0);
-                if (row + 32 * u < r.end) v[u] = *reinterpret_cast<const uint4*>(a.dY + (row + 32 * u) * a.lddy + col);
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sum[2 * i] += __uint_as_float(w[i] << 16);
-                    sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
-                }
-            }
-        }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) part[threadIdx.x / 8][threadIdx.x % 8 * 8 + i] = sum[i];
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
-    const int64_t c = blockIdx.x % blocks * 64 + threadIdx.x;
-    if (c >= a.N) return;
-    if (a.f32) static_cast<float*>(a.bias_out)[e * a.N + c] = s;
-    else static_cast<uint16_t*>(a.bias_out)[e * a.N + c] = (uint16_t)f32_to_bf16_rne(s);
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
@@ -485,8 +494,6 @@ hipError_t prepare_grouped_grad_kernels() {
     hipError_t e = hipSuccess;
     for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_dgrad(i, [](auto k) { return decltype(k)::prepare_dgrad(); });
     for (int i = 0; i < 2 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
-    hipFuncAttributes attr;
-    if (e == hipSuccess) e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(bgrad_kernel));
     return e;
 }
 
@@ -495,10 +502,7 @@ hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, hipStream_t stream) {
-    const hipError_t e = with_wgrad(wgrad_shape(a.experts, a.N, a.K), [&](auto k) { return decltype(k)::wgrad(a, stream); });
-    if (e != hipSuccess || !a.bias_out) return e;
-    hipLaunchKernelGGL(bgrad_kernel, dim3((unsigned)(a.experts * ((a.N + 63) / 64))), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return with_wgrad(wgrad_shape(a.experts, a.N, a.K), [&](auto k) { return decltype(k)::wgrad(a, stream); });
 }
 
 }  // namespace rtl

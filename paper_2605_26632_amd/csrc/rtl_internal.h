@@ -156,8 +156,17 @@ int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn);
 hipError_t prepare_grouped_kernels();
 // a: M the rows of X, W and the bias of expert 0 (bias [experts, N]); 4-bit: w_scale_rows = experts * N.
 // Workgroups of the launch (the calls refuse kMaxGroupGrid and more).
-int64_t grouped_grid(int64_t T, int64_t E, int64_t N, bool fp4);
+int64_t grouped_grid(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
+// Few rows (few_rows.hip): Y = X W^T read straight through, for 4-bit and grouped products. 4-bit: a.A holds codes with a.a_scale set, and is bf16,
+// quantised inside, without. M: rows of the product, or of an expert on average, `most` at most; `quantise`: worth quantising inside.
+enum class FewRows { no, direct, quantise };
+FewRows few_rows_choice(int64_t M, int64_t most, int64_t K, bool fp4);
+hipError_t prepare_few_rows_kernels();
+hipError_t launch_few_rows(const GemmArgs& a, hipStream_t stream);
+hipError_t launch_grouped_few_rows(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
+int64_t few_rows_grid(int64_t E, int64_t N);
+FewRows grouped_few_rows(int64_t T, int64_t E, int64_t K, bool fp4);       // what launch_grouped decides
 struct GroupedGradArgs {
     const int* offsets;
     int experts;

@@ -38,9 +38,10 @@ def strided(t, pad=8, fill=float("nan")):
     return wide[..., pad:-pad]
 
 
-# T, E, N, K, share of empty experts: from one row to several tiles an expert, every tile shape, more experts than one wave has lanes
+# T, E, N, K, share of empty experts: from one row to several tiles an expert, every tile shape, more experts than one wave has lanes, few rows
+# on average and more than sixteen of them with one expert
 SIZES = [(1, 1, 40, 64, 0.0), (1, 5, 24, 128, 0.0), (7, 3, 264, 192, 0.3), (70, 70, 64, 64, 0.5), (90, 2, 136, 320, 0.0), (300, 130, 72, 128, 0.3),
-         (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0)]
+         (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0), (60, 8, 96, 704, 0.6)]
 
 
 @pytest.mark.parametrize("T,E,N,K,empty", SIZES)

@@ -104,7 +104,7 @@ def test_dequantize_every_code_and_scale():
     assert (full[:, 288:] == 0).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 1, 32), (1, 130, 288), (2, 33, 64), (17, 257, 992), (33, 16, 256), (100, 520, 1024), (128, 128, 2016),
+@pytest.mark.parametrize("M,N,K", [(1, 1, 32), (1, 130, 288), (16, 75, 2400), (3, 40, 15360), (16, 33, 9056), (2, 33, 64), (17, 257, 992), (33, 16, 256), (100, 520, 1024), (128, 128, 2016),
                                    (257, 300, 544), (300, 1031, 96), (513, 257, 768)])
 @pytest.mark.parametrize("bias", [False, True])
 def test_packed_linear(M, N, K, bias):
@@ -142,7 +142,7 @@ def test_packed_linear_every_launch(M, N, K):
     ref.check_product(y[torch.from_numpy(rows).to(DEV)], ref.decode(xc[rows], xb[rows]), ref.decode(wc, wb))
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 300, 640), (5, 64, 96), (64, 96, 1056), (333, 258, 1536)])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 640), (5, 64, 96), (16, 70, 2080), (9, 33, 9056), (64, 96, 1056), (333, 258, 1536)])
 def test_linear_is_quantize_then_packed_linear(M, N, K):
     X = (torch.randn(M, K + 8, device=DEV) * torch.randn(M, 1, device=DEV).exp()).to(torch.bfloat16)[:, :K]
     rng = np.random.default_rng(1)
