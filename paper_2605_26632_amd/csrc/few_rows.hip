@@ -153,8 +153,9 @@ for (int q = tid; q < rows * pieces; q += WAVES * 64) {                   // (pi
                     if (a.bias) y += __uint_as_float((uint32_t)a.bias[n + min(e, valid - 1)] << 16);
                     out[e] = f32_to_bf16_rne(y);
                 }
-                if (valid == 4 && (reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
-                    *reinterpret_cast<uint2*>(dst) = make_uint2(out[0] | out[1] << 16, out[2] | out[3] << 16);
+                const uint2 four = make_uint2(out[0] | out[1] << 16, out[2] | out[3] << 16);
+                if (valid == 4) {
+                    __builtin_memcpy(dst, &four, 8);                                       // (at any address)
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)

@@ -229,11 +229,13 @@ __device__ __forceinline__ float mul_add_rn(float a, float b, float add) {
 // PART: the workgroup covers the k blocks [kblk0, kblk0 + kblks) only and leaves its fp32 sums in plane `part` of
 // a.partials; the factors (MODE 0), the bias and the rounding are split_reduce_kernel's.
 // FOLDED: with a.rowsums set the TENSOR factor is a.folded.
+// ANY_ROW: 16-byte stores of eight columns whatever the alignment of the rows of Y (global memory takes them at any address); without it rows that
+// are not aligned are written two bytes at a time. 4-bit [333, 2739, 4000]: 12.5 -> STORE_US us.
 // WAVES_K > 1: the waves divide the contraction too. K group g of the WAVES_K groups of WAVES_M x WAVES_N
 // waves takes the k blocks g, g + WAVES_K, ... with operands and accumulators of its own, and the groups'
 // tiles are added up in LDS, in the order of g, when the loop is done.
 template <bool SPARSE, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int MODE = 0, bool FP8 = false,
-          int WAVES_K = 1, bool PART = false, bool FOLDED = false, bool PIN = true, bool FP4 = false>
+          int WAVES_K = 1, bool PART = false, bool FOLDED = false, bool PIN = true, bool FP4 = false, bool ANY_ROW = FP4>
 __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, const int part = 0, const int kblk0 = 0,
                                           const int kblks = 0) {
     static_assert(!PART || WAVES_K == 1, "partial sums leave from the accumulators");
@@ -715,7 +717,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     static_assert(STAGES == 2 || STAGES == 3 || STAGES == 4, "ring depth");
     using P = std::integral_constant<int, STAGES - 2>;
     int kt = 0;
-    if constexpr (LEAN) {
+    if constexpr (ANY_ROW && STAGES == 2 && WAVES_K == 1) {
         // (the last stage reads fragments that nobody uses: as a step of its own, without them, it came out of the compiler with spills)
         for (; kt < KT - 2; ++kt) stage_step(kt, F{}, T{}, T{}, P{});
         for (; kt < KT; ++kt) stage_step(kt, F{}, F{}, T{}, P{});
@@ -842,7 +844,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
             f[u] = has_row_scale ? a.row_scale[min(row, a.M - 1)] : 1.0f;
         }
         const float ts = tensor_scale();
-        const bool wide_ok = ((reinterpret_cast<uintptr_t>(a.Y) & 15) == 0) && (a.ldy % 8 == 0) && valid == 8;
+        bool wide_ok = ((reinterpret_cast<uintptr_t>(a.Y) & 15) == 0) && (a.ldy % 8 == 0) && valid == 8;
+        if constexpr (ANY_ROW) wide_ok = valid == 8;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int q = u * THREADS + (int)threadIdx.x;
@@ -864,7 +867,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
             }
             uint16_t* dst = a.Y + row * a.ldy + col;
             if (wide_ok) {
-                *reinterpret_cast<uint4*>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+                if constexpr (ANY_ROW) __builtin_memcpy(dst, out, 16);
+                else *reinterpret_cast<uint4*>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -968,7 +972,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         if (a.bias) v += bv;
         return (uint16_t)f32_to_bf16_rne(v);
     };
-    const bool wide_ok = ((reinterpret_cast<uintptr_t>(a.Y) & 15) == 0) && (a.ldy % 8 == 0);
+    bool wide_ok = ((reinterpret_cast<uintptr_t>(a.Y) & 15) == 0) && (a.ldy % 8 == 0);
+    if constexpr (ANY_ROW) wide_ok = true;
     if (wide_ok) {
         // The accumulator layout gives a lane one column and scattered rows, i.e. 2-byte stores.
         // Each wave therefore transposes its tile through a private LDS region (the ring is no
@@ -1064,7 +1069,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
                     const uint4 v = *reinterpret_cast<const uint4*>(ep + rl * ROWB + c * 16);
                     uint16_t* dst = a.Y + row * a.ldy + col;
                     if (col + 8 <= a.N) {
-                        *reinterpret_cast<uint4*>(dst) = v;
+                        if constexpr (ANY_ROW) __builtin_memcpy(dst, &v, 16);
+                        else *reinterpret_cast<uint4*>(dst) = v;
                     } else {
                         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
                         for (int e = 0; e < 8 && col + e < a.N; ++e)

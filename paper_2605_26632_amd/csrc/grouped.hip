@@ -27,8 +27,8 @@ __global__ __launch_bounds__(512) void grouped_mixed_kernel(const GemmArgs a, co
     MixedTile t;
     if (!group_tile_mixed(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), t)) return;
     const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
-    if (t.tall) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4>(b, t.tile);
-    else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4>(b, t.tile);
+    if (t.tall) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+    else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
 }
 
 template <bool FP4>
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * WAVES_K * 64) void grouped_kern
     GroupTile t;
     if (!group_tile(g.offsets, g.experts, (int)a.M, BM, (int)((a.N + BN - 1) / BN), t)) return;
     const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
-    gemm_tile<false, BM, BN, WAVES_M, WAVES_N, STAGES, 0, false, WAVES_K, false, false, true, FP4>(b, t.tile);
+    gemm_tile<false, BM, BN, WAVES_M, WAVES_N, STAGES, 0, false, WAVES_K, false, false, true, FP4, true>(b, t.tile);
 }
 
 template <bool FP4, int BM, int BN, int WAVES_M, int WAVES_N, int WAVES_K, int STAGES>

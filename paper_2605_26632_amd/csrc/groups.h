@@ -66,8 +66,8 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
 }
 
 // Two tile heights in one launch, for experts of many rows: as many 256-row panels as fill whole rounds of the chip, the rest of the rows in 128-row
-// ones. An expert's last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts,
-// 4096 columns: 576 tiles of 256 x 256, 2.25 rounds that cost 3).
+// ones. An expert's last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with
+// 2048 columns 296 tiles, 1.16 rounds that cost 2).
 struct MixedTile {
     bool tall;                           // 256 rows, else 128
     int expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
@@ -75,9 +75,21 @@ struct MixedTile {
 constexpr int kUnits = 256;              // compute units
 constexpr float kHalfCost = 0.6f;        // time of a 128 x 256 tile in those of a 256 x 256 one
 
-__device__ __forceinline__ float mixed_rounds(int tall, int half) {      // rounds that `tall` tiles and then `half` tiles take
-    const int full = (tall + kUnits - 1) / kUnits, over = max(0, half - (full * kUnits - tall));
-    return (float)full + (float)((over + kUnits - 1) / kUnits) * kHalfCost;
+// Time of `tall` tiles and then `half` tiles on the chip, in those of a tall tile, each tile to the unit that frees first: after the whole rounds
+// of tall tiles x units work at one more, the others at half tiles, whose k-th ends at k c there and at 1 + k c on the x.
+__device__ __forceinline__ float mixed_time(int tall, int half) {
+    constexpr float c = kHalfCost;
+    const int x = tall % kUnits, rest = kUnits - x;
+    const float least = max(((float)half * c + (float)x) / kUnits, x ? 1.0f : 0.0f);
+    auto held = [&](float t) { return rest * (int)(t / c + 0.01f) + x * (int)(max(t - 1.0f, 0.0f) / c + 0.01f); };
+    float best = 1e9f;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const float a = max((ceilf(least / c - 0.01f) + k) * c, least), b = 1.0f + (ceilf(max(least - 1.0f, 0.0f) / c - 0.01f) + k) * c;
+        if (held(a) >= half) best = min(best, a);
+        if (x && held(b) >= half) best = min(best, b);
+    }
+    return (float)(tall / kUnits) + best;
 }
 
 __device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int T, int tiles_n, MixedTile& out) {
@@ -104,16 +116,20 @@ __device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int 
         full = min(full + __builtin_amdgcn_readlane(scan(n / 256), 63), most);
         rest = min(rest + __builtin_amdgcn_readlane(scan((n % 256 + 127) / 128), 63), most);
     }
-    int p = full;
-    float best = mixed_rounds(full * tiles_n, rest * tiles_n);
-    for (int k = full * tiles_n / kUnits, i = 0; i < 2 && k >= 0; ++i, --k) {
-        const int q = min(k * kUnits / tiles_n, full);
-        const float c = mixed_rounds(q * tiles_n, (2 * (full - q) + rest) * tiles_n);
-        if (c < best) {
-            best = c;
+    // how many full panels are tall ones: each lane prices one number, the fewest halves among equals
+    const int mine = max(full - lane, 0);
+    float best = mixed_time(mine * tiles_n, (2 * (full - mine) + rest) * tiles_n);
+    int p = mine;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        const float t = __shfl_xor(best, d);
+        const int q = __shfl_xor(p, d);
+        if (t < best - 1e-4f || (t < best + 1e-4f && q > p)) {
+            best = t;
             p = q;
         }
     }
+    p = __builtin_amdgcn_readfirstlane(p);
     const int nb = p * tiles_n, nt = (2 * (full - p) + rest) * tiles_n;
     const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8, nb_x = nb / 8 + (xcd < nb % 8);
     if (local >= xcd_share_start(nb + nt, xcd + 1) - xcd_share_start(nb + nt, xcd)) return false;
