@@ -25,9 +25,10 @@ __device__ __forceinline__ GemmArgs expert_problem(const GemmArgs& a, const Grou
 template <bool FP4>
 __global__ __launch_bounds__(512) void grouped_mixed_kernel(const GemmArgs a, const GroupArgs g) {
     MixedTile t;
-    if (!group_tile_mixed(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), t)) return;
+    if (!group_tile_mixed(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), (int)(FP4 ? (a.K + 255) / 256 : a.K / 64), t)) return;
     const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
-    if (t.tall) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+    if (t.height == 256) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+    else if (t.height == 192) gemm_tile<false, 192, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
     else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
 }
 

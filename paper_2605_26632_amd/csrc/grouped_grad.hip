@@ -383,12 +383,15 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void dgrad_kernel(const Gro
 __global__ __launch_bounds__(512) void dgrad_mixed_kernel(const GroupedGradArgs a) {
     MixedTile t;
     const int tiles_n = (int)((a.K + 255) / 256);
-    if (!group_tile_mixed(a.offsets, a.experts, (int)a.T, tiles_n, t)) return;
+    if (!group_tile_mixed(a.offsets, a.experts, (int)a.T, tiles_n, (int)((a.N + 63) / 64), t)) return;
     const GradArgs g = dgrad_problem(a, t.expert, t.begin, t.rows);
     int pm, pn;
-    if (t.tall) {
+    if (t.height == 256) {
         tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
         grad_tile<false, false, 256, 256, 2, 4, 2>(g, (int64_t)pm * 256, (int64_t)pn * 256);
+    } else if (t.height == 192) {
+        tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
+        grad_tile<false, false, 192, 256, 2, 4, 2>(g, (int64_t)pm * 192, (int64_t)pn * 256);
     } else {
         tile_walk<16>(t.tile, t.panels, tiles_n, pm, pn);
         grad_tile<false, false, 128, 256, 2, 4, 3>(g, (int64_t)pm * 128, (int64_t)pn * 256);

@@ -15,6 +15,25 @@ __device__ __forceinline__ RowRange expert_rows(const int* offsets, int e, int T
     return RowRange{b, max(b, n)};
 }
 
+// Over the lanes of a wave, in lane moves (a few cycles each; shuffles through LDS took 1.5 us of a workgroup's start): inclusive sums, and the
+// smallest number, which lands in lane 63.
+template <class F>
+__device__ __forceinline__ int over_lanes(int v, int none, F f) {
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x111, 0xF, 0xF, false));       // from 1, 2, 4, 8 lanes below, inside 16
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x112, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x114, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x118, 0xF, 0xF, false));
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x142, 0xA, 0xF, false));       // the 16 before, then the 32
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x143, 0xC, 0xF, false));
+    return v;
+}
+__device__ __forceinline__ int lane_scan(int n) {
+    return over_lanes(n, 0, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int lane_min(int n) {
+    return __builtin_amdgcn_readlane(over_lanes(n, 0x7FFFFFFF, [](int a, int b) { return min(a, b); }), 63);
+}
+
 struct GroupTile {
     int expert, begin, rows, tile;       // tile: index in the walk of the expert's own grid of tiles
 };
@@ -30,17 +49,9 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
         return r;
     };
     auto count = [&](const RowRange& r) { return (int)min((int64_t)((r.end - r.begin + bm - 1) / bm) * tiles_n, (int64_t)grid); };
-    auto scan = [&](int n) {             // inclusive
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int up = __shfl_up(n, d);
-            if (lane >= d) n += up;
-        }
-        return n;
-    };
     RowRange r = lane_rows(0);
-    int n = count(r), upto = scan(n), total = min(__builtin_amdgcn_readlane(upto, 63), grid);
-    for (int e0 = 64; e0 < E; e0 += 64) total = min(total + __builtin_amdgcn_readlane(scan(count(lane_rows(e0))), 63), grid);
+    int n = count(r), upto = lane_scan(n), total = min(__builtin_amdgcn_readlane(upto, 63), grid);
+    for (int e0 = 64; e0 < E; e0 += 64) total = min(total + __builtin_amdgcn_readlane(lane_scan(count(lane_rows(e0))), 63), grid);
     const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8;
     const int t = xcd_share_start(total, xcd) + local;
     if (t >= xcd_share_start(total, xcd + 1)) return false;
@@ -49,7 +60,7 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
         if (e0 > 0) {
             r = lane_rows(e0);
             n = count(r);
-            upto = scan(n);
+            upto = lane_scan(n);
         }
         const uint64_t hit = __ballot(before + upto > t);
         if (hit) {
@@ -65,20 +76,20 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
     return false;
 }
 
-// Two tile heights in one launch, for experts of many rows: as many 256-row panels as fill whole rounds of the chip, the rest of the rows in 128-row
-// ones. An expert's last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with
-// 2048 columns 296 tiles, 1.16 rounds that cost 2).
+// Two tile heights in one launch, for experts of many rows: 256 or 192 rows for as many panels as suit, 128 for the rest of the rows. An expert's
+// last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with 2048 columns 296
+// tiles of 256 x 256, 1.16 rounds that cost 2).
 struct MixedTile {
-    bool tall;                           // 256 rows, else 128
-    int expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
+    int height, expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
 };
 constexpr int kUnits = 256;              // compute units
-constexpr float kHalfCost = 0.6f;        // time of a 128 x 256 tile in those of a 256 x 256 one
+// us of a tile of 256 columns with every unit at work: 8 and this for each stage of 128 bytes of the contraction. Measured, 8 and 32 (4-bit) or 64 stages:
+// 128 rows bf16 14.7 / 62, 4-bit 16.4 / 33.9, input gradient 14.7 / 57; 192 rows 18.4 / 79, 19.5 / 45, 19.1 / 83; 256 rows 21.8 / 106, 23.1 / 60, 22.4 / 105.
+constexpr float kTileFixed = 8.0f, kTile128 = 0.78f, kTile192 = 1.09f, kTile256 = 1.5f;
 
-// Time of `tall` tiles and then `half` tiles on the chip, in those of a tall tile, each tile to the unit that frees first: after the whole rounds
-// of tall tiles x units work at one more, the others at half tiles, whose k-th ends at k c there and at 1 + k c on the x.
-__device__ __forceinline__ float mixed_time(int tall, int half) {
-    constexpr float c = kHalfCost;
+// Time of `tall` tiles and then `half` tiles on the chip, in those of a tall tile (c: time of a half tile in those), each tile to the unit that frees
+// first: after the whole rounds of tall tiles x units work at one more, the others at half tiles, whose k-th ends at k c there and at 1 + k c on the x.
+__device__ __forceinline__ float mixed_time(int tall, int half, float c) {
     const int x = tall % kUnits, rest = kUnits - x;
     const float least = max(((float)half * c + (float)x) / kUnits, x ? 1.0f : 0.0f);
     auto held = [&](float t) { return rest * (int)(t / c + 0.01f) + x * (int)(max(t - 1.0f, 0.0f) / c + 0.01f); };
@@ -92,69 +103,74 @@ __device__ __forceinline__ float mixed_time(int tall, int half) {
     return (float)(tall / kUnits) + best;
 }
 
-__device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int T, int tiles_n, MixedTile& out) {
+__device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int T, int tiles_n, int stages, MixedTile& out) {
     const int lane = threadIdx.x & 63, grid = (int)gridDim.x, most = grid / tiles_n;
     auto lane_rows = [&](int e0) {
         RowRange r{0, 0};
         if (e0 + lane < E) r = expert_rows(offsets, e0 + lane, T);
         return r;
     };
-    auto scan = [&](int n) {             // inclusive
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int up = __shfl_up(n, d);
-            if (lane >= d) n += up;
-        }
-        return n;
-    };
-    // panels of all experts: full ones, and 128-row ones of what is left of each (sums cut to the grid's size: see group_tile)
+    auto halves = [](int n) { return (n + 127) / 128; };
+    auto add = [&](int& sum, int n) { sum = min(sum + __builtin_amdgcn_readlane(lane_scan(n), 63), most); };       // (cut to the grid's size: see group_tile)
     RowRange r = lane_rows(0);
-    int full = 0, rest = 0;
+    int full256 = 0, rest256 = 0, full192 = 0, rest192 = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {
         const RowRange x = e0 ? lane_rows(e0) : r;
         const int n = x.end - x.begin;
-        full = min(full + __builtin_amdgcn_readlane(scan(n / 256), 63), most);
-        rest = min(rest + __builtin_amdgcn_readlane(scan((n % 256 + 127) / 128), 63), most);
+        add(full256, n / 256);
+        add(rest256, halves(n % 256));
+        add(full192, n / 192);
+        add(rest192, halves(n % 192));
     }
-    // how many full panels are tall ones: each lane prices one number, the fewest halves among equals
-    const int mine = max(full - lane, 0);
-    float best = mixed_time(mine * tiles_n, (2 * (full - mine) + rest) * tiles_n);
-    int p = mine;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        const float t = __shfl_xor(best, d);
-        const int q = __shfl_xor(p, d);
-        if (t < best - 1e-4f || (t < best + 1e-4f && q > p)) {
-            best = t;
-            p = q;
-        }
+    // how many panels are tall, and how tall: each lane prices one choice, all full panels or fewer, in steps of 16 tiles or more
+    const bool low = lane >= 32;
+    const int full = low ? full192 : full256, step = max(1, 16 / tiles_n), mine = max(full - (lane & 31) * step, 0);
+    const float cost128 = kTileFixed + kTile128 * stages, cost = kTileFixed + (low ? kTile192 : kTile256) * stages;
+    const int left = low ? ((full - mine) * 3 + 1) / 2 + rest192 : (full - mine) * 2 + rest256;
+    const float us = mixed_time(mine * tiles_n, left * tiles_n, cost128 / cost) * cost;
+    const int pick = lane_min((int)min(us * 16.0f, 3e7f) << 6 | lane) & 63;          // (the lowest lane among equals)
+    const int tall = pick >= 32 ? 192 : 256, p = __builtin_amdgcn_readlane(mine, pick);
+    // the tall panels go to the first experts; the 128-row ones are counted as they come of it
+    int halves_all = 0, full_before = 0;
+    auto taken_of = [&](int n) {
+        const int f = n / tall, f_upto = lane_scan(f), taken = min(max(p - (full_before + f_upto - f), 0), f);
+        full_before = min(full_before + __builtin_amdgcn_readlane(f_upto, 63), 1 << 28);
+        return taken;
+    };
+    int taken = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const RowRange x = e0 ? lane_rows(e0) : r;
+        const int n = x.end - x.begin, t = taken_of(n);
+        if (e0 == 0) taken = t;
+        add(halves_all, halves(n - t * tall));
     }
-    p = __builtin_amdgcn_readfirstlane(p);
-    const int nb = p * tiles_n, nt = (2 * (full - p) + rest) * tiles_n;
+    const int nb = p * tiles_n, nt = halves_all * tiles_n;
     const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8, nb_x = nb / 8 + (xcd < nb % 8);
     if (local >= xcd_share_start(nb + nt, xcd + 1) - xcd_share_start(nb + nt, xcd)) return false;
-    out.tall = local < nb_x;
-    const int t = out.tall ? xcd_share_start(nb, xcd) + local : xcd_share_start(nb + nt, xcd) - xcd_share_start(nb, xcd) + (local - nb_x);
+    const bool body = local < nb_x;
+    const int t = body ? xcd_share_start(nb, xcd) + local : xcd_share_start(nb + nt, xcd) - xcd_share_start(nb, xcd) + (local - nb_x);
     const int panel = t / tiles_n;
-    int before = 0, full_before = 0;
+    int before = 0;
+    full_before = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {
-        if (e0) r = lane_rows(e0);
-        const int n = r.end - r.begin, f = n / 256, f_upto = scan(f);
-        const int taken = min(max(p - (full_before + f_upto - f), 0), f);         // tall panels of the lane's expert
-        const int count = out.tall ? taken : 2 * (f - taken) + (n % 256 + 127) / 128, upto = scan(count);
+        if (E > 64) {
+            r = lane_rows(e0);
+            taken = taken_of(r.end - r.begin);
+        }
+        const int count = body ? taken : halves(r.end - r.begin - taken * tall), upto = lane_scan(count);
         const uint64_t hit = __ballot(before + upto > panel);
         if (hit) {
-            const int l = __builtin_ctzll(hit), cut = __builtin_amdgcn_readlane(taken, l) * 256;
+            const int l = __builtin_ctzll(hit), cut = __builtin_amdgcn_readlane(taken, l) * tall;
             const int begin = __builtin_amdgcn_readlane(r.begin, l), end = __builtin_amdgcn_readlane(r.end, l);
+            out.height = body ? tall : 128;
             out.expert = e0 + l;
-            out.begin = out.tall ? begin : begin + cut;
-            out.rows = out.tall ? cut : end - begin - cut;
+            out.begin = body ? begin : begin + cut;
+            out.rows = body ? cut : end - begin - cut;
             out.panels = __builtin_amdgcn_readlane(count, l);
             out.tile = t - (before + __builtin_amdgcn_readlane(upto, l) - out.panels) * tiles_n;
             return true;
         }
         before = min(before + __builtin_amdgcn_readlane(upto, 63), 1 << 28);
-        full_before = min(full_before + __builtin_amdgcn_readlane(f_upto, 63), 1 << 28);
     }
     return false;
 }
