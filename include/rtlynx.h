@@ -333,7 +333,8 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
  *            (RTL_BF16 or RTL_F32): dW [E, N, K] (lddw, stride_dw >= (N - 1) lddw + K), dbias NULL or [E, N]. Every element is written, zeros for an expert
  *            without rows. Sizes and alignment as for dgrad. fp32 sums in a fixed order; a row of dY or X enters its own expert's
  *            gradient only, whatever it holds.
- *   workspace  rtl_grouped_linear_wgrad_workspace(T, E, N, K) bytes (may be 0), all of it optional, 256-byte aligned.
+ *   workspace  rtl_grouped_linear_wgrad_workspace(T, E, N, K) bytes (may be 0), all of it optional, as for rtl_dense_linear: room to cut many rows of
+ *            few experts into parts; a smaller one groups the fp32 sums differently.
  * rtl_grouped_mxfp4_linear the forward product with the weights as MXFP4 codes and X quantised in the call: Wq [E, N, K / 2] bytes (ldw, stride_w
  *            in bytes, % 16 == 0), Ws the scales of the [E * N, K] matrix of all experts' rows (what rtl_quantize_mxfp4 makes of it in one call).
  *            K % 32 == 0; X as for rtl_mxfp4_linear.

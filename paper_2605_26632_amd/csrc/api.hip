@@ -733,7 +733,7 @@ rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const
     g.bias = static_cast<const uint16_t*>(bias);
     g.Y = static_cast<uint16_t*>(Y);
     g.M = T; g.N = N; g.K = K; g.ldw = ldw; g.ldy = ldy;
-    if (rtl::grouped_few_rows(T, E, K, true) == rtl::FewRows::quantise) {
+    if (rtl::grouped_few_rows(T, E, N, K, true) == rtl::FewRows::quantise) {
         g.A = X;
         g.lda = ldx;
     } else {
@@ -754,7 +754,7 @@ rtl_status rtl_grouped_linear_dgrad(const void* dY, const int32_t* offsets, cons
     if (bad_strides({lddy, ldw, lddx})) return RTL_ERR_SHAPE;
     if (T == 0 || E == 0 || K == 0) return RTL_OK;
     if (N == 0) return RTL_ERR_SHAPE;                      // no gradient to speak of, and nothing that would write dX
-    if (rtl::dgrad_grid(T, E, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (rtl::dgrad_grid(T, E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
     if (!dY || !offsets || !W || !dX) return RTL_ERR_NULL;
     if (lddy % 8 != 0 || ldw % 8 != 0 || lddx % 8 != 0 || stride_w % 8 != 0 || !aligned(dY, 16) || !aligned(offsets, 4) || !aligned(W, 16) ||
         !aligned(dX, 16))
@@ -771,20 +771,19 @@ rtl_status rtl_grouped_linear_dgrad(const void* dY, const int32_t* offsets, cons
 }
 
 size_t rtl_grouped_linear_wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K) {
-    (void)T; (void)E; (void)N; (void)K;
-    return 0;
+    if (T <= 0 || E <= 0 || N <= 0 || K <= 0) return 0;
+    return rtl::wgrad_workspace(T, E, N, K, (size_t)RTL_STATIC_SCRATCH_BYTES);
 }
 
 rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t* offsets, void* dW, void* dbias, rtl_dtype dw_type, int64_t T, int64_t E,
                                     int64_t N, int64_t K, int64_t lddy, int64_t ldx, int64_t lddw, int64_t stride_dw, void* workspace,
                                     size_t workspace_bytes, void* stream) {
-    (void)workspace; (void)workspace_bytes;
     if (dw_type != RTL_BF16 && dw_type != RTL_F32) return RTL_ERR_ARG;
     if (bad_group_sizes(T, E, N, K) || N % 8 != 0 || K % 8 != 0 || lddy < N || ldx < K || lddw < K) return RTL_ERR_SHAPE;
     if (bad_strides({lddy, ldx, lddw})) return RTL_ERR_SHAPE;
     if (E == 0 || N == 0 || K == 0) return RTL_OK;
     if (E > 1 && stride_dw < (N - 1) * lddw + K) return RTL_ERR_SHAPE;       // experts' gradients must not overlap
-    if (rtl::wgrad_grid(E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (64 * rtl::wgrad_grid(E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
     if (!offsets || !dW || (T > 0 && (!dY || !X))) return RTL_ERR_NULL;
     if (lddy % 8 != 0 || ldx % 8 != 0 || lddw % 8 != 0 || stride_dw % 8 != 0 || !aligned(dY, 16) || !aligned(X, 16) || !aligned(offsets, 4) ||
         !aligned(dW, 16) || (dbias && !aligned(dbias, dw_type == RTL_F32 ? 4 : 2)))
@@ -799,7 +798,9 @@ rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t
     g.bias_out = dbias;
     g.f32 = dw_type == RTL_F32;
     g.T = T; g.N = N; g.K = K; g.lddy = lddy; g.ldx = ldx; g.ldo = lddw; g.o_stride = stride_dw;
-    return rtl::launch_grouped_wgrad(g, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+    size_t room = workspace && aligned(workspace, 16) ? workspace_bytes : 0;                // none of it is mandatory
+    if (room > (size_t)RTL_STATIC_SCRATCH_BYTES) room = (size_t)RTL_STATIC_SCRATCH_BYTES;
+    return rtl::launch_grouped_wgrad(g, workspace, room, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
 }  // extern "C"

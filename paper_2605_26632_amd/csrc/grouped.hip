@@ -87,19 +87,46 @@ int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn) {
     return (T / bm + (E < T ? E : T)) * ((cols + bn - 1) / bn);
 }
 
-static int grouped_shape(int64_t T, int64_t E) {
-    const int64_t rows = T / E;
-    return rows <= 24 ? 0 : rows <= 64 ? 1 : rows <= 160 ? 2 : 3;
+double group_panels(int64_t T, int64_t E, int64_t bm) {
+    const double experts = (double)(E < T ? E : T), panels = (double)T / experts / (double)bm + 0.5;
+    return experts * (panels > 1 ? panels : 1);
 }
 
-FewRows grouped_few_rows(int64_t T, int64_t E, int64_t K, bool fp4) {
-    return T <= 8 * E ? few_rows_choice((T + E - 1) / E, T, K, fp4) : FewRows::no;
+// Form of a launch: index of with_grouped, or kFew for few_rows.hip, the one with the least estimated time. us of a form: `fixed` and `stage` per 128-byte stage
+// of the contraction while its tiles find a unit each, more passes in proportion (but only 0.6 of `fixed` again: the next tile starts while another ends).
+// Measured at 8, 128, 256 and 512 tiles and 8 and 64 stages. Over 630 problems ([1..64 experts, 1..2000 rows each, 256..4096, 512..6144], uneven experts), bf16 and
+// 4-bit, the choice is 5 and 7 % slower in the mean than the best form; by rows per expert alone a form could take six times as long as the best.
+constexpr int kFew = 4;
+int grouped_form(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
+    struct Form { int bm, bn; double fixed, stage; };
+    static constexpr Form kForms[] = {{32, 32, 3.7, 0.09}, {64, 64, 4.2, 0.185}, {128, 128, 5.0, 0.43}};
+    const double stages = (double)(fp4 ? (K + 255) / 256 : K / 64);
+    int pick = 3;
+    const double halves = group_panels(T, E, 128) * (double)((N + 255) / 256), rounds = halves > 256 ? halves / 256 : 1;
+    double best = 6.5 + (rounds - 1) * 5 + (0.6 + 0.15 * (halves < 256 ? halves / 256 : 1)) * stages * rounds;
+    for (int i = 0; i < 3; ++i) {
+        const Form& f = kForms[i];
+        const double tiles = group_panels(T, E, f.bm) * (double)((N + f.bn - 1) / f.bn), passes = tiles > 256 ? tiles / 256 : 1;
+        const double us = f.fixed * (1 + 0.6 * (passes - 1)) + f.stage * stages * passes;
+        if (us < best) {
+            best = us;
+            pick = i;
+        }
+    }
+    const FewRows few = T <= 8 * E ? few_rows_choice((T + E - 1) / E, T, K, fp4) : FewRows::no;
+    if (few != FewRows::no && few_rows_us(T, E, N, K, fp4) - (few == FewRows::quantise ? 2.5 : 0) < best) pick = kFew;
+    return pick;
+}
+
+FewRows grouped_few_rows(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
+    return grouped_form(T, E, N, K, fp4) == kFew ? few_rows_choice((T + E - 1) / E, T, K, fp4) : FewRows::no;
 }
 
 int64_t grouped_grid(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
-    if (grouped_few_rows(T, E, K, fp4) != FewRows::no) return few_rows_grid(E, N);
+    const int form = grouped_form(T, E, N, K, fp4);
+    if (form == kFew) return few_rows_grid(E, N);
     auto grid = [&](auto k) { return decltype(k)::grid(T, E, N); };
-    return fp4 ? with_grouped<true>(grouped_shape(T, E), grid) : with_grouped<false>(grouped_shape(T, E), grid);
+    return fp4 ? with_grouped<true>(form, grid) : with_grouped<false>(form, grid);
 }
 
 hipError_t prepare_grouped_kernels() {
@@ -113,10 +140,10 @@ hipError_t prepare_grouped_kernels() {
 }
 
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream) {
+    const int form = grouped_form(a.M, g.experts, a.N, a.K, a.fp4);
+    if (form == kFew) return launch_grouped_few_rows(a, g, stream);
     auto go = [&](auto k) { return decltype(k)::launch(a, g, stream); };
-    if (grouped_few_rows(a.M, g.experts, a.K, a.fp4) != FewRows::no) return launch_grouped_few_rows(a, g, stream);
-    const int shape = grouped_shape(a.M, g.experts);
-    return a.fp4 ? with_grouped<true>(shape, go) : with_grouped<false>(shape, go);
+    return a.fp4 ? with_grouped<true>(form, go) : with_grouped<false>(form, go);
 }
 
 }  // namespace rtl

@@ -45,7 +45,7 @@ struct GradArgs {
 };
 
 template <bool A_COL, bool F32, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
-__device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, const int64_t n0) {
+__device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, const int64_t n0, const int part = 0, const int parts = 1) {
     using L = GradSmem<BM, BN, WAVES_M, WAVES_N, STAGES>;
     constexpr int NW = WAVES_M * WAVES_N, WTM = BM / WAVES_M, WTN = BN / WAVES_N, TM = WTM / 16, TN = WTN / 16;
     static_assert(!A_COL || BM % 128 == 0, "eight 32-byte chunks to a row");
@@ -60,7 +60,10 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
     const int64_t rows_a = a.m - m0, cols_b = a.n - n0;
-    const int KT = (int)((a.depth + 63) / 64), tail = (int)(a.depth % 64);
+    // part `part` of `parts` of the contraction: an even share of its blocks
+    const int blocks = (int)((a.depth + 63) / 64), tail = (int)(a.depth % 64);
+    const int blk0 = (int)((int64_t)blocks * part / parts), KT = (int)((int64_t)blocks * (part + 1) / parts) - blk0;
+    const bool tail_first = tail && blk0 == 0;
 
     // ---- global -> LDS: a lane's chunks; beyond the matrix's edge it repeats the last one (only outputs that are not stored see it) ----
     const int64_t step_a = A_COL ? 64 * a.lda * 2 : 128, step_b = 64 * a.ldb * 2;
@@ -71,6 +74,8 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
         base_a -= step_a;
         base_b -= step_b;
     }
+    base_a += blk0 * step_a;
+    base_b += blk0 * step_b;
     base_a = reinterpret_cast<const uint8_t*>(uniform64(base_a));
     base_b = reinterpret_cast<const uint8_t*>(uniform64(base_b));
     using wA = std::integral_constant<int, BM>;
@@ -84,7 +89,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
     };
     uint32_t oa, ob;
     int a_row = 0;                                         // row-major A: the lane's row of request 0; oa its chunk in the row
-    auto row_unit = [&](int s) { return (wave & 1) | s << 1 | (wave >> 1) * (2 * A_PER_W); };      // 8 rows each, one chunk order
+    auto row_unit = [&](int s) { return (wave & 1) + 2 * s + (wave >> 1) * (2 * A_PER_W); };      // 8 rows each, one chunk order
     auto col_offset = [&](auto width, int64_t ld, int64_t valid) {
         constexpr int W = decltype(width)::value, CH = W / 8;
         const int row = col_unit(width, 0) * (512 / W) + lane / CH, c = (lane % CH) ^ (row_key(row) << 1);
@@ -133,7 +138,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
                 in = u * (512 / BN) + lane / (BN / 8) < tail;
                 at = L::kA + u * 1024;
             }
-            if (in) gload_one(KT, 0, n_tag);
+            if (in) gload_one(blocks, 0, n_tag);
             else *reinterpret_cast<uint4*>(smem + at + lane * 16) = make_uint4(0, 0, 0, 0);
         });
     };
@@ -227,7 +232,7 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
 #pragma unroll
         for (int s = 0; s < STAGES; ++s)
             if (s < KT) {
-                if (s == 0 && tail) gload_tail();
+                if (s == 0 && tail_first) gload_tail();
                 else gload(s, s);
             }
         if (KT >= STAGES) wait_vmcnt_lgkm0<(STAGES - 1) * LOADS>();
@@ -403,8 +408,9 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
     // Every XCD takes an eighth of every expert's tiles (neighbours in the walk), so that uneven experts do not make uneven XCDs; which
     // eighth turns with the expert, for experts of fewer than eight tiles.
     const int tiles_m = (int)((a.N + BM - 1) / BM), tiles_n = (int)((a.K + BN - 1) / BN), tiles = tiles_m * tiles_n, per = (tiles + 7) / 8;
-    const int e = (int)blockIdx.x / 8 / per, share = ((int)blockIdx.x + e) % 8;
-    const int t = xcd_share_start(tiles, share) + (int)blockIdx.x / 8 % per;
+    const int one = a.experts * 8 * per, part = (int)blockIdx.x / one, id = (int)blockIdx.x % one;
+    const int e = id / 8 / per, share = (id + e + part) % 8;
+    const int t = xcd_share_start(tiles, share) + id / 8 % per;
     if (t >= xcd_share_start(tiles, share + 1)) return;
     const RowRange r = expert_rows(a.offsets, e, (int)a.T);
     GradArgs g;
@@ -412,17 +418,44 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
     g.lda = a.lddy;
     g.B = a.X + r.begin * a.ldx;
     g.ldb = a.ldx;
-    if constexpr (F32) g.C = static_cast<float*>(a.out) + e * a.o_stride;
+    if constexpr (F32) g.C = static_cast<float*>(a.out) + (part * a.experts + e) * a.o_stride;
     else g.C = static_cast<uint16_t*>(a.out) + e * a.o_stride;
     g.ldc = a.ldo;
     g.m = a.N;
     g.n = a.K;
     g.depth = r.end - r.begin;
-    if constexpr (F32) g.row_sums = a.bias_out ? static_cast<float*>(a.bias_out) + e * a.N : nullptr;
+    if constexpr (F32) g.row_sums = a.bias_out ? static_cast<float*>(a.bias_out) + (part * a.experts + e) * a.N : nullptr;
     else g.row_sums = a.bias_out ? static_cast<uint16_t*>(a.bias_out) + e * a.N : nullptr;
     int pm, pn;
     tile_walk<8>(t, tiles_m, tiles_n, pm, pn);
-    grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN);
+    grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN, part, a.parts);
+}
+
+// Adds the parts' planes up in order: dW four columns to a thread, behind them the bias gradient one element to a thread.
+__global__ __launch_bounds__(256) void wgrad_reduce_kernel(const GroupedGradArgs a, const float* planes, const float* bias_planes) {
+    const int64_t all = (int64_t)a.experts * a.N * (a.K / 4), q = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (q < all) {
+        const int64_t row = q / (a.K / 4), col = q % (a.K / 4) * 4, e = row / a.N, n = row % a.N;
+        const float* p = planes + row * a.K + col;
+        float4 s = *reinterpret_cast<const float4*>(p);
+        for (int i = 1; i < a.parts; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(p + i * ((int64_t)a.experts * a.N * a.K));
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const int64_t at = e * a.o_stride + n * a.ldo + col;
+        if (a.f32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(a.out) + at) = s;
+        } else {
+            const uint32_t lo = f32_to_bf16_rne(s.x) | f32_to_bf16_rne(s.y) << 16, hi = f32_to_bf16_rne(s.z) | f32_to_bf16_rne(s.w) << 16;
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(lo, hi);
+        }
+    } else if (a.bias_out && q - all < a.experts * a.N) {
+        const int64_t n = q - all;
+        float s = bias_planes[n];
+        for (int i = 1; i < a.parts; ++i) s += bias_planes[i * (a.experts * a.N) + n];
+        if (a.f32) static_cast<float*>(a.bias_out)[n] = s;
+        else static_cast<uint16_t*>(a.bias_out)[n] = (uint16_t)f32_to_bf16_rne(s);
+    }
 }
 
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
@@ -443,7 +476,7 @@ struct Grad {
         return hipGetLastError();
     }
     static hipError_t wgrad(const GroupedGradArgs& a, hipStream_t stream) {
-        const dim3 grid((unsigned)wgrad_grid(a.experts, a.N, a.K));
+        const dim3 grid((unsigned)(wgrad_grid(a.experts, a.N, a.K) * a.parts));
         if (a.f32) hipLaunchKernelGGL((wgrad_kernel<true, BM, BN, WAVES_M, WAVES_N, STAGES>), grid, block(), L::kTotal, stream, a);
         else hipLaunchKernelGGL((wgrad_kernel<false, BM, BN, WAVES_M, WAVES_N, STAGES>), grid, block(), L::kTotal, stream, a);
         return hipGetLastError();
@@ -468,44 +501,109 @@ template <class Op>
 auto with_dgrad(int shape, Op op) {
     switch (shape) {
         case 0: return op(Grad<64, 128, 1, 4, 4>{});
-        case 1: return op(Grad<128, 128, 2, 2, 2>{});
+        case 1: return op(Grad<128, 128, 2, 2, 4>{});
         default: return op(DgradMixed{});
     }
 }
 template <class Op>
 auto with_wgrad(int shape, Op op) {
-    if (shape == 0) return op(Grad<128, 128, 2, 2, 2>{});
+    if (shape == 0) return op(Grad<128, 128, 2, 2, 4>{});
     return op(Grad<256, 256, 2, 4, 2>{});
 }
 
 }  // namespace
 
-static int dgrad_shape(int64_t T, int64_t E) {
-    const int64_t rows = T / E;
-    return rows <= 64 ? 0 : rows <= 160 ? 1 : 2;
+// The tile with the least estimated time (as in grouped.hip; `stage`: 64 of the contraction). Over 315 problems as there the input gradient's choice is 3 %, the
+// weight gradient's 1 % slower in the mean than the best.
+int dgrad_shape(int64_t T, int64_t E, int64_t N, int64_t K) {
+    const double stages = (double)((N + 63) / 64), halves = group_panels(T, E, 128) * (double)((K + 255) / 256), rounds = halves > 256 ? halves / 256 : 1;
+    double best = 6.0 + (rounds - 1) * 4.5 + (0.6 + 0.15 * (halves < 256 ? halves / 256 : 1)) * stages * rounds;
+    int pick = 2;
+    for (int i = 0; i < 2; ++i) {
+        const double tiles = group_panels(T, E, i ? 128 : 64) * (double)((K + 127) / 128), passes = tiles > 256 ? tiles / 256 : 1;
+        const double fixed = i ? 4.8 : 3.8, stage = (i ? 0.53 : 0.305) * (1 + (i ? 0.06 : 0.13) * (passes < 2 ? passes - 1 : 1));
+        const double us = fixed * (1 + 0.6 * (passes - 1)) + stage * stages * passes;
+        if (us < best) {
+            best = us;
+            pick = i;
+        }
+    }
+    return pick;
 }
-static int wgrad_shape(int64_t E, int64_t N, int64_t K) { return E * ((N + 255) / 256) * ((K + 255) / 256) < 192 ? 0 : 1; }
+// Weight gradient: the tile, and in how many parts the rows are cut where the tiles leave units idle and there are many rows to an expert: each part leaves an fp32
+// plane in the workspace and a second launch adds them up (3.5 us and the planes' way there and back at 3.5 TB/s).
+struct WgradPlan {
+    int shape, parts;
+};
+static size_t wgrad_plane(int64_t E, int64_t N, int64_t K) { return (size_t)E * (size_t)N * (size_t)(K + 1) * 4; }
+static WgradPlan wgrad_plan(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
+    const double rows = T > 0 ? (double)T / (double)(E < T ? E : T) : 0, stages = rows / 64 + 0.5;
+    auto us = [&](int64_t side, double fixed, double stage, int parts) {
+        const double tiles = (double)parts * (double)(E * ((N + side - 1) / side) * ((K + side - 1) / side)), passes = tiles > 256 ? tiles / 256 : 1;
+        return fixed * (1 + (side == 128 ? 0.6 : 0.9) * (passes - 1)) + stage * (stages / parts) * passes;
+    };
+    const double small = us(128, 4.8, 0.53, 1), big = us(256, 9.0, 1.5, 1);
+    WgradPlan plan{small < big ? 0 : 1, 1};
+    double best = small < big ? small : big;
+    for (int parts = 2; parts <= 64 && parts * 2 <= stages; parts *= 2) {
+        const double bytes = (double)parts * (double)wgrad_plane(E, N, K);
+        if (bytes > (double)room) break;
+        const double t = us(128, 4.8, 0.53, parts) + 3.5 + bytes * 2 / 3.5e6;
+        if (t < best * 0.95) {
+            best = t;
+            plan = WgradPlan{0, parts};
+        }
+    }
+    return plan;
+}
+void wgrad_choice(int64_t T, int64_t E, int64_t N, int64_t K, size_t room, int out[2]) {
+    const WgradPlan plan = wgrad_plan(T, E, N, K, room);
+    out[0] = plan.shape;
+    out[1] = plan.parts;
+}
+size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
+    const int parts = wgrad_plan(T, E, N, K, room).parts;
+    return parts > 1 ? (size_t)parts * wgrad_plane(E, N, K) : 0;
+}
 
-int64_t dgrad_grid(int64_t T, int64_t E, int64_t K) {
-    return with_dgrad(dgrad_shape(T, E), [&](auto k) { return decltype(k)::dgrad_grid(T, E, K); });
+int64_t dgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K) {
+    return with_dgrad(dgrad_shape(T, E, N, K), [&](auto k) { return decltype(k)::dgrad_grid(T, E, K); });
 }
 int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) {
-    return with_wgrad(wgrad_shape(E, N, K), [&](auto k) { return decltype(k)::wgrad_grid(E, N, K); });
+    return with_wgrad(0, [&](auto k) { return decltype(k)::wgrad_grid(E, N, K); });      // (of the smaller tile)
 }
 
 hipError_t prepare_grouped_grad_kernels() {
     hipError_t e = hipSuccess;
     for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_dgrad(i, [](auto k) { return decltype(k)::prepare_dgrad(); });
     for (int i = 0; i < 2 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
+    hipFuncAttributes attr;
+    if (e == hipSuccess) e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(wgrad_reduce_kernel));
     return e;
 }
 
 hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream) {
-    return with_dgrad(dgrad_shape(a.T, a.experts), [&](auto k) { return decltype(k)::dgrad(a, stream); });
+    return with_dgrad(dgrad_shape(a.T, a.experts, a.N, a.K), [&](auto k) { return decltype(k)::dgrad(a, stream); });
 }
 
-hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, hipStream_t stream) {
-    return with_wgrad(wgrad_shape(a.experts, a.N, a.K), [&](auto k) { return decltype(k)::wgrad(a, stream); });
+hipError_t launch_grouped_wgrad(const GroupedGradArgs& a_in, void* workspace, size_t room, hipStream_t stream) {
+    GroupedGradArgs a = a_in;
+    const WgradPlan plan = wgrad_plan(a.T, a.experts, a.N, a.K, room);
+    a.parts = plan.parts;
+    if (plan.parts == 1) return with_wgrad(plan.shape, [&](auto k) { return decltype(k)::wgrad(a, stream); });
+    GroupedGradArgs part = a;
+    float* planes = static_cast<float*>(workspace);
+    float* bias_planes = planes + (size_t)plan.parts * a.experts * a.N * a.K;
+    part.f32 = true;
+    part.out = planes;
+    part.bias_out = a.bias_out ? bias_planes : nullptr;
+    part.ldo = a.K;
+    part.o_stride = a.N * a.K;
+    const hipError_t e = with_wgrad(plan.shape, [&](auto k) { return decltype(k)::wgrad(part, stream); });
+    if (e != hipSuccess) return e;
+    const int64_t work = a.experts * a.N * (a.K / 4) + (a.bias_out ? a.experts * a.N : 0);
+    hipLaunchKernelGGL(wgrad_reduce_kernel, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, stream, a, planes, bias_planes);
+    return hipGetLastError();
 }
 
 }  // namespace rtl

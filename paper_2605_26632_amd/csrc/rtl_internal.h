@@ -155,6 +155,11 @@ constexpr int64_t kMaxGroupGrid = (int64_t)1 << 24;
 int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn);
 hipError_t prepare_grouped_kernels();
 // a: M the rows of X, W and the bias of expert 0 (bias [experts, N]); 4-bit: w_scale_rows = experts * N.
+// The forms that launches pick (host arithmetic, for the tests): forward 0 .. 2: 32 x 32, 64 x 64, 128 x 128 tiles, 3: 128- to 256-row panels, 4: few rows; input
+// gradient 0, 1: 64 x 128, 128 x 128, 2: panels; weight gradient out = {0: 128 x 128, 1: 256 x 256, parts of the rows}.
+int grouped_form(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);
+int dgrad_shape(int64_t T, int64_t E, int64_t N, int64_t K);
+void wgrad_choice(int64_t T, int64_t E, int64_t N, int64_t K, size_t room, int out[2]);
 // Workgroups of the launch (the calls refuse kMaxGroupGrid and more).
 int64_t grouped_grid(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
@@ -162,11 +167,14 @@ hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t str
 // quantised inside, without. M: rows of the product, or of an expert on average, `most` at most; `quantise`: worth quantising inside.
 enum class FewRows { no, direct, quantise };
 FewRows few_rows_choice(int64_t M, int64_t most, int64_t K, bool fp4);
+double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);      // estimate for a grouped product
 hipError_t prepare_few_rows_kernels();
 hipError_t launch_few_rows(const GemmArgs& a, hipStream_t stream);
 hipError_t launch_grouped_few_rows(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
 int64_t few_rows_grid(int64_t E, int64_t N);
-FewRows grouped_few_rows(int64_t T, int64_t E, int64_t K, bool fp4);       // what launch_grouped decides
+FewRows grouped_few_rows(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);       // what launch_grouped decides
+// Panels of `bm` rows that T rows over E experts make on average: half a panel is lost at each expert's end.
+double group_panels(int64_t T, int64_t E, int64_t bm);
 struct GroupedGradArgs {
     const int* offsets;
     int experts;
@@ -175,12 +183,15 @@ struct GroupedGradArgs {
     void* bias_out;         // wgrad: nullable, [experts, N], the type of out
     bool f32;
     int64_t T, N, K, lddy, ldw, w_stride, ldx, ldo, o_stride;
+    int parts;              // filled in by launch_grouped_wgrad
 };
 hipError_t prepare_grouped_grad_kernels();
-int64_t dgrad_grid(int64_t T, int64_t E, int64_t K);
+int64_t dgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K);
 int64_t wgrad_grid(int64_t E, int64_t N, int64_t K);
 hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream);
-hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, hipStream_t stream);
+// workspace: 16-byte aligned, `room` bytes of it at most for partial planes; wgrad_workspace: how much of `room` the call would use.
+size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
+hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_t room, hipStream_t stream);
 
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------
 // Issue-rate probe: `blocks` workgroups of four waves, each wave issuing 4 * iters matrix

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import grouped_plan as plan
 import mx_ref as ref
 from paper_2605_26632_amd import binding as rtl
 
@@ -41,7 +42,8 @@ def strided(t, pad=8, fill=float("nan")):
 # T, E, N, K, share of empty experts: from one row to several tiles an expert, every tile shape, more experts than one wave has lanes, few rows
 # on average and more than sixteen of them with one expert
 SIZES = [(1, 1, 40, 64, 0.0), (1, 5, 24, 128, 0.0), (7, 3, 264, 192, 0.3), (70, 70, 64, 64, 0.5), (90, 2, 136, 320, 0.0), (300, 130, 72, 128, 0.3),
-         (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0), (60, 8, 96, 704, 0.6)]
+         (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0), (60, 8, 96, 704, 0.6),
+         (8, 2, 1304, 64, 0.0), (40, 5, 4752, 64, 0.2), (160, 20, 2504, 64, 0.3), (12, 20, 1000, 320, 0.3)]
 
 
 @pytest.mark.parametrize("T,E,N,K,empty", SIZES)
@@ -65,7 +67,10 @@ def test_forward(T, E, N, K, empty, bias):
                 ref.check_product(Y[o[e]:o[e + 1]], ref.values(X[o[e]:o[e + 1]]), ref.values(W[e]), None if b is None else ref.values(b[e]))
 
 
-@pytest.mark.parametrize("T,E,N,K,empty", SIZES)
+DGRAD_SIZES = SIZES + [(545, 8, 40, 3744, 0.0), (8, 8, 40, 8216, 0.3)]
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", DGRAD_SIZES)
 def test_input_gradient(T, E, N, K, empty):
     gen, rng = generator(T + E + N + K + 1), np.random.default_rng(T * E + 1)
     counts, front, behind = split(rng, T, E, empty), 2, 4
@@ -83,7 +88,10 @@ def test_input_gradient(T, E, N, K, empty):
             ref.check_product(dX[o[e]:o[e + 1]], ref.values(dY[o[e]:o[e + 1]]), ref.values(W[e]).T)
 
 
-@pytest.mark.parametrize("T,E,N,K,empty", SIZES + [(700, 2, 1040, 3080, 0.0), (200, 40, 520, 640, 0.5)])
+WGRAD_SIZES = SIZES + [(700, 2, 1040, 3080, 0.0), (200, 40, 520, 640, 0.5), (5000, 1, 136, 200, 0.0), (7001, 3, 264, 64, 0.3)]
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", WGRAD_SIZES)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_weight_and_bias_gradient(T, E, N, K, empty, dtype):
     """Every element is written; NaN in the rows of nobody and between the rows stays out; an expert's NaN reaches its own gradient only."""
@@ -118,6 +126,47 @@ def test_weight_and_bias_gradient(T, E, N, K, empty, dtype):
     assert torch.equal(again[0][keep], dW[keep]) and torch.equal(again[1][keep], db[keep])      # the same bits every time
 
 
+# rows of the experts, columns of Y in tiles of 256, and the heights that they are cut into
+HEIGHTS = [([47, 85, 20], 68, {128}), ([18, 151, 398], 41, {192, 128}), ([197, 139, 337], 41, {256, 128}), ([1152], 33, {192}),
+           ([0, 700, 5, 0, 900, 1], 40, {192, 128})]
+
+
+@pytest.mark.parametrize("counts,tiles_n,want", HEIGHTS)
+def test_panels_of_every_height(counts, tiles_n, want):
+    """Forward (bf16 and 4-bit) and input gradient on panels of 256, 192 and 128 rows."""
+    tall, p = plan.heights(counts, tiles_n, 2)
+    left = sum(-(-(n % tall) // 128) for n in counts) > 0 or p < sum(n // tall for n in counts)
+    assert want == ({tall} if p else set()) | ({128} if left else set())
+    gen, rng = generator(11), np.random.default_rng(11)
+    T, E, wide = sum(counts), len(counts), tiles_n * 256 - 40
+    off = offsets_of(counts)
+    o = off.tolist()
+    assert plan.forward_form(T, E, wide, 128) == 3 and plan.forward_form(T, E, wide, 512, True) == 3 and plan.dgrad_form(T, E, 128, wide) == 2
+    X, W, b = bf16(gen, T, 128), bf16(gen, E, wide, 128), bf16(gen, E, wide)
+    Y = rtl.grouped_linear(X, off, W, bias=b)
+    X4 = bf16(gen, T, 512)
+    wc, wb = ref.random_codes(rng, E * wide, 512)
+    wq, ws = ref.on_device(wc, wb)
+    Y4 = rtl.grouped_mxfp4_linear(X4, off, wq.reshape(E, wide, 256), ws, bias=b)
+    G, V = bf16(gen, T, 128), bf16(gen, E, 128, wide)
+    dX = rtl.grouped_linear_dgrad(G, off, V)
+    x4 = ref.decode(*ref.quantize(ref.values(X4)))
+    w4 = ref.decode(wc, wb).reshape(E, wide, 512)
+    for e in range(E):
+        if counts[e]:
+            r = slice(o[e], o[e + 1])
+            ref.check_product(Y[r], ref.values(X[r]), ref.values(W[e]), ref.values(b[e]))
+            ref.check_product(Y4[r], x4[r], w4[e], ref.values(b[e]))
+            ref.check_product(dX[r], ref.values(G[r]), ref.values(V[e]).T)
+
+
+def test_sizes_reach_every_form():
+    assert {plan.forward_form(T + 8, E, N - 3, K) for T, E, N, K, _ in SIZES} == {0, 1, 2, 3, 4}
+    assert {plan.forward_form(T + 3, E, N - 3, K, True) for T, E, N, K, _ in MX_SIZES} == {0, 1, 2, 3, 4}
+    assert {plan.dgrad_form(T + 6, E, N, K - 24) for T, E, N, K, _ in DGRAD_SIZES} == {0, 1, 2}
+    assert {(s, p > 1) for s, p in (plan.wgrad_form(T + 160, E, N, K) for T, E, N, K, _ in WGRAD_SIZES)} == {(0, False), (1, False), (0, True)}
+
+
 def test_gradients_against_differences():
     """Small integers, so that everything is exact: moving X, W or b by a step changes sum(Y * G) by the step times the gradient."""
     rng = np.random.default_rng(7)
@@ -136,7 +185,11 @@ def test_gradients_against_differences():
         assert loss(X, W, b + sb) - loss(X, W, b) == (db.double() * sb.double()).sum().item()
 
 
-@pytest.mark.parametrize("T,E,N,K,empty", SIZES + [(64, 32, 300, 992, 0.3), (2000, 3, 700, 544, 0.0)])
+# (the last three: few rows on average of stacks with many columns, quantised by the workgroups and before them; few rows not quantised by them)
+MX_SIZES = SIZES + [(64, 32, 300, 992, 0.3), (2000, 3, 700, 544, 0.0), (40, 33, 2051, 288, 0.2), (200, 33, 2051, 2080, 0.2), (60, 8, 96, 1600, 0.6)]
+
+
+@pytest.mark.parametrize("T,E,N,K,empty", MX_SIZES)
 @pytest.mark.parametrize("bias", [False, True])
 def test_mxfp4_forward(T, E, N, K, empty, bias):
     gen, rng = generator(T + E + N + K + 3), np.random.default_rng(T * E + 3)
