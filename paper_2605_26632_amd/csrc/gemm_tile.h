@@ -269,7 +269,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
 
     extern __shared__ __align__(16) uint8_t smem[];
 
-    const int tid = threadIdx.x, lane = tid & 63;
+    int tid = threadIdx.x;
+    if constexpr (ANY_ROW) asm volatile("" : "+v"(tid));         // (in a loop over tiles: formed anew for each, not kept across it)
+    const int lane = tid & 63;
     const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);    // wave-uniform, lives in an SGPR
     const int wk = WAVES_K > 1 ? wid / NW : 0, wave = WAVES_K > 1 ? wid % NW : wid;   // K group, wave inside it
     uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;

@@ -24,12 +24,11 @@ __device__ __forceinline__ GemmArgs expert_problem(const GemmArgs& a, const Grou
 
 template <bool FP4>
 __global__ __launch_bounds__(512) void grouped_mixed_kernel(const GemmArgs a, const GroupArgs g) {
-    MixedTile t;
-    if (!group_tile_mixed(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), (int)(FP4 ? (a.K + 255) / 256 : a.K / 64), t)) return;
-    const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
-    if (t.height == 256) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
-    else if (t.height == 192) gemm_tile<false, 192, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
-    else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+    mixed_tiles(g.offsets, g.experts, (int)a.M, (int)((a.N + 255) / 256), (int)(FP4 ? (a.K + 255) / 256 : a.K / 64), [&](const MixedTile& t) {
+        const GemmArgs b = expert_problem<FP4>(a, g, t.expert, t.begin, t.rows);
+        if (t.tall) gemm_tile<false, 256, 256, 2, 4, 2, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+        else gemm_tile<false, 128, 256, 2, 4, 3, 0, false, 1, false, false, true, FP4, true>(b, t.tile);
+    });
 }
 
 template <bool FP4>
@@ -42,7 +41,7 @@ struct GroupedMixed {
         return hipFuncSetAttribute(reinterpret_cast<const void*>(grouped_mixed_kernel<FP4>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     }
     static hipError_t launch(const GemmArgs& a, const GroupArgs& g, hipStream_t stream) {
-        hipLaunchKernelGGL(grouped_mixed_kernel<FP4>, dim3((unsigned)grid(a.M, g.experts, a.N)), dim3(512), kLds, stream, a, g);
+        hipLaunchKernelGGL(grouped_mixed_kernel<FP4>, dim3(kUnits), dim3(512), kLds, stream, a, g);
         return hipGetLastError();
     }
 };

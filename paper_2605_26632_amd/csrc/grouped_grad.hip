@@ -55,7 +55,9 @@ __device__ __forceinline__ void grad_tile(const GradArgs a, const int64_t m0, co
     static_assert(L::kA % (1024 * NW) == 0 && L::kB % (1024 * NW) == 0, "tile loads must divide over the waves");
 
     extern __shared__ __align__(1024) uint8_t smem[];
-    const int tid = threadIdx.x, lane = tid & 63;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                                // (in a loop over tiles: formed anew for each, not kept across it)
+    const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
@@ -386,21 +388,18 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void dgrad_kernel(const Gro
 }
 
 __global__ __launch_bounds__(512) void dgrad_mixed_kernel(const GroupedGradArgs a) {
-    MixedTile t;
     const int tiles_n = (int)((a.K + 255) / 256);
-    if (!group_tile_mixed(a.offsets, a.experts, (int)a.T, tiles_n, (int)((a.N + 63) / 64), t)) return;
-    const GradArgs g = dgrad_problem(a, t.expert, t.begin, t.rows);
-    int pm, pn;
-    if (t.height == 256) {
-        tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
-        grad_tile<false, false, 256, 256, 2, 4, 2>(g, (int64_t)pm * 256, (int64_t)pn * 256);
-    } else if (t.height == 192) {
-        tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
-        grad_tile<false, false, 192, 256, 2, 4, 2>(g, (int64_t)pm * 192, (int64_t)pn * 256);
-    } else {
-        tile_walk<16>(t.tile, t.panels, tiles_n, pm, pn);
-        grad_tile<false, false, 128, 256, 2, 4, 3>(g, (int64_t)pm * 128, (int64_t)pn * 256);
-    }
+    mixed_tiles(a.offsets, a.experts, (int)a.T, tiles_n, (int)((a.N + 63) / 64), [&](const MixedTile& t) {
+        const GradArgs g = dgrad_problem(a, t.expert, t.begin, t.rows);
+        int pm, pn;
+        if (t.tall) {
+            tile_walk<8>(t.tile, t.panels, tiles_n, pm, pn);
+            grad_tile<false, false, 256, 256, 2, 4, 2>(g, (int64_t)pm * 256, (int64_t)pn * 256);
+        } else {
+            tile_walk<16>(t.tile, t.panels, tiles_n, pm, pn);
+            grad_tile<false, false, 128, 256, 2, 4, 3>(g, (int64_t)pm * 128, (int64_t)pn * 256);
+        }
+    });
 }
 
 template <bool F32, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
@@ -492,7 +491,7 @@ struct DgradMixed {
         return hipFuncSetAttribute(reinterpret_cast<const void*>(dgrad_mixed_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     }
     static hipError_t dgrad(const GroupedGradArgs& a, hipStream_t stream) {
-        hipLaunchKernelGGL(dgrad_mixed_kernel, dim3((unsigned)dgrad_grid(a.T, a.experts, a.K)), dim3(512), kLds, stream, a);
+        hipLaunchKernelGGL(dgrad_mixed_kernel, dim3(kUnits), dim3(512), kLds, stream, a);
         return hipGetLastError();
     }
 };

@@ -76,16 +76,18 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
     return false;
 }
 
-// Two tile heights in one launch, for experts of many rows: 256 or 192 rows for as many panels as suit, 128 for the rest of the rows. An expert's
-// last rows are seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with 2048 columns 296
-// tiles of 256 x 256, 1.16 rounds that cost 2).
+// Two tile heights in one launch, for experts of many rows: 256 rows for as many panels as suit, 128 for the rest of the rows. An expert's last rows are
+// seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with 2048 columns 296 tiles of
+// 256 x 256, 1.16 rounds that cost 2). (192 rows as a third height end launches sooner by this count and not by the clock: the matrix instructions run at the power
+// limit, and lower tiles take more energy per product. Sustained, on inputs that change: [8192, 4096, 2048] over uneven experts 163 us without, 170 with.)
 struct MixedTile {
-    int height, expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
+    bool tall;
+    int expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
 };
 constexpr int kUnits = 256;              // compute units
 // us of a tile of 256 columns with every unit at work: 8 and this for each stage of 128 bytes of the contraction. Measured, 8 and 32 (4-bit) or 64 stages:
-// 128 rows bf16 14.7 / 62, 4-bit 16.4 / 33.9, input gradient 14.7 / 57; 192 rows 18.4 / 79, 19.5 / 45, 19.1 / 83; 256 rows 21.8 / 106, 23.1 / 60, 22.4 / 105.
-constexpr float kTileFixed = 8.0f, kTile128 = 0.78f, kTile192 = 1.09f, kTile256 = 1.5f;
+// 128 rows bf16 14.7 / 62, 4-bit 16.4 / 33.9, input gradient 14.7 / 57; 256 rows 21.8 / 106, 23.1 / 60, 22.4 / 105.
+constexpr float kTileFixed = 8.0f, kTile128 = 0.78f, kTile256 = 1.5f;
 
 // Time of `tall` tiles and then `half` tiles on the chip, in those of a tall tile (c: time of a half tile in those), each tile to the unit that frees
 // first: after the whole rounds of tall tiles x units work at one more, the others at half tiles, whose k-th ends at k c there and at 1 + k c on the x.
@@ -103,66 +105,47 @@ __device__ __forceinline__ float mixed_time(int tall, int half, float c) {
     return (float)(tall / kUnits) + best;
 }
 
-__device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int T, int tiles_n, int stages, MixedTile& out) {
-    const int lane = threadIdx.x & 63, grid = (int)gridDim.x, most = grid / tiles_n;
-    auto lane_rows = [&](int e0) {
+__device__ __forceinline__ int half_panels(int rows) { return (rows + 127) / 128; }
+
+struct MixedPlan {
+    int p, tall, half;                   // tall panels, tall tiles, half tiles
+};
+__device__ __forceinline__ MixedPlan plan_mixed(const int* offsets, int E, int T, int tiles_n, int stages) {
+    const int lane = threadIdx.x & 63, most = T / 128 + min(E, T);                   // no offsets that ascend make more panels
+    int full = 0, rest = 0;
+    auto add = [&](int& sum, int n) { sum = min(sum + __builtin_amdgcn_readlane(lane_scan(n), 63), most); };
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        int n = 0;
+        if (e0 + lane < E) {
+            const RowRange r = expert_rows(offsets, e0 + lane, T);
+            n = r.end - r.begin;
+        }
+        add(full, n / 256);
+        add(rest, half_panels(n % 256));
+    }
+    // how many panels are tall: each lane prices one number, all full panels or fewer, in steps of 16 tiles or more
+    const int mine = max(full - lane * max(1, 16 / tiles_n), 0), left = (full - mine) * 2 + rest;
+    const float cost128 = kTileFixed + kTile128 * stages, cost256 = kTileFixed + kTile256 * stages;
+    const float us = mixed_time(mine * tiles_n, left * tiles_n, cost128 / cost256) * cost256;
+    const int pick = lane_min((int)min(us * 16.0f, 3e7f) << 6 | lane) & 63;          // (the lowest lane among equals)
+    const int p = __builtin_amdgcn_readlane(mine, pick);
+    return MixedPlan{p, p * tiles_n, ((full - p) * 2 + rest) * tiles_n};
+}
+
+// Number t of the tall (body) or of the half tiles: the tall panels go to the first experts.
+__device__ __forceinline__ bool find_mixed(const int* offsets, int E, int T, int tiles_n, const MixedPlan& plan, bool body, int t, MixedTile& out) {
+    const int lane = threadIdx.x & 63, panel = t / tiles_n;
+    int before = 0, full_before = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
         RowRange r{0, 0};
         if (e0 + lane < E) r = expert_rows(offsets, e0 + lane, T);
-        return r;
-    };
-    auto halves = [](int n) { return (n + 127) / 128; };
-    auto add = [&](int& sum, int n) { sum = min(sum + __builtin_amdgcn_readlane(lane_scan(n), 63), most); };       // (cut to the grid's size: see group_tile)
-    RowRange r = lane_rows(0);
-    int full256 = 0, rest256 = 0, full192 = 0, rest192 = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        const RowRange x = e0 ? lane_rows(e0) : r;
-        const int n = x.end - x.begin;
-        add(full256, n / 256);
-        add(rest256, halves(n % 256));
-        add(full192, n / 192);
-        add(rest192, halves(n % 192));
-    }
-    // how many panels are tall, and how tall: each lane prices one choice, all full panels or fewer, in steps of 16 tiles or more
-    const bool low = lane >= 32;
-    const int full = low ? full192 : full256, step = max(1, 16 / tiles_n), mine = max(full - (lane & 31) * step, 0);
-    const float cost128 = kTileFixed + kTile128 * stages, cost = kTileFixed + (low ? kTile192 : kTile256) * stages;
-    const int left = low ? ((full - mine) * 3 + 1) / 2 + rest192 : (full - mine) * 2 + rest256;
-    const float us = mixed_time(mine * tiles_n, left * tiles_n, cost128 / cost) * cost;
-    const int pick = lane_min((int)min(us * 16.0f, 3e7f) << 6 | lane) & 63;          // (the lowest lane among equals)
-    const int tall = pick >= 32 ? 192 : 256, p = __builtin_amdgcn_readlane(mine, pick);
-    // the tall panels go to the first experts; the 128-row ones are counted as they come of it
-    int halves_all = 0, full_before = 0;
-    auto taken_of = [&](int n) {
-        const int f = n / tall, f_upto = lane_scan(f), taken = min(max(p - (full_before + f_upto - f), 0), f);
-        full_before = min(full_before + __builtin_amdgcn_readlane(f_upto, 63), 1 << 28);
-        return taken;
-    };
-    int taken = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        const RowRange x = e0 ? lane_rows(e0) : r;
-        const int n = x.end - x.begin, t = taken_of(n);
-        if (e0 == 0) taken = t;
-        add(halves_all, halves(n - t * tall));
-    }
-    const int nb = p * tiles_n, nt = halves_all * tiles_n;
-    const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8, nb_x = nb / 8 + (xcd < nb % 8);
-    if (local >= xcd_share_start(nb + nt, xcd + 1) - xcd_share_start(nb + nt, xcd)) return false;
-    const bool body = local < nb_x;
-    const int t = body ? xcd_share_start(nb, xcd) + local : xcd_share_start(nb + nt, xcd) - xcd_share_start(nb, xcd) + (local - nb_x);
-    const int panel = t / tiles_n;
-    int before = 0;
-    full_before = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        if (E > 64) {
-            r = lane_rows(e0);
-            taken = taken_of(r.end - r.begin);
-        }
-        const int count = body ? taken : halves(r.end - r.begin - taken * tall), upto = lane_scan(count);
+        const int n = r.end - r.begin, f = n / 256, f_upto = lane_scan(f), taken = min(max(plan.p - (full_before + f_upto - f), 0), f);
+        const int count = body ? taken : half_panels(n - taken * 256), upto = lane_scan(count);
         const uint64_t hit = __ballot(before + upto > panel);
         if (hit) {
-            const int l = __builtin_ctzll(hit), cut = __builtin_amdgcn_readlane(taken, l) * tall;
+            const int l = __builtin_ctzll(hit), cut = __builtin_amdgcn_readlane(taken, l) * 256;
             const int begin = __builtin_amdgcn_readlane(r.begin, l), end = __builtin_amdgcn_readlane(r.end, l);
-            out.height = body ? tall : 128;
+            out.tall = body;
             out.expert = e0 + l;
             out.begin = body ? begin : begin + cut;
             out.rows = body ? cut : end - begin - cut;
@@ -171,8 +154,29 @@ __device__ __forceinline__ bool group_tile_mixed(const int* offsets, int E, int 
             return true;
         }
         before = min(before + __builtin_amdgcn_readlane(upto, 63), 1 << 28);
+        full_before = min(full_before + __builtin_amdgcn_readlane(f_upto, 63), 1 << 28);
     }
     return false;
+}
+
+// All tiles of the launch on kUnits workgroups: an XCD's share of the list (tall tiles first) is dealt to its workgroups to and fro, so that who got a
+// late, small tile gets an early one next. (Left to the hardware a tile waits for a unit of the shader engine that is next in turn, whatever
+// units are free elsewhere: 248 tall tiles and 16 half ones took DISPATCH_US.) `work` is called with each tile of this workgroup.
+template <class Work>
+__device__ __forceinline__ void mixed_tiles(const int* offsets, int E, int T, int tiles_n, int stages, Work work) {
+    const MixedPlan plan = plan_mixed(offsets, E, T, tiles_n, stages);
+    constexpr int kPer = kUnits / 8;
+    const int xcd = (int)blockIdx.x % 8, l = (int)blockIdx.x / 8;
+    const int nb = plan.tall, all = plan.tall + plan.half, nb0 = xcd_share_start(nb, xcd), nb_x = nb / 8 + (xcd < nb % 8);
+    const int first = xcd_share_start(all, xcd), n = all / 8 + (xcd < all % 8);
+    for (int k = 0; k * kPer < n; ++k) {
+        const int local = k * kPer + (k % 2 ? kPer - 1 - l : l);
+        if (local >= n) continue;
+        MixedTile t;
+        if (!find_mixed(offsets, E, T, tiles_n, plan, local < nb_x, local < nb_x ? nb0 + local : first - nb0 + (local - nb_x), t)) return;
+        if (k > 0) __syncthreads();                      // the last tile's rows have left LDS
+        work(t);
+    }
 }
 
 }  // namespace

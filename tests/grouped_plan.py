@@ -40,15 +40,13 @@ def _time(tall, half, c):
 
 
 def heights(counts, tiles_n, stages):
-    """(height of the tall panels, how many of them) for experts of these row counts."""
+    """How many panels of 256 rows experts of these row counts get; the rest of the rows is cut into panels of 128."""
+    full, rest = sum(n // 256 for n in counts), sum(-(-(n % 256) // 128) for n in counts)
+    cost = 8 + 1.5 * stages
     best = None
-    for height, stage in ((256, 1.5), (192, 1.09)):
-        full, rest = sum(n // height for n in counts), sum(-(-(n % height) // 128) for n in counts)
-        cost = 8 + stage * stages
-        for lane in range(32):
-            p = max(full - lane * max(1, 16 // tiles_n), 0)
-            halves = (full - p) * 2 + rest if height == 256 else ((full - p) * 3 + 1) // 2 + rest
-            us = int(_time(p * tiles_n, halves * tiles_n, (8 + 0.78 * stages) / cost) * cost * 16)
-            if best is None or us < best[0]:
-                best = (us, height, p)
-    return best[1:]
+    for lane in range(64):
+        p = max(full - lane * max(1, 16 // tiles_n), 0)
+        us = int(_time(p * tiles_n, ((full - p) * 2 + rest) * tiles_n, (8 + 0.78 * stages) / cost) * cost * 16)
+        if best is None or us < best[0]:
+            best = (us, p)
+    return best[1]
