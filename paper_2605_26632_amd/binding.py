@@ -398,7 +398,7 @@ def _whole(t, shape, dtype, name):
 def _output(out, rows, cols, dtype, like, new=torch.empty):
     """(out or a new tensor, its row stride)."""
     if out is None:
-        return new((rows, cols), dtype=dtype, device=like.device), cols
+        return new(rows, cols, dtype=dtype, device=like.device), cols
     m, n, ld = _matrix(out, dtype, "out")
     if m != rows or n != cols:
         raise ValueError("out: shape (%d, %d) expected" % (rows, cols))
@@ -430,12 +430,12 @@ def quantize_mxfp4(X, along="cols", out=None):
     if along != "rows":
         q, ldq = _output(out and out[0], rows, cols // 2, u8, X)
         shape = mxfp4_scales_shape(rows, cols)
-        s = out[1] if out else torch.empty(shape, dtype=u8, device=X.device)
+        s = out[1] if out else torch.empty(*shape, dtype=u8, device=X.device)
         _whole(s, shape, u8, "out")
     if along != "cols":
         qt, ldqt = _output(out and out[-2], cols, pad // 2, u8, X)
         shape = mxfp4_scales_shape(cols, pad)
-        st = out[-1] if out else torch.empty(shape, dtype=u8, device=X.device)
+        st = out[-1] if out else torch.empty(*shape, dtype=u8, device=X.device)
         _whole(st, shape, u8, "out")
     _check(lib().rtl_quantize_mxfp4(_p(X), rows, cols, ld, _p(q), ldq, _p(s), _p(qt), ldqt, _p(st), _on(dev)), "rtl_quantize_mxfp4")
     return (q, s, qt, st) if along == "both" else (q, s) if along == "cols" else (qt, st)

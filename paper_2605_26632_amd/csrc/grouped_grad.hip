@@ -507,6 +507,7 @@ auto with_dgrad(int shape, Op op) {
 template <class Op>
 auto with_wgrad(int shape, Op op) {
     if (shape == 0) return op(Grad<128, 128, 2, 2, 4>{});
+    if (shape == 2) return op(Grad<128, 128, 2, 2, 2>{});
     return op(Grad<256, 256, 2, 4, 2>{});
 }
 
@@ -537,17 +538,25 @@ struct WgradPlan {
 static size_t wgrad_plane(int64_t E, int64_t N, int64_t K) { return (size_t)E * (size_t)N * (size_t)(K + 1) * 4; }
 static WgradPlan wgrad_plan(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
     const double rows = T > 0 ? (double)T / (double)(E < T ? E : T) : 0, stages = rows / 64 + 0.5;
-    auto us = [&](int64_t side, double fixed, double stage, int parts) {
+    auto us = [&](int shape, int parts) {
+        const int64_t side = shape == 1 ? 256 : 128;
         const double tiles = (double)parts * (double)(E * ((N + side - 1) / side) * ((K + side - 1) / side)), passes = tiles > 256 ? tiles / 256 : 1;
-        return fixed * (1 + (side == 128 ? 0.6 : 0.9) * (passes - 1)) + stage * (stages / parts) * passes;
+        const double fixed = shape == 0 ? 4.8 : shape == 1 ? 9.0 : 4.0;
+        // (a ring of two leaves room for two workgroups a unit, which pull more slowly each)
+        const double stage = shape == 0 ? 0.53 : shape == 1 ? 1.5 : passes < 2 ? 0.785 - 0.255 * (passes - 1) : 0.53;
+        return fixed * (1 + (shape == 1 ? 0.9 : 0.78) * (passes - 1)) + stage * (stages / parts) * passes;
     };
-    const double small = us(128, 4.8, 0.53, 1), big = us(256, 9.0, 1.5, 1);
-    WgradPlan plan{small < big ? 0 : 1, 1};
-    double best = small < big ? small : big;
+    WgradPlan plan{0, 1};
+    double best = us(0, 1);
+    for (int shape = 1; shape < 3; ++shape)
+        if (us(shape, 1) < best) {
+            best = us(shape, 1);
+            plan.shape = shape;
+        }
     for (int parts = 2; parts <= 64 && parts * 2 <= stages; parts *= 2) {
         const double bytes = (double)parts * (double)wgrad_plane(E, N, K);
         if (bytes > (double)room) break;
-        const double t = us(128, 4.8, 0.53, parts) + 3.5 + bytes * 2 / 3.5e6;
+        const double t = us(0, parts) + 3.5 + bytes * 2 / 3.5e6;
         if (t < best * 0.95) {
             best = t;
             plan = WgradPlan{0, parts};
@@ -575,7 +584,7 @@ int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) {
 hipError_t prepare_grouped_grad_kernels() {
     hipError_t e = hipSuccess;
     for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_dgrad(i, [](auto k) { return decltype(k)::prepare_dgrad(); });
-    for (int i = 0; i < 2 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
+    for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
     hipFuncAttributes attr;
     if (e == hipSuccess) e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(wgrad_reduce_kernel));
     return e;

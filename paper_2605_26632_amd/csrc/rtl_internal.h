@@ -156,7 +156,8 @@ int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn);
 hipError_t prepare_grouped_kernels();
 // a: M the rows of X, W and the bias of expert 0 (bias [experts, N]); 4-bit: w_scale_rows = experts * N.
 // The forms that launches pick (host arithmetic, for the tests): forward 0 .. 2: 32 x 32, 64 x 64, 128 x 128 tiles, 3: panels of 256 and 128 rows, 4: few rows; input
-// gradient 0, 1: 64 x 128, 128 x 128, 2: panels; weight gradient out = {0: 128 x 128, 1: 256 x 256, parts of the rows}.
+// gradient 0, 1: 64 x 128, 128 x 128, 2: panels; weight gradient out = {0: 128 x 128, 1: 256 x 256, 2: 128 x 128 with
+// a ring of two, parts of the rows}.
 int grouped_form(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);
 int dgrad_shape(int64_t T, int64_t E, int64_t N, int64_t K);
 void wgrad_choice(int64_t T, int64_t E, int64_t N, int64_t K, size_t room, int out[2]);

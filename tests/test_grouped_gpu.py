@@ -164,7 +164,7 @@ def test_sizes_reach_every_form():
     assert {plan.forward_form(T + 8, E, N - 3, K) for T, E, N, K, _ in SIZES} == {0, 1, 2, 3, 4}
     assert {plan.forward_form(T + 3, E, N - 3, K, True) for T, E, N, K, _ in MX_SIZES} == {0, 1, 2, 3, 4}
     assert {plan.dgrad_form(T + 6, E, N, K - 24) for T, E, N, K, _ in DGRAD_SIZES} == {0, 1, 2}
-    assert {(s, p > 1) for s, p in (plan.wgrad_form(T + 160, E, N, K) for T, E, N, K, _ in WGRAD_SIZES)} == {(0, False), (1, False), (0, True)}
+    assert {(s, p > 1) for s, p in (plan.wgrad_form(T + 160, E, N, K) for T, E, N, K, _ in WGRAD_SIZES)} == {(0, False), (1, False), (2, False), (0, True)}
 
 
 def test_gradients_against_differences():
