@@ -234,14 +234,16 @@ FewRows few_rows_choice(int64_t M, int64_t most, int64_t K, bool fp4) {
     return M * K <= 8192 && FewQuantWide::lds(most, K) <= kFewLds ? FewRows::quantise : FewRows::direct;
 }
 
-// us of a grouped launch: the weights of the experts that can have rows at the rate of a stream, or the chain of 16-row blocks of an expert of one and a half
-// times the average, whichever is longer, and the start of the workgroups. Against 250 measured problems ([1..64 experts, 1..16 rows each, 256..4096, 512..6144])
-// off by 3 % (bf16) and 12 % (4-bit) in the mean, by a third where many workgroups have little to read.
-double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
-    const double experts = (double)(E < T ? E : T), rows = (double)T / experts;
-    const double batches = (double)(fp4 ? (K + 2047) / 2048 : (K + 1023) / 1024), chain = (double)(int64_t)((rows * 1.5 + 15) / 16);
-    const double stream = experts * (double)N * (double)K * (fp4 ? 17.0 / 32 : 2.0) * (1 + 0.35 * (chain - 1)) / 4.9e6, serial = chain * (0.5 + 1.4 * batches);
-    return 2.6 + (stream > serial ? stream : serial) + experts * (double)((N + 15) / 16) / 256 * 0.045 * (1 + rows / 8);
+// us of a grouped launch that cannot be shorter than `stream` us: its workgroups, three to a unit at a time, each as long as its batches of lines and its
+// expert's 16-row blocks (an expert of one and a half times the average rows). More than two rounds of workgroups read at a lower rate than tiles do: bf16
+// [64, 64, 1024, 2048] 37.5 us against 29.5 with panels, where [24, 32, 1408, 1024], two rounds, takes 12.0 against 14.2 with 64 x 64 tiles (changing inputs).
+double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4, double stream) {
+    const double experts = group_experts(T, E), rows = (double)T / experts, cols = fp4 && (double)(E < T ? E : T) * (double)N >= (double)kWide ? 32 : 16;
+    const double many = rows * 1.5 / 16, batches = (double)(fp4 ? (K + 2047) / 2048 : (K + 1023) / 1024);
+    const double waves = experts * (double)(int64_t)(((double)N + cols - 1) / cols) / (256 * 3);
+    const double chain = 2.0 + (waves > 1 ? waves : 1) * ((fp4 ? 1.0 : 2.0) + 1.4 * batches) * (many > 1 ? many : 1);
+    const double read = stream * (waves > 2 ? 1 + 0.1 * (waves - 2) : 1);
+    return chain > read ? chain : read;
 }
 
 hipError_t prepare_few_rows_kernels() {

@@ -1,5 +1,6 @@
 // Linears grouped by expert: Y[rows of e] = X[rows of e] W[e]^T (+ b[e]), bf16 or microscaled 4-bit operands, on the dense tile loop.
 // An expert's rows are a problem of their own inside the launch: same loop, operands shifted to the expert's first row and weight.
+#include <cmath>
 #include "groups.h"
 
 namespace rtl {
@@ -86,34 +87,39 @@ int64_t group_grid(int64_t T, int64_t E, int64_t cols, int64_t bm, int64_t bn) {
     return (T / bm + (E < T ? E : T)) * ((cols + bn - 1) / bn);
 }
 
+double group_experts(int64_t T, int64_t E) { return E > 1 ? (double)E * (1 - std::pow(1 - 1.0 / (double)E, (double)T)) : 1.0; }
+
 double group_panels(int64_t T, int64_t E, int64_t bm) {
-    const double experts = (double)(E < T ? E : T), panels = (double)T / experts / (double)bm + 0.5;
+    const double experts = group_experts(T, E), panels = (double)T / experts / (double)bm + 0.5;
     return experts * (panels > 1 ? panels : 1);
 }
 
-// Form of a launch: index of with_grouped, or kFew for few_rows.hip, the one with the least estimated time. us of a form: `fixed` and `stage` per 128-byte stage
-// of the contraction while its tiles find a unit each, more passes in proportion (but only 0.6 of `fixed` again: the next tile starts while another ends).
-// Measured at 8, 128, 256 and 512 tiles and 8 and 64 stages. Over 630 problems ([1..64 experts, 1..2000 rows each, 256..4096, 512..6144], uneven experts), bf16 and
-// 4-bit, the choice is 5 and 7 % slower in the mean than the best form; by rows per expert alone a form could take six times as long as the best.
+// Form of a launch: index of with_grouped, or kFew for few_rows.hip, the one with the least estimated time. us of a tile form: `fixed` and `stage` per 128-byte
+// stage of the contraction while its tiles find a unit each, more passes in proportion (but only 0.6 of `fixed` again: the next tile starts while another
+// ends); measured at 8, 128, 256 and 512 tiles and 8 and 64 stages. No form is faster than what it reads and writes (6.5 TB/s, part of it in the MALL).
+// Over 610 problems ([1..64 experts, 1..2000 rows each, 256..4096, 512..6144], uneven experts), bf16 and 4-bit, the choice is 6 and 5 % slower in the mean
+// than the best form; by rows per expert alone it could take six times as long.
 constexpr int kFew = 4;
 int grouped_form(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4) {
     struct Form { int bm, bn; double fixed, stage; };
     static constexpr Form kForms[] = {{32, 32, 3.7, 0.09}, {64, 64, 4.2, 0.185}, {128, 128, 5.0, 0.43}};
-    const double stages = (double)(fp4 ? (K + 255) / 256 : K / 64);
-    int pick = 3;
+    const double stages = (double)(fp4 ? (K + 255) / 256 : K / 64), t = (double)T, n = (double)N, k = (double)K;
+    const double stream = 2.5 + (group_experts(T, E) * n * k * (fp4 ? 17.0 / 32 : 2.0) + t * k * (fp4 ? 17.0 / 32 : 2.0) + t * n * 2) / 6.5e6;
+    auto floored = [&](double us) { return us > stream ? us : stream; };
     const double halves = group_panels(T, E, 128) * (double)((N + 255) / 256), rounds = halves > 256 ? halves / 256 : 1;
-    double best = 6.5 + (rounds - 1) * 5 + (0.6 + 0.15 * (halves < 256 ? halves / 256 : 1)) * stages * rounds;
+    int pick = 3;
+    double best = floored(6.5 + (rounds - 1) * 5 + (0.6 + 0.15 * (halves < 256 ? halves / 256 : 1)) * stages * rounds);
     for (int i = 0; i < 3; ++i) {
         const Form& f = kForms[i];
         const double tiles = group_panels(T, E, f.bm) * (double)((N + f.bn - 1) / f.bn), passes = tiles > 256 ? tiles / 256 : 1;
-        const double us = f.fixed * (1 + 0.6 * (passes - 1)) + f.stage * stages * passes;
+        const double us = floored(f.fixed * (1 + 0.6 * (passes - 1)) + f.stage * stages * passes);
         if (us < best) {
             best = us;
             pick = i;
         }
     }
     const FewRows few = T <= 8 * E ? few_rows_choice((T + E - 1) / E, T, K, fp4) : FewRows::no;
-    if (few != FewRows::no && few_rows_us(T, E, N, K, fp4) - (few == FewRows::quantise ? 2.5 : 0) < best) pick = kFew;
+    if (few != FewRows::no && few_rows_us(T, E, N, K, fp4, stream) - (few == FewRows::quantise ? 2.5 : 0) <= best) pick = kFew;
     return pick;
 }
 

@@ -168,12 +168,14 @@ hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t str
 // quantised inside, without. M: rows of the product, or of an expert on average, `most` at most; `quantise`: worth quantising inside.
 enum class FewRows { no, direct, quantise };
 FewRows few_rows_choice(int64_t M, int64_t most, int64_t K, bool fp4);
-double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);      // estimate for a grouped product
+double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4, double stream);      // estimate for a grouped product
 hipError_t prepare_few_rows_kernels();
 hipError_t launch_few_rows(const GemmArgs& a, hipStream_t stream);
 hipError_t launch_grouped_few_rows(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
 int64_t few_rows_grid(int64_t E, int64_t N);
 FewRows grouped_few_rows(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);       // what launch_grouped decides
+// How many of E experts have rows when T rows fall on them evenly at random.
+double group_experts(int64_t T, int64_t E);
 // Panels of `bm` rows that T rows over E experts make on average: half a panel is lost at each expert's end.
 double group_panels(int64_t T, int64_t E, int64_t bm);
 struct GroupedGradArgs {

@@ -43,7 +43,7 @@ def strided(t, pad=8, fill=float("nan")):
 # on average and more than sixteen of them with one expert
 SIZES = [(1, 1, 40, 64, 0.0), (1, 5, 24, 128, 0.0), (7, 3, 264, 192, 0.3), (70, 70, 64, 64, 0.5), (90, 2, 136, 320, 0.0), (300, 130, 72, 128, 0.3),
          (130, 3, 256, 576, 0.0), (500, 4, 200, 256, 0.2), (600, 2, 520, 192, 0.0), (1030, 3, 312, 448, 0.3), (777, 1, 264, 320, 0.0), (60, 8, 96, 704, 0.6),
-         (8, 2, 1304, 64, 0.0), (40, 5, 4752, 64, 0.2), (160, 20, 2504, 64, 0.3), (12, 20, 1000, 320, 0.3)]
+         (8, 2, 1304, 64, 0.0), (40, 5, 4752, 64, 0.2), (160, 20, 2504, 64, 0.3), (9, 8, 1400, 704, 0.3)]
 
 
 @pytest.mark.parametrize("T,E,N,K,empty", SIZES)
@@ -67,7 +67,7 @@ def test_forward(T, E, N, K, empty, bias):
                 ref.check_product(Y[o[e]:o[e + 1]], ref.values(X[o[e]:o[e + 1]]), ref.values(W[e]), None if b is None else ref.values(b[e]))
 
 
-DGRAD_SIZES = SIZES + [(545, 8, 40, 3744, 0.0), (8, 8, 40, 8216, 0.3)]
+DGRAD_SIZES = SIZES + [(1230, 20, 40, 1720, 0.0), (22, 20, 40, 4264, 0.3)]
 
 
 @pytest.mark.parametrize("T,E,N,K,empty", DGRAD_SIZES)
