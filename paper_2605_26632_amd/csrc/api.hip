@@ -566,7 +566,7 @@ rtl_status rtl_quantize_mxfp4(const void* X, int64_t rows, int64_t cols, int64_t
     if (too_large(rows) || too_large(cols) || ld < cols || cols % (along ? 32 : 8) != 0) return RTL_ERR_SHAPE;
     if (along && ldq < cols / 2) return RTL_ERR_SHAPE;
     if (down && ldqt < (rows + 31) / 32 * 16) return RTL_ERR_SHAPE;
-    if (((rows + 31) / 32) * ((cols + 127) / 128) >= ((int64_t)1 << 31)) return RTL_ERR_SHAPE;      // workgroups
+    if (((rows + 31) / 32) * ((cols + 255) / 256) >= ((int64_t)1 << 24)) return RTL_ERR_SHAPE;      // workgroups of 256
     if (rows == 0 || cols == 0) return RTL_OK;
     if (!X || (!along && !down) || (along && (!Q || !S)) || (down && (!Qt || !St))) return RTL_ERR_NULL;
     if (ld % 8 != 0 || !aligned(X, 16)) return RTL_ERR_ALIGN;

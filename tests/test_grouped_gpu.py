@@ -282,3 +282,40 @@ def test_training_step_captured_and_replayed():
         torch.cuda.synchronize()
         for got, w in zip((Y, Yq, dX, dW, db), want):
             assert torch.equal(got, w)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements in front of the rows that count: the last ones of every operand against the definition."""
+    T, E, N, K = 36000, 2, 40, 65536                       # X and dX: 4.7 GB
+    off = torch.tensor([0, T - 70, T], dtype=torch.int32, device=DEV)
+    gen = generator(8)
+    X = torch.zeros(T, K, dtype=torch.bfloat16, device=DEV)
+    X[T - 70:] = bf16(gen, 70, K)
+    W = bf16(gen, E, N, K)
+    G = torch.zeros(T, N, dtype=torch.bfloat16, device=DEV)
+    G[T - 70:] = bf16(gen, 70, N)
+    x, w, g = X[T - 70:].double(), W[1].double(), G[T - 70:].double()
+    half = 2.0 ** -8
+
+    def near(y, a, b):
+        want, mag = a @ b.contiguous(), a.abs() @ b.abs().contiguous()
+        assert ((y.double() - want).abs() <= (a.shape[1] + 2) * 2.0 ** -24 * mag * (1 + half) + half * want.abs()).all()
+
+    Y = rtl.grouped_linear(X, off, W)
+    near(Y[T - 70:], x, w.t())
+    assert (Y[:T - 70] == 0).all()
+    dX = rtl.grouped_linear_dgrad(G, off, W)
+    near(dX[T - 70:], g, w)
+    del dX
+    dW, _ = rtl.grouped_linear_wgrad(G, X, off)
+    near(dW[1], g.t().contiguous(), x)
+    assert (dW[0] == 0).all()
+    q, s = rtl.quantize_mxfp4(X)
+    tail = rtl.quantize_mxfp4(X[T - 70:])
+    assert torch.equal(q[T - 70:], tail[0]) and torch.equal(s[:, T - 70:], tail[1])
+    values = rtl.dequantize_mxfp4(q, s)
+    assert torch.equal(values[T - 70:], rtl.dequantize_mxfp4(*tail))
+    del values
+    wq, ws = rtl.quantize_mxfp4(W.view(E * N, K))
+    Yq = rtl.grouped_mxfp4_linear(X, off, wq.view(E, N, K // 2), ws)
+    near(Yq[T - 70:], rtl.dequantize_mxfp4(*tail).double(), rtl.dequantize_mxfp4(wq, ws)[N:].double().t())

@@ -17,7 +17,7 @@ def test_quantize_refusals():
     d = dict(X=FAKE, rows=4, cols=64, ld=64, Q=FAKE, ldq=32, S=FAKE, Qt=FAKE, ldqt=16, St=FAKE, stream=None)
     f = lambda **kw: call(rtl.lib().rtl_quantize_mxfp4, d, **kw)
     assert f(cols=40, ld=64) == SHAPE and f(cols=44, ld=64, Q=None, S=None) == SHAPE and f(ld=56) == SHAPE
-    assert f(rows=-1) == SHAPE and f(cols=-32) == SHAPE and f(rows=(1 << 30) + 1, ldqt=1 << 40) == SHAPE
+    assert f(rows=-1) == SHAPE and f(cols=-32) == SHAPE and f(rows=(1 << 30) + 1, ldqt=1 << 40) == SHAPE and f(rows=1 << 29, ldqt=1 << 28) == SHAPE
     assert f(ldq=16) == SHAPE and f(rows=33, ldqt=16) == SHAPE
     assert f(X=None) == NULL and f(Q=None) == NULL and f(S=None) == NULL and f(Qt=None) == NULL and f(St=None) == NULL
     assert f(Q=None, S=None, Qt=None, St=None) == NULL
