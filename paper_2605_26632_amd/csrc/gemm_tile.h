@@ -316,7 +316,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         }
     }
     // FP4 256 x 256: scales and fragments leave no room for an offset per request. A wave takes requests of one chunk order (eight rows each, all
-    // even or all odd), so that they differ in the row only, and forms each offset anew from the lane's first row and its chunk.
+    // even or all odd), so that they differ in the row only, and forms each offset anew from the lane's first row and its chunk. [4608, 3072, 12288]
+    // 83.5 us (256 x 192 tiles, which need none of this, 98.1), 216 tiles, matrix cores busy 44 % at 2.16 GHz.
     constexpr bool LEAN = FP4 && BM == 256 && BN == 256 && NW == 8;
     constexpr int OA = LEAN ? 2 : A_PER_W, OB = LEAN ? 2 : B_PER_W;
     auto lean_unit = [&](int s) { return (wave & 1) | s << 1 | (wave >> 1) << 3; };

@@ -79,7 +79,7 @@ __device__ __forceinline__ bool group_tile(const int* offsets, int E, int T, int
 // Two tile heights in one launch, for experts of many rows: 256 rows for as many panels as suit, 128 for the rest of the rows. An expert's last rows are
 // seldom a full panel, and uniform tiles leave the last round mostly empty (8192 rows over eight experts: 37 panels, with 2048 columns 296 tiles of
 // 256 x 256, 1.16 rounds that cost 2). (192 rows as a third height end launches sooner by this count and not by the clock: the matrix instructions run at the power
-// limit, and lower tiles take more energy per product. Sustained, on inputs that change: [8192, 4096, 2048] over uneven experts 163 us without, 176 with.)
+// limit, and lower tiles take more energy per product. Sustained, on inputs that change: [8192, 4096, 2048] over uneven experts 163 us without, 177 with, medians of three runs.)
 struct MixedTile {
     bool tall;
     int expert, begin, rows, panels, tile;       // begin, rows: the expert's rows that are cut into `panels` of this height
@@ -161,7 +161,7 @@ __device__ __forceinline__ bool find_mixed(const int* offsets, int E, int T, int
 
 // All tiles of the launch on kUnits workgroups: an XCD's share of the list (tall tiles first) is dealt to its workgroups to and fro, so that who got a
 // late, small tile gets an early one next. (Left to the hardware a tile waits for a unit of the shader engine that is next in turn, whatever
-// units are free elsewhere: input gradient of 248 tall tiles and 16 half ones, 64 stages, 146 -> 120 us; forward of 496 and 32, 32 stages, 133 -> 123.) `work` is called with each tile of this workgroup.
+// units are free elsewhere: input gradient of 248 tall tiles and 16 half ones, 64 stages, 151 -> 126 us; forward of 496 and 32, 32 stages, 137 -> 128.) `work` is called with each tile of this workgroup.
 template <class Work>
 __device__ __forceinline__ void mixed_tiles(const int* offsets, int E, int T, int tiles_n, int stages, Work work) {
     const MixedPlan plan = plan_mixed(offsets, E, T, tiles_n, stages);

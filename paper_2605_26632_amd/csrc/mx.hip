@@ -6,7 +6,8 @@
 // In bf16 bits floor(log2 max|x|) is the exponent field of the largest magnitude: the scale byte is max(field - 2, 0). The division by the
 // power of two, the rounding and the saturation are one conversion instruction for two values. A block with a NaN or an infinity gets the
 // scale byte 0xFF (NaN), which makes all of it NaN: no finite value stands for something that was not finite.
-// All of it is bound by memory: 2 bytes read and 17/32 written per value and direction.
+// All of it is bound by memory: 2 bytes read and 17/32 written per value and direction. The same inputs again and again (so partly in the MALL):
+// rows [4608, 12288] 21.0 us = 6.8 TB/s, back 22.6 us = 6.3 TB/s; columns and rows of [2111, 2048] in one read 7.7 us (144 workgroups: latency).
 #include "mx_codes.h"
 
 namespace rtl {
