@@ -339,8 +339,11 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
  *            in bytes, % 16 == 0), Ws the scales of the [E * N, K] matrix of all experts' rows (what rtl_quantize_mxfp4 makes of it in one call).
  *            K % 32 == 0; X as for rtl_mxfp4_linear.
  *   workspace  rtl_grouped_mxfp4_linear_workspace(T, E, N, K) bytes, 256-byte aligned.
+ * rtl_grouped_clear        zeros into the rows of a [T, cols] bf16 matrix (ld, 2-byte aligned) that belong to nobody, all of them for E == 0; the others
+ *            stay as they are. In front of a product it makes a whole result of memory that was never written. T == 0, cols == 0: RTL_OK.
  * ------------------------------------------------------------------------------------------- */
 typedef enum { RTL_BF16 = 0, RTL_F32 = 1 } rtl_dtype;
+rtl_status rtl_grouped_clear(const int32_t* offsets, void* Y, int64_t T, int64_t E, int64_t cols, int64_t ld, void* stream);
 rtl_status rtl_grouped_linear(const void* X, const int32_t* offsets, const void* W, const void* bias, void* Y,
                               int64_t T, int64_t E, int64_t N, int64_t K,
                               int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, void* stream);

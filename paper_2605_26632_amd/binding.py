@@ -24,7 +24,7 @@ SYMBOLS = ["rtl_sparsify_pack_workspace", "rtl_sparsify_pack", "rtl_packed_linea
            "rtl_sparse_lora_linear_fp8_workspace", "rtl_sparse_lora_linear_fp8",
            "rtl_quantize_mxfp4", "rtl_dequantize_mxfp4", "rtl_mxfp4_packed_linear_workspace", "rtl_mxfp4_packed_linear",
            "rtl_mxfp4_linear_workspace", "rtl_mxfp4_linear",
-           "rtl_grouped_linear", "rtl_grouped_linear_dgrad", "rtl_grouped_linear_wgrad_workspace", "rtl_grouped_linear_wgrad",
+           "rtl_grouped_clear", "rtl_grouped_linear", "rtl_grouped_linear_dgrad", "rtl_grouped_linear_wgrad_workspace", "rtl_grouped_linear_wgrad",
            "rtl_grouped_mxfp4_linear_workspace", "rtl_grouped_mxfp4_linear",
            "rtl_diag_matrix_rate", "rtl_diag_fill_rate", "rtl_diag_pack_sweep", "rtl_diag_tile_plan", "rtl_init", "rtl_status_str", "rtl_version"]
 
@@ -100,6 +100,8 @@ def lib():
         L.rtl_mxfp4_linear_workspace.restype = sz
         L.rtl_mxfp4_linear.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, sz, vp]
         L.rtl_mxfp4_linear.restype = ci
+        L.rtl_grouped_clear.argtypes = [vp, vp] + [i64] * 4 + [vp]
+        L.rtl_grouped_clear.restype = ci
         L.rtl_grouped_linear.argtypes = [vp, vp, vp, vp, vp] + [i64] * 8 + [vp]
         L.rtl_grouped_linear.restype = ci
         L.rtl_grouped_linear_dgrad.argtypes = [vp, vp, vp, vp] + [i64] * 8 + [vp]
@@ -395,10 +397,10 @@ def _whole(t, shape, dtype, name):
         raise ValueError("%s: contiguous %s tensor of shape %s expected" % (name, dtype, tuple(shape)))
 
 
-def _output(out, rows, cols, dtype, like, new=torch.empty):
+def _output(out, rows, cols, dtype, like):
     """(out or a new tensor, its row stride)."""
     if out is None:
-        return new(rows, cols, dtype=dtype, device=like.device), cols
+        return torch.empty(rows, cols, dtype=dtype, device=like.device), cols
     m, n, ld = _matrix(out, dtype, "out")
     if m != rows or n != cols:
         raise ValueError("out: shape (%d, %d) expected" % (rows, cols))
@@ -504,6 +506,26 @@ def mxfp4_linear(X, Wq, Ws, bias=None, out=None, ws=None):
 # ---- linears grouped by expert: rows offsets[e] .. offsets[e + 1] of the activation belong to weight e ------------
 # `out` of the row-wise results: rows of no expert keep what it held; without `out` they are zeros.
 
+def _rows_output(out, rows, cols, like, offsets, E, dev):
+    """(out, or a new tensor with zeros in the rows of no expert, its row stride)."""
+    Y, ld = _output(out, rows, cols, torch.bfloat16, like)
+    if out is None:
+        _check(lib().rtl_grouped_clear(_p(offsets), _p(Y), rows, E, cols, ld, _on(dev)), "rtl_grouped_clear")
+    return Y, ld
+
+
+def grouped_clear(offsets, out):
+    """rtl_grouped_clear: zeros into the rows of `out` (bf16 [T,N]) that belong to no expert."""
+    dev = _here(offsets, out)
+    T, N, ld = _matrix(out, torch.bfloat16, "out")
+    E = offsets.numel() - 1
+    if E < 0:
+        raise ValueError("offsets: at least one number expected")
+    _whole(offsets, (E + 1,), torch.int32, "offsets")
+    _check(lib().rtl_grouped_clear(_p(offsets), _p(out), T, E, N, ld, _on(dev)), "rtl_grouped_clear")
+    return out
+
+
 def grouped_linear(X, offsets, W, bias=None, out=None):
     """rtl_grouped_linear: Y[rows of e] = X[rows of e] W[e]^T (+ bias[e]); X bf16 [T,K], offsets int32 [E+1] on the device,
     W bf16 [E,N,K], bias [E,N]; bf16 [T,N]."""
@@ -514,7 +536,7 @@ def grouped_linear(X, offsets, W, bias=None, out=None):
         raise ValueError("X and W differ in K")
     _whole(offsets, (E + 1,), torch.int32, "offsets")
     _whole(bias, (E, N), torch.bfloat16, "bias")
-    Y, ldy = _output(out, T, N, torch.bfloat16, X, torch.zeros)
+    Y, ldy = _rows_output(out, T, N, X, offsets, E, dev)
     st = lib().rtl_grouped_linear(_p(X), _p(offsets), _p(W), _p(bias), _p(Y), T, E, N, K, ldx, ldw, stride, ldy, _on(dev))
     _check(st, "rtl_grouped_linear")
     return Y
@@ -528,7 +550,7 @@ def grouped_linear_dgrad(dY, offsets, W, out=None):
     if N_w != N:
         raise ValueError("dY and W differ in N")
     _whole(offsets, (E + 1,), torch.int32, "offsets")
-    dX, ldx = _output(out, T, K, torch.bfloat16, dY, torch.zeros)
+    dX, ldx = _rows_output(out, T, K, dY, offsets, E, dev)
     st = lib().rtl_grouped_linear_dgrad(_p(dY), _p(offsets), _p(W), _p(dX), T, E, N, K, lddy, ldw, stride, ldx, _on(dev))
     _check(st, "rtl_grouped_linear_dgrad")
     return dX
@@ -585,7 +607,7 @@ def grouped_mxfp4_linear(X, offsets, Wq, Ws, bias=None, out=None, ws=None):
     _whole(offsets, (E + 1,), torch.int32, "offsets")
     _whole(Ws, mxfp4_scales_shape(E * N, K), torch.uint8, "Ws")
     _whole(bias, (E, N), torch.bfloat16, "bias")
-    Y, ldy = _output(out, T, N, torch.bfloat16, X, torch.zeros)
+    Y, ldy = _rows_output(out, T, N, X, offsets, E, dev)
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_grouped_mxfp4_linear_workspace(T, E, N, K), X.device)

@@ -692,6 +692,16 @@ static rtl_status check_grouped(const void* X, const int32_t* offsets, const voi
     return RTL_OK;
 }
 
+rtl_status rtl_grouped_clear(const int32_t* offsets, void* Y, int64_t T, int64_t E, int64_t cols, int64_t ld, void* stream) {
+    if (bad_group_sizes(T, E, cols, 0) || ld < cols) return RTL_ERR_SHAPE;
+    if (T == 0 || cols == 0) return RTL_OK;
+    if (!offsets || !Y) return RTL_ERR_NULL;
+    if (!aligned(offsets, 4) || !aligned(Y, 2)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    return rtl::launch_grouped_clear(offsets, (int)E, static_cast<uint16_t*>(Y), T, cols, ld, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK
+                                                                                                                                              : RTL_ERR_HIP;
+}
+
 rtl_status rtl_grouped_linear(const void* X, const int32_t* offsets, const void* W, const void* bias, void* Y, int64_t T, int64_t E, int64_t N, int64_t K,
                               int64_t ldx, int64_t ldw, int64_t stride_w, int64_t ldy, void* stream) {
     const rtl_status st = check_grouped(X, offsets, W, bias, Y, T, E, N, K, ldx, ldw, stride_w, ldy, false);

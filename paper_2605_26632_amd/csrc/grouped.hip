@@ -1,7 +1,7 @@
 // Linears grouped by expert: Y[rows of e] = X[rows of e] W[e]^T (+ b[e]), bf16 or microscaled 4-bit operands, on the dense tile loop.
 // An expert's rows are a problem of their own inside the launch: same loop, operands shifted to the expert's first row and weight.
-// [8192, 4096, 2048] over eight experts, inputs that change: 131 us with 1024 rows each, 152 with 484 to 1997 (uneven rounds), where the dense linear takes
-// 109 with a single weight. 4-bit, uneven, the same inputs again: 56.5 us, eight stages a tile; bf16 then 127.9, matrix cores busy 51 % at 2.09 GHz.
+// [8192, 4096, 2048] over eight experts, inputs that change: 124 us with 1024 rows each, 147 with 484 to 1997 (uneven rounds). Into a given
+// result one expert takes 108, eight even ones that share a weight 106, with weights of their own 118, the dense linear 107. 4-bit, uneven, the same inputs again: 56.5 us, eight stages a tile; bf16 then 127.9, matrix cores busy 51 % at 2.09 GHz.
 #include <cmath>
 #include "groups.h"
 
@@ -72,6 +72,21 @@ struct Grouped {
         return hipGetLastError();
     }
 };
+
+// Zeros into the rows in front of the first expert's and behind the last one's, a thread to eight columns at a time. What it writes is seldom more than a
+// few rows, so that it costs its launch, where a fill of the whole result writes all of it twice ([8192, 4096] beside the product into a given result: 13.0 -> 1.6 to 4.2 us).
+constexpr int kClearGrid = 1024;
+__global__ __launch_bounds__(256) void grouped_clear_kernel(const int* offsets, int E, uint16_t* Y, int64_t T, int64_t cols, int64_t ld) {
+    const int64_t first = min((int64_t)max(offsets[0], 0), T), last = min(max((int64_t)offsets[E], first), T);
+    const int64_t chunks = (cols + 7) / 8, all = (first + T - last) * chunks;
+    for (int64_t n = blockIdx.x * (int64_t)256 + threadIdx.x; n < all; n += (int64_t)gridDim.x * 256) {
+        const int64_t i = n / chunks, col = n % chunks * 8;
+        uint16_t* p = Y + (i < first ? i : i - first + last) * ld + col;
+        if (col + 8 <= cols && reinterpret_cast<uintptr_t>(p) % 16 == 0) *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
+        else
+            for (int64_t j = 0; j < 8 && col + j < cols; ++j) p[j] = 0;
+    }
+}
 
 template <bool FP4, class Op>
 auto with_grouped(int shape, Op op) {
@@ -144,6 +159,12 @@ hipError_t prepare_grouped_kernels() {
         if (e == hipSuccess) e = with_grouped<true>(i, prep);
     }
     return e;
+}
+
+hipError_t launch_grouped_clear(const int* offsets, int E, uint16_t* Y, int64_t T, int64_t cols, int64_t ld, hipStream_t stream) {
+    const int64_t want = (T * ((cols + 7) / 8) + 255) / 256;
+    hipLaunchKernelGGL(grouped_clear_kernel, dim3((unsigned)(want < kClearGrid ? want : kClearGrid)), dim3(256), 0, stream, offsets, E, Y, T, cols, ld);
+    return hipGetLastError();
 }
 
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream) {

@@ -12,8 +12,8 @@
 // halves of 32; the fragments of a half are read behind the matrix instructions of the half before it.
 // A contraction that is no multiple of 64 takes its last, partial block first: there the places behind its end are filled with zeros instead
 // of loaded (on both sides: what lies in memory behind an expert's rows may be NaN), at no cost to the loop.
-// 8192 rows, [4096, 2048], eight experts, inputs that change: input gradient 127 us with 1024 rows each, 165 with 484 to 1997 (216 tall and 104 half
-// tiles: the units are active 65 % of the launch); weight gradient 140 and 143. Matrix cores busy 42 and 43 % at 2.18 GHz, uneven.
+// 8192 rows, [4096, 2048], eight experts, inputs that change: input gradient 122 us with 1024 rows each, 161 with 484 to 1997 (216 tall and 104 half
+// tiles: the units are active 65 % of the launch); weight gradient 141 and 143. Matrix cores busy 42 and 43 % at 2.18 GHz, uneven.
 #include "groups.h"
 
 namespace rtl {

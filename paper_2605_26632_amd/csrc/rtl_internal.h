@@ -164,6 +164,7 @@ void wgrad_choice(int64_t T, int64_t E, int64_t N, int64_t K, size_t room, int o
 // Workgroups of the launch (the calls refuse kMaxGroupGrid and more).
 int64_t grouped_grid(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4);
 hipError_t launch_grouped(const GemmArgs& a, const GroupArgs& g, hipStream_t stream);
+hipError_t launch_grouped_clear(const int* offsets, int E, uint16_t* Y, int64_t T, int64_t cols, int64_t ld, hipStream_t stream);
 // Few rows (few_rows.hip): Y = X W^T read straight through, for 4-bit and grouped products. 4-bit: a.A holds codes with a.a_scale set, and is bf16,
 // quantised inside, without. M: rows of the product, or of an expert on average, `most` at most; `quantise`: worth quantising inside.
 enum class FewRows { no, direct, quantise };

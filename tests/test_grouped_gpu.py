@@ -319,3 +319,38 @@ def test_offsets_past_32_bits():
     wq, ws = rtl.quantize_mxfp4(W.view(E * N, K))
     Yq = rtl.grouped_mxfp4_linear(X, off, wq.view(E, N, K // 2), ws)
     near(Yq[T - 70:], rtl.dequantize_mxfp4(*tail).double(), rtl.dequantize_mxfp4(wq, ws)[N:].double().t())
+
+
+@pytest.mark.parametrize("T,offsets", [(1, [0, 1]), (1, [1, 1]), (9, [0, 4, 9]), (9, [3, 3, 5]), (9, [9]), (700, [1, 2, 699]), (700, [690, 700]), (40, [-5, 7, 90]),
+                                       (40, [2 ** 31 - 1, -2 ** 31]), (40, [30, 10, 20])])
+@pytest.mark.parametrize("cols,front", [(1, 0), (7, 1), (64, 0), (1027, 3), (1024, 8)])
+def test_clear_rows_of_no_expert(T, offsets, cols, front):
+    """Zeros in the rows before the first expert's and behind the last one's, at any alignment; the others, and what lies between rows, stay."""
+    full = torch.full((T, cols + front + 5), float("nan"), dtype=torch.bfloat16, device=DEV)
+    rtl.grouped_clear(torch.tensor(offsets, dtype=torch.int32, device=DEV), full[:, front:front + cols])
+    first = min(max(offsets[0], 0), T)
+    last = max(first, min(max(offsets[-1], 0), T))
+    want = torch.full_like(full, float("nan"))
+    want[:first, front:front + cols] = 0
+    want[last:, front:front + cols] = 0
+    assert torch.equal(full.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("offsets", [[4, 10, 10, 25], [0, 0, 0, 0], [31, 31, 31, 31], [0, 5, 20, 31]])
+def test_new_results_hold_zeros_in_rows_of_no_expert(offsets):
+    """Results the calls allocate, in memory that held NaN before; three experts, and none at all."""
+    gen, T, N, K, first, last = generator(3), 31, 72, 64, offsets[0], offsets[-1]
+    X, G, W = bf16(gen, T, K), bf16(gen, T, N), bf16(gen, 3, N, K)
+    off, (Wq, Ws) = torch.tensor(offsets, dtype=torch.int32, device=DEV), rtl.quantize_mxfp4(W.view(3 * N, K))
+    calls = [lambda out=None: rtl.grouped_linear(X, off, W, out=out), lambda out=None: rtl.grouped_linear_dgrad(G, off, W, out=out),
+             lambda out=None: rtl.grouped_mxfp4_linear(X, off, Wq.view(3, N, K // 2), Ws, out=out)]
+    for call, cols in zip(calls, (N, K, N)):
+        for _ in range(3):
+            dirty = torch.full((T, cols), float("nan"), dtype=torch.bfloat16, device=DEV)
+            given = call(torch.zeros_like(dirty))
+            del dirty
+            new = call()
+            assert torch.equal(new.view(torch.int16), given.view(torch.int16))
+            assert (new[:first] == 0).all() and (new[last:] == 0).all()
+    empty = rtl.grouped_linear(X, off[:1].contiguous(), W[:0])
+    assert empty.shape == (T, N) and (empty == 0).all()

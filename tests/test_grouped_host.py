@@ -73,3 +73,12 @@ def test_binding_refuses_host_tensors():
               lambda: rtl.grouped_mxfp4_linear(x, off, w, w)):
         with pytest.raises(ValueError):
             f()
+
+
+def test_clear_refusals():
+    f = caller("rtl_grouped_clear", dict(off=FAKE, Y=FAKE, T=16, E=2, cols=24, ld=24, stream=None))
+    assert f(T=-1) == SHAPE and f(E=-1) == SHAPE and f(cols=-1) == SHAPE and f(ld=23) == SHAPE and f(T=BIG + 1) == SHAPE and f(E=65537) == SHAPE
+    assert f(off=None) == NULL and f(Y=None) == NULL and f(off=FAKE + 2) == ALIGN and f(Y=FAKE + 1) == ALIGN
+    assert f(T=0) == 0 and f(cols=0) == 0
+    with pytest.raises(ValueError):
+        rtl.grouped_clear(torch.zeros(3, dtype=torch.int32), torch.zeros(4, 8, dtype=torch.bfloat16))
