@@ -321,8 +321,9 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
  *            Rows in front of o_0 and from o_E on belong to nobody: they are neither used nor written. (Offsets are read by the
  *            kernels alone. Whatever they hold, nothing outside of the tensors is touched: they are cut to [0, T], and an
  *            expert that would end before it begins has no rows. What overlapping experts write is unspecified.)
- *   T        rows of the activation, E experts, 0 <= E <= 65536. T == 0, E == 0, N == 0 or K == 0 as for the other linears; a weight
- *            gradient is written for T == 0 too (zeros).
+ *   T        rows of the activation, E experts, 0 <= E <= 65536. A call with no experts or an empty result is RTL_OK with no launch (a weight gradient
+ *            is written for T == 0 too: zeros). An empty contraction is RTL_ERR_SHAPE: K == 0 in the forward products, N == 0 in dgrad with a result
+ *            that is not empty; likewise K == 0 in wgrad with dbias, which nothing would write.
  *   X [T, K] bf16 (ldx), W [E, N, K] bf16 (ldw between rows, stride_w between experts, both in elements, stride_w % 8 == 0; stride_w of
  *            0: one weight for all), bias NULL or bf16 [E, N], Y [T, N] bf16 (ldy).
  *

@@ -791,7 +791,8 @@ rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t
     if (dw_type != RTL_BF16 && dw_type != RTL_F32) return RTL_ERR_ARG;
     if (bad_group_sizes(T, E, N, K) || N % 8 != 0 || K % 8 != 0 || lddy < N || ldx < K || lddw < K) return RTL_ERR_SHAPE;
     if (bad_strides({lddy, ldx, lddw})) return RTL_ERR_SHAPE;
-    if (E == 0 || N == 0 || K == 0) return RTL_OK;
+    if (E == 0 || N == 0) return RTL_OK;
+    if (K == 0) return dbias ? RTL_ERR_SHAPE : RTL_OK;      // no tile whose first columns would write dbias
     if (E > 1 && stride_dw < (N - 1) * lddw + K) return RTL_ERR_SHAPE;       // experts' gradients must not overlap
     if (64 * rtl::wgrad_grid(E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
     if (!offsets || !dW || (T > 0 && (!dY || !X))) return RTL_ERR_NULL;

@@ -82,3 +82,11 @@ def test_clear_refusals():
     assert f(T=0) == 0 and f(cols=0) == 0
     with pytest.raises(ValueError):
         rtl.grouped_clear(torch.zeros(3, dtype=torch.int32), torch.zeros(4, 8, dtype=torch.bfloat16))
+
+
+def test_weight_gradient_refuses_a_bias_gradient_without_columns():
+    """K == 0 leaves no weight gradient to write, and nothing would write dbias, which is not empty."""
+    f = caller("rtl_grouped_linear_wgrad", dict(dY=FAKE, X=FAKE, off=FAKE, dW=FAKE, db=FAKE, type=0, T=16, E=2, N=24, K=0, lddy=24, ldx=0, lddw=0,
+                                                sdw=0, ws=None, wsb=0, stream=None))
+    assert f() == SHAPE and f(T=0) == SHAPE and f(type=1) == SHAPE
+    assert f(db=None) == 0 and f(E=0) == 0 and f(N=0) == 0
