@@ -329,11 +329,11 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
  *
  * rtl_grouped_linear       K % 64 == 0; alignment as for rtl_dense_linear. T, E, N must leave fewer than 2^24 workgroups (RTL_ERR_SHAPE).
  * rtl_grouped_linear_dgrad dX[o_e .. o_{e+1}) = dY[o_e .. o_{e+1}) W_e, bf16 [T, K] (lddx). N % 8 == 0, K % 8 == 0; dY [T, N] (lddy), W and
- *            dX 16-byte aligned with strides % 8 == 0.
+ *            dX 16-byte aligned with strides % 8 == 0. T, E, K must leave fewer than 2^24 workgroups.
  * rtl_grouped_linear_wgrad dW_e = dY_e^T X_e and, with dbias, db_e = the sum of the rows of dY_e, both of type dw_type
  *            (RTL_BF16 or RTL_F32): dW [E, N, K] (lddw, stride_dw >= (N - 1) lddw + K), dbias NULL or [E, N]. Every element is written, zeros for an expert
- *            without rows. Sizes and alignment as for dgrad. fp32 sums in a fixed order; a row of dY or X enters its own expert's
- *            gradient only, whatever it holds.
+ *            without rows. Sizes and alignment as for dgrad; E * ceil(N / 128) * ceil(K / 128) below 2^23 is always taken, 2^25 and more never (RTL_ERR_SHAPE).
+ *            fp32 sums in a fixed order; a row of dY or X enters its own expert's gradient only, whatever it holds.
  *   workspace  rtl_grouped_linear_wgrad_workspace(T, E, N, K) bytes (may be 0), all of it optional, as for rtl_dense_linear: room to cut many rows of
  *            few experts into parts; a smaller one groups the fp32 sums differently.
  * rtl_grouped_mxfp4_linear the forward product with the weights as MXFP4 codes and X quantised in the call: Wq [E, N, K / 2] bytes (ldw, stride_w

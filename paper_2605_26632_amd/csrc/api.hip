@@ -794,7 +794,9 @@ rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t
     if (E == 0 || N == 0) return RTL_OK;
     if (K == 0) return dbias ? RTL_ERR_SHAPE : RTL_OK;      // no tile whose first columns would write dbias
     if (E > 1 && stride_dw < (N - 1) * lddw + K) return RTL_ERR_SHAPE;       // experts' gradients must not overlap
-    if (64 * rtl::wgrad_grid(E, N, K) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    size_t room = workspace && aligned(workspace, 16) ? workspace_bytes : 0;                // none of it is mandatory
+    if (room > (size_t)RTL_STATIC_SCRATCH_BYTES) room = (size_t)RTL_STATIC_SCRATCH_BYTES;
+    if (rtl::wgrad_grid(T, E, N, K, room) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
     if (!offsets || !dW || (T > 0 && (!dY || !X))) return RTL_ERR_NULL;
     if (lddy % 8 != 0 || ldx % 8 != 0 || lddw % 8 != 0 || stride_dw % 8 != 0 || !aligned(dY, 16) || !aligned(X, 16) || !aligned(offsets, 4) ||
         !aligned(dW, 16) || (dbias && !aligned(dbias, dw_type == RTL_F32 ? 4 : 2)))
@@ -809,8 +811,6 @@ rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t
     g.bias_out = dbias;
     g.f32 = dw_type == RTL_F32;
     g.T = T; g.N = N; g.K = K; g.lddy = lddy; g.ldx = ldx; g.ldo = lddw; g.o_stride = stride_dw;
-    size_t room = workspace && aligned(workspace, 16) ? workspace_bytes : 0;                // none of it is mandatory
-    if (room > (size_t)RTL_STATIC_SCRATCH_BYTES) room = (size_t)RTL_STATIC_SCRATCH_BYTES;
     return rtl::launch_grouped_wgrad(g, workspace, room, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 

@@ -579,8 +579,9 @@ size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) 
 int64_t dgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K) {
     return with_dgrad(dgrad_shape(T, E, N, K), [&](auto k) { return decltype(k)::dgrad_grid(T, E, K); });
 }
-int64_t wgrad_grid(int64_t E, int64_t N, int64_t K) {
-    return with_wgrad(0, [&](auto k) { return decltype(k)::wgrad_grid(E, N, K); });      // (of the smaller tile)
+int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
+    const WgradPlan plan = wgrad_plan(T, E, N, K, room);
+    return with_wgrad(plan.shape, [&](auto k) { return decltype(k)::wgrad_grid(E, N, K) * (decltype(k)::block().x / 256); }) * plan.parts;
 }
 
 hipError_t prepare_grouped_grad_kernels() {

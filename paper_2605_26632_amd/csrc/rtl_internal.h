@@ -191,10 +191,11 @@ struct GroupedGradArgs {
 };
 hipError_t prepare_grouped_grad_kernels();
 int64_t dgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K);
-int64_t wgrad_grid(int64_t E, int64_t N, int64_t K);
 hipError_t launch_grouped_dgrad(const GroupedGradArgs& a, hipStream_t stream);
 // workspace: 16-byte aligned, `room` bytes of it at most for partial planes; wgrad_workspace: how much of `room` the call would use.
 size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
+// Workgroups of the launch with that room, those of 512 threads counted twice (a launch takes fewer than 2^32 threads).
+int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_t room, hipStream_t stream);
 
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------

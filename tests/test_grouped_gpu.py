@@ -354,3 +354,40 @@ def test_new_results_hold_zeros_in_rows_of_no_expert(offsets):
             assert (new[:first] == 0).all() and (new[last:] == 0).all()
     empty = rtl.grouped_linear(X, off[:1].contiguous(), W[:0])
     assert empty.shape == (T, N) and (empty == 0).all()
+
+
+def test_weight_gradient_of_more_experts_than_rows():
+    """40000 experts of one small tile each: every expert's gradient, in small integers and so exact."""
+    gen = generator(21)
+    T, E, N, K = 30000, 40000, 8, 16
+    where = torch.sort(torch.randint(0, E, (T,), generator=gen, device=DEV)).values
+    counts = torch.bincount(where, minlength=E)
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), counts.cumsum(0)]).to(torch.int32)
+    X, G = (torch.randint(-3, 4, (T, n), generator=gen, device=DEV).to(torch.bfloat16) for n in (K, N))
+    dW = torch.full((E, N, K), 7.0, device=DEV)
+    db = torch.full((E, N), 7.0, device=DEV)
+    rtl.grouped_linear_wgrad(G, X, off, out=(dW, db))
+    want = torch.zeros(E, N, K, device=DEV).index_add_(0, where, G.float()[:, :, None] * X.float()[:, None, :])
+    assert torch.equal(dW, want) and torch.equal(db, torch.zeros(E, N, device=DEV).index_add_(0, where, G.float()))
+
+
+def test_weight_gradient_of_a_large_stack():
+    """More than 2^18 tiles of 128 x 128: 52 experts of [16384, 5120], rows with three of them."""
+    gen = generator(22)
+    E, N, K = 52, 16384, 5120
+    counts = [0] * E
+    counts[0], counts[30], counts[51] = 3, 70, 1
+    off = offsets_of(counts)
+    X, G = bf16(gen, sum(counts), K), bf16(gen, sum(counts), N)
+    dW = torch.full((E, N, K), 7.0, dtype=torch.bfloat16, device=DEV)
+    db = torch.full((E, N), 7.0, dtype=torch.bfloat16, device=DEV)
+    rtl.grouped_linear_wgrad(G, X, off, out=(dW, db))
+    o, pick = off.tolist(), torch.randint(0, N, (64,), generator=gen, device=DEV)
+    pick[0], pick[1] = 0, N - 1
+    for e in range(E):
+        if counts[e] == 0:
+            assert (dW[e] == 0).all() and (db[e] == 0).all()
+            continue
+        r = slice(o[e], o[e + 1])
+        ref.check_product(dW[e][pick], ref.values(G[r][:, pick]).T, ref.values(X[r]).T)
+        ref.check_product(db[e:e + 1], np.ones((1, counts[e])), ref.values(G[r]).T)

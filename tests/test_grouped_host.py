@@ -90,3 +90,25 @@ def test_weight_gradient_refuses_a_bias_gradient_without_columns():
                                                 sdw=0, ws=None, wsb=0, stream=None))
     assert f() == SHAPE and f(T=0) == SHAPE and f(type=1) == SHAPE
     assert f(db=None) == 0 and f(E=0) == 0 and f(N=0) == 0
+
+
+@pytest.mark.parametrize("E,N,K", [(256, 4096, 7168), (384, 4096, 7168), (128, 16384, 5120), (32768, 128, 128), (65536, 1024, 1024), (2048, 8192, 8192)])
+@pytest.mark.parametrize("T", [0, 1, 8192, 65536])
+def test_weight_gradient_takes_large_stacks(T, E, N, K):
+    """What is refused is the launch that the call would make (2^32 threads and more), not one of more parts or smaller tiles: forward and input
+    gradient take these stacks too. (Every size check comes before the pointers are looked at.)"""
+    rows = max(T, 1)
+    f = caller("rtl_grouped_linear_wgrad", dict(dY=FAKE, X=FAKE, off=FAKE, dW=None, db=None, type=0, T=T, E=E, N=N, K=K, lddy=N, ldx=K, lddw=K, sdw=N * K,
+                                                ws=None, wsb=0, stream=None))
+    assert f() == NULL and f(type=1) == NULL and f(ws=FAKE, wsb=1 << 40) == NULL
+    fwd = caller("rtl_grouped_linear", dict(X=FAKE, off=FAKE, W=None, bias=None, Y=FAKE, T=rows, E=E, N=N, K=K, ldx=K, ldw=K, sw=N * K, ldy=N, stream=None))
+    grad = caller("rtl_grouped_linear_dgrad", dict(dY=FAKE, off=FAKE, W=None, dX=FAKE, T=rows, E=E, N=N, K=K, lddy=N, ldw=K, sw=N * K, lddx=K, stream=None))
+    assert fwd() == NULL and grad() == NULL
+
+
+@pytest.mark.parametrize("T", [0, 1, 65536])
+def test_weight_gradient_refuses_more_workgroups_than_a_launch_takes(T):
+    """Tiles of 256 x 256 have 512 threads, tiles of 128 x 128 have 256: fewer than 2^23 or 2^24 of them, an expert's rounded up to eights."""
+    f = caller("rtl_grouped_linear_wgrad", dict(dY=FAKE, X=FAKE, off=FAKE, dW=None, db=None, type=0, T=T, E=65536, N=4096, K=4096, lddy=4096, ldx=4096,
+                                                lddw=4096, sdw=4096 * 4096, ws=None, wsb=0, stream=None))
+    assert f() == SHAPE and f(N=2048) == SHAPE and f(N=1024, K=1024) == NULL
