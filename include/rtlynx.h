@@ -284,6 +284,8 @@ rtl_status rtl_sparse_lora_linear_fp8(const void* X, const void* Wq, const float
  *            (a training step's gradient, weight or activation) then is the left or right operand of
  *            rtl_mxfp4_packed_linear in either.
  *   Q, Qt 16-byte aligned, ldq, ldqt % 16 == 0; S, St 8-byte aligned.
+ *   ceil(rows / 32) ceil(cols / 256) < 2^24 and ceil(rows / 256) ceil(cols / 128) < 2^23, else RTL_ERR_SHAPE (one launch); so for the activation of the
+ *   linears that quantise it. Products: ceil(M / 256) ceil(N / 192) < 2^23.
  *
  * rtl_dequantize_mxfp4 - the values of codes and scales as bf16 (exact up to the range of bf16).
  *   Q, ldq, S as above, cols % 32 == 0; X [rows, cols] bf16 (ld), 16-byte aligned, ld % 8 == 0.

@@ -566,8 +566,8 @@ rtl_status rtl_quantize_mxfp4(const void* X, int64_t rows, int64_t cols, int64_t
     if (too_large(rows) || too_large(cols) || ld < cols || cols % (along ? 32 : 8) != 0) return RTL_ERR_SHAPE;
     if (along && ldq < cols / 2) return RTL_ERR_SHAPE;
     if (down && ldqt < (rows + 31) / 32 * 16) return RTL_ERR_SHAPE;
-    if (((rows + 31) / 32) * ((cols + 255) / 256) >= ((int64_t)1 << 24)) return RTL_ERR_SHAPE;      // workgroups of 256
     if (rows == 0 || cols == 0) return RTL_OK;
+    if (!rtl::quantize_mxfp4_fits(rows, cols)) return RTL_ERR_SHAPE;
     if (!X || (!along && !down) || (along && (!Q || !S)) || (down && (!Qt || !St))) return RTL_ERR_NULL;
     if (ld % 8 != 0 || !aligned(X, 16)) return RTL_ERR_ALIGN;
     if (along && (ldq % 16 != 0 || !aligned(Q, 16) || !aligned(S, 8))) return RTL_ERR_ALIGN;
@@ -590,14 +590,16 @@ rtl_status rtl_dequantize_mxfp4(const void* Q, int64_t ldq, const void* S, int64
     return e == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
-// Sizes and pointers of a product with a 4-bit weight; a_extent, a_granule: row extent and stride granule of the left operand.
+// Sizes and pointers of a product with a 4-bit weight; a_extent, a_granule: row extent and stride granule of the left operand, codes or (bf16) what the
+// quantiser takes first.
 static rtl_status check_mx(const void* A, const void* Wq, const void* Ws, const void* bias, const void* Y, int64_t M, int64_t N, int64_t K,
-                           int64_t lda, int64_t ldw, int64_t ldy, int64_t a_extent, int64_t a_granule) {
+                           int64_t lda, int64_t ldw, int64_t ldy, int64_t a_extent, int64_t a_granule, bool bf16) {
     if (too_large(M) || too_large(N) || K <= 0 || too_large(K) || K % 32 != 0 || lda < a_extent || ldw < K / 2 || ldy < N)
         return RTL_ERR_SHAPE;
     if (lda > ((int64_t)1 << 22) || ldw > ((int64_t)1 << 22)) return RTL_ERR_SHAPE;      // 32-bit offsets inside a tile
-    if (((M + 255) / 256) * ((N + 127) / 128) >= ((int64_t)1 << 31)) return RTL_ERR_SHAPE;
     if (M == 0 || N == 0) return RTL_OK;
+    // threads of a launch: fewer than 2^32 (the product's tiles are 256 x 192 at the least where there are many, with 512 threads)
+    if (((M + 255) / 256) * ((N + 191) / 192) >= ((int64_t)1 << 23) || (bf16 && !rtl::quantize_mxfp4_fits(M, K))) return RTL_ERR_SHAPE;
     if (!A || !Wq || !Ws || !Y) return RTL_ERR_NULL;
     if (lda % a_granule != 0 || ldw % 16 != 0 || !aligned(A, 16) || !aligned(Wq, 16) || !aligned(Ws, 8) || !aligned(Y, 2) ||
         (bias && !aligned(bias, 2)))
@@ -631,7 +633,7 @@ size_t rtl_mxfp4_packed_linear_workspace(int64_t M, int64_t N, int64_t K) {
 
 rtl_status rtl_mxfp4_packed_linear(const void* Xq, const void* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
                                    int64_t K, int64_t ldx, int64_t ldw, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
-    const rtl_status st = check_mx(Xq, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K / 2, 16);
+    const rtl_status st = check_mx(Xq, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K / 2, 16, false);
     if (st != RTL_OK || M == 0 || N == 0) return st;
     if (!Xs) return RTL_ERR_NULL;
     if (!aligned(Xs, 8)) return RTL_ERR_ALIGN;
@@ -650,7 +652,7 @@ size_t rtl_mxfp4_linear_workspace(int64_t M, int64_t N, int64_t K) {
 
 rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N, int64_t K, int64_t ldx,
                             int64_t ldw, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
-    const rtl_status st = check_mx(X, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K, 8);
+    const rtl_status st = check_mx(X, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, K, 8, true);
     if (st != RTL_OK || M == 0 || N == 0) return st;
     const size_t need = mx_ws(M, K);
     if (!workspace || workspace_bytes < need) return RTL_ERR_WORKSPACE;
@@ -684,7 +686,7 @@ static rtl_status check_grouped(const void* X, const int32_t* offsets, const voi
     if (bad_group_sizes(T, E, N, K) || K == 0 || K % (fp4 ? 32 : 64) != 0 || ldx < K || ldw < wide || ldy < N || stride_w < 0) return RTL_ERR_SHAPE;
     if (bad_strides({ldx, ldw})) return RTL_ERR_SHAPE;
     if (T == 0 || E == 0 || N == 0) return RTL_OK;
-    if (rtl::grouped_grid(T, E, N, K, fp4) >= rtl::kMaxGroupGrid) return RTL_ERR_SHAPE;
+    if (rtl::grouped_grid(T, E, N, K, fp4) >= rtl::kMaxGroupGrid || (fp4 && !rtl::quantize_mxfp4_fits(T, K))) return RTL_ERR_SHAPE;
     if (!X || !offsets || !W || !Y) return RTL_ERR_NULL;
     if (ldx % 8 != 0 || ldw % granule != 0 || stride_w % granule != 0 || !aligned(X, 16) || !aligned(offsets, 4) || !aligned(W, 16) || !aligned(Y, 2) ||
         (bias && !aligned(bias, 2)))

@@ -136,6 +136,13 @@ hipError_t prepare_mx_kernels() {
     return hipSuccess;
 }
 
+// (whatever directions are asked for, so that a matrix that goes along its rows also goes down its columns)
+bool quantize_mxfp4_fits(int64_t rows, int64_t cols) {
+    const int64_t along = ((rows + kQuantRows - 1) / kQuantRows) * ((cols + 255) / 256) * 256;
+    const int64_t down = ((rows + kTRows - 1) / kTRows) * ((cols + kTCols - 1) / kTCols) * 512;
+    return along < (int64_t)1 << 32 && down < (int64_t)1 << 32;
+}
+
 hipError_t launch_quantize_mxfp4(const uint16_t* X, int64_t rows, int64_t cols, int64_t ld, uint8_t* Q, int64_t ldq, uint8_t* S, uint8_t* Qt,
                                  int64_t ldqt, uint8_t* St, hipStream_t stream) {
     if (Qt) {

@@ -139,6 +139,7 @@ hipError_t launch_tensor_scale(const float* rowsums, int64_t M, float eps, float
 // ---- microscaled 4-bit codes (mx.hip) ---------------------------------------------------------
 // Codes and scale records as in the header. (Q, S) and (Qt, St) are each optional, not both absent.
 hipError_t prepare_mx_kernels();
+bool quantize_mxfp4_fits(int64_t rows, int64_t cols);       // threads of the launch: fewer than 2^32
 hipError_t launch_quantize_mxfp4(const uint16_t* X, int64_t rows, int64_t cols, int64_t ld, uint8_t* Q, int64_t ldq, uint8_t* S, uint8_t* Qt,
                                  int64_t ldqt, uint8_t* St, hipStream_t stream);
 hipError_t launch_dequantize_mxfp4(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64_t rows, int64_t cols, uint16_t* X, int64_t ld,

@@ -68,3 +68,22 @@ def test_binding_refuses_host_tensors_and_wrong_arguments():
         rtl.quantize_mxfp4(x, along="depth")
     with pytest.raises(ValueError):
         rtl.mxfp4_linear(x, x, x)
+
+
+def test_launches_that_do_not_fit_are_refused():
+    """A launch takes fewer than 2^32 threads: the quantiser's (either kernel of it, also inside the linears) and the product's, before anything is launched."""
+    d = dict(X=FAKE, rows=4, cols=64, ld=64, Q=FAKE, ldq=32, S=FAKE, Qt=None, ldqt=0, St=None, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_quantize_mxfp4, d, **kw)
+    big = 1 << 30
+    assert f(rows=1 << 29) == SHAPE and f(rows=(1 << 29) - 32, X=None) == NULL
+    assert f(rows=1, cols=big, ld=big, Q=None, S=None, Qt=FAKE, St=FAKE, ldqt=16) == SHAPE
+    assert f(rows=1, cols=big - 128, ld=big, Q=None, S=None, Qt=FAKE, St=FAKE, ldqt=16, X=None) == NULL
+    d = dict(X=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, M=4, N=8, K=32, ldx=32, ldw=16, ldy=8, ws=FAKE, wsb=1 << 50, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_mxfp4_linear, d, **kw)
+    assert f(M=1 << 29) == SHAPE and f(M=1 << 29, Y=None) == SHAPE and f(M=(1 << 29) - 32, Y=None) == NULL
+    d = dict(Xq=FAKE, Xs=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, M=257, N=1 << 29, K=32, ldx=16, ldw=16, ldy=1 << 30, ws=None, wsb=0, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_mxfp4_packed_linear, d, **kw)
+    assert f(N=1 << 30) == SHAPE and f(M=1024) == SHAPE and f(Y=None) == NULL and f(N=1 << 30, M=256, Y=None) == NULL and f(N=1 << 30, M=1, Y=None) == NULL
+    d = dict(X=FAKE, off=FAKE, Wq=FAKE, Ws=FAKE, bias=None, Y=FAKE, T=1 << 29, E=2, N=8, K=32, ldx=32, ldw=16, sw=128, ldy=8, ws=FAKE, wsb=1 << 50, stream=None)
+    f = lambda **kw: call(rtl.lib().rtl_grouped_mxfp4_linear, d, **kw)
+    assert f() == SHAPE and f(Wq=None) == SHAPE and f(T=(1 << 29) - 32, Wq=None) == NULL
