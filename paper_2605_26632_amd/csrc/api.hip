@@ -607,6 +607,11 @@ static rtl_status check_mx(const void* A, const void* Wq, const void* Ws, const 
     return RTL_OK;
 }
 
+// The few-row form has a workgroup of 256 threads to 16 columns; more of them than a launch takes go through the tile loop.
+static rtl::FewRows mx_few_rows(int64_t M, int64_t N, int64_t K) {
+    return rtl::few_rows_grid(1, N) < rtl::kMaxGroupGrid ? rtl::few_rows_choice(M, M, K, true) : rtl::FewRows::no;
+}
+
 static rtl_status mx_product(const void* Xq, const uint8_t* Xs, const void* Wq, const void* Ws, const void* bias, void* Y, int64_t M, int64_t N,
                              int64_t K, int64_t ldx, int64_t ldw, int64_t ldy, uint8_t* workspace, size_t used, size_t bytes, hipStream_t s) {
     rtl::GemmArgs g{};
@@ -621,8 +626,8 @@ static rtl_status mx_product(const void* Xq, const uint8_t* Xs, const void* Wq, 
     g.bias = static_cast<const uint16_t*>(bias);
     g.Y = static_cast<uint16_t*>(Y);
     g.M = M; g.N = N; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldy;
-    // (Xs NULL: X is bf16 still, and few_rows_choice has said `quantise`)
-    const bool few = rtl::few_rows_choice(M, M, K, true) != rtl::FewRows::no;
+    // (Xs NULL: X is bf16 still, and mx_few_rows has said `quantise`)
+    const bool few = mx_few_rows(M, N, K) != rtl::FewRows::no;
     return (few ? rtl::launch_few_rows(g, s) : rtl::launch_gemm(false, g, s)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
@@ -661,7 +666,7 @@ rtl_status rtl_mxfp4_linear(const void* X, const void* Wq, const void* Ws, const
     uint8_t* base = static_cast<uint8_t*>(workspace);
     uint8_t* scales = base + mx_codes_bytes(M, K);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (rtl::few_rows_choice(M, M, K, true) == rtl::FewRows::quantise)
+    if (mx_few_rows(M, N, K) == rtl::FewRows::quantise)
         return mx_product(X, nullptr, Wq, Ws, bias, Y, M, N, K, ldx, ldw, ldy, nullptr, 0, 0, s);
     if (rtl::launch_quantize_mxfp4(static_cast<const uint16_t*>(X), M, K, ldx, base, K / 2, scales, nullptr, 0, nullptr, s) != hipSuccess)
         return RTL_ERR_HIP;

@@ -214,3 +214,24 @@ def test_captured_on_another_stream_and_replayed():
         want = rtl.mxfp4_linear(X, wq, ws, ws=room2)
         torch.cuda.synchronize()
         assert torch.equal(Y, want)
+
+
+@pytest.mark.parametrize("M", [1, 3])
+def test_few_rows_of_more_columns_than_the_few_row_launch_takes(M):
+    """2^28 columns and more go through the tile loop; sampled columns, the last ones among them."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(M)
+    N, K = (1 << 28) + 5, 32
+    wq = torch.randint(0, 256, (N, K // 2), generator=gen, device=DEV, dtype=torch.uint8)
+    ws = torch.zeros(rtl.mxfp4_scales_shape(N, K), dtype=torch.uint8, device=DEV)
+    ws[0, :, 0] = torch.randint(120, 130, (N,), generator=gen, device=DEV, dtype=torch.uint8)
+    X = torch.randn(M, K, generator=gen, device=DEV).to(torch.bfloat16)
+    xq, xs = rtl.quantize_mxfp4(X)
+    y = rtl.mxfp4_linear(X, wq, ws)
+    packed = rtl.mxfp4_packed_linear(xq, xs, wq, ws)
+    cols = torch.cat([torch.arange(300, device=DEV), torch.randint(0, N, (2000,), generator=gen, device=DEV), torch.arange(N - 300, N, device=DEV)])
+    q = wq[cols].cpu().numpy()
+    code = np.stack([q & 15, q >> 4], axis=2).reshape(len(q), K)
+    w = ref.decode(code, ws[0, cols, :1].cpu().numpy())
+    for out in (y, packed):
+        ref.check_product(out[:, cols], ref.decode(*ref.quantize(ref.values(X))), w)
