@@ -600,10 +600,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         constexpr int i = decltype(i_tag)::value, n = decltype(n_tag)::value, j = n % TN, c = n / TN;
         if constexpr (FP4) {
             acc[i][j] = fp4_mma<2 * (i % 2) + c, 2 * ((TM + j) % 2) + c>(fa[a_set(i)].u[c], fb[j].u[c], acc[i][j], (int)sc[i / 2], (int)sc[(TM + j) / 2]);
-            return;
+        } else {
+            const bf16x16 x = fa[i].v, y = fb[j].v;
+            acc[i][j] = dense_mma<S>(c == 0 ? bf16x8(x.lo) : bf16x8(x.hi), c == 0 ? bf16x8(y.lo) : bf16x8(y.hi), acc[i][j]);
         }
-        const bf16x16 x = fa[i].v, y = fb[j].v;
-        if constexpr (!FP4) acc[i][j] = dense_mma<S>(c == 0 ? bf16x8(x.lo) : bf16x8(x.hi), c == 0 ? bf16x8(y.lo) : bf16x8(y.hi), acc[i][j]);
     };
     // Requests LO <= n < HI of stage kt_load behind the first HI - LO of every D-th of NM matrix instructions (spread evenly
     // where that does not reach). D = 1 / 2 / 3 / 4 / even, us: [4608, 9216, 3072] 226.0 / 217.3 / 216.4 / 217.3 / 218.3, [4096,
