@@ -69,7 +69,7 @@ __device__ __forceinline__ void few_rows(const GemmArgs& a, const int64_t n0, ui
         if constexpr (QUANT) {
             // eight values per thread, a block of 32 in four neighbouring lanes; zeros up to the end of the last unit
             const int pieces = units * 32;
-for (int q = tid; q < rows * pieces; q += WAVES * 64) {                   // (pieces: whole multiples of four per row)
+            for (int q = tid; q < rows * pieces; q += WAVES * 64) {                   // (pieces: whole multiples of four per row)
                 const int r = q / pieces, c = q % pieces;
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (c * 8 < a.K) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.A) + (m0 + r) * a.lda + c * 8);
