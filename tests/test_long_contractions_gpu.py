@@ -69,7 +69,7 @@ def check_rows(rng, y, x_of, w_of, bias, counts, front, width):
     at = front
     for e, n in enumerate(counts):
         if n:
-            r, c = at + sample(rng, n, 48), sample(rng, width, 160)
+            r, c = at + sample(rng, n, 48), sample(rng, width, 160 if len(counts) < 64 else 48)
             ref.check_product(y[r][:, c], x_of(r), w_of(e, c), None if bias is None else ref.values(bias[e][c]))
         at += n
 
@@ -223,3 +223,34 @@ def test_what_lds_held_does_not_reach_a_result(M, N, negative):
         if not x_code:
             rtl.mxfp4_packed_linear(a, s, w, s)
             assert (rtl.mxfp4_packed_linear(*args).view(torch.int16) == 0).all()
+
+
+@pytest.mark.parametrize("E,T,tiles_n,stages", [(130, 9000, 8, 4), (200, 20000, 6, 9), (70, 12000, 9, 5), (300, 4000, 9, 5)])
+def test_panels_of_more_experts_than_a_wave_has_lanes(E, T, tiles_n, stages):
+    """Tall panels on both sides of the 64th expert, experts without rows between them, several rounds of tiles."""
+    rng, N = np.random.default_rng(E), tiles_n * 256 - 40
+    w = rng.random(E) ** 3
+    w[::7] = 0
+    counts = rng.multinomial(T, w / w.sum()).tolist()
+    K, K4, D = stages * 64, stages * 256 - 96, stages * 64 - 24
+    assert plan.forward_form(T + 3, E, N, K) == 3 and plan.forward_form(T + 3, E, N, K4, True) == 3
+    assert E == 300 or 0 < sum(n // 256 for n in counts[:64]) < plan.heights(counts, tiles_n, stages)
+    gen, off = generator(E), offsets_of(counts, 1)
+    X, W, b = surrounded(bf16(gen, T, K), 1, 2), bf16(gen, E, N, K), bf16(gen, E, N)
+    check_rows(rng, rtl.grouped_linear(X, off, W, bias=b), lambda r: ref.values(X[r]), lambda e, c: ref.values(W[e][c]), b, counts, 1, N)
+    X4 = surrounded(bf16(gen, T, K4), 1, 2)
+    wq, ws = codes(gen, E * N, K4)
+    Y4 = rtl.grouped_mxfp4_linear(X4, off, wq.view(E, N, K4 // 2), ws, bias=b)
+    check_rows(rng, Y4, lambda r: ref.decode(*ref.quantize(ref.values(X4[r]))), lambda e, c: decoded(wq, ws, e * N + c), b, counts, 1, N)
+    G, V = surrounded(bf16(gen, T, D), 1, 2), bf16(gen, E, D, N)
+    check_rows(rng, rtl.grouped_linear_dgrad(G, off, V), lambda r: ref.values(G[r]), lambda e, c: ref.values(V[e][:, c]).T, None, counts, 1, N)
+    dW, db = rtl.grouped_linear_wgrad(G, X, off, with_bias=True)
+    at = 1
+    for e, n in enumerate(counts):
+        g, x = G[at:at + n], X[at:at + n]
+        if n and (e % 8 == 1 or e > E - 3):
+            ref.check_product(dW[e], ref.values(g).T, ref.values(x).T)
+            ref.check_product(db[e:e + 1], np.ones((1, n)), ref.values(g).T)
+        elif n == 0:
+            assert (dW[e] == 0).all() and (db[e] == 0).all()
+        at += n
