@@ -391,3 +391,73 @@ def test_weight_gradient_of_a_large_stack():
         r = slice(o[e], o[e + 1])
         ref.check_product(dW[e][pick], ref.values(G[r][:, pick]).T, ref.values(X[r]).T)
         ref.check_product(db[e:e + 1], np.ones((1, counts[e])), ref.values(G[r]).T)
+
+
+def test_products_of_a_large_stack():
+    """Weights of more than 2^31 elements: the last expert's rows of forward, input gradient and 4-bit product."""
+    gen = generator(23)
+    E, N, K = 52, 16384, 5120
+    counts = [0] * E
+    counts[0], counts[50], counts[51] = 2, 40, 9
+    off, T = offsets_of(counts), sum(counts)
+    W = torch.zeros(E, N, K, dtype=torch.bfloat16, device=DEV)
+    for e in (0, 50, 51):
+        W[e] = bf16(gen, N, K, std=0.05)
+    X, G, pick = bf16(gen, T, K), bf16(gen, T, N), torch.cat([torch.arange(40, device=DEV), torch.arange(N - 40, N, device=DEV)])
+    Y, dX = rtl.grouped_linear(X, off, W), rtl.grouped_linear_dgrad(G, off, W)
+    wq, ws = rtl.quantize_mxfp4(W.view(E * N, K))
+    Y4 = rtl.grouped_mxfp4_linear(X, off, wq.view(E, N, K // 2), ws)
+    x4, o = ref.decode(*ref.quantize(ref.values(X))), off.tolist()
+    for e in (0, 50, 51):
+        r = slice(o[e], o[e + 1])
+        ref.check_product(Y[r][:, pick], ref.values(X[r]), ref.values(W[e][pick]))
+        ref.check_product(dX[r][:, :80], ref.values(G[r]), ref.values(W[e][:, :80]).T)
+        ref.check_product(Y4[r][:, pick], x4[r], ref.decode(*ref.quantize(ref.values(W[e][pick]))))
+
+
+@pytest.mark.parametrize("counts", [[130, 0, 126], [3, 7, 1]])
+def test_row_strides_at_the_limit(counts):
+    """Row strides of 2^22 elements, the largest that is taken: matrices that are the first columns of much wider ones."""
+    gen, ld, T, E, N, K = generator(24), 1 << 22, sum(counts), len(counts), 256, 192
+    off = offsets_of(counts)
+
+    def wide(t):
+        full = torch.empty(t.shape[0], ld, dtype=t.dtype, device=DEV)
+        view = full[:, 8:8 + t.shape[1]]
+        view.copy_(t)
+        return view
+
+    X, G, W = wide(bf16(gen, T, K)), wide(bf16(gen, T, N)), wide(bf16(gen, E * N, K)).unflatten(0, (E, N))
+    Y, dX = wide(torch.zeros(T, N, dtype=torch.bfloat16, device=DEV)), wide(torch.zeros(T, K, dtype=torch.bfloat16, device=DEV))
+    dW = wide(torch.zeros(E * N, K, dtype=torch.bfloat16, device=DEV)).unflatten(0, (E, N))
+    rtl.grouped_linear(X, off, W, out=Y)
+    rtl.grouped_linear_dgrad(G, off, W, out=dX)
+    rtl.grouped_linear_wgrad(G, X, off, out=(dW, None))
+    o = off.tolist()
+    for e in range(E):
+        r = slice(o[e], o[e + 1])
+        if counts[e]:
+            ref.check_product(Y[r], ref.values(X[r]), ref.values(W[e]))
+            ref.check_product(dX[r], ref.values(G[r]), ref.values(W[e]).T)
+            ref.check_product(dW[e], ref.values(G[r]).T, ref.values(X[r]).T)
+        else:
+            assert (dW[e] == 0).all()
+
+
+@pytest.mark.parametrize("T", [300, 70000])
+def test_as_many_experts_as_are_taken(T):
+    """65536 experts; small integers, so that every sum is exact, in 4 bits too."""
+    gen, E, N, K = generator(25), 65536, 24, 64
+    where = torch.sort(torch.randint(0, E, (T,), generator=gen, device=DEV)).values
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), torch.bincount(where, minlength=E).cumsum(0)]).to(torch.int32)
+    ints = lambda *s: torch.randint(-3, 4, s, generator=gen, device=DEV).to(torch.bfloat16)
+    X, G, W, b = ints(T, K), ints(T, N), ints(E, N, K), ints(E, N)
+    Y = (W[where].float() @ X.float()[:, :, None])[:, :, 0]
+    bf = lambda t: t.to(torch.bfloat16)
+    assert torch.equal(rtl.grouped_linear(X, off, W, bias=b), bf(Y + b[where].float()))
+    wq, ws = rtl.quantize_mxfp4(W.view(E * N, K))
+    assert torch.equal(rtl.grouped_mxfp4_linear(X, off, wq.view(E, N, K // 2), ws, bias=b), bf(Y + b[where].float()))
+    assert torch.equal(rtl.grouped_linear_dgrad(G, off, W), bf((G.float()[:, None, :] @ W[where].float())[:, 0]))
+    dW, db = rtl.grouped_linear_wgrad(G, X, off, with_bias=True, dtype=torch.float32)
+    assert torch.equal(dW, torch.zeros(E, N, K, device=DEV).index_add_(0, where, G.float()[:, :, None] * X.float()[:, None, :]))
+    assert torch.equal(db, torch.zeros(E, N, device=DEV).index_add_(0, where, G.float()))

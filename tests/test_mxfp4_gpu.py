@@ -235,3 +235,22 @@ def test_few_rows_of_more_columns_than_the_few_row_launch_takes(M):
     w = ref.decode(code, ws[0, cols, :1].cpu().numpy())
     for out in (y, packed):
         ref.check_product(out[:, cols], ref.decode(*ref.quantize(ref.values(X))), w)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 300, 352), (256, 300, 352), (2552, 1558, 288)])
+def test_row_strides_at_the_limit(M, N, K):
+    """Codes whose rows are 2^22 bytes apart, the largest stride that is taken."""
+    rng, ld = np.random.default_rng(M), 1 << 22
+    xc, xb = ref.random_codes(rng, M, K)
+    wc, wb = ref.random_codes(rng, N, K)
+    xq, xs = ref.on_device(xc, xb)
+    wq, ws = ref.on_device(wc, wb)
+
+    def wide(t):
+        view = torch.empty(t.shape[0], ld, dtype=t.dtype, device=DEV)[:, 16:16 + t.shape[1]]
+        view.copy_(t)
+        return view
+
+    rows = np.unique(np.concatenate([np.arange(min(M, 8)), rng.integers(0, M, 40), [M - 1]]))
+    y = rtl.mxfp4_packed_linear(wide(xq), xs, wide(wq), ws)
+    ref.check_product(y[torch.from_numpy(rows).to(DEV)], ref.decode(xc[rows], xb[rows]), ref.decode(wc, wb))
