@@ -216,13 +216,15 @@ struct Few {
 // 16 columns and eight lines of W per row in flight in a workgroup; 4-bit stacks of experts that fill the chip several times over take more columns per
 // workgroup instead, fewer lines (kWide columns and more of experts that can have rows). us, [T, E, N, K] 4-bit, quantised inside: NB 1 U 2 | NB 4 U 1 | NB 4 U 2
 // | NB 2 U 4: [24, 32, 2816, 2048] 12.1 | 11.1 | 13.9 | 20.4, [64, ..] 24.3 | 19.5; from codes NB 1 U 2 | NB 2 U 2: [64, ..] 23.0 | 20.2, [200, ..] 23.6 | 21.1. One row,
-// [12288, 3072], launches back to back on one weight (each for itself, traced, 7.2): NB 1 U 2 6.2, NB 1 U 4 6.7, NB 2 U 2 7.1, NB 4 U 2 7.4; eight waves 6.3 to 8.5. bf16 [24, 32, 1408, 1024]: NB 1 U 4 9.2, U 2 10.8, NB 2 U 4 9.4, NB 4 U 4 12.4.
+// [12288, 3072], launches back to back on one weight (7.2 traced one by one): NB 1 U 2 6.2, NB 1 U 4 6.7, NB 2 U 2 7.1, NB 4 U 2 7.4; eight waves 6.3
+// to 8.5. bf16 [24, 32, 1408, 1024]: NB 1 U 4 9.2, U 2 10.8, NB 2 U 4 9.4, NB 4 U 4 12.4.
 using FewQuant = Few<true, true, 1, 4, 2>;
 using FewQuantWide = Few<true, true, 4, 4, 1>;
 using FewCodes = Few<true, false, 1, 4, 2>;
 using FewCodesWide = Few<true, false, 2, 4, 2>;
 using FewBf16 = Few<false, false, 1, 4, 4>;
-constexpr int64_t kWide = 65536;         // just under the smallest stack that was better off wide (24 x 2816 columns); 12288 were not; between them nothing is measured
+// (Just under the smallest stack that was better off wide, 24 x 2816 columns; 12288 columns were not; nothing between them is measured.)
+constexpr int64_t kWide = 65536;
 
 }  // namespace
 
@@ -237,7 +239,8 @@ FewRows few_rows_choice(int64_t M, int64_t most, int64_t K, bool fp4) {
 // us of a grouped launch that cannot be shorter than `stream` us: its workgroups, three to a unit at a time, each as long as its batches of lines and its
 // expert's 16-row blocks (an expert of one and a half times the average rows). More than two rounds of workgroups read at a lower rate than tiles do: bf16
 // [64, 64, 1024, 2048] 37.5 us against 29.5 with panels, where [24, 32, 1408, 1024], two rounds, takes 12.0 against 14.2 with 64 x 64 tiles (changing inputs).
-// (An expert of many times the average is not priced, the offsets are on the device: 4-bit [512, 64, 1408, 1024] 16 us even, 48 with a quarter of the rows on one.)
+// (An expert of many times the average is not priced, the offsets are on the device: 4-bit [512, 64, 1408, 1024] 16 us even, 48 with a quarter of the rows
+// on one expert, 139 with all.)
 double few_rows_us(int64_t T, int64_t E, int64_t N, int64_t K, bool fp4, double stream) {
     const double experts = group_experts(T, E), rows = (double)T / experts, cols = fp4 && (double)(E < T ? E : T) * (double)N >= (double)kWide ? 32 : 16;
     const double many = rows * 1.5 / 16, batches = (double)(fp4 ? (K + 2047) / 2048 : (K + 1023) / 1024);
