@@ -365,6 +365,98 @@ rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const
                                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Gated linear, the first half of a gated feed-forward layer, in one kernel:
+ *     G = X Wg^T (+ bg),  U = X Wu^T (+ bu),  H = act(G) U,
+ * and its backward pass.
+ *   act  RTL_ACT_SILU g / (1 + e^-g), RTL_ACT_GELU g Phi(g), RTL_ACT_GELU_TANH its tanh form. fp32, H rounded once.
+ *   X    [M, K] bf16 (ldx); W [2F, K] bf16 (ldw), the F rows of Wg first; bias NULL or bf16 [2F], those of Wg first.
+ *   H    [M, F] bf16 (ldh); P NULL or [M, 2F] bf16 (ldp): G in its first F columns, U behind them, for the backward pass.
+ *   K % 64 == 0, sizes, X and W as for rtl_dense_linear (F for N, F <= 2^29; a result of 2^23 and more tiles of 256 x 128 is RTL_ERR_SHAPE); H, P and
+ *   bias 2-byte aligned, any row stride.
+ *
+ * rtl_gated_linear_backward: from dH and the P of the forward call
+ *     dG = dH U act'(G), dU = dH act(G);  dX = dG Wg + dU Wu,  dW = [dG dU]^T X,  dbias = column sums of [dG dU],  H = act(G) U again
+ *   (what the gradient of the layer behind it needs). dX, dW, dbias and H may be NULL each; dbias needs dW. X is needed for dW, W for dX.
+ *   [dG dU] is rounded to bf16 for the products, whose sums are fp32. dW [2F, K] (lddw) and dbias [2F] of type dw_type.
+ *   F % 4 == 0, F <= 2^21, K % 8 == 0; X, W, dX, dW 16-byte aligned with strides % 8 == 0, at most 2^22; dH (lddh), P, H (ldh) 2-byte aligned. M == 0
+ *   writes dW and dbias as zeros; an empty contraction (K == 0, F == 0 with a dX that is not empty) is RTL_ERR_SHAPE.
+ *   workspace  rtl_gated_linear_backward_workspace(M, F, K) bytes, 256-byte aligned; what lies behind its first 256 + 4 M F bytes (rounded up to 256) is
+ *              optional, as for rtl_grouped_linear_wgrad.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { RTL_ACT_SILU = 0, RTL_ACT_GELU = 1, RTL_ACT_GELU_TANH = 2 } rtl_act;
+rtl_status rtl_gated_linear(const void* X, const void* W, const void* bias, void* H, void* P, rtl_act act, int64_t M, int64_t F, int64_t K,
+                            int64_t ldx, int64_t ldw, int64_t ldh, int64_t ldp, void* stream);
+size_t rtl_gated_linear_backward_workspace(int64_t M, int64_t F, int64_t K);
+rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* W, const void* P, void* dX, void* dW, void* dbias, void* H,
+                                     rtl_act act, rtl_dtype dw_type, int64_t M, int64_t F, int64_t K,
+                                     int64_t lddh, int64_t ldx, int64_t ldw, int64_t ldp, int64_t lddx, int64_t lddw, int64_t ldh,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The norm behind one half of a transformer block and the norm in front of the next, with the gate, the residual and the modulation between
+ * them, in one pass: for the rows of sequence s
+ *     x' = alpha x + gate_s (w_post norm_post(y)),     h = w_pre norm_pre(x') (1 + scale_s) + shift_s.
+ *   norms    RTL_NORM_NONE v, RTL_NORM_RMS v / sqrt(mean v^2 + eps), RTL_NORM_LAYER (v - mean v) / sqrt(mean (v - mean v)^2 + eps), along D.
+ *   x, x_out [T, D] of x_type, RTL_BF16 or RTL_F32 (ldx, ldxo); y, h [T, D] bf16 (ldy, ldh). y NULL: x' = alpha x. x_out or h may be NULL. x_out may be x,
+ *            and h may be y, in place (same rows, same stride). h is made of the x' that is not rounded yet.
+ *   gate     bf16 [S, D] (ld_gate); scale, shift bf16 [S, D] (ld_mod, one for both); w_post, w_pre bf16 [D]. Any may be NULL: a gate or weight of ones,
+ *            a scale or shift of zeros.
+ *   offsets  device int32 [S + 1], ascending, read by the kernels alone: rows o_s up to o_{s+1} are sequence s, which may be empty. Rows in front of
+ *            o_0 and from o_S on belong to nobody: they are not read, and left as they were in the results, or written as zeros with `clear`.
+ *            NULL: all rows are one sequence (S must be 1). Whatever they hold, nothing outside of the tensors is touched; results of
+ *            offsets that do not ascend are unspecified.
+ *   T < 2^24, S <= 65535, D % 8 == 0, D <= 8192 (RTL_ERR_SHAPE); all rows 16-byte aligned (strides % 8 == 0 bf16, % 4 == 0 fp32).
+ *
+ * rtl_residual_norm_backward: from the gradients dx_out (of x_type) and dh, either of which may be NULL (none), x' as the forward call gave it, and y:
+ *   dx [T, D] of x_type, dy [T, D] bf16 and the sums over rows, fp32: dgate, dscale, dshift [S, D], dw_post, dw_pre [D], all dense. Any result may be
+ *   NULL; the gradient of a vector that is NULL can be asked for. dy, dgate and dw_post need y, x' is needed with dh. An empty sequence has zeros. The
+ *   sums are formed in a fixed order. dx may be dx_out, dy may be dh or y, in place.
+ *   workspace  rtl_residual_norm_backward_workspace(T, S, D) bytes, 256-byte aligned; needed for the sums only.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { RTL_NORM_NONE = 0, RTL_NORM_RMS = 1, RTL_NORM_LAYER = 2 } rtl_norm;
+rtl_status rtl_residual_norm(const void* x, const void* y, const void* gate, const void* w_post, const void* w_pre, const void* scale,
+                             const void* shift, const int32_t* offsets, void* x_out, void* h, rtl_dtype x_type, rtl_norm post, rtl_norm pre,
+                             float alpha, float eps, int clear, int64_t T, int64_t S, int64_t D,
+                             int64_t ldx, int64_t ldy, int64_t ld_gate, int64_t ld_mod, int64_t ldxo, int64_t ldh, void* stream);
+size_t rtl_residual_norm_backward_workspace(int64_t T, int64_t S, int64_t D);
+rtl_status rtl_residual_norm_backward(const void* dx_out, const void* dh, const void* x_out, const void* y, const void* gate, const void* w_post,
+                                      const void* w_pre, const void* scale, const int32_t* offsets, void* dx, void* dy, float* dgate,
+                                      float* dscale, float* dshift, float* dw_post, float* dw_pre, rtl_dtype x_type, rtl_norm post,
+                                      rtl_norm pre, float alpha, float eps, int clear, int64_t T, int64_t S, int64_t D,
+                                      int64_t lddxo, int64_t lddh, int64_t ldxo, int64_t ldy, int64_t ld_gate, int64_t ld_mod,
+                                      int64_t lddx, int64_t lddy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Norm and rotary positions of several axes (time, height, width) for the heads of q and k, in one pass over both:
+ *     n = w v / sqrt(mean v^2 + eps) along a head of D values (norm == RTL_NORM_RMS; v itself with RTL_NORM_NONE), and pair j of n turned by the angle
+ *     pos[t, axis[j]] freq[j]:  (a, b) -> (a cos - b sin, a sin + b cos),  j < pairs.
+ *   Pairs are values (2j, 2j + 1) of a head (interleaved != 0) or (j, j + pairs); values behind 2 pairs pass (normed).
+ *   q, k     [T, Hq, D], [T, Hk, D] bf16; ldq, ldk elements between tokens, sq, sk between heads (so that heads in front of tokens, and the
+ *            parts of one product that makes q, k and v, are taken as they are). Results likewise; they may be the inputs, in place (same strides).
+ *            Hq or Hk of 0: without q or k.
+ *   pos      fp32 [T, axes] dense; freq fp32 [pairs]; axis int32 [pairs], 0 .. axes - 1 (others are cut to that). The product is exact and reduced in 64 bits:
+ *            |pos freq| up to 2^30. pos, freq, axis may be NULL with pairs == 0.
+ *   wq, wk   NULL (ones) or bf16 [D], with the norm only (else RTL_ERR_ARG).
+ *   T < 2^24, Hq + Hk <= 65535, 8 <= D <= 512, D % 8 == 0, pairs % 4 == 0 (interleaved) or % 8 == 0, 2 pairs <= D, 1 <= axes <= 16; 16-byte aligned, strides % 8 == 0,
+ *   and at least D.
+ *
+ * rtl_norm_rotary_backward: dq, dk from the gradients of the results; with the norm q and k are needed too, and dwq, dwk (fp32 [D], NULL: not wanted) can be had,
+ *   summed over tokens and heads in a fixed order. dq may be dq_out or q, in place.
+ *   workspace  rtl_norm_rotary_backward_workspace(D) bytes, 256-byte aligned; needed with dwq or dwk only.
+ * ------------------------------------------------------------------------------------------- */
+rtl_status rtl_norm_rotary(const void* q, const void* k, const float* pos, const float* freq, const int32_t* axis, const void* wq, const void* wk,
+                           void* q_out, void* k_out, rtl_norm norm, float eps, int interleaved, int64_t T, int64_t Hq, int64_t Hk, int64_t D,
+                           int64_t pairs, int64_t axes, int64_t ldq, int64_t sq, int64_t ldk, int64_t sk, int64_t ldqo, int64_t sqo,
+                           int64_t ldko, int64_t sko, void* stream);
+size_t rtl_norm_rotary_backward_workspace(int64_t D);
+rtl_status rtl_norm_rotary_backward(const void* dq_out, const void* dk_out, const void* q, const void* k, const float* pos, const float* freq,
+                                    const int32_t* axis, const void* wq, const void* wk, void* dq, void* dk, float* dwq, float* dwk,
+                                    rtl_norm norm, float eps, int interleaved, int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t pairs,
+                                    int64_t axes, int64_t lddqo, int64_t sdqo, int64_t lddko, int64_t sdko, int64_t ldq, int64_t sq,
+                                    int64_t ldk, int64_t sk, int64_t lddq, int64_t sdq, int64_t lddk, int64_t sdk,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * rtl_diag_matrix_rate - diagnostic, not a step of the method: measures the issue rate of the matrix
  * instruction the linears are built on with nothing else running (operands in registers), so that a
  * benchmark can quote the tile loops against a ceiling measured on the device at hand.

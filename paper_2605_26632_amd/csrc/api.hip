@@ -41,7 +41,8 @@ rtl_status device_ready(void** scratch_out = nullptr) {
             } else {
                 if (rtl::prepare_pack_kernels() != hipSuccess || rtl::prepare_gemm_kernels() != hipSuccess ||
                     rtl::prepare_pack_lora_kernels() != hipSuccess || rtl::prepare_mx_kernels() != hipSuccess ||
-                    rtl::prepare_grouped_kernels() != hipSuccess || rtl::prepare_few_rows_kernels() != hipSuccess || rtl::prepare_grouped_grad_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
+                    rtl::prepare_grouped_kernels() != hipSuccess || rtl::prepare_few_rows_kernels() != hipSuccess || rtl::prepare_grouped_grad_kernels() != hipSuccess || rtl::prepare_gated_kernels() != hipSuccess ||
+                    rtl::prepare_norm_kernels() != hipSuccess || rtl::prepare_rotary_kernels() != hipSuccess || rtl::prepare_diag_kernels() != hipSuccess)
                     return RTL_ERR_HIP;
                 void* ptr = nullptr;
                 if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return RTL_ERR_HIP;
@@ -819,6 +820,274 @@ rtl_status rtl_grouped_linear_wgrad(const void* dY, const void* X, const int32_t
     g.f32 = dw_type == RTL_F32;
     g.T = T; g.N = N; g.K = K; g.lddy = lddy; g.ldx = ldx; g.ldo = lddw; g.o_stride = stride_dw;
     return rtl::launch_grouped_wgrad(g, workspace, room, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// ---- gated linears --------------------------------------------------------------------------------
+static bool act_ok(rtl_act act) { return act >= RTL_ACT_SILU && act <= RTL_ACT_GELU_TANH; }
+
+rtl_status rtl_gated_linear(const void* X, const void* W, const void* bias, void* H, void* P, rtl_act act, int64_t M, int64_t F, int64_t K, int64_t ldx,
+                            int64_t ldw, int64_t ldh, int64_t ldp, void* stream) {
+    if (!act_ok(act)) return RTL_ERR_ARG;
+    if (F > ((int64_t)1 << 29) || (P && ldp < 2 * F)) return RTL_ERR_SHAPE;
+    const rtl_status st = check_linear(X, W, H, M, F, K, ldx, ldw, ldh, K);
+    if (st != RTL_OK && st != RTL_ERR_NULL && st != RTL_ERR_ALIGN) return st;
+    if (M == 0 || F == 0) return st;
+    if (((M + 255) / 256) * ((F + 127) / 128) >= (int64_t)1 << 23) return RTL_ERR_SHAPE;
+    if (st != RTL_OK) return st;
+    if ((P && !aligned(P, 2)) || (bias && !aligned(bias, 2))) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    rtl::GemmArgs g{};
+    g.A = X;
+    g.W = W;
+    g.bias = static_cast<const uint16_t*>(bias);
+    g.Y = static_cast<uint16_t*>(H);
+    g.P = static_cast<uint16_t*>(P);
+    g.ldp = ldp;
+    g.act = act;
+    g.M = M; g.N = F; g.K = K; g.lda = ldx; g.ldw = ldw; g.ldy = ldh;
+    return rtl::launch_gated(g, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// rtl_gated_linear_backward workspace: [offsets of the products | dG, dU | the weight gradient's partial planes]
+static size_t gated_backward_ws(int64_t M, int64_t F) { return 256 + round_up((size_t)M * (size_t)F * 4, 256); }
+size_t rtl_gated_linear_backward_workspace(int64_t M, int64_t F, int64_t K) {
+    if (M < 0 || F <= 0 || K <= 0) return 0;
+    return gated_backward_ws(M, F) + rtl_grouped_linear_wgrad_workspace(M, 1, 2 * F, K);
+}
+
+rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* W, const void* P, void* dX, void* dW, void* dbias, void* H, rtl_act act,
+                                     rtl_dtype dw_type, int64_t M, int64_t F, int64_t K, int64_t lddh, int64_t ldx, int64_t ldw, int64_t ldp, int64_t lddx,
+                                     int64_t lddw, int64_t ldh, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!act_ok(act) || (dw_type != RTL_BF16 && dw_type != RTL_F32)) return RTL_ERR_ARG;
+    const int64_t most = (int64_t)1 << 21;
+    if (M < 0 || F < 0 || K < 0 || too_large(M) || F > most || too_large(K) || F % 4 != 0 || K % 8 != 0) return RTL_ERR_SHAPE;
+    if (lddh < F || ldp < 2 * F || (H && ldh < F) || (dX && (ldw < K || lddx < K)) || (dW && (ldx < K || lddw < K))) return RTL_ERR_SHAPE;
+    if ((dX && bad_strides({ldw, lddx})) || (dW && bad_strides({ldx, lddw}))) return RTL_ERR_SHAPE;
+    if (K == 0 && (dX || dW)) return RTL_ERR_SHAPE;
+    if (F == 0) return dX && M > 0 ? RTL_ERR_SHAPE : RTL_OK;
+    const size_t need = gated_backward_ws(M, F);
+    size_t room = workspace_bytes > need ? workspace_bytes - need : 0;
+    if (room > (size_t)RTL_STATIC_SCRATCH_BYTES) room = (size_t)RTL_STATIC_SCRATCH_BYTES;
+    if (rtl::gated_grad_grid(M, F) >= rtl::kMaxGroupGrid || (dX && M > 0 && rtl::dgrad_grid(M, 1, 2 * F, K) >= rtl::kMaxGroupGrid) ||
+        (dW && rtl::wgrad_grid(M, 1, 2 * F, K, room) >= rtl::kMaxGroupGrid))
+        return RTL_ERR_SHAPE;
+    if (M == 0 && !dW && !dbias) return RTL_OK;
+    if ((M > 0 && (!dH || !P)) || (dbias && !dW) || (dX && M > 0 && !W) || (dW && M > 0 && !X)) return RTL_ERR_NULL;
+    if (!aligned(dH, 2) || !aligned(P, 2) || (H && !aligned(H, 2))) return RTL_ERR_ALIGN;
+    if (dX && (ldw % 8 != 0 || lddx % 8 != 0 || !aligned(W, 16) || !aligned(dX, 16))) return RTL_ERR_ALIGN;
+    if (dW && (ldx % 8 != 0 || lddw % 8 != 0 || !aligned(X, 16) || !aligned(dW, 16) || (dbias && !aligned(dbias, dw_type == RTL_F32 ? 4 : 2))))
+        return RTL_ERR_ALIGN;
+    if (!workspace || workspace_bytes < need) return RTL_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    uint8_t* const base = static_cast<uint8_t*>(workspace);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rtl::GatedGradArgs e{};
+    e.dH = static_cast<const uint16_t*>(dH);
+    e.P = static_cast<const uint16_t*>(P);
+    e.dP = reinterpret_cast<uint16_t*>(base + 256);
+    e.H = static_cast<uint16_t*>(H);
+    e.offsets = reinterpret_cast<int*>(base);
+    e.M = M; e.F = F; e.lddh = lddh; e.ldp = ldp; e.lddp = 2 * F; e.ldh = ldh;
+    e.act = act;
+    if (rtl::launch_gated_grad(e, s) != hipSuccess) return RTL_ERR_HIP;
+    rtl::GroupedGradArgs g{};
+    g.offsets = e.offsets;
+    g.experts = 1;
+    g.dY = e.dP;
+    g.T = M; g.N = 2 * F; g.K = K; g.lddy = 2 * F;
+    if (dX && M > 0) {
+        g.W = static_cast<const uint16_t*>(W);
+        g.out = dX;
+        g.ldw = ldw; g.ldo = lddx;
+        if (rtl::launch_grouped_dgrad(g, s) != hipSuccess) return RTL_ERR_HIP;
+    }
+    if (dW) {
+        g.X = static_cast<const uint16_t*>(X);
+        g.out = dW;
+        g.bias_out = dbias;
+        g.f32 = dw_type == RTL_F32;
+        g.ldx = ldx; g.ldo = lddw;
+        if (rtl::launch_grouped_wgrad(g, room ? base + need : nullptr, room, s) != hipSuccess) return RTL_ERR_HIP;
+    }
+    return RTL_OK;
+}
+
+// ---- norms of a block with gate, residual and modulation ----------------------------------------------
+static bool norm_ok(rtl_norm n) { return n >= RTL_NORM_NONE && n <= RTL_NORM_LAYER; }
+static const int64_t kMaxRows = (int64_t)1 << 24, kMaxSequences = 65535, kMaxNormWidth = 8192, kMaxStride = (int64_t)1 << 36;
+// A matrix of rows that are read or written 16 bytes at a time; NULL is none.
+static rtl_status check_rows(const void* p, int64_t ld, int64_t cols, bool f32 = false) {
+    if (!p) return RTL_OK;
+    if (ld < cols || ld > kMaxStride) return RTL_ERR_SHAPE;
+    return ld % (f32 ? 4 : 8) != 0 || !aligned(p, 16) ? RTL_ERR_ALIGN : RTL_OK;
+}
+// The first error of a list, sizes before alignment.
+static rtl_status first_error(std::initializer_list<rtl_status> list) {
+    for (rtl_status kind : {RTL_ERR_SHAPE, RTL_ERR_ALIGN})
+        for (rtl_status st : list)
+            if (st == kind) return st;
+    return RTL_OK;
+}
+static rtl_status check_norm(rtl_dtype x_type, rtl_norm post, rtl_norm pre, float alpha, float eps, int64_t T, int64_t S, int64_t D, const int32_t* offsets) {
+    if ((x_type != RTL_BF16 && x_type != RTL_F32) || !norm_ok(post) || !norm_ok(pre) || !std::isfinite(alpha) || !eps_ok(eps)) return RTL_ERR_ARG;
+    if (T < 0 || T >= kMaxRows || S < 0 || S > kMaxSequences || D < 0 || D % 8 != 0 || D > kMaxNormWidth || (!offsets && S != 1)) return RTL_ERR_SHAPE;
+    return RTL_OK;
+}
+
+rtl_status rtl_residual_norm(const void* x, const void* y, const void* gate, const void* w_post, const void* w_pre, const void* scale, const void* shift,
+                             const int32_t* offsets, void* x_out, void* h, rtl_dtype x_type, rtl_norm post, rtl_norm pre, float alpha, float eps, int clear,
+                             int64_t T, int64_t S, int64_t D, int64_t ldx, int64_t ldy, int64_t ld_gate, int64_t ld_mod, int64_t ldxo, int64_t ldh,
+                             void* stream) {
+    rtl_status st = check_norm(x_type, post, pre, alpha, eps, T, S, D, offsets);
+    if (st != RTL_OK) return st;
+    const bool f32 = x_type == RTL_F32;
+    st = first_error({check_rows(x, ldx, D, f32), check_rows(y, ldy, D), check_rows(gate, ld_gate, D), check_rows(scale, ld_mod, D),
+                      check_rows(shift, ld_mod, D), check_rows(x_out, ldxo, D, f32), check_rows(h, ldh, D), check_rows(w_post, D, D),
+                      check_rows(w_pre, D, D), offsets && !aligned(offsets, 4) ? RTL_ERR_ALIGN : RTL_OK});
+    if (st == RTL_ERR_SHAPE || T == 0 || D == 0) return st;
+    if (!x || (!x_out && !h)) return RTL_ERR_NULL;
+    if (st != RTL_OK) return st;
+    RTL_REQUIRE_DEVICE();
+    rtl::NormArgs a{};
+    auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    a.x = x;
+    a.y = bf(y); a.gate = bf(gate); a.w_post = bf(w_post); a.w_pre = bf(w_pre); a.scale = bf(scale); a.shift = bf(shift);
+    a.offsets = offsets;
+    a.x_out = x_out;
+    a.h = static_cast<uint16_t*>(h);
+    a.T = T; a.S = S; a.D = D; a.ldx = ldx; a.ldy = ldy; a.ld_gate = ld_gate; a.ld_mod = ld_mod; a.ldxo = ldxo; a.ldh = ldh;
+    a.post = post; a.pre = pre; a.alpha = alpha; a.eps = eps; a.x_f32 = f32; a.clear = clear != 0;
+    return rtl::launch_residual_norm(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// rtl_residual_norm_backward workspace: [sums of the teams' rows | sums of the sequences]
+static size_t norm_sums_bytes(int64_t T, int64_t S, int64_t D) { return round_up(rtl::residual_norm_backward_slots(T, S) * 3 * (size_t)D * sizeof(float), 256); }
+size_t rtl_residual_norm_backward_workspace(int64_t T, int64_t S, int64_t D) {
+    if (T < 0 || S <= 0 || D <= 0) return 0;
+    return norm_sums_bytes(T, S, D) + (size_t)S * 2 * (size_t)D * sizeof(float);
+}
+
+rtl_status rtl_residual_norm_backward(const void* dx_out, const void* dh, const void* x_out, const void* y, const void* gate, const void* w_post,
+                                      const void* w_pre, const void* scale, const int32_t* offsets, void* dx, void* dy, float* dgate, float* dscale,
+                                      float* dshift, float* dw_post, float* dw_pre, rtl_dtype x_type, rtl_norm post, rtl_norm pre, float alpha, float eps,
+                                      int clear, int64_t T, int64_t S, int64_t D, int64_t lddxo, int64_t lddh, int64_t ldxo, int64_t ldy, int64_t ld_gate,
+                                      int64_t ld_mod, int64_t lddx, int64_t lddy, void* workspace, size_t workspace_bytes, void* stream) {
+    rtl_status st = check_norm(x_type, post, pre, alpha, eps, T, S, D, offsets);
+    if (st != RTL_OK) return st;
+    const bool f32 = x_type == RTL_F32;
+    auto floats = [](const float* p) { return p && !aligned(p, 4) ? RTL_ERR_ALIGN : RTL_OK; };
+    st = first_error({check_rows(dx_out, lddxo, D, f32), check_rows(dh, lddh, D), check_rows(x_out, ldxo, D, f32), check_rows(y, ldy, D),
+                      check_rows(gate, ld_gate, D), check_rows(scale, ld_mod, D), check_rows(w_post, D, D), check_rows(w_pre, D, D),
+                      check_rows(dx, lddx, D, f32), check_rows(dy, lddy, D), floats(dgate), floats(dscale), floats(dshift), floats(dw_post),
+                      floats(dw_pre), offsets && !aligned(offsets, 4) ? RTL_ERR_ALIGN : RTL_OK});
+    if (st == RTL_ERR_SHAPE || D == 0) return st;
+    const bool sums = dgate || dscale || dshift || dw_post || dw_pre;
+    if (T == 0 && !sums) return st;
+    if (T > 0 && ((!dx_out && !dh) || (dh && !x_out) || ((dy || dgate || dw_post) && !y))) return RTL_ERR_NULL;
+    if (st != RTL_OK) return st;
+    if (sums && S > 0) {
+        if (!workspace || workspace_bytes < rtl_residual_norm_backward_workspace(T, S, D)) return RTL_ERR_WORKSPACE;
+        if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
+    }
+    RTL_REQUIRE_DEVICE();
+    rtl::NormGradArgs a{};
+    auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    a.dx_out = dx_out;
+    a.x = x_out;
+    a.dh = bf(dh); a.y = bf(y); a.gate = bf(gate); a.w_post = bf(w_post); a.w_pre = bf(w_pre); a.scale = bf(scale);
+    a.offsets = offsets;
+    a.dx = dx;
+    a.dy = static_cast<uint16_t*>(dy);
+    a.dgate = dgate; a.dscale = dscale; a.dshift = dshift; a.dw_post = dw_post; a.dw_pre = dw_pre;
+    a.T = T; a.S = S; a.D = D; a.lddxo = lddxo; a.lddh = lddh; a.ldx = ldxo; a.ldy = ldy; a.ld_gate = ld_gate; a.ld_mod = ld_mod; a.lddx = lddx; a.lddy = lddy;
+    a.post = post; a.pre = pre; a.alpha = alpha; a.eps = eps; a.x_f32 = f32; a.clear = clear != 0;
+    if (sums && S > 0) {
+        a.sums = static_cast<float*>(workspace);
+        a.totals = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + norm_sums_bytes(T, S, D));
+    }
+    return rtl::launch_residual_norm_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+// ---- head norm and rotary positions ---------------------------------------------------------------------
+// Heads of D values; no heads are no tensor.
+static rtl_status check_heads(const void* p, int64_t T, int64_t H, int64_t D, int64_t ld, int64_t stride) {
+    if (!p || T == 0 || H == 0) return RTL_OK;
+    if ((T > 1 && (ld < D || ld > kMaxStride)) || (H > 1 && (stride < D || stride > kMaxStride))) return RTL_ERR_SHAPE;
+    return (T > 1 && ld % 8 != 0) || (H > 1 && stride % 8 != 0) || !aligned(p, 16) ? RTL_ERR_ALIGN : RTL_OK;
+}
+static rtl_status check_rotary(const float* pos, const float* freq, const int32_t* axis, const void* wq, const void* wk, rtl_norm norm, float eps,
+                               int interleaved, int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t pairs, int64_t axes) {
+    if ((norm != RTL_NORM_NONE && norm != RTL_NORM_RMS) || !eps_ok(eps) || (norm == RTL_NORM_NONE && (wq || wk))) return RTL_ERR_ARG;
+    if (T < 0 || T >= kMaxRows || Hq < 0 || Hk < 0 || Hq + Hk > 65535 || D < 8 || D > 512 || D % 8 != 0 || pairs < 0 || 2 * pairs > D ||
+        pairs % (interleaved ? 4 : 8) != 0 || axes < 1 || axes > 16)
+        return RTL_ERR_SHAPE;
+    if (T == 0 || Hq + Hk == 0) return RTL_OK;
+    if (pairs > 0 && (!pos || !freq || !axis)) return RTL_ERR_NULL;
+    if (!aligned(pos, 4) || !aligned(freq, 4) || !aligned(axis, 4) || !aligned(wq, 16) || !aligned(wk, 16)) return RTL_ERR_ALIGN;
+    return RTL_OK;
+}
+
+rtl_status rtl_norm_rotary(const void* q, const void* k, const float* pos, const float* freq, const int32_t* axis, const void* wq, const void* wk, void* q_out,
+                           void* k_out, rtl_norm norm, float eps, int interleaved, int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t pairs, int64_t axes,
+                           int64_t ldq, int64_t sq, int64_t ldk, int64_t sk, int64_t ldqo, int64_t sqo, int64_t ldko, int64_t sko, void* stream) {
+    const rtl_status st = check_rotary(pos, freq, axis, wq, wk, norm, eps, interleaved, T, Hq, Hk, D, pairs, axes);
+    if (st == RTL_ERR_ARG || st == RTL_ERR_SHAPE) return st;
+    const rtl_status of = first_error({check_heads(q, T, Hq, D, ldq, sq), check_heads(k, T, Hk, D, ldk, sk), check_heads(q_out, T, Hq, D, ldqo, sqo),
+                                       check_heads(k_out, T, Hk, D, ldko, sko)});
+    if (of == RTL_ERR_SHAPE || T == 0 || Hq + Hk == 0) return of == RTL_ERR_SHAPE ? of : RTL_OK;
+    if (st == RTL_ERR_NULL || (Hq > 0 && (!q || !q_out)) || (Hk > 0 && (!k || !k_out))) return RTL_ERR_NULL;
+    if (st != RTL_OK || of != RTL_OK) return RTL_ERR_ALIGN;
+    RTL_REQUIRE_DEVICE();
+    rtl::RotaryArgs a{};
+    auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    a.q = bf(q); a.k = bf(k); a.wq = bf(wq); a.wk = bf(wk);
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.k_out = static_cast<uint16_t*>(k_out);
+    a.pos = pos; a.freq = freq; a.axis = axis;
+    a.T = T; a.Hq = (int)Hq; a.Hk = (int)Hk; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
+    a.ldq = ldq; a.sq = sq; a.ldk = ldk; a.sk = sk; a.ldqo = ldqo; a.sqo = sqo; a.ldko = ldko; a.sko = sko;
+    a.norm = norm == RTL_NORM_RMS; a.eps = eps; a.interleaved = interleaved != 0;
+    return rtl::launch_rotary(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+}
+
+size_t rtl_norm_rotary_backward_workspace(int64_t D) { return D > 0 ? rtl::rotary_backward_scratch(D) : 0; }
+
+rtl_status rtl_norm_rotary_backward(const void* dq_out, const void* dk_out, const void* q, const void* k, const float* pos, const float* freq,
+                                    const int32_t* axis, const void* wq, const void* wk, void* dq, void* dk, float* dwq, float* dwk, rtl_norm norm, float eps,
+                                    int interleaved, int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t pairs, int64_t axes, int64_t lddqo, int64_t sdqo,
+                                    int64_t lddko, int64_t sdko, int64_t ldq, int64_t sq, int64_t ldk, int64_t sk, int64_t lddq, int64_t sdq, int64_t lddk,
+                                    int64_t sdk, void* workspace, size_t workspace_bytes, void* stream) {
+    const rtl_status st = check_rotary(pos, freq, axis, wq, wk, norm, eps, interleaved, T, Hq, Hk, D, pairs, axes);
+    if (st == RTL_ERR_ARG || st == RTL_ERR_SHAPE) return st;
+    const bool rms = norm == RTL_NORM_RMS;
+    if (!rms && (dwq || dwk)) return RTL_ERR_ARG;
+    const rtl_status of = first_error({check_heads(dq_out, T, Hq, D, lddqo, sdqo), check_heads(dk_out, T, Hk, D, lddko, sdko),
+                                       check_heads(rms ? q : nullptr, T, Hq, D, ldq, sq), check_heads(rms ? k : nullptr, T, Hk, D, ldk, sk),
+                                       check_heads(dq, T, Hq, D, lddq, sdq), check_heads(dk, T, Hk, D, lddk, sdk)});
+    if (of == RTL_ERR_SHAPE) return of;
+    const bool sums = dwq || dwk, any = T > 0 && Hq + Hk > 0;
+    if (!any && !sums) return RTL_OK;
+    if (any && (st == RTL_ERR_NULL || (Hq > 0 && (!dq_out || !dq || (rms && !q))) || (Hk > 0 && (!dk_out || !dk || (rms && !k))))) return RTL_ERR_NULL;
+    if (st != RTL_OK || of != RTL_OK || !aligned(dwq, 4) || !aligned(dwk, 4)) return RTL_ERR_ALIGN;
+    if (sums) {
+        if (!workspace || workspace_bytes < rtl_norm_rotary_backward_workspace(D)) return RTL_ERR_WORKSPACE;
+        if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
+    }
+    RTL_REQUIRE_DEVICE();
+    rtl::RotaryArgs a{};
+    auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    a.q = bf(q); a.k = bf(k); a.wq = bf(wq); a.wk = bf(wk); a.dq_out = bf(dq_out); a.dk_out = bf(dk_out);
+    a.dq = static_cast<uint16_t*>(dq);
+    a.dk = static_cast<uint16_t*>(dk);
+    a.pos = pos; a.freq = freq; a.axis = axis;
+    a.dwq = dwq; a.dwk = dwk;
+    a.sums = sums ? static_cast<float*>(workspace) : nullptr;
+    a.T = any ? T : 0; a.Hq = (int)Hq; a.Hk = (int)Hk; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
+    a.ldq = ldq; a.sq = sq; a.ldk = ldk; a.sk = sk; a.lddqo = lddqo; a.sdqo = sdqo; a.lddko = lddko; a.sdko = sdko;
+    a.lddq = lddq; a.sdq = sdq; a.lddk = lddk; a.sdk = sdk;
+    a.norm = rms; a.eps = eps; a.interleaved = interleaved != 0;
+    return rtl::launch_rotary_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
 }  // extern "C"

@@ -62,6 +62,7 @@
 #pragma once
 #include <type_traits>
 #include <utility>
+#include "gate.h"
 #include "rtl_internal.h"
 
 namespace rtl {
@@ -223,8 +224,30 @@ __device__ __forceinline__ float mul_add_rn(float a, float b, float add) {
     return p + add;
 }
 
+// Eight fp32 values, rounded, into a row at any address; the first `valid` of them.
+__device__ __forceinline__ void store_run(uint16_t* dst, const float (&y)[8], int valid) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    uint32_t out[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const f32x2 v = {y[e], y[e + 1]};
+        out[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));       // RNE
+    }
+    if (valid == 8) {
+        __builtin_memcpy(dst, out, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < valid) dst[e] = (uint16_t)(out[e >> 1] >> (16 * (e & 1)));
+    }
+}
+
 // MODE 0: plain linear. MODE 1 (sparse only): LoRA tail, the accumulators also receive T L_A^T before
 // the epilogue.
+// MODE 2 (dense bf16 only): gated linear. a.N counts columns of Y; W has 2 a.N rows, the gates' first. A tile holds BN / 2 columns: its
+// rows of W are blocks of 16 gate rows and the 16 up rows of the same columns in turn, so that both factors of an output meet in one lane, a row block's
+// neighbouring accumulators, and Y = act(G) U leaves without another pass. With a.P set the two factors are stored too.
 // `tile`: index of this workgroup's output tile in the walk of the (M / BM) x (N / BN) tile grid.
 // PART: the workgroup covers the k blocks [kblk0, kblk0 + kblks) only and leaves its fp32 sums in plane `part` of
 // a.partials; the factors (MODE 0), the bias and the rounding are split_reduce_kernel's.
@@ -235,17 +258,20 @@ __device__ __forceinline__ float mul_add_rn(float a, float b, float add) {
 // waves takes the k blocks g, g + WAVES_K, ... with operands and accumulators of its own, and the groups'
 // tiles are added up in LDS, in the order of g, when the loop is done.
 template <bool SPARSE, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int MODE = 0, bool FP8 = false,
-          int WAVES_K = 1, bool PART = false, bool FOLDED = false, bool PIN = true, bool FP4 = false, bool ANY_ROW = FP4>
+          int WAVES_K = 1, bool PART = false, bool FOLDED = false, bool PIN = true, bool FP4 = false, bool ANY_ROW = FP4 || MODE == 2>
 __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, const int part = 0, const int kblk0 = 0,
                                           const int kblks = 0) {
     static_assert(!PART || WAVES_K == 1, "partial sums leave from the accumulators");
-    static_assert(MODE == 0 || (MODE == 1 && SPARSE), "mode/operand combination");
+    constexpr bool GATED = MODE == 2;
+    static_assert(MODE == 0 || (MODE == 1 && SPARSE) || (GATED && !SPARSE && !FP4 && !PART), "mode/operand combination");
     static_assert(!FP8 || SPARSE, "FP8 operands: sparse kernels only");
     static_assert(!FP4 || !SPARSE, "4-bit operands: dense kernels only");
     constexpr int NW = WAVES_M * WAVES_N;             // waves that share a block of operands
     constexpr int WTM = BM / WAVES_M, WTN = BN / WAVES_N;
     constexpr int S = kMmaSize<SPARSE>, TM = WTM / S, TN = WTN / S;
     static_assert(WTM % S == 0 && WTN % S == 0 && (S == 32 || TM > 1), "wave tile must be made of S x S blocks");
+    static_assert(!GATED || (S == 16 && TN % 2 == 0), "both factors of an output in one wave");
+    constexpr int BNY = GATED ? BN / 2 : BN;          // columns of Y in a tile
     using L = Smem<SPARSE, BM, BN, STAGES, WAVES_M, WAVES_N, FP8, WAVES_K, FP4>;
     using Acc = typename AccOf<S>::type;
     constexpr int RB = S == 32 ? 16 : 4;              // accumulator registers of a block
@@ -281,10 +307,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         else return (const uint8_t*)(smem + stage * L::kStage);
     };
     const int wm = wave / WAVES_N, wn = wave % WAVES_N;
-    const int tiles_m = (int)((a.M + BM - 1) / BM), tiles_n = (int)((a.N + BN - 1) / BN);
+    const int tiles_m = (int)((a.M + BM - 1) / BM), tiles_n = (int)((a.N + BNY - 1) / BNY);
     int pm, pn;
     tile_walk<(BM >= 256 ? 8 : 16)>(tile, tiles_m, tiles_n, pm, pn);
-    const int64_t m0 = (int64_t)pm * BM, n0 = (int64_t)pn * BN;
+    const int64_t m0 = (int64_t)pm * BM, n0 = (int64_t)pn * BNY;
     const int all_blocks = FP4 ? (int)((a.K + 255) / 256) : (int)(a.K / KSTAGE);
     const int blocks = PART ? kblks : all_blocks;
     const int KT = WAVES_K > 1 ? (blocks - wk + WAVES_K - 1) / WAVES_K : blocks;   // stages in which this wave's group has a block
@@ -304,7 +330,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         base_a += kblk0 * a_stride;
         base_b += (int64_t)kblk0 * (KSTAGE * ESZ);
     }
-    const int64_t rows_a = a.M - m0, rows_b = a.N - n0;     // valid rows from the tile's first row
+    const int64_t rows_a = a.M - m0, rows_b = a.N - n0;     // valid rows from the tile's first row (of W: of either factor)
+    const uint8_t* base_u = base_b + (GATED ? a.N * a.ldw * ESZ : 0);       // the up rows of the tile's columns
     // FP4: K is any multiple of 32. When its last block of 256 is not full, the walk takes that block first, where the chunks
     // behind K can be left out of the prologue's loads at no cost to the loop: block b > 0 is block b - 1 of memory.
     const int tail_chunks = FP4 ? (int)(a.K % 256) / 32 : 0;
@@ -352,6 +379,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         const int p = wave * B_CH + min(s * 64 + lane, B_CH - 1);   // masked lanes of a half load: any valid chunk
         int row, c;
         unswz8(p, row, c);
+        if constexpr (GATED) row = (row >> 5) * 16 + (row & 15);
         const int64_t gr = min((int64_t)row, rows_b - 1);
         ob[s] = (uint32_t)(gr * a.ldw * ESZ + chunk_at(c) * 16);
     }
@@ -396,6 +424,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
     if constexpr (PIN) {
         base_a = reinterpret_cast<const uint8_t*>(uniform64(base_a));
         base_b = reinterpret_cast<const uint8_t*>(uniform64(base_b));
+        if constexpr (GATED) base_u = reinterpret_cast<const uint8_t*>(uniform64(base_u));
         if constexpr (SPARSE) base_m = reinterpret_cast<const uint8_t*>(uniform64(base_m));
     }
     // Load number n (0 .. LOADS_PER_STAGE-1) of this wave for stage kt into ring buffer `stage`.
@@ -417,6 +446,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
             const uint32_t dst = base + L::kABytes + L::kMetaBytes + (wave * B_CH + s * 64) * 16;
             if constexpr (B_HALF && s == B_PER_W - 1) {
                 if (lane < 32) lds_dma16_so(base_b + (int64_t)(kt * WAVES_K + wk) * (KSTAGE * ESZ), ob[s], dst);
+            } else if constexpr (GATED) {
+                // eight rows of W to a request, sixteen to a block
+                static_assert(!B_HALF, "a request lies in one block");
+                const bool up = B_PER_W % 4 == 0 ? (s >> 1) & 1 : ((wave * B_PER_W + s) >> 1) & 1;
+                lds_dma16_so((up ? base_u : base_b) + (int64_t)(kt * WAVES_K + wk) * (KSTAGE * ESZ), ob[s], dst);
             } else {
                 lds_dma16_so(base_b + (int64_t)(kt * WAVES_K + wk) * (KSTAGE * ESZ), ob[s], dst);
             }
@@ -783,6 +817,41 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         };
         put_plane(acc);
         __syncthreads();
+        if constexpr (GATED) {
+            // a thread finishes runs of eight columns of Y: eight columns of the planes and the eight sixteen further on
+            constexpr int RUNS = BNY / 8;
+            static_assert(THREADS % RUNS == 0, "a thread keeps its columns");
+            const int run = (int)threadIdx.x % RUNS;
+            const int64_t col = n0 + run * 8;
+            const int valid = (int)min((int64_t)8, a.N - col);
+            if (valid <= 0) return;
+            float bg[8], bu[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t at = col + min(e, valid - 1);
+                bg[e] = a.bias ? __uint_as_float((uint32_t)a.bias[at] << 16) : 0.f;
+                bu[e] = a.bias ? __uint_as_float((uint32_t)a.bias[a.N + at] << 16) : 0.f;
+            }
+            const GateForm form = gate_form(a.act);
+            for (int row = (int)threadIdx.x / RUNS; row < BM && m0 + row < a.M; row += THREADS / RUNS) {
+                float g[8], u[8], y[8];
+                add_planes(g, row, (run >> 1) * 4 + (run & 1));
+                add_planes(u, row, (run >> 1) * 4 + (run & 1) + 2);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g[e] += bg[e];
+                    u[e] += bu[e];
+                    y[e] = (a.act == RTL_ACT_GELU ? gate_value<true>(g[e], form) : gate_value<false>(g[e], form)) * u[e];
+                }
+                store_run(a.Y + (m0 + row) * a.ldy + col, y, valid);
+                if (a.P) {
+                    uint16_t* const p = a.P + (m0 + row) * a.ldp + col;
+                    store_run(p, g, valid);
+                    store_run(p + a.N, u, valid);
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int q = u * THREADS + (int)threadIdx.x;
@@ -1011,6 +1080,71 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs a, const int tile, cons
         };
         auto first_of_pair = [](int q) { return S == 32 ? 2 * q : q; };     // registers r, r + PS, q = 0 .. RB / 2 - 1
         const bool scaled = MODE != 1 && (has_row_scale || has_tensor_scale);
+        if constexpr (GATED) {
+            // same wave reads back what it wrote: LDS operations of a wave complete in order
+            auto leave = [&](uint16_t* to, int64_t ld, int first, auto cols_tag) {      // columns first .. first + cols of the staged rows
+                constexpr int RUNS = decltype(cols_tag)::value / 8;
+#pragma unroll
+                for (int q0 = 0; q0 < WTM * RUNS; q0 += 64) {
+                    const int q = q0 + lane, rl = q / RUNS, c = q % RUNS;
+                    const int64_t row = m0 + wm * WTM + rl, col = n0 + wn * (WTN / 2) + c * 8;
+                    if (q < WTM * RUNS && row < a.M && col < a.N) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(ep + rl * ROWB + first * 2 + c * 16);
+                        uint16_t* dst = to + row * ld + col;
+                        if (col + 8 <= a.N) {
+                            __builtin_memcpy(dst, &v, 16);
+                        } else {
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                            for (int e = 0; e < 8 && col + e < a.N; ++e) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                        }
+                    }
+                }
+            };
+            if (a.bias) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int64_t col = min(n0 + wn * (WTN / 2) + j / 2 * S + li, a.N - 1);
+                    const float b = __uint_as_float((uint32_t)a.bias[j % 2 ? a.N + col : col] << 16);
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) acc[i][j][r] += b;
+                }
+            }
+            using half_cols = std::integral_constant<int, WTN / 2>;
+            if (a.P) {
+                // the factors, gates in the left half of the staged rows
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int q = 0; q < RB / 2; ++q) {
+                            const int r = first_of_pair(q);
+                            put2(acc[i][j][r], acc[i][j][r + PS], i * S + reg_row(r), j % 2 * (WTN / 2) + j / 2 * S);
+                        }
+                leave(a.P, a.ldp, 0, half_cols{});
+                leave(a.P + a.N, a.ldp, WTN / 2, half_cols{});
+            }
+            const GateForm form = gate_form(a.act);
+            auto products = [&](auto erf_tag) {
+                constexpr bool ERF = decltype(erf_tag)::value;
+#pragma unroll
+                for (int j = 0; j < TN; j += 2)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int q = 0; q < RB / 2; ++q) {
+                            const int r = first_of_pair(q);
+                            put2(gate_value<ERF>(acc[i][j][r], form) * acc[i][j + 1][r], gate_value<ERF>(acc[i][j][r + PS], form) * acc[i][j + 1][r + PS],
+                                 i * S + reg_row(r), j / 2 * S);
+                        }
+            };
+            if (a.act == RTL_ACT_GELU) products(std::true_type{});
+            else products(std::false_type{});
+            leave(a.Y, a.ldy, 0, half_cols{});
+            return;
+        }
         if (!scaled && !a.bias) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)

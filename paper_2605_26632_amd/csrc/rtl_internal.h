@@ -93,6 +93,10 @@ struct GemmArgs {
     const uint8_t* a_scale; // rows: a_scale_rows
     const uint8_t* w_scale;
     int64_t a_scale_rows, w_scale_rows;
+    // gated linears: N counts columns of Y, W has 2 N rows (gates first), bias 2 N values
+    uint16_t* P;            // nullable [M,2N] (ldp): both factors, gates first
+    int64_t ldp;
+    int act;                // rtl_act
 };
 // Bytes of partial planes launch_gemm would use of `room` bytes.
 size_t gemm_partial_bytes(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t room, bool fp4 = false);
@@ -198,6 +202,70 @@ size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 // Workgroups of the launch with that room, those of 512 threads counted twice (a launch takes fewer than 2^32 threads).
 int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_t room, hipStream_t stream);
+
+// ---- gated linears (gated.hip) -------------------------------------------------------------------
+// a: A, lda, W (2 N rows), bias, Y, ldy, M, N, K, P, ldp, act.
+hipError_t prepare_gated_kernels();
+hipError_t launch_gated(const GemmArgs& a, hipStream_t stream);
+struct GatedGradArgs {
+    const uint16_t *dH, *P;
+    uint16_t *dP, *H;       // H nullable
+    int* offsets;           // nullable: receives {0, M}
+    int64_t M, F, lddh, ldp, lddp, ldh;
+    int act;
+};
+int64_t gated_grad_grid(int64_t M, int64_t F);
+hipError_t launch_gated_grad(const GatedGradArgs& a, hipStream_t stream);
+
+// ---- norms of a block with gate, residual and modulation (block_norm.hip) -----------------------------
+struct NormArgs {
+    const void* x;          // bf16, or fp32 with x_f32 (x_out too)
+    const uint16_t *y, *gate, *w_post, *w_pre, *scale, *shift;       // nullable
+    const int* offsets;     // nullable: all rows are sequence 0
+    void* x_out;            // written when y is set
+    uint16_t* h;            // nullable
+    int64_t T, S, D, ldx, ldy, ld_gate, ld_mod, ldxo, ldh;
+    int post, pre;          // rtl_norm
+    float alpha, eps;
+    bool x_f32, clear;
+};
+struct NormGradArgs {
+    const void *dx_out, *x;                                          // x: x' of the forward pass; dx_out nullable
+    const uint16_t *dh, *y, *gate, *w_post, *w_pre, *scale;          // nullable
+    const int* offsets;
+    void* dx;               // nullable
+    uint16_t* dy;           // nullable
+    float *dgate, *dscale, *dshift, *dw_post, *dw_pre;               // nullable
+    int64_t T, S, D, lddxo, lddh, ldx, ldy, ld_gate, ld_mod, lddx, lddy;
+    int post, pre;
+    float alpha, eps;
+    bool x_f32, clear;
+    float *sums, *totals;   // residual_norm_backward_slots(T, S) x 3 D, S x 2 D
+    int rows;               // filled in by the launch
+};
+hipError_t prepare_norm_kernels();
+hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream);
+size_t residual_norm_backward_slots(int64_t T, int64_t S);
+hipError_t launch_residual_norm_backward(const NormGradArgs& a, hipStream_t stream);
+
+// ---- head norm and rotary positions (rotary.hip) --------------------------------------------------------
+// Strides in elements: ld* between tokens, s* between heads.
+struct RotaryArgs {
+    const uint16_t *q, *k, *wq, *wk, *dq_out, *dk_out;
+    uint16_t *q_out, *k_out, *dq, *dk;
+    const float *pos, *freq;
+    const int* axis;
+    float *dwq, *dwk, *sums;
+    int64_t T, ldq, sq, ldk, sk, ldqo, sqo, ldko, sko, lddqo, sdqo, lddko, sdko, lddq, sdq, lddk, sdk;
+    int Hq, Hk, D, pairs, axes;
+    float eps;
+    bool norm, interleaved;
+    int heads_per, splits;  // filled in by the launches
+};
+hipError_t prepare_rotary_kernels();
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
+size_t rotary_backward_scratch(int64_t D);
+hipError_t launch_rotary_backward(const RotaryArgs& a, hipStream_t stream);
 
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------
 // Issue-rate probe: `blocks` workgroups of four waves, each wave issuing 4 * iters matrix

@@ -1,0 +1,225 @@
+"""Gated linears and their backward pass on the GPU against the formulas in 64 bits."""
+import pytest
+import torch
+
+import block_ref as ref
+from paper_2605_26632_amd import binding as rtl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ACTS = ["silu", "gelu", "gelu_tanh"]
+
+
+def generator(seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    return gen
+
+
+def bf16(gen, *shape, std=1.0):
+    return (torch.randn(*shape, generator=gen, device=DEV) * std).to(torch.bfloat16)
+
+
+def strided(t, pad=8, fill=float("nan")):
+    """The same matrix with rows further apart, NaN between them."""
+    wide = torch.full((t.shape[0], t.shape[1] + 2 * pad), fill, dtype=t.dtype, device=DEV)
+    wide[:, pad:-pad] = t
+    return wide[:, pad:-pad]
+
+
+def room(rows, cols, pitch, first=0, fill=3.0):
+    """A place for a result inside a larger tensor, and what lies around it."""
+    full = torch.full((rows + 2, pitch), fill, dtype=torch.bfloat16, device=DEV)
+    return full[1:-1, first:first + cols], full
+
+
+def untouched(full, cols, first=0, fill=3.0):
+    around = full.clone()
+    around[1:-1, first:first + cols] = fill
+    assert bool((around == fill).all())
+
+
+# M, F, K: one row to several tiles, odd widths, one to many stages of the contraction
+SIZES = [(1, 1, 64), (1, 704, 512), (2, 17, 128), (16, 200, 192), (17, 65, 64), (31, 130, 320), (37, 1000, 128), (64, 64, 64), (100, 333, 1088), (129, 129, 192),
+         (200, 2739, 576), (257, 264, 448), (300, 1100, 64), (513, 520, 256), (700, 1536, 640), (1030, 1029, 128), (2100, 1800, 192)]
+
+
+@pytest.mark.parametrize("M,F,K", SIZES)
+@pytest.mark.parametrize("kind,bias,pre", [("silu", False, True), ("gelu", True, False), ("gelu_tanh", True, True)])
+def test_forward(M, F, K, kind, bias, pre):
+    gen = generator(M + F + K)
+    X, W = strided(bf16(gen, M, K)), strided(bf16(gen, 2 * F, K, std=K ** -0.5))
+    b = bf16(gen, 2 * F) if bias else None
+    h, eh, p, ep = ref.gated(X, W, b, kind)
+    for odd in (0, 1):                                             # rows of 16-byte alignment, and of none
+        H, around = room(M, F, (F + 23) // 8 * 8 + odd, first=8 * (1 - odd))
+        P, around_p = room(M, 2 * F, (2 * F + 23) // 8 * 8 + odd, first=8 * (1 - odd))
+        got = rtl.gated_linear(X, W, b, act=kind, out=H, pre=P if pre else None)
+        assert (got[0] if pre else got) is H
+        ref.close(H, h, eh, "H")
+        untouched(around, F, first=8 * (1 - odd))
+        if pre:
+            ref.close(P, p, ep, "P")
+            untouched(around_p, 2 * F, first=8 * (1 - odd))
+        else:
+            assert bool((around_p == 3.0).all())
+
+
+def test_new_tensors():
+    gen = generator(3)
+    X, W = bf16(gen, 40, 128), bf16(gen, 96, 128, std=0.1)
+    h, eh, p, ep = ref.gated(X, W, None, "silu")
+    ref.close(rtl.gated_linear(X, W), h, eh)
+    H, P = rtl.gated_linear(X, W, with_pre=True)
+    ref.close(H, h, eh)
+    ref.close(P, p, ep)
+
+
+@pytest.mark.parametrize("M", [1, 5, 130, 600])
+def test_rows_do_not_meet(M):
+    """A row of NaN or of infinities stays the only one that has any."""
+    gen = generator(M)
+    X, W = bf16(gen, M, 256), bf16(gen, 400, 256, std=0.1)
+    h, eh, _, _ = ref.gated(X, W, None, "silu")
+    bad = M // 2
+    X[bad] = float("nan")
+    H = rtl.gated_linear(X, W)
+    assert bool(torch.isnan(H[bad]).all())
+    keep = torch.arange(M, device=DEV) != bad
+    if M > 1:
+        ref.close(H[keep], h[keep], eh[keep])
+
+
+def test_large_gates():
+    """Far from zero the activations are g or nothing: no overflow on the way."""
+    for kind in ACTS:
+        X = torch.eye(64, dtype=torch.bfloat16, device=DEV)
+        W = torch.zeros(2 * 64, 64, dtype=torch.bfloat16, device=DEV)
+        g = torch.cat([torch.linspace(-3e4, 3e4, 32), torch.tensor([-100.0, -20.0, -10.0, -5.0, -1.0, -0.0, 0.0, 1.0, 5.0, 10.0, 20.0, 100.0]), torch.zeros(20)])
+        W[:64] = torch.diag(g).to(torch.bfloat16)
+        W[64:] = 1.0
+        h, eh, _, _ = ref.gated(X, W, None, kind)
+        ref.close(rtl.gated_linear(X, W, act=kind), h, eh, kind)
+
+
+def test_weight_beyond_32_bits():
+    """More than 2^32 bytes of gate rows: the up rows lie behind them."""
+    F, K = 1 << 18, 8192 + 64
+    gen = generator(4)
+    W = torch.zeros(2 * F, K, dtype=torch.bfloat16, device=DEV)
+    for rows in (slice(0, 256), slice(F - 256, F + 256), slice(2 * F - 256, 2 * F)):
+        W[rows] = bf16(gen, W[rows].shape[0], K, std=K ** -0.5)
+    some = torch.cat([torch.arange(256), torch.arange(F - 256, F)]).to(DEV)
+    for M in (1, 40):
+        X = bf16(gen, M, K)
+        H = rtl.gated_linear(X, W)
+        h, eh, _, _ = ref.gated(X, torch.cat([W[some], W[F + some]]), None, "silu")
+        ref.close(H[:, some], h, eh)
+        assert bool((H[:, 256:F - 256] == 0).all())
+
+
+BACK_SIZES = [(1, 4, 8), (1, 704, 512), (5, 20, 72), (37, 60, 64), (64, 128, 256), (129, 132, 200), (300, 704, 512), (701, 260, 136), (1500, 520, 640)]
+
+
+@pytest.mark.parametrize("M,F,K", BACK_SIZES)
+@pytest.mark.parametrize("kind,dtype", [("silu", torch.bfloat16), ("gelu", torch.float32), ("gelu_tanh", torch.bfloat16)])
+def test_backward(M, F, K, kind, dtype):
+    gen = generator(M * F + K)
+    X, W, P, dH = strided(bf16(gen, M, K)), strided(bf16(gen, 2 * F, K, std=K ** -0.5)), strided(bf16(gen, M, 2 * F, std=2.0), pad=3), strided(bf16(gen, M, F), pad=5)
+    want = ref.gated_backward(dH, X, W, P, kind)
+    got = dict(zip(("dX", "dW", "db", "H"), rtl.gated_linear_backward(dH, X, W, P, act=kind, with_bias=True, with_hidden=True, dtype=dtype)))
+    for name, (value, err) in want.items():
+        assert got[name].dtype is (dtype if name in ("dW", "db") else torch.bfloat16)
+        ref.close(got[name], value, err, name)
+
+
+def test_backward_in_parts():
+    """Only what is asked for, into places of the caller's."""
+    gen = generator(8)
+    M, F, K = 70, 36, 64
+    X, W, P, dH = bf16(gen, M, K), bf16(gen, 2 * F, K, std=0.1), bf16(gen, M, 2 * F), bf16(gen, M, F)
+    want = ref.gated_backward(dH, X, W, P, "silu")
+    full = rtl.gated_linear_backward(dH, X, W, P, with_bias=True, with_hidden=True)
+    dX, dW, db, H = rtl.gated_linear_backward(dH, None, W, P)
+    assert dW is None and db is None and H is None and torch.equal(dX, full[0])
+    dX, dW, db, H = rtl.gated_linear_backward(dH, X, None, P)
+    assert dX is None and db is None and H is None and torch.equal(dW, full[1])
+    place, around = room(M, F, F + 9, first=1)
+    dX, dW, db, H = rtl.gated_linear_backward(dH, X, W, P, out=(None, None, None, place))
+    assert dX is None and dW is None and db is None and H is place
+    ref.close(H, *want["H"])
+    untouched(around, F, first=1)
+    place, around = room(M, K, K + 16, first=8)
+    assert rtl.gated_linear_backward(dH, X, W, P, out=(place, None, None, None))[0] is place
+    ref.close(place, *want["dX"])
+    untouched(around, K, first=8)
+    ws = torch.full((rtl.gated_linear_backward_workspace(M, F, K),), 255, dtype=torch.uint8, device=DEV)
+    for a, b in zip(full, rtl.gated_linear_backward(dH, X, W, P, with_bias=True, with_hidden=True, ws=ws)):
+        assert torch.equal(a, b)
+
+
+def test_backward_without_rows():
+    X, W = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV), torch.ones(16, 64, dtype=torch.bfloat16, device=DEV)
+    dH, P = torch.empty(0, 8, dtype=torch.bfloat16, device=DEV), torch.empty(0, 16, dtype=torch.bfloat16, device=DEV)
+    dX, dW, db, H = rtl.gated_linear_backward(dH, X, W, P, with_bias=True, with_hidden=True)
+    assert dX.shape == (0, 64) and H.shape == (0, 8) and bool((dW == 0).all()) and bool((db == 0).all())
+    assert rtl.gated_linear(X, W).shape == (0, 8)
+
+
+def test_backward_exact():
+    """Gates of 0 and 64 and small integers: every value is exact, so is the place of each."""
+    gen = generator(9)
+    M, F, K = 300, 136, 264
+    whole = lambda *shape: torch.randint(-2, 3, shape, generator=gen, device=DEV).to(torch.bfloat16)  # noqa: E731
+    X, W, dH, U = whole(M, K), whole(2 * F, K), whole(M, F), whole(M, F)
+    G = 64.0 * torch.randint(0, 2, (M, F), generator=gen, device=DEV).to(torch.bfloat16)
+    dX, dW, db, H = rtl.gated_linear_backward(dH, X, W, torch.cat([G, U], 1), with_bias=True, with_hidden=True, dtype=torch.float32)
+    g, u, dh = G.double(), U.double(), dH.double()
+    dp = torch.cat([dh * u * torch.where(g > 0, 1.0, 0.5), dh * g], 1)
+    assert torch.equal(dW.double(), dp.t() @ X.double()) and torch.equal(db.double(), dp.sum(0)) and torch.equal(H.double(), g * u)
+    ref.close(dX, dp @ W.double(), torch.zeros(M, K, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("kind", ACTS)
+def test_backward_against_differences(kind):
+    """The gradients are those of the forward formula: central differences in 64 bits of sum(dH act(G) U)."""
+    gen = generator(10)
+    M, F = 24, 32
+    P, dH = bf16(gen, M, 2 * F, std=2.0), bf16(gen, M, F)
+    eye = torch.eye(2 * F, dtype=torch.bfloat16, device=DEV)
+    dP = rtl.gated_linear_backward(dH, None, eye, P, act=kind)[0].double()          # W of ones on the diagonal: dX is [dG dU]
+    f = lambda p: ref.act(p[:, :F], kind)[0] * p[:, F:] * dH.double()  # noqa: E731
+    e = 1e-5
+    for half in (0, 1):
+        step = torch.zeros(M, 2 * F, dtype=torch.float64, device=DEV)
+        step[:, half * F:(half + 1) * F] = e
+        slope = (f(P.double() + step) - f(P.double() - step)) / (2 * e)
+        # rounded to bf16 twice to the same value; the differences are off by about e^2 |f'''| and 1e-16 / e of |f|
+        room_ = 2 * ref.HALF[torch.bfloat16] * slope.abs() + 1e-6 * (1 + (dH.double() * (1 + P.double().abs().amax())).abs())
+        assert bool(((dP[:, half * F:(half + 1) * F] - slope).abs() <= room_).all())
+
+
+def test_captured_and_replayed():
+    """Forward and backward in one graph, inputs changed between the replays, eager calls in between."""
+    gen = generator(11)
+    M, F, K = 333, 264, 192
+    X, W, dH = bf16(gen, M, K), bf16(gen, 2 * F, K, std=0.1), bf16(gen, M, F)
+    H, P = torch.empty(M, F, dtype=torch.bfloat16, device=DEV), torch.empty(M, 2 * F, dtype=torch.bfloat16, device=DEV)
+    out = (torch.empty_like(X), torch.empty_like(W), torch.empty(2 * F, dtype=torch.bfloat16, device=DEV), torch.empty_like(H))
+    ws = torch.empty(rtl.gated_linear_backward_workspace(M, F, K), dtype=torch.uint8, device=DEV)
+    rtl.init()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        rtl.gated_linear(X, W, act="gelu", out=H, pre=P)
+        rtl.gated_linear_backward(dH, X, W, P, act="gelu", out=out, ws=ws)
+    for _ in range(3):
+        X.copy_(bf16(gen, M, K))
+        dH.copy_(bf16(gen, M, F))
+        graph.replay()
+        torch.cuda.synchronize()
+        h, p = rtl.gated_linear(X, W, act="gelu", with_pre=True)
+        again = rtl.gated_linear_backward(dH, X, W, p, act="gelu", with_bias=True, with_hidden=True)
+        assert torch.equal(h, H) and torch.equal(p, P)
+        for a, b in zip(out, again):
+            assert torch.equal(a, b)
