@@ -962,7 +962,7 @@ rtl_status rtl_residual_norm(const void* x, const void* y, const void* gate, con
 }
 
 // rtl_residual_norm_backward workspace: [sums of the teams' rows | sums of the sequences]
-static size_t norm_sums_bytes(int64_t T, int64_t S, int64_t D) { return round_up(rtl::residual_norm_backward_slots(T, S) * 3 * (size_t)D * sizeof(float), 256); }
+static size_t norm_sums_bytes(int64_t T, int64_t S, int64_t D) { return round_up(rtl::residual_norm_backward_slots(T, S, D) * 3 * (size_t)D * sizeof(float), 256); }
 size_t rtl_residual_norm_backward_workspace(int64_t T, int64_t S, int64_t D) {
     if (T < 0 || S <= 0 || D <= 0) return 0;
     return norm_sums_bytes(T, S, D) + (size_t)S * 2 * (size_t)D * sizeof(float);
@@ -975,6 +975,7 @@ rtl_status rtl_residual_norm_backward(const void* dx_out, const void* dh, const 
                                       int64_t ld_mod, int64_t lddx, int64_t lddy, void* workspace, size_t workspace_bytes, void* stream) {
     rtl_status st = check_norm(x_type, post, pre, alpha, eps, T, S, D, offsets);
     if (st != RTL_OK) return st;
+    if (S * ((D + 63) / 64) >= (int64_t)1 << 22) return RTL_ERR_SHAPE;       // workgroups of 1024 threads
     const bool f32 = x_type == RTL_F32;
     auto floats = [](const float* p) { return p && !aligned(p, 4) ? RTL_ERR_ALIGN : RTL_OK; };
     st = first_error({check_rows(dx_out, lddxo, D, f32), check_rows(dh, lddh, D), check_rows(x_out, ldxo, D, f32), check_rows(y, ldy, D),
@@ -1041,12 +1042,10 @@ rtl_status rtl_norm_rotary(const void* q, const void* k, const float* pos, const
     RTL_REQUIRE_DEVICE();
     rtl::RotaryArgs a{};
     auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
-    a.q = bf(q); a.k = bf(k); a.wq = bf(wq); a.wk = bf(wk);
-    a.q_out = static_cast<uint16_t*>(q_out);
-    a.k_out = static_cast<uint16_t*>(k_out);
+    a.side[0] = rtl::HeadSide{bf(q), bf(wq), nullptr, static_cast<uint16_t*>(q_out), nullptr, nullptr, ldq, sq, ldqo, sqo, 0, 0, (int)Hq, 0, 0, 0};
+    a.side[1] = rtl::HeadSide{bf(k), bf(wk), nullptr, static_cast<uint16_t*>(k_out), nullptr, nullptr, ldk, sk, ldko, sko, 0, 0, (int)Hk, 0, 0, 0};
     a.pos = pos; a.freq = freq; a.axis = axis;
-    a.T = T; a.Hq = (int)Hq; a.Hk = (int)Hk; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
-    a.ldq = ldq; a.sq = sq; a.ldk = ldk; a.sk = sk; a.ldqo = ldqo; a.sqo = sqo; a.ldko = ldko; a.sko = sko;
+    a.T = T; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
     a.norm = norm == RTL_NORM_RMS; a.eps = eps; a.interleaved = interleaved != 0;
     return rtl::launch_rotary(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
@@ -1077,17 +1076,13 @@ rtl_status rtl_norm_rotary_backward(const void* dq_out, const void* dk_out, cons
     RTL_REQUIRE_DEVICE();
     rtl::RotaryArgs a{};
     auto bf = [](const void* p) { return static_cast<const uint16_t*>(p); };
-    a.q = bf(q); a.k = bf(k); a.wq = bf(wq); a.wk = bf(wk); a.dq_out = bf(dq_out); a.dk_out = bf(dk_out);
-    a.dq = static_cast<uint16_t*>(dq);
-    a.dk = static_cast<uint16_t*>(dk);
+    a.side[0] = rtl::HeadSide{bf(q), bf(wq), bf(dq_out), static_cast<uint16_t*>(dq), dwq, nullptr, ldq, sq, lddq, sdq, lddqo, sdqo, (int)Hq, 0, 0, 0};
+    a.side[1] = rtl::HeadSide{bf(k), bf(wk), bf(dk_out), static_cast<uint16_t*>(dk), dwk, nullptr, ldk, sk, lddk, sdk, lddko, sdko, (int)Hk, 0, 0, 0};
     a.pos = pos; a.freq = freq; a.axis = axis;
-    a.dwq = dwq; a.dwk = dwk;
-    a.sums = sums ? static_cast<float*>(workspace) : nullptr;
-    a.T = any ? T : 0; a.Hq = (int)Hq; a.Hk = (int)Hk; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
-    a.ldq = ldq; a.sq = sq; a.ldk = ldk; a.sk = sk; a.lddqo = lddqo; a.sdqo = sdqo; a.lddko = lddko; a.sdko = sdko;
-    a.lddq = lddq; a.sdq = sdq; a.lddk = lddk; a.sdk = sdk;
+    a.T = any ? T : 0; a.D = (int)D; a.pairs = (int)pairs; a.axes = (int)axes;
     a.norm = rms; a.eps = eps; a.interleaved = interleaved != 0;
-    return rtl::launch_rotary_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
+    return rtl::launch_rotary_backward(a, sums ? static_cast<float*>(workspace) : nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK
+                                                                                                                                    : RTL_ERR_HIP;
 }
 
 }  // extern "C"

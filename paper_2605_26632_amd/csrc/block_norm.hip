@@ -37,25 +37,30 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void load8(const uint16_t* p, float (&f)[8]) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
+// A row's address is the same in all lanes of a team (scalar registers), the column a 32-bit offset from it.
 template <bool F32>
-__device__ __forceinline__ void load8_as(const void* p, int64_t at, float (&f)[8]) {
+__device__ __forceinline__ const void* row_at(const void* p, int64_t at) { return static_cast<const uint8_t*>(p) + at * (F32 ? 4 : 2); }
+__device__ __forceinline__ void load8(const uint16_t* row, uint32_t col, float (&f)[8]) { unpack8(*reinterpret_cast<const uint4*>(row + col), f); }
+template <bool F32>
+__device__ __forceinline__ void load8_as(const void* p, int64_t at, uint32_t col, float (&f)[8]) {
+    const void* row = row_at<F32>(p, at);
     if constexpr (F32) {
-        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(row) + col);
         const float4 u = q[0], v = q[1];
         f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
     } else {
-        load8(static_cast<const uint16_t*>(p) + at, f);
+        load8(static_cast<const uint16_t*>(row), col, f);
     }
 }
 template <bool F32>
-__device__ __forceinline__ void store8_as(void* p, int64_t at, const float (&f)[8]) {
+__device__ __forceinline__ void store8_as(void* p, int64_t at, uint32_t col, const float (&f)[8]) {
+    void* row = const_cast<void*>(row_at<F32>(p, at));
     if constexpr (F32) {
-        float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(row) + col);
         q[0] = make_float4(f[0], f[1], f[2], f[3]);
         q[1] = make_float4(f[4], f[5], f[6], f[7]);
     } else {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = pack8(f);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + col) = pack8(f);
     }
 }
 
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
     __shared__ float slots[4 * WAVES];
     constexpr int TEAM = WAVES * 64, TEAMS = team_threads(WAVES) / TEAM;
     const int tl = threadIdx.x % TEAM;
-    const int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+    const int64_t row = (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
     if (row >= a.T) return;
     const int D = (int)a.D;
     const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.offsets, (int)a.S, (int)row));
@@ -178,8 +183,8 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
         for (int c = 0; c < NCH; ++c) {
             const int col = (c * TEAM + tl) * 8;
             if (col < D) {
-                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo + col, zero);
-                if (a.h) store8_as<false>(a.h, row * a.ldh + col, zero);
+                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, col, zero);
+                if (a.h) store8_as<false>(a.h, row * a.ldh, col, zero);
             }
         }
         return;
@@ -192,8 +197,8 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[c][e] = y[c][e] = 0.f;
         if (col < D) {
-            load8_as<F32>(a.x, row * a.ldx + col, x[c]);
-            if (a.y) load8(a.y + row * a.ldy + col, y[c]);
+            load8_as<F32>(a.x, row * a.ldx, col, x[c]);
+            if (a.y) load8(a.y + row * a.ldy, col, y[c]);
         }
     }
     Stats sy, sx;
@@ -206,11 +211,11 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
                 float w[8], g[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = g[e] = 1.0f;
-                if (a.w_post) load8(a.w_post + col, w);
-                if (a.gate) load8(a.gate + s * a.ld_gate + col, g);
+                if (a.w_post) load8(a.w_post, col, w);
+                if (a.gate) load8(a.gate + s * a.ld_gate, col, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
-                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo + col, x[c]);
+                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, col, x[c]);
             }
         }
     }
@@ -226,170 +231,251 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
                 w[e] = 1.0f;
                 g[e] = b[e] = 0.f;
             }
-            if (a.w_pre) load8(a.w_pre + col, w);
-            if (a.scale) load8(a.scale + s * a.ld_mod + col, g);
-            if (a.shift) load8(a.shift + s * a.ld_mod + col, b);
+            if (a.w_pre) load8(a.w_pre, col, w);
+            if (a.scale) load8(a.scale + s * a.ld_mod, col, g);
+            if (a.shift) load8(a.shift + s * a.ld_mod, col, b);
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[e] = w[e] * ((x[c][e] - sx.mean) * sx.scale) * (1.0f + g[e]) + b[e];
-            store8_as<false>(a.h, row * a.ldh + col, h);
+            store8_as<false>(a.h, row * a.ldh, col, h);
         }
     }
 }
 
-// A team takes `rows` neighbouring rows and keeps the columns' sums of the sequence it is in; where the sequence changes, and behind the last row, they go to
-// the workspace. Team b and sequence s have slot b + s: over a team's rows and from team to team one of the two grows and neither falls, so no two
-// share a slot. Sums of a slot: [dt norm(y) | dh n | dh], D floats each.
-template <int WAVES, int NCH, bool F32>
-__global__ __launch_bounds__(team_threads(WAVES)) void norm_backward_kernel(const NormGradArgs a) {
-    __shared__ float slots[4 * WAVES];
-    constexpr int TEAM = WAVES * 64, TEAMS = team_threads(WAVES) / TEAM;
-    const int tl = threadIdx.x % TEAM;
-    const int64_t team = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM, first = team * a.rows;
-    if (first >= a.T) return;
-    const int64_t end = min(first + a.rows, a.T);
-    const int D = (int)a.D;
-    const float inv = 1.0f / (float)D;
-    TeamSum<WAVES> sum{slots};
-    float of_gate[NCH][8], of_scale[NCH][8], of_shift[NCH][8];
-    int now = -1;
-    auto leave = [&]() {
-        if (now < 0 || !a.sums) return;
-        float* to = a.sums + (team + now) * 3 * a.D;
+// Sums of two values over the workgroup's waves (any number up to 16), in a fixed order: the waves' sums meet in LDS, and the lanes of each row of sixteen add
+// all of them up. `slot`: 2 x 32 floats, used by turns as in TeamSum.
+__device__ __forceinline__ void group_sum(float& a, float& b, float* slot, int& turn, int waves) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    float* s = slot + turn * 32;
+    turn ^= 1;
+    if (lane == 0) {
+        s[wave] = a;
+        s[16 + wave] = b;
+    }
+    __syncthreads();
+    const int at = lane & 15;
+    a = at < waves ? s[at] : 0.f;
+    b = at < waves ? s[16 + at] : 0.f;
+    auto step = [](float& x, auto ctrl) { x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    auto both = [&](auto ctrl) {
+        step(a, ctrl);
+        step(b, ctrl);
+    };
+    both(std::integral_constant<int, 0xB1>{});           // the neighbour, the other pair, the other four, the other eight
+    both(std::integral_constant<int, 0x4E>{});
+    both(std::integral_constant<int, 0x141>{});
+    both(std::integral_constant<int, 0x140>{});
+}
+
+// Eight values as they lie in memory.
+template <bool F32>
+struct Raw8 {
+    uint4 v[F32 ? 2 : 1];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-            if (col < D) {
-                store8_as<true>(to, col, of_gate[c]);
-                store8_as<true>(to, a.D + col, of_scale[c]);
-                store8_as<true>(to, 2 * a.D + col, of_shift[c]);
+        for (uint4& q : v) q = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void load(const void* p, int64_t at, uint32_t col) {
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(row_at<F32>(p, at)) + col * (F32 ? 4 : 2));
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) v[i] = q[i];
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f[4 * i] = __uint_as_float(v[i].x);
+                f[4 * i + 1] = __uint_as_float(v[i].y);
+                f[4 * i + 2] = __uint_as_float(v[i].z);
+                f[4 * i + 3] = __uint_as_float(v[i].w);
             }
+        } else {
+            unpack8(v[0], f);
+        }
+    }
+};
+
+// A team of a.waves waves, a chunk of eight columns to a lane, takes a.rows neighbouring rows and keeps the columns' sums of the sequence it is in; where the
+// sequence changes, and behind the last row, they go to the workspace. Team b and sequence s have slot b + s: over a team's rows and from team to team one of
+// the two grows and neither falls, so no two share a slot. Sums of a slot: [dt norm(y) | dh n | dh], D floats each.
+// The next row is under way while a row is worked on, and the factors of a sequence stay in registers as products: a row takes three or four sums over the
+// team one after the other, and the few teams that a compute unit holds would not hide the loads behind them.
+// Lanes behind the end of the row work on the row's first columns and are left out of the sums and stores only: branches around the arithmetic made the
+// compiler keep two copies of what lives across them, and spill.
+// SOLO: a wave to a team, four teams to a workgroup. POST: norm(y) is not y.
+template <bool F32, bool SOLO, bool POST>
+__global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(const NormGradArgs a) {
+    __shared__ float slots[64];
+    const int tl = SOLO ? threadIdx.x & 63 : threadIdx.x, D = (int)a.D;
+    const int team = SOLO ? (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int)blockIdx.x;
+    const int first = team * a.rows;
+    if (first >= a.T) return;
+    const int end = (int)min((int64_t)first + a.rows, a.T);
+    const bool mine = tl * 8 < D;
+    const uint32_t own = mine ? tl * 8 : 0;
+    // (formed anew where it is used: kept across the loops, the sums of the arrays' addresses and the column took 26 registers)
+    auto column = [&]() {
+        uint32_t c = own;
+        asm volatile("" : "+v"(c));
+        return c;
+    };
+    const float inv = 1.0f / (float)D;
+    int turn = 0;
+    auto sum = [&](float& u, float& v) {
+        u = mine ? u : 0.f;
+        v = mine ? v : 0.f;
+        if constexpr (SOLO) {
+            u = wave_sum(u);
+            v = wave_sum(v);
+        } else {
+            group_sum(u, v, slots, turn, a.waves);
         }
     };
-    for (int64_t row = first; row < end; ++row) {
-        const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.offsets, (int)a.S, (int)row));
+    const bool layer_pre = a.pre == RTL_NORM_LAYER, norm_pre = a.dh && a.pre != RTL_NORM_NONE, layer_post = POST && a.post == RTL_NORM_LAYER;
+
+    for (int row = first; row < end;) {
+        // a run of rows of one sequence
+        const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.offsets, (int)a.S, row));
         if (s < 0) {
-            if (a.clear) {
+            if (a.clear && mine) {
+                const uint32_t col = column();
                 const float zero[8] = {};
-#pragma unroll
-                for (int c = 0; c < NCH; ++c) {
-                    const int col = (c * TEAM + tl) * 8;
-                    if (col < D) {
-                        if (a.dx) store8_as<F32>(a.dx, row * a.lddx + col, zero);
-                        if (a.dy) store8_as<false>(a.dy, row * a.lddy + col, zero);
-                    }
-                }
+                if (a.dx) store8_as<F32>(a.dx, (int64_t)row * a.lddx, col, zero);
+                if (a.dy) store8_as<false>(a.dy, (int64_t)row * a.lddy, col, zero);
             }
+            ++row;
             continue;
         }
-        if (s != now) {
-            leave();
-            now = s;
-#pragma unroll
-            for (int c = 0; c < NCH; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) of_gate[c][e] = of_scale[c][e] = of_shift[c][e] = 0.f;
-        }
-        float x[NCH][8], y[NCH][8], dh[NCH][8], dt[NCH][8];
-#pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] = y[c][e] = dh[c][e] = dt[c][e] = 0.f;
-            if (col < D) {
-                if (a.dh) {
-                    load8_as<F32>(a.x, row * a.ldx + col, x[c]);
-                    load8(a.dh + row * a.lddh + col, dh[c]);
-                }
-                if (a.y) load8(a.y + row * a.ldy + col, y[c]);
-                if (a.dx_out) load8_as<F32>(a.dx_out, row * a.lddxo + col, dt[c]);
+        const int run_end = a.offsets ? max(min(a.offsets[s + 1], end), row + 1) : end;
+        Raw8<F32> rx, rd;
+        Raw8<false> ry, rh;
+        rx.zero();
+        rd.zero();
+        ry.zero();
+        rh.zero();
+        auto fetch = [&](int64_t row) {
+            const uint32_t col = column();
+            if (a.dh) {
+                rx.load(a.x, row * a.ldx, col);
+                rh.load(a.dh, row * a.lddh, col);
             }
+            if (a.y) ry.load(a.y, row * a.ldy, col);
+            if (a.dx_out) rd.load(a.dx_out, row * a.lddxo, col);
+        };
+        fetch(row);
+        float of_gate[8], of_scale[8], of_shift[8], f_pre[8], f_post[8];       // f_pre = w_pre (1 + scale), f_post = gate w_post
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            of_gate[e] = of_scale[e] = of_shift[e] = 0.f;
+            f_pre[e] = f_post[e] = 1.0f;
         }
-        Stats sx, sy;
-        row_stats<WAVES, NCH>(x, a.dh ? a.pre : RTL_NORM_NONE, sx, y, a.y ? a.post : RTL_NORM_NONE, sy, tl, D, a.eps, sum);
-        // n in x's place, norm(y) in y's; the columns' sums of dh; then dn in dh's place
+        const uint32_t col = column();
+        if (a.w_pre) load8(a.w_pre, col, f_pre);
+        if (a.w_post) load8(a.w_post, col, f_post);
+        if (a.scale) {
+            float v[8];
+            load8(a.scale + s * a.ld_mod, col, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f_pre[e] *= 1.0f + v[e];
+        }
+        if (a.gate) {
+            float v[8];
+            load8(a.gate + s * a.ld_gate, col, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f_post[e] *= v[e];
+        }
+#pragma unroll 1
+      for (; row < run_end; ++row) {
+        float x[8], y[8], dh[8], dt[8];
+        rx.get(x);
+        ry.get(y);
+        rh.get(dh);
+        rd.get(dt);
+        if (row + 1 < run_end) fetch(row + 1);
+        float mx = 0.f, rsx = 1.0f, my = 0.f, rsy = 1.0f;
+        if (layer_pre || layer_post) {
+            float u = 0.f, v = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u += x[e];
+                v += y[e];
+            }
+            sum(u, v);
+            if (layer_pre) mx = u * inv;
+            if (layer_post) my = v * inv;
+        }
+        if (norm_pre || POST) {
+            float u = 0.f, v = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] -= mx;
+                u += x[e] * x[e];
+                if constexpr (POST) {
+                    y[e] -= my;
+                    v += y[e] * y[e];
+                }
+            }
+            sum(u, v);
+            if (norm_pre) rsx = 1.0f / sqrtf(u * inv + a.eps);
+            if constexpr (POST) rsy = 1.0f / sqrtf(v * inv + a.eps);
+        }
+        // n in x's place, norm(y) in y's; the columns' sums; dn in dh's place
         float m = 0.f, mn = 0.f;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-            if (col < D) {
-                float w[8], g[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = 1.0f;
-                    g[e] = 0.f;
-                }
-                if (a.w_pre) load8(a.w_pre + col, w);
-                if (a.scale) load8(a.scale + s * a.ld_mod + col, g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[c][e] = (x[c][e] - sx.mean) * sx.scale;
-                    y[c][e] = (y[c][e] - sy.mean) * sy.scale;
-                    of_scale[c][e] += dh[c][e] * x[c][e];
-                    of_shift[c][e] += dh[c][e];
-                    dh[c][e] *= w[e] * (1.0f + g[e]);
-                    m += dh[c][e];
-                    mn += dh[c][e] * x[c][e];
-                }
-            }
+        for (int e = 0; e < 8; ++e) {
+            x[e] *= rsx;
+            if constexpr (POST) y[e] *= rsy;
+            of_scale[e] += dh[e] * x[e];
+            of_shift[e] += dh[e];
+            dh[e] *= f_pre[e];
+            m += dh[e];
+            mn += dh[e] * x[e];
         }
-        if (a.dh && a.pre != RTL_NORM_NONE) {
+        if (norm_pre) {
             sum(m, mn);
-            m = a.pre == RTL_NORM_LAYER ? m * inv : 0.f;
+            m = layer_pre ? m * inv : 0.f;
             mn *= inv;
         } else {
             m = mn = 0.f;
         }
-        float p = 0.f, pn = 0.f;
+        float p = 0.f, pn = 0.f, out[8];
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-            if (col < D) {
-                float w[8], g[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = g[e] = 1.0f;
-                if (a.w_post) load8(a.w_post + col, w);
-                if (a.gate) load8(a.gate + s * a.ld_gate + col, g);
-                float dx[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dt[c][e] += sx.scale * (dh[c][e] - m - x[c][e] * mn);
-                    dx[e] = a.alpha * dt[c][e];
-                    of_gate[c][e] += dt[c][e] * y[c][e];
-                    dt[c][e] *= g[e] * w[e];
-                    p += dt[c][e];
-                    pn += dt[c][e] * y[c][e];
-                }
-                if (a.dx) store8_as<F32>(a.dx, row * a.lddx + col, dx);
+        for (int e = 0; e < 8; ++e) {
+            dt[e] += rsx * (dh[e] - m - x[e] * mn);
+            out[e] = a.alpha * dt[e];
+            of_gate[e] += dt[e] * y[e];
+            dt[e] *= f_post[e];
+            if constexpr (POST) {
+                p += dt[e];
+                pn += dt[e] * y[e];
             }
         }
-        if (!a.y) continue;
-        if (a.post != RTL_NORM_NONE) {
+        if (a.dx && mine) store8_as<F32>(a.dx, (int64_t)row * a.lddx, column(), out);
+        if constexpr (POST) {
             sum(p, pn);
-            p = a.post == RTL_NORM_LAYER ? p * inv : 0.f;
+            p = layer_post ? p * inv : 0.f;
             pn *= inv;
-        } else {
-            p = pn = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dt[e] = rsy * (dt[e] - p - y[e] * pn);
         }
-        if (a.dy) {
-#pragma unroll
-            for (int c = 0; c < NCH; ++c) {
-                const int col = (c * TEAM + tl) * 8;
-                if (col < D) {
-                    float dy[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dy[e] = sy.scale * (dt[c][e] - p - y[c][e] * pn);
-                    store8_as<false>(a.dy, row * a.lddy + col, dy);
-                }
-            }
+        if (a.dy && mine) store8_as<false>(a.dy, (int64_t)row * a.lddy, column(), dt);
+      }
+        if (a.sums && mine) {
+            float* to = a.sums + (int64_t)(team + s) * 3 * a.D;
+            const uint32_t at = column();
+            store8_as<true>(to, 0, at, of_gate);
+            store8_as<true>(to, a.D, at, of_scale);
+            store8_as<true>(to, 2 * a.D, at, of_shift);
         }
     }
-    leave();
 }
 
-// Adds the slots of a sequence up in the order of its rows: 64 columns to a workgroup, the slots dealt to its four waves in turn and the four sums added in
-// order. What the weights' gradients need of it goes to a.totals ([S][2][D]).
-__global__ __launch_bounds__(256) void norm_reduce_kernel(const NormGradArgs a) {
-    __shared__ float part[3][4][64];
+// Adds the slots of a sequence up in the order of its rows: 64 columns to a workgroup, the slots dealt to its waves in turn and the waves' sums added in order.
+// What the weights' gradients need of it goes to a.totals ([S][2][D]); of a single sequence they are made here.
+constexpr int kReduceWaves = 16;
+__global__ __launch_bounds__(kReduceWaves * 64) void norm_reduce_kernel(const NormGradArgs a) {
+    __shared__ float part[3][kReduceWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = (int64_t)blockIdx.x * 64 + lane, s = blockIdx.y;
     int64_t b0 = 0, b1 = -1;
@@ -400,35 +486,42 @@ __global__ __launch_bounds__(256) void norm_reduce_kernel(const NormGradArgs a) 
         b1 = (end - 1) / a.rows;
     }
     float v[3] = {};
-    if (col < a.D)
-        for (int64_t b = b0 + wave; b <= b1; b += 4) {
-            const float* p = a.sums + (b + s) * 3 * a.D + col;
+    if (col < a.D) {
+        const float* p = a.sums + (b0 + wave + s) * 3 * a.D + col;
+#pragma unroll 4
+        for (int64_t b = b0 + wave; b <= b1; b += kReduceWaves, p += kReduceWaves * 3 * a.D) {
 #pragma unroll
             for (int k = 0; k < 3; ++k) v[k] += p[k * a.D];
         }
+    }
 #pragma unroll
     for (int k = 0; k < 3; ++k) part[k][wave][lane] = v[k];
     __syncthreads();
     if (wave != 0 || col >= a.D) return;
 #pragma unroll
     for (int k = 0; k < 3; ++k)
-        for (int w = 1; w < 4; ++w) v[k] += part[k][w][lane];
+        for (int w = 1; w < kReduceWaves; ++w) v[k] += part[k][w][lane];
     auto one = [](const uint16_t* p, int64_t at) { return p ? __uint_as_float((uint32_t)p[at] << 16) : 1.0f; };
     if (a.dgate) a.dgate[s * a.D + col] = v[0] * one(a.w_post, col);
     if (a.dscale) a.dscale[s * a.D + col] = v[1] * one(a.w_pre, col);
     if (a.dshift) a.dshift[s * a.D + col] = v[2];
-    if (a.dw_post) a.totals[s * 2 * a.D + col] = v[0];
-    if (a.dw_pre) a.totals[(s * 2 + 1) * a.D + col] = v[1];
+    if (a.S == 1) {
+        if (a.dw_post) a.dw_post[col] = v[0] * one(a.gate, col);
+        if (a.dw_pre) a.dw_pre[col] = v[1] * (a.scale ? 1.0f + one(a.scale, col) : 1.0f);
+    } else {
+        if (a.dw_post) a.totals[s * 2 * a.D + col] = v[0];
+        if (a.dw_pre) a.totals[(s * 2 + 1) * a.D + col] = v[1];
+    }
 }
 
-// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s, the sequences dealt to four waves as the slots above.
-__global__ __launch_bounds__(256) void norm_weights_kernel(const NormGradArgs a) {
-    __shared__ float part[2][4][64];
+// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s, the sequences dealt to the waves as the slots above.
+__global__ __launch_bounds__(kReduceWaves * 64) void norm_weights_kernel(const NormGradArgs a) {
+    __shared__ float part[2][kReduceWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = (int64_t)blockIdx.x * 64 + lane;
     float v[2] = {};
     if (col < a.D)
-        for (int64_t s = wave; s < a.S; s += 4) {
+        for (int64_t s = wave; s < a.S; s += kReduceWaves) {
             if (a.dw_post) v[0] += a.totals[s * 2 * a.D + col] * (a.gate ? __uint_as_float((uint32_t)a.gate[s * a.ld_gate + col] << 16) : 1.0f);
             if (a.dw_pre) v[1] += a.totals[(s * 2 + 1) * a.D + col] * (1.0f + (a.scale ? __uint_as_float((uint32_t)a.scale[s * a.ld_mod + col] << 16) : 0.0f));
         }
@@ -438,7 +531,7 @@ __global__ __launch_bounds__(256) void norm_weights_kernel(const NormGradArgs a)
     if (wave != 0 || col >= a.D) return;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-        for (int w = 1; w < 4; ++w) v[k] += part[k][w][lane];
+        for (int w = 1; w < kReduceWaves; ++w) v[k] += part[k][w][lane];
     if (a.dw_post) a.dw_post[col] = v[0];
     if (a.dw_pre) a.dw_pre[col] = v[1];
 }
@@ -454,7 +547,12 @@ hipError_t with_team(int64_t D, F f) {
     return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
 }
 
-constexpr int kBackwardRows = 16;            // rows of a team in the backward pass
+// Backward pass: waves of a team, and rows of one: the rows dealt once over the teams that the chip holds, 16 waves to a compute unit.
+int team_waves(int64_t D) { return (int)((D + 511) / 512); }
+int64_t team_rows(int64_t T, int64_t D) {
+    const int64_t teams = 256 * (16 / team_waves(D));
+    return T > teams ? (T + teams - 1) / teams : 1;
+}
 
 }  // namespace
 
@@ -469,30 +567,42 @@ hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream) {
     });
 }
 
-// [slots | totals], the slots' rows three times D floats
-size_t residual_norm_backward_slots(int64_t T, int64_t S) { return (size_t)((T + kBackwardRows - 1) / kBackwardRows + S); }
+size_t residual_norm_backward_slots(int64_t T, int64_t S, int64_t D) {
+    const int64_t rows = team_rows(T, D);
+    return (size_t)((T + rows - 1) / rows + S);
+}
 
 hipError_t launch_residual_norm_backward(const NormGradArgs& a_in, hipStream_t stream) {
     NormGradArgs a = a_in;
-    a.rows = kBackwardRows;
+    a.rows = (int)team_rows(a.T, a.D);
+    a.waves = team_waves(a.D);
     hipError_t e = hipSuccess;
-    if (a.T > 0)
-        e = with_team(a.D, [&](auto waves, auto chunks) {
-            constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
-            const int64_t rows = team_threads(W) / (W * 64) * a.rows;
-            const dim3 grid((unsigned)((a.T + rows - 1) / rows));
-            if (a.x_f32) hipLaunchKernelGGL((norm_backward_kernel<W, C, true>), grid, dim3(team_threads(W)), 0, stream, a);
-            else hipLaunchKernelGGL((norm_backward_kernel<W, C, false>), grid, dim3(team_threads(W)), 0, stream, a);
-            return hipGetLastError();
-        });
+    if (a.T > 0) {
+        const int64_t teams = (a.T + a.rows - 1) / a.rows;
+        auto go = [&](auto f32, auto solo, auto post) {
+            constexpr bool F32 = decltype(f32)::value, SOLO = decltype(solo)::value, POST = decltype(post)::value;
+            hipLaunchKernelGGL((norm_backward_kernel<F32, SOLO, POST>), dim3((unsigned)(SOLO ? (teams + 3) / 4 : teams)), dim3(SOLO ? 256 : a.waves * 64), 0, stream, a);
+        };
+        using T = std::true_type;
+        using F = std::false_type;
+        const bool solo = a.waves == 1, post = a.y && a.post != RTL_NORM_NONE;
+        if (a.x_f32) {
+            if (solo) post ? go(T{}, T{}, T{}) : go(T{}, T{}, F{});
+            else post ? go(T{}, F{}, T{}) : go(T{}, F{}, F{});
+        } else {
+            if (solo) post ? go(F{}, T{}, T{}) : go(F{}, T{}, F{});
+            else post ? go(F{}, F{}, T{}) : go(F{}, F{}, F{});
+        }
+        e = hipGetLastError();
+    }
     const unsigned cols = (unsigned)((a.D + 63) / 64);
     const bool weights = a.dw_post || a.dw_pre;
     if (e == hipSuccess && a.S > 0 && (weights || a.dgate || a.dscale || a.dshift)) {
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3(cols, (unsigned)a.S), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(norm_reduce_kernel, dim3(cols, (unsigned)a.S), dim3(kReduceWaves * 64), 0, stream, a);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && weights) {
-        hipLaunchKernelGGL(norm_weights_kernel, dim3(cols), dim3(256), 0, stream, a);
+    if (e == hipSuccess && weights && a.S != 1) {
+        hipLaunchKernelGGL(norm_weights_kernel, dim3(cols), dim3(kReduceWaves * 64), 0, stream, a);
         e = hipGetLastError();
     }
     return e;

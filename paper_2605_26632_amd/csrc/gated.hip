@@ -27,6 +27,112 @@ struct Gated {
     }
 };
 
+// The 256-row plan: body tiles of 256 x BN rows of W, tail tiles of 256 x 128 over the rows of X behind m_split (gemm.hip has the reasons).
+template <int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(512) void gated_mixed_kernel(const GemmArgs a) {
+    const int xcd = (int)blockIdx.x % 8, local = (int)blockIdx.x / 8;
+    const int nb = a.body_tiles, nt = a.tail_tiles, nb_x = nb / 8 + (xcd < nb % 8);
+    if (local < nb_x) {
+        GemmArgs b = a;
+        if (nt > 0) b.M = a.m_split;
+        gemm_tile<false, 256, BN, WAVES_M, WAVES_N, 2, 2>(b, xcd_share_start(nb, xcd) + local);
+    } else {
+        GemmArgs t = a;
+        t.M = a.M - a.m_split;
+        t.A = static_cast<const uint16_t*>(a.A) + a.m_split * a.lda;
+        t.Y = a.Y + a.m_split * a.ldy;
+        if (a.P) t.P = a.P + a.m_split * a.ldp;
+        gemm_tile<false, 256, 128, 4, 2, 3, 2>(t, xcd_share_start(nb + nt, xcd) - xcd_share_start(nb, xcd) + (local - nb_x));
+    }
+}
+
+template <int BN, int WAVES_M, int WAVES_N>
+struct GatedMixed {
+    static constexpr int kBody = Smem<false, 256, BN, 2, WAVES_M, WAVES_N, false>::kTotal, kTail = Smem<false, 256, 128, 3, 4, 2, false>::kTotal;
+    static constexpr int kLds = kBody > kTail ? kBody : kTail;
+    static hipError_t prepare() {
+        return hipFuncSetAttribute(reinterpret_cast<const void*>(gated_mixed_kernel<BN, WAVES_M, WAVES_N>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    }
+    static hipError_t launch(const GemmArgs& a, hipStream_t stream) {
+        hipLaunchKernelGGL((gated_mixed_kernel<BN, WAVES_M, WAVES_N>), dim3((unsigned)(a.body_tiles + a.tail_tiles)), dim3(512), kLds, stream, a);
+        return hipGetLastError();
+    }
+};
+
+// Up to sixteen rows of X: reading W is all there is, and it goes straight from memory into the registers that the matrix instruction takes (few_rows.hip has
+// the layout). A workgroup owns sixteen columns of H, so sixteen gate rows and the sixteen up rows; its waves divide the contraction in lines of 128
+// bytes, neighbouring waves on neighbouring lines, four lines of a row in flight, and their sums meet in LDS in a fixed order.
+constexpr int kFewRows = 16, kFewWaves = 4, kFewLines = 4;
+__global__ __launch_bounds__(kFewWaves * 64) void gated_few_rows_kernel(const GemmArgs a) {
+    __shared__ __align__(16) float sums[kFewWaves][2][64][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, kb = lane >> 4;
+    const int units = (int)(a.K / 64);
+    const int64_t n0 = (int64_t)blockIdx.x * 16, n = min(n0 + li, a.N - 1);
+    const uint16_t* const w_row[2] = {static_cast<const uint16_t*>(a.W) + n * a.ldw + kb * 16, static_cast<const uint16_t*>(a.W) + (a.N + n) * a.ldw + kb * 16};
+    const uint16_t* const x_row = static_cast<const uint16_t*>(a.A) + min((int64_t)li, a.M - 1) * a.lda + kb * 16;     // (rows behind the last repeat it, never stored)
+    f32x4 acc[2] = {};
+    for (int u0 = wave; u0 < units; u0 += kFewWaves * kFewLines) {
+        Frag8 w[kFewLines][2][2], x[kFewLines][2];
+#pragma unroll
+        for (int u = 0; u < kFewLines; ++u) {
+            const int64_t at = (int64_t)min(u0 + u * kFewWaves, units - 1) * 64;                  // (behind the end: loaded again, not used)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int f = 0; f < 2; ++f) w[u][f][c].u = *reinterpret_cast<const uint4*>(w_row[f] + at + c * 8);
+                x[u][c].u = *reinterpret_cast<const uint4*>(x_row + at + c * 8);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);                                                       // all the loads first
+#pragma unroll
+        for (int u = 0; u < kFewLines; ++u) {
+            if (u0 + u * kFewWaves >= units) break;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][f][c].v, x[u][c].v, acc[f], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < 2; ++f) *reinterpret_cast<f32x4*>(sums[wave][f][lane]) = acc[f];
+    __syncthreads();
+    if (wave != 0) return;
+    // row li of X, columns 4 kb .. of the sixteen
+    const int64_t col = n0 + 4 * kb;
+    const int valid = (int)min((int64_t)4, a.N - col);
+    if (li >= a.M || valid <= 0) return;
+    const GateForm form = gate_form(a.act);
+    uint16_t out[3][4];
+    f32x4 s[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+        s[f] = *reinterpret_cast<const f32x4*>(sums[0][f][lane]);
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) s[f] += *reinterpret_cast<const f32x4*>(sums[w][f][lane]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int64_t at = col + min(e, valid - 1);
+        const float g = s[0][e] + (a.bias ? __uint_as_float((uint32_t)a.bias[at] << 16) : 0.f);
+        const float u = s[1][e] + (a.bias ? __uint_as_float((uint32_t)a.bias[a.N + at] << 16) : 0.f);
+        out[0][e] = (uint16_t)f32_to_bf16_rne((a.act == RTL_ACT_GELU ? gate_value<true>(g, form) : gate_value<false>(g, form)) * u);
+        out[1][e] = (uint16_t)f32_to_bf16_rne(g);
+        out[2][e] = (uint16_t)f32_to_bf16_rne(u);
+    }
+    uint16_t* const to[3] = {a.Y + li * a.ldy + col, a.P + li * a.ldp + col, a.P + li * a.ldp + a.N + col};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        if (k > 0 && !a.P) break;
+        if (valid == 4) {
+            __builtin_memcpy(to[k], out[k], 8);                                                  // (at any address)
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < valid) to[k][e] = out[k][e];
+        }
+    }
+}
+
 // dP = [dH U act'(G), dH act(G)] and, with H set, H = act(G) U again. Eight columns to a thread, F a multiple of four, rows of any 8-byte alignment. Bound by
 // memory: five or six values of two bytes per element of H. dP is rounded to bf16, the type that the matrix cores take in the products behind it. The
 // workspace's two offsets for those products, all rows for the one expert, are written on the way.
@@ -70,11 +176,35 @@ __global__ __launch_bounds__(kGradThreads) void gated_grad_kernel(const GatedGra
     if (a.H) store_run(a.H + row * a.ldh + col, h, valid);
 }
 
-using Gated128 = Gated<128, 128, 2, 2, 1, 3>;
+// Runs `op` (launch or prepare) of small tile `i`; shapes and rings as in gemm.hip.
+template <class Op>
+hipError_t with_gated(int i, Op op) {
+    switch (i) {
+        case 0: return op(Gated<32, 32, 1, 1, 4, 4>{});
+        case 1: return op(Gated<64, 32, 1, 1, 4, 3>{});
+        case 2: return op(Gated<64, 64, 1, 2, 2, 4>{});
+        case 3: return op(Gated<128, 64, 2, 2, 2, 3>{});
+        default: return op(Gated<128, 128, 2, 2, 1, 3>{});
+    }
+}
+using Gated256 = GatedMixed<256, 2, 4>;
+using Gated192 = GatedMixed<192, 4, 2>;
 
 }  // namespace
 
-hipError_t launch_gated(const GemmArgs& a, hipStream_t stream) { return Gated128::launch(a, stream); }
+hipError_t launch_gated(const GemmArgs& a_in, hipStream_t stream) {
+    GemmArgs a = a_in;
+    if (a.M <= kFewRows && a.N < (int64_t)1 << 27) {               // (a launch takes fewer than 2^32 threads)
+        hipLaunchKernelGGL(gated_few_rows_kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(kFewWaves * 64), 0, stream, a);
+        return hipGetLastError();
+    }
+    const GatedForm form = gated_form(a.M, a.N, a.K);
+    if (form.shape >= 0) return with_gated(form.shape, [&](auto k) { return decltype(k)::launch(a, stream); });
+    a.m_split = form.m_split;
+    a.body_tiles = form.body_tiles;
+    a.tail_tiles = form.tail_tiles;
+    return form.use_192 ? Gated192::launch(a, stream) : Gated256::launch(a, stream);
+}
 
 int64_t gated_grad_grid(int64_t M, int64_t F) { return (M * ((F + 7) / 8) + kGradThreads - 1) / kGradThreads; }
 hipError_t launch_gated_grad(const GatedGradArgs& a, hipStream_t stream) {
@@ -85,6 +215,11 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t prepare_gated_kernels() { return Gated128::prepare(); }
+hipError_t prepare_gated_kernels() {
+    hipError_t e = Gated256::prepare();
+    if (e == hipSuccess) e = Gated192::prepare();
+    for (int i = 0; i < 5 && e == hipSuccess; ++i) e = with_gated(i, [](auto k) { return decltype(k)::prepare(); });
+    return e;
+}
 
 }  // namespace rtl

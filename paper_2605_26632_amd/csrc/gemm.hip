@@ -331,7 +331,8 @@ struct SplitChoice {
     bool part_256;
 };
 static int64_t part_pitch(int64_t N) { return (N + 7) / 8 * 8; }     // columns of a plane: whole eight-column chunks
-static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_t blocks, bool dense, bool fp8, size_t room) {
+// gated: a gated linear of N rows of W, which has no 256 x 96 tile.
+static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_t blocks, bool dense, bool fp8, size_t room, bool gated = false) {
     const double busy = (double)(plan.body_tiles + plan.tail_tiles < 256 ? plan.body_tiles + plan.tail_tiles : 256);
     const double load = busy > 96 ? (busy - 96) / 160 : 0.0;
     const double per_kb = dense ? 0.0146 + 0.0053 * load : 0.0107 + 0.0065 * load;
@@ -344,6 +345,7 @@ static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_
         const int64_t tiles = ((M + s.bm - 1) / s.bm) * ((N + s.bn - 1) / s.bn);
         if (tiles > 4096) continue;                        // far more than a few passes: never the better one
         double block = s.block;
+        if (gated && s.bm == 256) continue;
         if (s.bm == 256) {                                 // one pass only, slower as the chip fills (its rivals are, in the sparse case)
             if (tiles > 256) continue;
             if (dense && tiles > 128) block += 0.0021 * (double)(tiles - 128);
@@ -396,6 +398,11 @@ void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t 
     out[0] = c.k_splits > 1 ? -1 : c.shape;
     out[1] = c.k_splits;
     out[2] = c.part_256 ? 256 : 128;
+}
+
+GatedForm gated_form(int64_t M, int64_t F, int64_t K) {
+    const TilePlan p = plan_for(M, 2 * F, true);
+    return GatedForm{pick_split(p, M, 2 * F, K / 64, true, false, 0, true).shape, p.use_192, p.m_split, p.body_tiles, p.tail_tiles};
 }
 
 void mx_choice(int64_t M, int64_t N, int64_t K, size_t room, int out[3]) {

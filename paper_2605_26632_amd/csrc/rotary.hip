@@ -4,9 +4,10 @@
 //             a sin + b cos); pairs are (2 j, 2 j + 1) or (j, j + pairs), what lies behind the pairs passes
 //   backward  the gradient is turned back by the angle; dw += d q r, and through the norm: dq = r (w d - q r mean(w d q r)), r = 1 / sqrt(mean q^2 + eps)
 //
-// Bound by memory (each head read once and written once). An angle belongs to a token: a lane holds 16 values of a head, so that the eight pairs that
-// they make are the same for all heads of the token, and their sines are taken once per wave. The product of position and frequency is exact in 64
-// bits and cut to a quarter turn there, since in 32 a far position's angle would be off by 2^-24 of itself; the rest is fp32.
+// Bound by memory (each head read once and written once). An angle belongs to a token: a wave takes heads of one token and has its lanes take the sines of
+// a pair each, which they share in LDS. The product of position and frequency is exact in 64 bits and cut to a quarter turn there, since in 32 a far
+// position's angle would be off by 2^-24 of itself; the rest is fp32. q and k are dealt to workgroups of their own, so that weights and strides are
+// the same throughout a wave.
 #include "rtl_internal.h"
 
 namespace rtl {
@@ -63,53 +64,59 @@ __device__ __forceinline__ void turn(float pos, float freq, float& sn, float& cs
     cs = (quarter + 1) & 2 ? -b : b;
 }
 
-// What a lane does in every head: its two chunks of eight values (first value, or -1 for none), whether they turn, and its eight pairs' sines. HALVES: element e of
-// the first chunk and of the second are pair e; else a chunk holds four pairs, of which the lane has the two chunks' eight.
+// What a lane does in every head: its two chunks of eight values (first value, or -1 for none) and its eight pairs. HALVES: element e of the first chunk and
+// of the second are pair e; else a chunk holds four pairs, of which the lane has the two chunks' eight. Pairs from `pairs` on are turned by nothing.
+constexpr int kMostPairs = 256 + 8;
 struct LanePlan {
-    int at[2];
-    bool turns[2];
-    int pair0;
+    int at[2], pair0;
 };
 template <bool HALVES>
 __device__ __forceinline__ LanePlan lane_plan(int c, int D, int pairs) {
-    LanePlan p;
-    const int chunks = D / 8;
+    const int chunks = D / 8, none = (pairs + 7) / 8 * 8;
     if constexpr (HALVES) {
-        const int half = pairs / 8;
-        if (c < half) {
-            p = LanePlan{{c * 8, (c + half) * 8}, {true, true}, c * 8};
-        } else {
-            const int rest = 2 * half + 2 * (c - half);
-            p = LanePlan{{rest < chunks ? rest * 8 : -1, rest + 1 < chunks ? (rest + 1) * 8 : -1}, {false, false}, 0};
-        }
+        const int half = pairs / 8, rest = 2 * half + 2 * (c - half);
+        if (c < half) return LanePlan{{c * 8, (c + half) * 8}, c * 8};
+        return LanePlan{{rest < chunks ? rest * 8 : -1, rest + 1 < chunks ? (rest + 1) * 8 : -1}, none};
     } else {
         const int i = 2 * c;
-        p = LanePlan{{i < chunks ? i * 8 : -1, i + 1 < chunks ? (i + 1) * 8 : -1}, {i * 4 < pairs, i * 4 + 4 < pairs}, c * 8};
+        return LanePlan{{i < chunks ? i * 8 : -1, i + 1 < chunks ? (i + 1) * 8 : -1}, min(c * 8, none)};
     }
-    return p;
 }
 
-template <bool HALVES>
-__device__ __forceinline__ void lane_turns(const RotaryArgs& a, const LanePlan& p, int64_t token, float (&sn)[8], float (&cs)[8]) {
+// The token's sines, a pair to a lane, through the wave's own part of LDS (whose operations stay in order): those of the lane's pairs come back.
+struct Turns {
+    float sn[8], cs[8];
+};
+__device__ __forceinline__ Turns token_turns(const RotaryArgs& a, const LanePlan& p, int64_t token, float (*lds)[kMostPairs]) {
+    const int fill = (a.pairs + 7) / 8 * 8 + 8;
+    for (int j = threadIdx.x & 63; j < fill; j += 64) {
+        float s = 0.f, c = 1.f;
+        if (j < a.pairs) {
+            const int ax = min(max(a.axis[j], 0), a.axes - 1);
+            turn(a.pos[token * a.axes + ax], a.freq[j], s, c);
+        }
+        lds[0][j] = s;
+        lds[1][j] = c;
+    }
+    __builtin_amdgcn_wave_barrier();
+    Turns t;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        sn[e] = 0.f;
-        cs[e] = 1.f;
-        if (p.turns[HALVES ? 0 : e / 4]) {
-            const int j = p.pair0 + e, ax = min(max(a.axis[j], 0), a.axes - 1);
-            turn(a.pos[token * a.axes + ax], a.freq[j], sn[e], cs[e]);
-        }
+        t.sn[e] = lds[0][p.pair0 + e];
+        t.cs[e] = lds[1][p.pair0 + e];
     }
+    __builtin_amdgcn_wave_barrier();
+    return t;
 }
 
 // Both chunks turned; BACK: by the negative angle.
 template <bool HALVES, bool BACK>
-__device__ __forceinline__ void apply_turns(float (&v)[2][8], const float (&sn)[8], const float (&cs)[8]) {
+__device__ __forceinline__ void apply_turns(float (&v)[2][8], const Turns& t) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float& x = HALVES ? v[0][e] : v[e / 4][2 * (e % 4)];
         float& y = HALVES ? v[1][e] : v[e / 4][2 * (e % 4) + 1];
-        const float s = BACK ? -sn[e] : sn[e], p = x * cs[e] - y * s, q = x * s + y * cs[e];
+        const float s = BACK ? -t.sn[e] : t.sn[e], p = x * t.cs[e] - y * s, q = x * s + y * t.cs[e];
         x = p;
         y = q;
     }
@@ -118,15 +125,25 @@ __device__ __forceinline__ void apply_turns(float (&v)[2][8], const float (&sn)[
 __device__ __forceinline__ void load_chunks(const uint16_t* p, const LanePlan& plan, float (&v)[2][8]) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] = 0.f;
-        if (plan.at[c] >= 0) unpack(*reinterpret_cast<const uint4*>(p + plan.at[c]), v[c]);
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (plan.at[c] >= 0) raw = *reinterpret_cast<const uint4*>(p + plan.at[c]);
+        unpack(raw, v[c]);
     }
 }
 __device__ __forceinline__ void store_chunks(uint16_t* p, const LanePlan& plan, const float (&v)[2][8]) {
 #pragma unroll
     for (int c = 0; c < 2; ++c)
         if (plan.at[c] >= 0) *reinterpret_cast<uint4*>(p + plan.at[c]) = pack(v[c]);
+}
+__device__ __forceinline__ void load_weights(const uint16_t* p, const LanePlan& plan, float (&w)[2][8]) {
+    if (p) {
+        load_chunks(p, plan, w);
+    } else {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[c][e] = 1.0f;
+    }
 }
 __device__ __forceinline__ float square_sum(const float (&v)[2][8]) {
     float s = 0.f;
@@ -137,143 +154,126 @@ __device__ __forceinline__ float square_sum(const float (&v)[2][8]) {
     return s;
 }
 
-// A wave takes one token and a.heads_per heads of it (those of q, then those of k), 64 / L at a time.
+// A wave takes one token and side.per heads of it, 64 / L at a time. The first side[0].groups workgroups have the heads of q, the others those of k.
 template <int L, bool HALVES>
 __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t task = (int64_t)blockIdx.x * kHeadWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t token = task / a.splits;
+    __shared__ float lds[kHeadWaves][2][kMostPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool is_k = blockIdx.x >= a.side[0].groups;
+    const HeadSide& side = a.side[is_k];
+    const uint32_t task = (blockIdx.x - (is_k ? a.side[0].groups : 0)) * kHeadWaves + wave, token = task / side.splits;
     if (token >= a.T) return;
-    const int heads = a.Hq + a.Hk, h0 = (int)(task % a.splits) * a.heads_per, h1 = min(h0 + a.heads_per, heads);
+    const int h0 = (int)(task % side.splits) * side.per, h1 = min(h0 + side.per, side.H);
     const LanePlan plan = lane_plan<HALVES>(lane % L, a.D, a.pairs);
-    float sn[8], cs[8], w[2][2][8];
-    lane_turns<HALVES>(a, plan, token, sn, cs);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const uint16_t* p = k ? a.wk : a.wq;
-        if (p) {
-            load_chunks(p, plan, w[k]);
-        } else {
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[k][c][e] = 1.0f;
-        }
-    }
+    const Turns turns = token_turns(a, plan, token, lds[wave]);
+    float w[2][8];
+    load_weights(side.w, plan, w);
+    const uint16_t* const in = side.in + token * side.ld;
+    uint16_t* const out = side.out + token * side.ldo;
     for (int h = h0 + lane / L; h < h1; h += 64 / L) {
-        const bool is_k = h >= a.Hq;
-        const uint16_t* from = is_k ? a.k + token * a.ldk + (h - a.Hq) * a.sk : a.q + token * a.ldq + h * a.sq;
-        uint16_t* to = is_k ? a.k_out + token * a.ldko + (h - a.Hq) * a.sko : a.q_out + token * a.ldqo + h * a.sqo;
         float v[2][8];
-        load_chunks(from, plan, v);
+        load_chunks(in + h * side.s, plan, v);
         if (a.norm) {
-            const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) / (float)a.D + a.eps);
+            const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) * (1.0f / (float)a.D) + a.eps);
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * r * (is_k ? w[1][c][e] : w[0][c][e]);
+                for (int e = 0; e < 8; ++e) v[c][e] *= r * w[c][e];
         }
-        apply_turns<HALVES, false>(v, sn, cs);
-        store_chunks(to, plan, v);
+        apply_turns<HALVES, false>(v, turns);
+        store_chunks(out + h * side.so, plan, v);
     }
 }
 
-// The same walk for the gradients; a wave goes on to further tokens, and what it has of the weights' gradients goes to the workspace at the end, a
+// The same walk for the gradients; a wave goes on to further tokens, and what it has of the weight's gradient goes to the workspace at the end, a
 // workgroup's four waves and a wave's 64 / L heads added up in order.
 template <int L, bool HALVES>
-__global__ __launch_bounds__(kHeadWaves * 64) void rotary_backward_kernel(const RotaryArgs a) {
-    __shared__ float part[kHeadWaves][2][L * 16];
+__global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(const RotaryArgs a) {
+    __shared__ float lds[kHeadWaves][2][kMostPairs];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int heads = a.Hq + a.Hk;
+    const bool is_k = blockIdx.x >= a.side[0].groups;
+    const HeadSide& side = a.side[is_k];
+    const uint32_t tasks = (uint32_t)a.T * side.splits;
     const LanePlan plan = lane_plan<HALVES>(lane % L, a.D, a.pairs);
-    float w[2][2][8], dw[2][2][8];
+    const float inv = 1.0f / (float)a.D;
+    float w[2][8], dw[2][8];
+    load_weights(side.w, plan, w);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const uint16_t* p = k ? a.wk : a.wq;
-        if (p) load_chunks(p, plan, w[k]);
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!p) w[k][c][e] = 1.0f;
-                dw[k][c][e] = 0.f;
-            }
-    }
-    const int64_t tasks = a.T * a.splits;
-    for (int64_t task = (int64_t)blockIdx.x * kHeadWaves + wave; task < tasks; task += (int64_t)gridDim.x * kHeadWaves) {
-        const int64_t token = task / a.splits;
-        const int h0 = (int)(task % a.splits) * a.heads_per, h1 = min(h0 + a.heads_per, heads);
-        float sn[8], cs[8];
-        lane_turns<HALVES>(a, plan, token, sn, cs);
+        for (int e = 0; e < 8; ++e) dw[c][e] = 0.f;
+    for (uint32_t task = (blockIdx.x - (is_k ? a.side[0].groups : 0)) * kHeadWaves + wave; task < tasks; task += side.groups * kHeadWaves) {
+        const uint32_t token = task / side.splits;
+        const int h0 = (int)(task % side.splits) * side.per, h1 = min(h0 + side.per, side.H);
+        const Turns turns = token_turns(a, plan, token, lds[wave]);
+        const uint16_t* const in = a.norm ? side.in + token * side.ld : nullptr;
+        const uint16_t* const grad = side.grad + token * side.ldg;
+        uint16_t* const out = side.out + token * side.ldo;
         for (int h = h0 + lane / L; h < h1; h += 64 / L) {
-            const bool is_k = h >= a.Hq;
-            const int64_t hk = h - a.Hq;
             float d[2][8];
-            load_chunks(is_k ? a.dk_out + token * a.lddko + hk * a.sdko : a.dq_out + token * a.lddqo + h * a.sdqo, plan, d);
-            apply_turns<HALVES, true>(d, sn, cs);
+            load_chunks(grad + h * side.sg, plan, d);
             if (a.norm) {
                 float v[2][8];
-                load_chunks(is_k ? a.k + token * a.ldk + hk * a.sk : a.q + token * a.ldq + h * a.sq, plan, v);
-                const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) / (float)a.D + a.eps);
+                load_chunks(in + h * side.s, plan, v);
+                apply_turns<HALVES, true>(d, turns);
+                const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) * inv + a.eps);
                 float m = 0.f;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         v[c][e] *= r;
-                        const float dn = d[c][e] * v[c][e];
-                        if (is_k) dw[1][c][e] += dn;
-                        else dw[0][c][e] += dn;
-                        d[c][e] *= is_k ? w[1][c][e] : w[0][c][e];
+                        dw[c][e] += d[c][e] * v[c][e];
+                        d[c][e] *= w[c][e];
                         m += d[c][e] * v[c][e];
                     }
-                m = head_sum<L>(m) / (float)a.D;
+                m = head_sum<L>(m) * inv;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[c][e] = r * (d[c][e] - v[c][e] * m);
+            } else {
+                apply_turns<HALVES, true>(d, turns);
             }
-            store_chunks(is_k ? a.dk + token * a.lddk + hk * a.sdk : a.dq + token * a.lddq + h * a.sdq, plan, d);
+            store_chunks(out + h * side.so, plan, d);
         }
     }
-    if (!a.sums) return;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float s = dw[k][c][e];
-#pragma unroll
-                for (int step = L; step < 64; step *= 2) s += __shfl_xor(s, step);
-                if (lane < L && plan.at[c] >= 0) part[wave][k][plan.at[c] + e] = s;
-            }
+    if (!side.sums) return;
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.D; i += kHeadWaves * 64) {
-        const int k = i / a.D, col = i % a.D;
-        float s = part[0][k][col];
+    float (*const part)[L * 16] = reinterpret_cast<float (*)[L * 16]>(&lds[0][0][0]);
+    static_assert(kHeadWaves * L * 16 <= kHeadWaves * 2 * kMostPairs, "the waves' sums fit");
 #pragma unroll
-        for (int v = 1; v < kHeadWaves; ++v) s += part[v][k][col];
-        a.sums[(int64_t)blockIdx.x * 2 * a.D + i] = s;
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float s = dw[c][e];
+#pragma unroll
+            for (int step = L; step < 64; step *= 2) s += __shfl_xor(s, step);
+            if (lane < L && plan.at[c] >= 0) part[wave][plan.at[c] + e] = s;
+        }
+    __syncthreads();
+    float* const to = side.sums + (int64_t)(blockIdx.x - (is_k ? a.side[0].groups : 0)) * a.D;
+    for (int i = threadIdx.x; i < a.D; i += kHeadWaves * 64) {
+        float s = part[0][i];
+#pragma unroll
+        for (int v = 1; v < kHeadWaves; ++v) s += part[v][i];
+        to[i] = s;
     }
 }
 
-// The workgroups' sums, 16 columns to a workgroup, dealt to its 16 lane groups in turn and those added in order.
-__global__ __launch_bounds__(256) void rotary_reduce_kernel(const RotaryArgs a, const int groups) {
-    __shared__ float part[16][16];
+// The workgroups' sums of a side (blockIdx.y), 16 columns to a workgroup, dealt to its 64 groups of 16 lanes in turn and those added in order.
+__global__ __launch_bounds__(1024) void rotary_reduce_kernel(const RotaryArgs a) {
+    __shared__ float part[64][16];
+    const HeadSide& side = a.side[blockIdx.y];
     const int i = blockIdx.x * 16 + (threadIdx.x & 15), g = threadIdx.x >> 4;
     float s = 0.f;
-    if (i < 2 * a.D)
-        for (int b = g; b < groups; b += 16) s += a.sums[(int64_t)b * 2 * a.D + i];
+    if (i < a.D && side.dw)
+        for (uint32_t b = g; b < side.groups; b += 64) s += side.sums[(int64_t)b * a.D + i];
     part[g][threadIdx.x & 15] = s;
     __syncthreads();
-    if (g != 0 || i >= 2 * a.D) return;
-    for (int v = 1; v < 16; ++v) s += part[v][threadIdx.x & 15];
-    if (i < a.D) {
-        if (a.dwq) a.dwq[i] = s;
-    } else if (a.dwk) {
-        a.dwk[i - a.D] = s;
-    }
+    if (g != 0 || i >= a.D || !side.dw) return;
+    for (int v = 1; v < 64; ++v) s += part[v][threadIdx.x & 15];
+    side.dw[i] = s;
 }
 
 // f(lanes of a head)
@@ -286,52 +286,79 @@ hipError_t with_lanes(int D, F f) {
     return f(integral_constant<int, 32>{});
 }
 
-constexpr int64_t kBackwardGroups = 1024;    // workgroups of the backward pass at most
+// Deals the heads of a side to waves: a task is a token and `per` of its heads. `waves` run at a time; a task costs about .7 of an iteration over 64 / L heads
+// besides its iterations, and the last round of tasks counts in full.
+void deal(HeadSide& side, int64_t T, int step, int64_t waves) {
+    const int most = (side.H + step - 1) / step;
+    double best = 0;
+    for (int splits = 1; splits <= most; splits += 1 + splits / 16) {
+        const int per = (most + splits - 1) / splits;
+        const int64_t n = (most + per - 1) / per, rounds = (T * n + waves - 1) / waves;
+        if (splits > 1 && T * n > (int64_t)1 << 25) break;             // (a launch takes fewer than 2^32 threads)
+        const double time = (double)rounds * (per + 0.7);
+        if (splits == 1 || time < best) {
+            best = time;
+            side.per = per * step;
+            side.splits = (int)n;
+        }
+    }
+}
 
-// Heads of a wave: all of a token's, fewer while there are not enough tokens to fill the chip with waves.
-void deal_heads(RotaryArgs& a, int lanes) {
-    const int heads = a.Hq + a.Hk, step = 64 / lanes;
-    int per = (heads + step - 1) / step;
-    while (per > 1 && a.T * ((heads + per * step - 1) / (per * step)) < 4096) per = (per + 1) / 2;
-    a.heads_per = per * step;
-    a.splits = (heads + a.heads_per - 1) / a.heads_per;
+constexpr int64_t kGroups = 1024;            // workgroups that the chip holds at a time, and of the backward pass at most
+
+// One side's share of them.
+int64_t share(const RotaryArgs& a, int i) {
+    const int64_t n = kGroups * a.side[i].H / (a.side[0].H + a.side[1].H);
+    return n > 0 ? n : 1;
 }
 
 }  // namespace
 
-size_t rotary_backward_scratch(int64_t D) { return (size_t)kBackwardGroups * 2 * (size_t)D * sizeof(float); }
+size_t rotary_backward_scratch(int64_t D) { return (size_t)(kGroups + 2) * (size_t)D * sizeof(float); }
 
 hipError_t launch_rotary(const RotaryArgs& a_in, hipStream_t stream) {
     return with_lanes(a_in.D, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         RotaryArgs a = a_in;
-        deal_heads(a, L);
-        const dim3 grid((unsigned)((a.T * a.splits + kHeadWaves - 1) / kHeadWaves)), block(kHeadWaves * 64);
+        for (int i = 0; i < 2; ++i) {
+            HeadSide& side = a.side[i];
+            side.splits = 1;
+            if (side.H > 0) deal(side, a.T, 64 / L, share(a, i) * kHeadWaves);
+            side.groups = side.H > 0 ? (unsigned)((a.T * side.splits + kHeadWaves - 1) / kHeadWaves) : 0;
+        }
+        const dim3 grid(a.side[0].groups + a.side[1].groups), block(kHeadWaves * 64);
         if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<L, false>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((rotary_kernel<L, true>), grid, block, 0, stream, a);
         return hipGetLastError();
     });
 }
 
-hipError_t launch_rotary_backward(const RotaryArgs& a_in, hipStream_t stream) {
-    int64_t groups = 0;
-    hipError_t e = with_lanes(a_in.D, [&](auto lanes) {
+hipError_t launch_rotary_backward(const RotaryArgs& a_in, float* sums, hipStream_t stream) {
+    return with_lanes(a_in.D, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         RotaryArgs a = a_in;
-        deal_heads(a, L);
-        groups = (a.T * a.splits + kHeadWaves - 1) / kHeadWaves;
-        if (groups > kBackwardGroups) groups = kBackwardGroups;
-        const dim3 grid((unsigned)groups), block(kHeadWaves * 64);
-        if (groups == 0) return hipSuccess;
-        if (a.interleaved) hipLaunchKernelGGL((rotary_backward_kernel<L, false>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((rotary_backward_kernel<L, true>), grid, block, 0, stream, a);
+        for (int i = 0; i < 2; ++i) {
+            HeadSide& side = a.side[i];
+            side.groups = 0;
+            side.splits = 1;
+            if (side.H > 0 && a.T > 0) {
+                const int64_t most = share(a, i);
+                deal(side, a.T, 64 / L, most * kHeadWaves);
+                const int64_t groups = (a.T * side.splits + kHeadWaves - 1) / kHeadWaves;
+                side.groups = (unsigned)(groups < most ? groups : most);
+            }
+            if (side.dw) side.sums = sums + (i ? (int64_t)a.side[0].groups * a.D : 0);
+        }
+        const unsigned groups = a.side[0].groups + a.side[1].groups;
+        if (groups > 0) {
+            if (a.interleaved) hipLaunchKernelGGL((rotary_backward_kernel<L, false>), dim3(groups), dim3(kHeadWaves * 64), 0, stream, a);
+            else hipLaunchKernelGGL((rotary_backward_kernel<L, true>), dim3(groups), dim3(kHeadWaves * 64), 0, stream, a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (a.side[0].dw || a.side[1].dw) hipLaunchKernelGGL(rotary_reduce_kernel, dim3((unsigned)((a.D + 15) / 16), 2), dim3(1024), 0, stream, a);
         return hipGetLastError();
     });
-    if (e == hipSuccess && a_in.sums) {
-        hipLaunchKernelGGL(rotary_reduce_kernel, dim3((unsigned)((2 * a_in.D + 15) / 16)), dim3(256), 0, stream, a_in, (int)groups);
-        e = hipGetLastError();
-    }
-    return e;
 }
 
 hipError_t prepare_rotary_kernels() {

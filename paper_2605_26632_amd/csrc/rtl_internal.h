@@ -205,6 +205,14 @@ hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_
 
 // ---- gated linears (gated.hip) -------------------------------------------------------------------
 // a: A, lda, W (2 N rows), bias, Y, ldy, M, N, K, P, ldp, act.
+// The form of the tile loop that a launch takes (gemm.hip, host arithmetic): a small tile by its index there, or -1 for the 256-row plan of 2 F rows of W.
+struct GatedForm {
+    int shape;
+    bool use_192;
+    int64_t m_split;
+    int body_tiles, tail_tiles;
+};
+GatedForm gated_form(int64_t M, int64_t F, int64_t K);
 hipError_t prepare_gated_kernels();
 hipError_t launch_gated(const GemmArgs& a, hipStream_t stream);
 struct GatedGradArgs {
@@ -240,32 +248,39 @@ struct NormGradArgs {
     int post, pre;
     float alpha, eps;
     bool x_f32, clear;
-    float *sums, *totals;   // residual_norm_backward_slots(T, S) x 3 D, S x 2 D
-    int rows;               // filled in by the launch
+    float *sums, *totals;   // residual_norm_backward_slots(T, S, D) x 3 D, S x 2 D
+    int rows, waves;        // filled in by the launch
 };
 hipError_t prepare_norm_kernels();
 hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream);
-size_t residual_norm_backward_slots(int64_t T, int64_t S);
+size_t residual_norm_backward_slots(int64_t T, int64_t S, int64_t D);
 hipError_t launch_residual_norm_backward(const NormGradArgs& a, hipStream_t stream);
 
 // ---- head norm and rotary positions (rotary.hip) --------------------------------------------------------
-// Strides in elements: ld* between tokens, s* between heads.
+// q or k. Strides in elements: ld* between tokens, s* between heads.
+struct HeadSide {
+    const uint16_t *in, *w, *grad;      // in: not read in the backward pass without a norm; w nullable; grad: backward pass
+    uint16_t* out;                      // the result, or the gradient of `in`
+    float *dw, *sums;                   // nullable; sums is filled in by the launch
+    int64_t ld, s, ldo, so, ldg, sg;
+    int H;
+    int per, splits;                    // filled in by the launches: heads of a wave, tasks of a token, workgroups
+    unsigned groups;
+};
 struct RotaryArgs {
-    const uint16_t *q, *k, *wq, *wk, *dq_out, *dk_out;
-    uint16_t *q_out, *k_out, *dq, *dk;
+    HeadSide side[2];
     const float *pos, *freq;
     const int* axis;
-    float *dwq, *dwk, *sums;
-    int64_t T, ldq, sq, ldk, sk, ldqo, sqo, ldko, sko, lddqo, sdqo, lddko, sdko, lddq, sdq, lddk, sdk;
-    int Hq, Hk, D, pairs, axes;
+    int64_t T;
+    int D, pairs, axes;
     float eps;
     bool norm, interleaved;
-    int heads_per, splits;  // filled in by the launches
 };
 hipError_t prepare_rotary_kernels();
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);
 size_t rotary_backward_scratch(int64_t D);
-hipError_t launch_rotary_backward(const RotaryArgs& a, hipStream_t stream);
+// sums: rotary_backward_scratch(D) bytes where a side has dw
+hipError_t launch_rotary_backward(const RotaryArgs& a, float* sums, hipStream_t stream);
 
 // ---- diagnostics (diag.hip) -------------------------------------------------------------------
 // Issue-rate probe: `blocks` workgroups of four waves, each wave issuing 4 * iters matrix
