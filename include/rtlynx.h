@@ -380,7 +380,7 @@ rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const
  *   [dG dU] is rounded to bf16 for the products, whose sums are fp32. dW [2F, K] (lddw) and dbias [2F] of type dw_type.
  *   F % 4 == 0, F <= 2^21, K % 8 == 0; X, W, dX, dW 16-byte aligned with strides % 8 == 0, at most 2^22; dH (lddh), P, H (ldh) 2-byte aligned. M == 0
  *   writes dW and dbias as zeros; an empty contraction (K == 0, F == 0 with a dX that is not empty) is RTL_ERR_SHAPE.
- *   workspace  rtl_gated_linear_backward_workspace(M, F, K) bytes, 256-byte aligned; what lies behind its first 256 + 4 M F bytes (rounded up to 256) is
+ *   workspace  rtl_gated_linear_backward_workspace(M, F, K) bytes, 256-byte aligned; what lies behind its first 4 M F bytes (rounded up to 256) is
  *              optional, as for rtl_grouped_linear_wgrad.
  * ------------------------------------------------------------------------------------------- */
 typedef enum { RTL_ACT_SILU = 0, RTL_ACT_GELU = 1, RTL_ACT_GELU_TANH = 2 } rtl_act;

@@ -736,14 +736,16 @@ def _residual_type(t, name):
     return t.dtype
 
 
-def _rows_of(t, T, D, dtype, name):
-    """Row stride of a [T, D] matrix; 0 for None."""
+def _rows_of(t, shape, dtype, name):
+    """Row stride of a matrix of this shape; 0 for None."""
     if t is None:
         return 0
-    rows, cols, ld = _matrix(t, dtype, name)
-    if rows != T or cols != D:
-        raise ValueError("%s: shape (%d, %d) expected" % (name, T, D))
-    return ld
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError("%s: %s matrix of shape %s expected" % (name, dtype, tuple(shape)))
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError("%s: contiguous rows expected" % name)
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _sequences(offsets):
@@ -755,9 +757,8 @@ def _sequences(offsets):
     return offsets.numel() - 1
 
 
-def _modulation(scale, shift, S, D):
-    bf = torch.bfloat16
-    a, b = _rows_of(scale, S, D, bf, "scale"), _rows_of(shift, S, D, bf, "shift")
+def _modulation(scale, shift, shape):
+    a, b = _rows_of(scale, shape, torch.bfloat16, "scale"), _rows_of(shift, shape, torch.bfloat16, "shift")
     if scale is not None and shift is not None and a != b:
         raise ValueError("scale and shift differ in their row stride")
     return a or b
@@ -773,16 +774,16 @@ def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shi
     dev = _here(x, y, gate, w_post, w_pre, scale, shift, offsets, xo, h)
     kind, S = _residual_type(x, "x"), _sequences(offsets)
     T, D, ldx = _matrix(x, kind, "x")
-    bf = torch.bfloat16
-    ldy, ld_gate, ld_mod = _rows_of(y, T, D, bf, "y"), _rows_of(gate, S, D, bf, "gate"), _modulation(scale, shift, S, D)
+    bf, rows, vectors = torch.bfloat16, (T, D), (S, D)
+    ldy, ld_gate, ld_mod = _rows_of(y, rows, bf, "y"), _rows_of(gate, vectors, bf, "gate"), _modulation(scale, shift, vectors)
     _whole(w_post, (D,), bf, "w_post")
     _whole(w_pre, (D,), bf, "w_pre")
     if out is None:
-        xo = torch.empty((T, D), dtype=kind, device=x.device) if with_x else None
-        h = torch.empty((T, D), dtype=bf, device=x.device) if with_h else None
+        xo = torch.empty(rows, dtype=kind, device=x.device) if with_x else None
+        h = torch.empty(rows, dtype=bf, device=x.device) if with_h else None
     st = lib().rtl_residual_norm(_p(x), _p(y), _p(gate), _p(w_post), _p(w_pre), _p(scale), _p(shift), _p(offsets), _p(xo), _p(h),
-                                 1 if kind is torch.float32 else 0, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps, out is None,
-                                 T, S, D, ldx, ldy, ld_gate, ld_mod, _rows_of(xo, T, D, kind, "x'"), _rows_of(h, T, D, bf, "h"), _on(dev))
+                                 kind is torch.float32, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps, out is None,
+                                 T, S, D, ldx, ldy, ld_gate, ld_mod, _rows_of(xo, rows, kind, "x'"), _rows_of(h, rows, bf, "h"), _on(dev))
     _check(st, "rtl_residual_norm")
     return xo, h
 
@@ -803,27 +804,29 @@ def residual_norm_backward(dx_out, dh, x_out, y=None, gate=None, w_post=None, w_
         raise ValueError("x' or its gradient expected")
     kind, S = _residual_type(like, "x'"), _sequences(offsets)
     T, D, _ = _matrix(like, kind, "x'")
-    bf, f32 = torch.bfloat16, torch.float32
-    strides = (_rows_of(dx_out, T, D, kind, "dx_out"), _rows_of(dh, T, D, bf, "dh"), _rows_of(x_out, T, D, kind, "x'"), _rows_of(y, T, D, bf, "y"),
-               _rows_of(gate, S, D, bf, "gate"), _rows_of(scale, S, D, bf, "scale"))
+    bf, f32, rows, vectors = torch.bfloat16, torch.float32, (T, D), (S, D)
+    lds = (_rows_of(dx_out, rows, kind, "dx_out"), _rows_of(dh, rows, bf, "dh"), _rows_of(x_out, rows, kind, "x'"), _rows_of(y, rows, bf, "y"),
+           _rows_of(gate, vectors, bf, "gate"), _rows_of(scale, vectors, bf, "scale"))
     _whole(w_post, (D,), bf, "w_post")
     _whole(w_pre, (D,), bf, "w_pre")
     if out is None:
-        def new(wanted, dtype, *shape):
+        def new(wanted, dtype, shape):
             return torch.empty(shape, dtype=dtype, device=like.device) if wanted else None
         shift = scale is not None if with_shift is None else with_shift
-        got = [new(True, kind, T, D), new(y is not None, bf, T, D), new(y is not None and gate is not None, f32, S, D), new(scale is not None, f32, S, D),
-               new(shift, f32, S, D), new(y is not None and w_post is not None, f32, D), new(w_pre is not None, f32, D)]
+        got = [new(True, kind, rows), new(y is not None, bf, rows), new(y is not None and gate is not None, f32, vectors), new(scale is not None, f32, vectors),
+               new(shift, f32, vectors), new(y is not None and w_post is not None, f32, (D,)), new(w_pre is not None, f32, (D,))]
     dx, dy, dgate, dscale, dshift, dw_post, dw_pre = got
-    for t, shape, name in ((dgate, (S, D), "dgate"), (dscale, (S, D), "dscale"), (dshift, (S, D), "dshift"), (dw_post, (D,), "dw_post"), (dw_pre, (D,), "dw_pre")):
-        _whole(t, shape, f32, name)
+    if out is not None:
+        for t, shape, name in ((dgate, vectors, "dgate"), (dscale, vectors, "dscale"), (dshift, vectors, "dshift"), (dw_post, (D,), "dw_post"),
+                               (dw_pre, (D,), "dw_pre")):
+            _whole(t, shape, f32, name)
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_residual_norm_backward_workspace(T, S, D), like.device)
     st = L.rtl_residual_norm_backward(_p(dx_out), _p(dh), _p(x_out), _p(y), _p(gate), _p(w_post), _p(w_pre), _p(scale), _p(offsets), _p(dx), _p(dy),
-                                      _p(dgate), _p(dscale), _p(dshift), _p(dw_post), _p(dw_pre), 1 if kind is f32 else 0, _choice(NORM, post, "post"),
-                                      _choice(NORM, pre, "pre"), alpha, eps, out is None, T, S, D, *strides, _rows_of(dx, T, D, kind, "dx"),
-                                      _rows_of(dy, T, D, bf, "dy"), _p(ws), _bytes(ws), _on(dev))
+                                      _p(dgate), _p(dscale), _p(dshift), _p(dw_post), _p(dw_pre), kind is f32, _choice(NORM, post, "post"),
+                                      _choice(NORM, pre, "pre"), alpha, eps, out is None, T, S, D, *lds, _rows_of(dx, rows, kind, "dx"),
+                                      _rows_of(dy, rows, bf, "dy"), _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_residual_norm_backward")
     return tuple(got)
 
@@ -837,12 +840,12 @@ def _heads(t, T, D, name, H=None):
     stride = t.stride()
     if len(stride) != 3 or t.dtype is not torch.bfloat16:
         raise ValueError("%s: bf16 tensor of shape [T, heads, D] expected" % name)
-    rows, heads, cols = t.shape
-    if rows != T or cols != D or (H is not None and heads != H):
+    shape = t.shape
+    if shape[0] != T or shape[2] != D or (H is not None and shape[1] != H):
         raise ValueError("%s: shape (%d, %s, %d) expected" % (name, T, "heads" if H is None else H, D))
     if stride[2] != 1:
         raise ValueError("%s: contiguous heads expected" % name)
-    return heads, stride[0], stride[1]
+    return shape[1], stride[0], stride[1]
 
 
 def _rotation(pos, freq, axis, T):

@@ -848,11 +848,11 @@ rtl_status rtl_gated_linear(const void* X, const void* W, const void* bias, void
     return rtl::launch_gated(g, static_cast<hipStream_t>(stream)) == hipSuccess ? RTL_OK : RTL_ERR_HIP;
 }
 
-// rtl_gated_linear_backward workspace: [offsets of the products | dG, dU | the weight gradient's partial planes]
-static size_t gated_backward_ws(int64_t M, int64_t F) { return 256 + round_up((size_t)M * (size_t)F * 4, 256); }
+// rtl_gated_linear_backward workspace: [dG, dU | the weight gradient's partial planes]
+static size_t gated_backward_ws(int64_t M, int64_t F) { return round_up((size_t)M * (size_t)F * 4, 256); }
 size_t rtl_gated_linear_backward_workspace(int64_t M, int64_t F, int64_t K) {
     if (M < 0 || F <= 0 || K <= 0) return 0;
-    return gated_backward_ws(M, F) + rtl_grouped_linear_wgrad_workspace(M, 1, 2 * F, K);
+    return gated_backward_ws(M, F) + rtl::grad_pair_workspace(M, 2 * F, K, (size_t)RTL_STATIC_SCRATCH_BYTES);
 }
 
 rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* W, const void* P, void* dX, void* dW, void* dbias, void* H, rtl_act act,
@@ -868,8 +868,7 @@ rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* 
     const size_t need = gated_backward_ws(M, F);
     size_t room = workspace_bytes > need ? workspace_bytes - need : 0;
     if (room > (size_t)RTL_STATIC_SCRATCH_BYTES) room = (size_t)RTL_STATIC_SCRATCH_BYTES;
-    if (rtl::gated_grad_grid(M, F) >= rtl::kMaxGroupGrid || (dX && M > 0 && rtl::dgrad_grid(M, 1, 2 * F, K) >= rtl::kMaxGroupGrid) ||
-        (dW && rtl::wgrad_grid(M, 1, 2 * F, K, room) >= rtl::kMaxGroupGrid))
+    if (rtl::gated_grad_grid(M, F) >= rtl::kMaxGroupGrid || ((dX || dW) && rtl::grad_pair_grid(M, 2 * F, K, dX != nullptr, dW != nullptr, room) >= rtl::kMaxGroupGrid))
         return RTL_ERR_SHAPE;
     if (M == 0 && !dW && !dbias) return RTL_OK;
     if ((M > 0 && (!dH || !P)) || (dbias && !dW) || (dX && M > 0 && !W) || (dW && M > 0 && !X)) return RTL_ERR_NULL;
@@ -877,7 +876,7 @@ rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* 
     if (dX && (ldw % 8 != 0 || lddx % 8 != 0 || !aligned(W, 16) || !aligned(dX, 16))) return RTL_ERR_ALIGN;
     if (dW && (ldx % 8 != 0 || lddw % 8 != 0 || !aligned(X, 16) || !aligned(dW, 16) || (dbias && !aligned(dbias, dw_type == RTL_F32 ? 4 : 2))))
         return RTL_ERR_ALIGN;
-    if (!workspace || workspace_bytes < need) return RTL_ERR_WORKSPACE;
+    if (M > 0 && (!workspace || workspace_bytes < need)) return RTL_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return RTL_ERR_ALIGN;
     RTL_REQUIRE_DEVICE();
     uint8_t* const base = static_cast<uint8_t*>(workspace);
@@ -885,30 +884,22 @@ rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* 
     rtl::GatedGradArgs e{};
     e.dH = static_cast<const uint16_t*>(dH);
     e.P = static_cast<const uint16_t*>(P);
-    e.dP = reinterpret_cast<uint16_t*>(base + 256);
+    e.dP = reinterpret_cast<uint16_t*>(base);
     e.H = static_cast<uint16_t*>(H);
-    e.offsets = reinterpret_cast<int*>(base);
     e.M = M; e.F = F; e.lddh = lddh; e.ldp = ldp; e.lddp = 2 * F; e.ldh = ldh;
     e.act = act;
     if (rtl::launch_gated_grad(e, s) != hipSuccess) return RTL_ERR_HIP;
-    rtl::GroupedGradArgs g{};
-    g.offsets = e.offsets;
-    g.experts = 1;
-    g.dY = e.dP;
-    g.T = M; g.N = 2 * F; g.K = K; g.lddy = 2 * F;
-    if (dX && M > 0) {
+    if (dX || dW) {
+        rtl::GroupedGradArgs g{};
+        g.experts = 1;
+        g.dY = e.dP;
         g.W = static_cast<const uint16_t*>(W);
-        g.out = dX;
-        g.ldw = ldw; g.ldo = lddx;
-        if (rtl::launch_grouped_dgrad(g, s) != hipSuccess) return RTL_ERR_HIP;
-    }
-    if (dW) {
         g.X = static_cast<const uint16_t*>(X);
         g.out = dW;
         g.bias_out = dbias;
         g.f32 = dw_type == RTL_F32;
-        g.ldx = ldx; g.ldo = lddw;
-        if (rtl::launch_grouped_wgrad(g, room ? base + need : nullptr, room, s) != hipSuccess) return RTL_ERR_HIP;
+        g.T = M; g.N = 2 * F; g.K = K; g.lddy = 2 * F; g.ldw = ldw; g.ldx = ldx; g.ldo = lddw;
+        if (rtl::launch_grad_pair(g, M > 0 ? dX : nullptr, lddx, room ? base + need : nullptr, room, s) != hipSuccess) return RTL_ERR_HIP;
     }
     return RTL_OK;
 }

@@ -1,5 +1,5 @@
 // Gated linears: H = act(X Wg^T + bg) (X Wu^T + bu) in one kernel, on the dense tile loop (gemm_tile.h, MODE 2), and the elementwise part of their
-// backward pass; its products are those of the linears grouped by expert, with one expert.
+// backward pass; its products are one launch of the weight and input gradient's tiles (grouped_grad.hip).
 #include "gemm_tile.h"
 
 namespace rtl {
@@ -134,12 +134,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void gated_few_rows_kernel(const Ge
 }
 
 // dP = [dH U act'(G), dH act(G)] and, with H set, H = act(G) U again. Eight columns to a thread, F a multiple of four, rows of any 8-byte alignment. Bound by
-// memory: five or six values of two bytes per element of H. dP is rounded to bf16, the type that the matrix cores take in the products behind it. The
-// workspace's two offsets for those products, all rows for the one expert, are written on the way.
+// memory: five or six values of two bytes per element of H. dP is rounded to bf16, the type that the matrix cores take in the products behind it.
 constexpr int kGradThreads = 256;
 template <bool ERF>
 __global__ __launch_bounds__(kGradThreads) void gated_grad_kernel(const GatedGradArgs a) {
-    if (a.offsets && blockIdx.x == 0 && threadIdx.x < 2) a.offsets[threadIdx.x] = threadIdx.x ? (int)a.M : 0;
     const int runs = (int)((a.F + 7) / 8);
     const int64_t first = (int64_t)blockIdx.x * kGradThreads, row0 = first / runs;
     const int q = (int)(first - row0 * runs) + (int)threadIdx.x;
@@ -209,7 +207,8 @@ hipError_t launch_gated(const GemmArgs& a_in, hipStream_t stream) {
 int64_t gated_grad_grid(int64_t M, int64_t F) { return (M * ((F + 7) / 8) + kGradThreads - 1) / kGradThreads; }
 hipError_t launch_gated_grad(const GatedGradArgs& a, hipStream_t stream) {
     const int64_t grid = gated_grad_grid(a.M, a.F);
-    const dim3 g((unsigned)(grid > 0 ? grid : 1));
+    if (grid == 0) return hipSuccess;
+    const dim3 g((unsigned)grid);
     if (a.act == RTL_ACT_GELU) hipLaunchKernelGGL(gated_grad_kernel<true>, g, dim3(kGradThreads), 0, stream, a);
     else hipLaunchKernelGGL(gated_grad_kernel<false>, g, dim3(kGradThreads), 0, stream, a);
     return hipGetLastError();

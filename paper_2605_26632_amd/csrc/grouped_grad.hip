@@ -14,6 +14,7 @@
 // of loaded (on both sides: what lies in memory behind an expert's rows may be NaN), at no cost to the loop.
 // 8192 rows, [4096, 2048], eight experts, inputs that change: input gradient 122 us with 1024 rows each, 161 with 484 to 1997 (216 tall and 104 half
 // tiles: the units are active 65 % of the launch); weight gradient 141 and 143. Matrix cores busy 42 and 43 % at 2.18 GHz, uneven.
+#include <cmath>
 #include "groups.h"
 
 namespace rtl {
@@ -432,6 +433,96 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
     grad_tile<true, F32, BM, BN, WAVES_M, WAVES_N, STAGES>(g, (int64_t)pm * BM, (int64_t)pn * BN, part, a.parts);
 }
 
+// Both gradients of one linear in one launch: the tiles of the longer contraction first, then the others, each workgroup to the unit that frees first. One
+// after the other, each of the two would end with units idle: a gated linear's [4096, 2 x 8192, 2048] has 128 tiles of 256 x 256 in dX, of 256 stages
+// each, and 512 in dW, of 64; 128 units with a tile of dX each and four of dW on each of the others end together.
+struct PairArgs {
+    GradArgs d, w;           // input and weight gradient
+    int nd, nw, parts;       // tiles of each, those of dW in each of `parts` parts of its contraction
+    int64_t w_plane, sums_plane;      // elements between the parts' planes
+    bool w_first;
+};
+template <bool F32, int DM, int WM, int BN, int THREADS>
+__global__ __launch_bounds__(THREADS) void grad_pair_kernel(const PairArgs a) {
+    constexpr bool BIG = THREADS == 512;
+    const int all_w = a.nw * a.parts, pad_d = (a.nd + 7) / 8 * 8, pad_w = (all_w + 7) / 8 * 8;
+    int id = (int)blockIdx.x;
+    const int lead = a.w_first ? pad_w : pad_d;
+    const bool is_w = (id < lead) == a.w_first;
+    if (id >= lead) id -= lead;
+    const int n = is_w ? all_w : a.nd, xcd = id % 8, t = xcd_share_start(n, xcd) + id / 8;       // an XCD's share: neighbouring tiles
+    if (t >= xcd_share_start(n, xcd + 1)) return;
+    int pm, pn;
+    if (is_w) {
+        const int part = t / a.nw;
+        GradArgs g = a.w;
+        if constexpr (F32) {
+            g.C = static_cast<float*>(g.C) + part * a.w_plane;
+            if (g.row_sums) g.row_sums = static_cast<float*>(g.row_sums) + part * a.sums_plane;
+        }
+        tile_walk<8>(t % a.nw, (int)((g.m + WM - 1) / WM), (int)((g.n + BN - 1) / BN), pm, pn);
+        if constexpr (!BIG) grad_tile<true, F32, WM, BN, 2, 2, 4>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.parts);
+        else grad_tile<true, F32, WM, BN, 2, 4, WM == 256 ? 2 : 3>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.parts);
+    } else {
+        tile_walk<(DM >= 256 ? 8 : 16)>(t, (int)((a.d.m + DM - 1) / DM), (int)((a.d.n + BN - 1) / BN), pm, pn);
+        if constexpr (!BIG) grad_tile<false, false, DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, 4>(a.d, (int64_t)pm * DM, (int64_t)pn * BN);
+        else grad_tile<false, false, DM, BN, 2, 4, DM == 256 ? 2 : 3>(a.d, (int64_t)pm * DM, (int64_t)pn * BN);
+    }
+}
+
+template <int DM, int WM, int BN, int THREADS>
+struct Pair {
+    static constexpr bool kBig = THREADS == 512;
+    using LD = std::conditional_t<kBig, GradSmem<DM, BN, 2, 4, DM == 256 ? 2 : 3>, GradSmem<DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, 4>>;
+    using LW = std::conditional_t<kBig, GradSmem<WM, BN, 2, 4, WM == 256 ? 2 : 3>, GradSmem<WM, BN, 2, 2, 4>>;
+    static constexpr int kLds = LD::kTotal > LW::kTotal ? LD::kTotal : LW::kTotal;
+    static hipError_t prepare() {
+        auto limit = [](const void* k) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds); };
+        const hipError_t e = limit(reinterpret_cast<const void*>(grad_pair_kernel<false, DM, WM, BN, THREADS>));
+        return e != hipSuccess ? e : limit(reinterpret_cast<const void*>(grad_pair_kernel<true, DM, WM, BN, THREADS>));
+    }
+    static hipError_t launch(const PairArgs& a, bool f32, hipStream_t stream) {
+        const dim3 grid((unsigned)((a.nd + 7) / 8 * 8 + (a.nw * a.parts + 7) / 8 * 8)), block(THREADS);
+        if (f32) hipLaunchKernelGGL((grad_pair_kernel<true, DM, WM, BN, THREADS>), grid, block, kLds, stream, a);
+        else hipLaunchKernelGGL((grad_pair_kernel<false, DM, WM, BN, THREADS>), grid, block, kLds, stream, a);
+        return hipGetLastError();
+    }
+};
+template <class Op>
+hipError_t with_pair(int form, Op op) {
+    switch (form) {
+        case 0: return op(Pair<64, 128, 128, 256>{});
+        case 1: return op(Pair<128, 128, 128, 256>{});
+        case 2: return op(Pair<128, 128, 256, 512>{});
+        case 3: return op(Pair<128, 256, 256, 512>{});
+        case 4: return op(Pair<256, 128, 256, 512>{});
+        default: return op(Pair<256, 256, 256, 512>{});
+    }
+}
+constexpr int kPairForms = 6;
+struct PairShape {
+    int dm, wm, bn;
+    double d_fixed, d_stage, w_fixed, w_stage;       // us of a tile with every unit at work (dgrad_shape, wgrad_plan)
+};
+constexpr PairShape kPairShapes[kPairForms] = {{64, 128, 128, 3.8, 0.305, 4.8, 0.53}, {128, 128, 128, 4.8, 0.53, 4.8, 0.53}, {128, 128, 256, 8, 0.78, 8, 0.78},
+                                               {128, 256, 256, 8, 0.78, 9, 1.5},      {256, 128, 256, 8, 1.5, 8, 0.78},      {256, 256, 256, 8, 1.5, 9, 1.5}};
+
+// End of n1 tiles of t1 and then n2 of t2, each to the unit that frees first (as mixed_time; t1 >= t2).
+double pair_time(int64_t n1, double t1, int64_t n2, double t2) {
+    const int64_t x = n1 % kUnits;
+    const double a = (double)(n1 / kUnits) * t1, b = x ? a + t1 : a;                 // when the units are done with the first, x of them at b
+    if (n2 == 0) return b;
+    const double least = (a * (double)(kUnits - x) + b * (double)x + (double)n2 * t2) / kUnits;
+    double best = 1e30;
+    for (int k = 0; k < 3; ++k)
+        for (double from : {a, b}) {
+            const double rounds = ceil((least - from) / t2 - 0.001) + k, end = from + (rounds > 0 ? rounds : 0) * t2;
+            const double held = (double)(kUnits - x) * floor((end - a) / t2 + 0.001) + (end >= b ? (double)x * floor((end - b) / t2 + 0.001) : 0.0);
+            if (held >= (double)n2 && end < best) best = end;
+        }
+    return best > b ? best : b;
+}
+
 // Adds the parts' planes up in order: dW four columns to a thread, behind them the bias gradient one element to a thread.
 __global__ __launch_bounds__(256) void wgrad_reduce_kernel(const GroupedGradArgs a, const float* planes, const float* bias_planes) {
     const int64_t all = (int64_t)a.experts * a.N * (a.K / 4), q = blockIdx.x * (int64_t)256 + threadIdx.x;
@@ -584,10 +675,84 @@ int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
     return with_wgrad(plan.shape, [&](auto k) { return decltype(k)::wgrad_grid(E, N, K) * (decltype(k)::block().x / 256); }) * plan.parts;
 }
 
+struct PairPlan {
+    int form, parts;
+    int64_t nd, nw;
+    bool w_first;
+};
+// The tiles of both gradients, and in how many parts the rows of the weight gradient are cut (wgrad_plan), by the end of the launch.
+static PairPlan pair_plan(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
+    PairPlan plan{0, 1, 0, 0, false};
+    double best = 1e30;
+    for (int i = 0; i < kPairForms; ++i) {
+        const PairShape& s = kPairShapes[i];
+        const int64_t across = (K + s.bn - 1) / s.bn, nd = dx ? (M + s.dm - 1) / s.dm * across : 0, nw = dw ? (N + s.wm - 1) / s.wm * across : 0;
+        const double td = s.d_fixed + s.d_stage * (double)((N + 63) / 64), stages = (double)((M + 63) / 64);
+        for (int parts = 1; parts == 1 || (dw && parts <= 64 && (double)(parts * 2) <= stages); parts *= 2) {
+            const double bytes = parts > 1 ? (double)parts * (double)wgrad_plane(1, N, K) : 0.0;
+            if (bytes > (double)room) break;
+            const double tw = s.w_fixed + s.w_stage * stages / parts;
+            double us = tw > td ? pair_time(nw * parts, tw, nd, td) : pair_time(nd, td, nw * parts, tw);
+            if (parts > 1) us = (us + 3.5 + bytes * 2 / 3.5e6) / 0.95;
+            if (us < best) {
+                best = us;
+                plan = PairPlan{i, parts, nd, nw, tw > td};
+            }
+        }
+    }
+    return plan;
+}
+void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[2]) {
+    const PairPlan plan = pair_plan(M, N, K, dx, dw, room);
+    out[0] = plan.form;
+    out[1] = plan.parts;
+}
+size_t grad_pair_workspace(int64_t M, int64_t N, int64_t K, size_t room) {
+    size_t most = 0;
+    for (bool dx : {false, true}) {
+        const int parts = pair_plan(M, N, K, dx, true, room).parts;
+        if (parts > 1 && (size_t)parts * wgrad_plane(1, N, K) > most) most = (size_t)parts * wgrad_plane(1, N, K);
+    }
+    return most;
+}
+int64_t grad_pair_grid(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
+    const PairPlan plan = pair_plan(M, N, K, dx, dw, room);
+    return (plan.nd + plan.nw * plan.parts + 16) * (plan.form >= 2 ? 2 : 1);
+}
+
+hipError_t launch_grad_pair(const GroupedGradArgs& a, void* dx, int64_t lddx, void* workspace, size_t room, hipStream_t stream) {
+    const PairPlan plan = pair_plan(a.T, a.N, a.K, dx != nullptr, a.out != nullptr, room);
+    PairArgs p{};
+    if (dx) p.d = GradArgs{a.dY, a.W, dx, nullptr, a.lddy, a.ldw, lddx, a.T, a.K, a.N};
+    if (a.out) p.w = GradArgs{a.dY, a.X, a.out, a.bias_out, a.lddy, a.ldx, a.ldo, a.N, a.K, a.T};
+    p.nd = (int)plan.nd;
+    p.nw = (int)plan.nw;
+    p.parts = plan.parts;
+    p.w_first = plan.w_first;
+    float* const planes = static_cast<float*>(workspace);
+    float* const bias_planes = planes + (size_t)plan.parts * a.N * a.K;
+    if (plan.parts > 1) {
+        p.w.C = planes;
+        p.w.row_sums = a.bias_out ? bias_planes : nullptr;
+        p.w.ldc = a.K;
+        p.w_plane = a.N * a.K;
+        p.sums_plane = a.N;
+    }
+    const hipError_t e = with_pair(plan.form, [&](auto k) { return decltype(k)::launch(p, a.f32 || plan.parts > 1, stream); });
+    if (e != hipSuccess || plan.parts == 1) return e;
+    GroupedGradArgs r = a;
+    r.parts = plan.parts;
+    r.o_stride = 0;
+    const int64_t work = a.N * (a.K / 4) + (a.bias_out ? a.N : 0);
+    hipLaunchKernelGGL(wgrad_reduce_kernel, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, stream, r, planes, bias_planes);
+    return hipGetLastError();
+}
+
 hipError_t prepare_grouped_grad_kernels() {
     hipError_t e = hipSuccess;
     for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_dgrad(i, [](auto k) { return decltype(k)::prepare_dgrad(); });
     for (int i = 0; i < 3 && e == hipSuccess; ++i) e = with_wgrad(i, [](auto k) { return decltype(k)::prepare_wgrad(); });
+    for (int i = 0; i < kPairForms && e == hipSuccess; ++i) e = with_pair(i, [](auto k) { return decltype(k)::prepare(); });
     hipFuncAttributes attr;
     if (e == hipSuccess) e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(wgrad_reduce_kernel));
     return e;

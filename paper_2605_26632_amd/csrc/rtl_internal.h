@@ -203,6 +203,13 @@ size_t wgrad_workspace(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_t room, hipStream_t stream);
 
+// Both gradients of one linear in one launch (a second one where the rows are cut into parts): a as for the weight gradient, with W, ldw for dX [T,K] (lddx);
+// dx or a.out may be NULL. room: bytes of the workspace for partial planes, of which grad_pair_workspace would be used. pair_choice: the form, parts (tests).
+size_t grad_pair_workspace(int64_t M, int64_t N, int64_t K, size_t room);
+int64_t grad_pair_grid(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room);
+void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[2]);
+hipError_t launch_grad_pair(const GroupedGradArgs& a, void* dx, int64_t lddx, void* workspace, size_t room, hipStream_t stream);
+
 // ---- gated linears (gated.hip) -------------------------------------------------------------------
 // a: A, lda, W (2 N rows), bias, Y, ldy, M, N, K, P, ldp, act.
 // The form of the tile loop that a launch takes (gemm.hip, host arithmetic): a small tile by its index there, or -1 for the 256-row plan of 2 F rows of W.
@@ -218,7 +225,6 @@ hipError_t launch_gated(const GemmArgs& a, hipStream_t stream);
 struct GatedGradArgs {
     const uint16_t *dH, *P;
     uint16_t *dP, *H;       // H nullable
-    int* offsets;           // nullable: receives {0, M}
     int64_t M, F, lddh, ldp, lddp, ldh;
     int act;
 };

@@ -64,7 +64,7 @@ def test_gated_backward_refusals():
     for p in ("X", "W", "dX", "dW"):
         assert f(**{p: FAKE + 8}) == ALIGN
     assert f(dH=FAKE + 1) == ALIGN and f(db=FAKE + 1) == ALIGN and f(db=FAKE + 2, type=1) == ALIGN and f(ldx=68) == ALIGN and f(lddw=68) == ALIGN
-    need = 256 + 4 * 16 * 24
+    need = 4 * 16 * 24
     assert f(ws=None) == WORKSPACE and f(wsb=need - 1) == WORKSPACE and f(ws=FAKE + 64) == ALIGN
     assert f(M=0, dW=None, db=None) == 0
     assert rtl.gated_linear_backward_workspace(16, 24, 64) >= need and rtl.gated_linear_backward_workspace(-1, 24, 64) == 0
@@ -73,7 +73,7 @@ def test_gated_backward_refusals():
 @no_gpu
 def test_gated_backward_accepts():
     f = gated_backward()
-    assert passes(f()) and passes(f(wsb=256 + 4 * 16 * 24)) and passes(f(X=None, dW=None, db=None, ldx=0, lddw=0)) and passes(f(W=None, dX=None, ldw=0, lddx=0))
+    assert passes(f()) and passes(f(wsb=4 * 16 * 24)) and passes(f(X=None, dW=None, db=None, ldx=0, lddw=0)) and passes(f(W=None, dX=None, ldw=0, lddx=0))
     assert passes(f(H=None, ldh=0)) and passes(f(X=None, W=None, dX=None, dW=None, db=None, K=0)) and passes(f(M=0)) and passes(f(dH=FAKE + 2, lddh=25, P=FAKE + 2, ldp=49))
 
 
