@@ -410,7 +410,7 @@ rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* 
  * rtl_residual_norm_backward: from the gradients dx_out (of x_type) and dh, either of which may be NULL (none), x' as the forward call gave it, and y:
  *   dx [T, D] of x_type, dy [T, D] bf16 and the sums over rows, fp32: dgate, dscale, dshift [S, D], dw_post, dw_pre [D], all dense. Any result may be
  *   NULL; the gradient of a vector that is NULL can be asked for. dy, dgate and dw_post need y, x' is needed with dh. An empty sequence has zeros. The
- *   sums are formed in a fixed order. dx may be dx_out, dy may be dh or y, in place.
+ *   sums are formed in a fixed order. dx may be dx_out, dy may be dh or y, in place. S * ceil(D / 32) < 2^22.
  *   workspace  rtl_residual_norm_backward_workspace(T, S, D) bytes, 256-byte aligned; needed for the sums only.
  * ------------------------------------------------------------------------------------------- */
 typedef enum { RTL_NORM_NONE = 0, RTL_NORM_RMS = 1, RTL_NORM_LAYER = 2 } rtl_norm;

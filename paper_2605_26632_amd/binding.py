@@ -392,6 +392,20 @@ def _here(*ts):
     return dev
 
 
+def _places(*ts):
+    """(number of the current device, which has to hold all of the tensors, their addresses)."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
+    at = []
+    for t in ts:
+        if t is None:
+            at.append(None)
+        elif t.get_device() != dev or dev < 0:
+            raise ValueError("librtlynx takes tensors of the current device (%d) only, not of %s" % (dev, t.device))
+        else:
+            at.append(t.data_ptr())
+    return dev, at
+
+
 def _matrix(t, dtype, name):
     """(rows, columns, row stride). torch leaves any stride there for a single row."""
     stride = t.stride()
@@ -651,7 +665,8 @@ def _choice(table, name, what):
 def gated_linear(X, W, bias=None, act="silu", with_pre=False, out=None, pre=None):
     """rtl_gated_linear: H = act(X W[:F]^T + bias[:F]) (X W[F:]^T + bias[F:]), X bf16 [M,K], W bf16 [2F,K], bias [2F]; act "silu", "gelu" or
     "gelu_tanh". H bf16 [M,F], or (H, P) with_pre or with a tensor `pre` for it: P bf16 [M,2F], what gated_linear_backward needs."""
-    dev = _here(X, W, bias, out, pre)
+    dev, at = _places(X, W, bias)
+    _here(out, pre)
     kind = _choice(ACT, act, "act")
     M, K, ldx = _matrix(X, torch.bfloat16, "X")
     rows, K_w, ldw = _matrix(W, torch.bfloat16, "W")
@@ -663,7 +678,7 @@ def gated_linear(X, W, bias=None, act="silu", with_pre=False, out=None, pre=None
     ldp = 0
     if with_pre or pre is not None:
         pre, ldp = _output(pre, M, rows, torch.bfloat16, X)
-    st = lib().rtl_gated_linear(_p(X), _p(W), _p(bias), _p(H), _p(pre), kind, M, F, K, ldx, ldw, ldh, ldp, _on(dev))
+    st = lib().rtl_gated_linear(*at, H.data_ptr(), _p(pre), kind, M, F, K, ldx, ldw, ldh, ldp, _on(dev))
     _check(st, "rtl_gated_linear")
     return H if pre is None else (H, pre)
 
@@ -677,7 +692,8 @@ def gated_linear_backward(dH, X, W, P, act="silu", with_bias=False, with_hidden=
     gradient of the layer behind) only with_hidden, else None. X None: no dW and db, W None: no dX. dW and db in `dtype` (bf16 or float32).
     `out`: the four tensors, None for what is not wanted; they then settle with_bias, with_hidden and dtype."""
     dX, dW, db, H = out if out is not None else (None,) * 4
-    dev = _here(dH, X, W, P, dX, dW, db, H, ws)
+    dev, at = _places(dH, X, W, P)
+    _here(dX, dW, db, H, ws)
     kind = _choice(ACT, act, "act")
     M, F, lddh = _matrix(dH, torch.bfloat16, "dH")
     m, f2, ldp = _matrix(P, torch.bfloat16, "P")
@@ -721,7 +737,7 @@ def gated_linear_backward(dH, X, W, P, act="silu", with_bias=False, with_hidden=
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_gated_linear_backward_workspace(M, F, max(K, 1)), device)
-    st = L.rtl_gated_linear_backward(_p(dH), _p(X), _p(W), _p(P), _p(dX), _p(dW), _p(db), _p(H), kind, 1 if dtype is torch.float32 else 0, M, F, K,
+    st = L.rtl_gated_linear_backward(*at, _p(dX), _p(dW), _p(db), _p(H), kind, 1 if dtype is torch.float32 else 0, M, F, K,
                                      lddh, ldx, ldw, ldp, lddx, lddw, ldh, _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_gated_linear_backward")
     return dX, dW, db, H
@@ -771,7 +787,8 @@ def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shi
     `post` of y and `pre` of x': "none", "rms", "layer". Returns (x' of x's type, h bf16), None for what is not wanted. `out`: the two tensors, None for what
     is not wanted; it then settles with_x and with_h."""
     xo, h = out if out is not None else (None, None)
-    dev = _here(x, y, gate, w_post, w_pre, scale, shift, offsets, xo, h)
+    dev, at = _places(x, y, gate, w_post, w_pre, scale, shift, offsets)
+    _here(xo, h)
     kind, S = _residual_type(x, "x"), _sequences(offsets)
     T, D, ldx = _matrix(x, kind, "x")
     bf, rows, vectors = torch.bfloat16, (T, D), (S, D)
@@ -781,8 +798,7 @@ def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shi
     if out is None:
         xo = torch.empty(rows, dtype=kind, device=x.device) if with_x else None
         h = torch.empty(rows, dtype=bf, device=x.device) if with_h else None
-    st = lib().rtl_residual_norm(_p(x), _p(y), _p(gate), _p(w_post), _p(w_pre), _p(scale), _p(shift), _p(offsets), _p(xo), _p(h),
-                                 kind is torch.float32, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps, out is None,
+    st = lib().rtl_residual_norm(*at, _p(xo), _p(h), kind is torch.float32, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps, out is None,
                                  T, S, D, ldx, ldy, ld_gate, ld_mod, _rows_of(xo, rows, kind, "x'"), _rows_of(h, rows, bf, "h"), _on(dev))
     _check(st, "rtl_residual_norm")
     return xo, h
@@ -798,7 +814,8 @@ def residual_norm_backward(dx_out, dh, x_out, y=None, gate=None, w_post=None, w_
     none), its x' and y. Gradients of what is not passed are None; dshift comes with scale's unless with_shift says otherwise. The last five are float32.
     `out`: the seven tensors, None for what is not wanted."""
     got = list(out) if out is not None else [None] * 7
-    dev = _here(dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets, *got, ws)
+    dev, at = _places(dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets)
+    _here(*got, ws)
     like = x_out if x_out is not None else dx_out
     if like is None:
         raise ValueError("x' or its gradient expected")
@@ -823,8 +840,7 @@ def residual_norm_backward(dx_out, dh, x_out, y=None, gate=None, w_post=None, w_
     L = lib()
     if ws is None:
         ws = _ws(L.rtl_residual_norm_backward_workspace(T, S, D), like.device)
-    st = L.rtl_residual_norm_backward(_p(dx_out), _p(dh), _p(x_out), _p(y), _p(gate), _p(w_post), _p(w_pre), _p(scale), _p(offsets), _p(dx), _p(dy),
-                                      _p(dgate), _p(dscale), _p(dshift), _p(dw_post), _p(dw_pre), kind is f32, _choice(NORM, post, "post"),
+    st = L.rtl_residual_norm_backward(*at, *map(_p, got), kind is f32, _choice(NORM, post, "post"),
                                       _choice(NORM, pre, "pre"), alpha, eps, out is None, T, S, D, *lds, _rows_of(dx, rows, kind, "dx"),
                                       _rows_of(dy, rows, bf, "dy"), _p(ws), _bytes(ws), _on(dev))
     _check(st, "rtl_residual_norm_backward")
@@ -866,7 +882,8 @@ def norm_rotary(q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, i
     and their pairs (2j, 2j+1), or (j, j + pairs) if not interleaved, turned by pos[t, axis[j]] freq[j]: pos float32 [T,axes], freq float32 [pairs], axis int32
     [pairs]; freq None: no rotation. Any strides with contiguous heads. Returns (q', k'), new dense tensors or those of `out`, which may be q and k themselves."""
     qo, ko = out if out is not None else (None, None)
-    dev = _here(q, k, pos, freq, axis, wq, wk, qo, ko)
+    dev, at = _places(q, k, pos, freq, axis, wq, wk)
+    _here(qo, ko)
     like = q if q is not None else k
     if like is None:
         raise ValueError("q or k expected")
@@ -881,7 +898,7 @@ def norm_rotary(q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, i
         ko = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=like.device) if k is not None else None
     if (q is None) != (qo is None) or (k is None) != (ko is None):
         raise ValueError("out: tensors for what is passed expected")
-    st = lib().rtl_norm_rotary(_p(q), _p(k), _p(pos), _p(freq), _p(axis), _p(wq), _p(wk), _p(qo), _p(ko), _choice(NORM, norm, "norm"), eps,
+    st = lib().rtl_norm_rotary(*at, _p(qo), _p(ko), _choice(NORM, norm, "norm"), eps,
                                int(interleaved), T, Hq, Hk, D, pairs, axes, ldq, sq, ldk, sk, *_heads(qo, T, D, "q'", Hq)[1:],
                                *_heads(ko, T, D, "k'", Hk)[1:], _on(dev))
     _check(st, "rtl_norm_rotary")
@@ -896,7 +913,8 @@ def norm_rotary_backward(dq_out, dk_out, q, k, pos, freq, axis, wq=None, wk=None
     """rtl_norm_rotary_backward: (dq, dk, dwq, dwk) of norm_rotary from the gradients of its results; q and k are needed with the norm only (else None will
     do), dwq and dwk (float32 [D]) come with wq and wk. `out`: the four tensors, None for what is not passed or not wanted."""
     dq, dk, dwq, dwk = out if out is not None else (None,) * 4
-    dev = _here(dq_out, dk_out, q, k, pos, freq, axis, wq, wk, dq, dk, dwq, dwk, ws)
+    dev, at = _places(dq_out, dk_out, q, k, pos, freq, axis, wq, wk)
+    _here(dq, dk, dwq, dwk, ws)
     like = dq_out if dq_out is not None else dk_out
     if like is None:
         raise ValueError("a gradient expected")
@@ -917,7 +935,7 @@ def norm_rotary_backward(dq_out, dk_out, q, k, pos, freq, axis, wq=None, wk=None
     L = lib()
     if ws is None and (dwq is not None or dwk is not None):
         ws = _ws(L.rtl_norm_rotary_backward_workspace(D), like.device)
-    st = L.rtl_norm_rotary_backward(_p(dq_out), _p(dk_out), _p(q), _p(k), _p(pos), _p(freq), _p(axis), _p(wq), _p(wk), _p(dq), _p(dk), _p(dwq), _p(dwk),
+    st = L.rtl_norm_rotary_backward(*at, _p(dq), _p(dk), _p(dwq), _p(dwk),
                                     _choice(NORM, norm, "norm"), eps, int(interleaved), T, Hq, Hk, D, pairs, axes, lddqo, sdqo, lddko, sdko,
                                     *_heads(q, T, D, "q", Hq if q is not None else None)[1:], *_heads(k, T, D, "k", Hk if k is not None else None)[1:],
                                     *_heads(dq, T, D, "dq", Hq)[1:], *_heads(dk, T, D, "dk", Hk)[1:], _p(ws), _bytes(ws) if ws is not None else 0, _on(dev))

@@ -966,7 +966,7 @@ rtl_status rtl_residual_norm_backward(const void* dx_out, const void* dh, const 
                                       int64_t ld_mod, int64_t lddx, int64_t lddy, void* workspace, size_t workspace_bytes, void* stream) {
     rtl_status st = check_norm(x_type, post, pre, alpha, eps, T, S, D, offsets);
     if (st != RTL_OK) return st;
-    if (S * ((D + 63) / 64) >= (int64_t)1 << 22) return RTL_ERR_SHAPE;       // workgroups of 1024 threads
+    if (S * ((D + 31) / 32) >= (int64_t)1 << 22) return RTL_ERR_SHAPE;       // workgroups of 1024 threads
     const bool f32 = x_type == RTL_F32;
     auto floats = [](const float* p) { return p && !aligned(p, 4) ? RTL_ERR_ALIGN : RTL_OK; };
     st = first_error({check_rows(dx_out, lddxo, D, f32), check_rows(dh, lddh, D), check_rows(x_out, ldxo, D, f32), check_rows(y, ldy, D),

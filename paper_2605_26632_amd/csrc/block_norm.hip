@@ -80,32 +80,24 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 
-// Sums of two values over a team of WAVES waves, in a fixed order. `slot` (team of several waves): LDS of 2 x 2 WAVES floats, used by turns, so that
-// one barrier a sum is enough: a wave that writes a half again has passed the barrier behind which everybody has read it.
+// Sum over a team of WAVES waves, in a fixed order. `slot` (team of several waves): LDS of 2 x WAVES floats, used by turns, so that one barrier a sum is
+// enough: a wave that writes a half again has passed the barrier behind which everybody has read it.
 template <int WAVES>
 struct TeamSum {
     float* slot;
     int turn = 0;
-    __device__ __forceinline__ void operator()(float& a, float& b) {
+    __device__ __forceinline__ float operator()(float a) {
         a = wave_sum(a);
-        b = wave_sum(b);
         if constexpr (WAVES > 1) {
-            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-            float* s = slot + turn * 2 * WAVES;
-            if (lane == 0) {
-                s[2 * wave] = a;
-                s[2 * wave + 1] = b;
-            }
+            float* s = slot + turn * WAVES;
+            if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = a;
             __syncthreads();
             a = s[0];
-            b = s[1];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) {
-                a += s[2 * w];
-                b += s[2 * w + 1];
-            }
+            for (int w = 1; w < WAVES; ++w) a += s[w];
             turn ^= 1;
         }
+        return a;
     }
 };
 
@@ -129,44 +121,38 @@ struct Stats {
     float mean, scale;
 };
 
-// Statistics of two rows at once (either may be without a norm). v: NCH chunks of eight of the lane, zeros behind the end of the row.
+// Statistics of a row. v: NCH chunks of eight of the lane, zeros behind the end of the row.
 template <int WAVES, int NCH>
-__device__ __forceinline__ void row_stats(const float (&u)[NCH][8], int kind_u, Stats& su, const float (&v)[NCH][8], int kind_v, Stats& sv, int team_lane, int D,
-                                          float eps, TeamSum<WAVES>& sum) {
-    su = sv = Stats{0.f, 1.f};
+__device__ __forceinline__ Stats row_stats(const float (&v)[NCH][8], int kind, int team_lane, int D, float eps, TeamSum<WAVES>& sum) {
+    Stats s{0.f, 1.f};
     const float inv = 1.0f / (float)D;
-    if (kind_u == RTL_NORM_LAYER || kind_v == RTL_NORM_LAYER) {
-        float a = 0.f, b = 0.f;
+    if (kind == RTL_NORM_LAYER) {
+        float a = 0.f;
 #pragma unroll
         for (int c = 0; c < NCH; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a += u[c][e];
-                b += v[c][e];
-            }
-        sum(a, b);
-        if (kind_u == RTL_NORM_LAYER) su.mean = a * inv;
-        if (kind_v == RTL_NORM_LAYER) sv.mean = b * inv;
+            for (int e = 0; e < 8; ++e) a += v[c][e];
+        s.mean = sum(a) * inv;
     }
-    if (kind_u != RTL_NORM_NONE || kind_v != RTL_NORM_NONE) {
-        float a = 0.f, b = 0.f;
+    if (kind != RTL_NORM_NONE) {
+        float a = 0.f;
 #pragma unroll
         for (int c = 0; c < NCH; ++c)
             if ((c * WAVES * 64 + team_lane) * 8 < D) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float p = u[c][e] - su.mean, q = v[c][e] - sv.mean;
+                    const float p = v[c][e] - s.mean;
                     a += p * p;
-                    b += q * q;
                 }
             }
-        sum(a, b);
-        if (kind_u != RTL_NORM_NONE) su.scale = 1.0f / sqrtf(a * inv + eps);
-        if (kind_v != RTL_NORM_NONE) sv.scale = 1.0f / sqrtf(b * inv + eps);
+        s.scale = 1.0f / sqrtf(sum(a) * inv + eps);
     }
+    return s;
 }
 
-template <int WAVES, int NCH, bool F32>
+// EARLY: the vectors of the sequence are loaded beside the rows, not behind the sums: for few rows, where a launch is as long as the loads that wait for each
+// other. With many rows the registers are worth more.
+template <int WAVES, int NCH, bool F32, bool EARLY>
 __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArgs a) {
     __shared__ float slots[4 * WAVES];
     constexpr int TEAM = WAVES * 64, TEAMS = team_threads(WAVES) / TEAM;
@@ -174,70 +160,73 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
     const int64_t row = (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
     if (row >= a.T) return;
     const int D = (int)a.D;
+    auto column = [&](int c) { return (uint32_t)((c * TEAM + tl) * 8); };
     const int s = __builtin_amdgcn_readfirstlane(sequence_of(a.offsets, (int)a.S, (int)row));
-    float x[NCH][8];
     if (s < 0) {
         if (!a.clear) return;
         const float zero[8] = {};
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-            if (col < D) {
-                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, col, zero);
-                if (a.h) store8_as<false>(a.h, row * a.ldh, col, zero);
+        for (int c = 0; c < NCH; ++c)
+            if (column(c) < (uint32_t)D) {
+                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, column(c), zero);
+                if (a.h) store8_as<false>(a.h, row * a.ldh, column(c), zero);
             }
-        }
         return;
     }
     TeamSum<WAVES> sum{slots};
-    float y[NCH][8];
+    constexpr uint32_t kOnes = 0x3F803F80u;
+    // a chunk of a vector, `none` where there is no vector
+    auto vector = [&](const uint16_t* p, int64_t at, int c, uint32_t none) {
+        uint4 v = make_uint4(none, none, none, none);
+        if (p && column(c) < (uint32_t)D) v = *reinterpret_cast<const uint4*>(p + at + column(c));
+        return v;
+    };
+    auto post_weight = [&](int c) { return vector(a.w_post, 0, c, kOnes); };
+    auto gates = [&](int c) { return vector(a.gate, s * a.ld_gate, c, kOnes); };
+    auto pre_weight = [&](int c) { return vector(a.w_pre, 0, c, kOnes); };
+    auto scales = [&](int c) { return vector(a.scale, s * a.ld_mod, c, 0); };
+    auto shifts = [&](int c) { return vector(a.shift, s * a.ld_mod, c, 0); };
+    float x[NCH][8], y[NCH][8];
+    uint4 early[EARLY ? NCH : 1][5];
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-        const int col = (c * TEAM + tl) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[c][e] = y[c][e] = 0.f;
-        if (col < D) {
-            load8_as<F32>(a.x, row * a.ldx, col, x[c]);
-            if (a.y) load8(a.y + row * a.ldy, col, y[c]);
+        if (column(c) < (uint32_t)D) {
+            load8_as<F32>(a.x, row * a.ldx, column(c), x[c]);
+            if (a.y) load8(a.y + row * a.ldy, column(c), y[c]);
+        }
+        if constexpr (EARLY) {
+            early[c][0] = post_weight(c);
+            early[c][1] = gates(c);
+            early[c][2] = pre_weight(c);
+            early[c][3] = scales(c);
+            early[c][4] = shifts(c);
         }
     }
-    Stats sy, sx;
-    row_stats<WAVES, NCH>(y, a.y ? a.post : RTL_NORM_NONE, sy, y, RTL_NORM_NONE, sx, tl, D, a.eps, sum);
-    {
+    const Stats sy = row_stats<WAVES, NCH>(y, a.y ? a.post : RTL_NORM_NONE, tl, D, a.eps, sum);
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            const int col = (c * TEAM + tl) * 8;
-            if (col < D) {
-                float w[8], g[8];
+    for (int c = 0; c < NCH; ++c) {
+        float w[8], g[8];
+        unpack8(EARLY ? early[EARLY ? c : 0][0] : post_weight(c), w);
+        unpack8(EARLY ? early[EARLY ? c : 0][1] : gates(c), g);
+        if (column(c) < (uint32_t)D) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = g[e] = 1.0f;
-                if (a.w_post) load8(a.w_post, col, w);
-                if (a.gate) load8(a.gate + s * a.ld_gate, col, g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
-                if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, col, x[c]);
-            }
+            for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
+            if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, column(c), x[c]);
         }
     }
     if (!a.h) return;
-    row_stats<WAVES, NCH>(x, a.pre, sx, x, RTL_NORM_NONE, sy, tl, D, a.eps, sum);
+    const Stats sx = row_stats<WAVES, NCH>(x, a.pre, tl, D, a.eps, sum);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-        const int col = (c * TEAM + tl) * 8;
-        if (col < D) {
-            float w[8], g[8], b[8], h[8];
+        float w[8], g[8], b[8], h[8];
+        unpack8(EARLY ? early[EARLY ? c : 0][2] : pre_weight(c), w);
+        unpack8(EARLY ? early[EARLY ? c : 0][3] : scales(c), g);
+        unpack8(EARLY ? early[EARLY ? c : 0][4] : shifts(c), b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = 1.0f;
-                g[e] = b[e] = 0.f;
-            }
-            if (a.w_pre) load8(a.w_pre, col, w);
-            if (a.scale) load8(a.scale + s * a.ld_mod, col, g);
-            if (a.shift) load8(a.shift + s * a.ld_mod, col, b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = w[e] * ((x[c][e] - sx.mean) * sx.scale) * (1.0f + g[e]) + b[e];
-            store8_as<false>(a.h, row * a.ldh, col, h);
-        }
+        for (int e = 0; e < 8; ++e) h[e] = w[e] * ((x[c][e] - sx.mean) * sx.scale) * (1.0f + g[e]) + b[e];
+        if (column(c) < (uint32_t)D) store8_as<false>(a.h, row * a.ldh, column(c), h);
     }
 }
 
@@ -471,69 +460,61 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(con
     }
 }
 
-// Adds the slots of a sequence up in the order of its rows: 64 columns to a workgroup, the slots dealt to its waves in turn and the waves' sums added in order.
-// What the weights' gradients need of it goes to a.totals ([S][2][D]); of a single sequence they are made here.
-constexpr int kReduceWaves = 16;
-__global__ __launch_bounds__(kReduceWaves * 64) void norm_reduce_kernel(const NormGradArgs a) {
-    __shared__ float part[3][kReduceWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane, s = blockIdx.y;
-    int64_t b0 = 0, b1 = -1;
-    const int64_t begin = a.offsets ? min(max((int64_t)a.offsets[s], (int64_t)0), a.T) : 0;
-    const int64_t end = a.offsets ? min(max((int64_t)a.offsets[s + 1], (int64_t)0), a.T) : a.T;
-    if (begin < end) {
-        b0 = begin / a.rows;
-        b1 = (end - 1) / a.rows;
-    }
+// Adds the slots of a sequence up (blockIdx.y): kReduceCols columns to a workgroup, the slots dealt to its kReduceSlices rows of threads in turn, their sums
+// added in order. What the weights' gradients need of it goes to a.totals ([S][2][D]); those of a single sequence are made here. (A workgroup that takes all
+// the sequences one after the other, which spares norm_weights_kernel, took 7 us longer with five.)
+constexpr int kReduceCols = 32, kReduceSlices = 32;
+__device__ __forceinline__ float bf16_or(const uint16_t* p, int64_t at, float none) { return p ? __uint_as_float((uint32_t)p[at] << 16) : none; }
+__global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_reduce_kernel(const NormGradArgs a) {
+    __shared__ float part[3][kReduceSlices][kReduceCols];
+    const int lane = threadIdx.x % kReduceCols, slice = threadIdx.x / kReduceCols, D = (int)a.D, T = (int)a.T, s = blockIdx.y;
+    const int col0 = blockIdx.x * kReduceCols, col = min(col0 + lane, D - 1);
+    const int begin = a.offsets ? min(max(a.offsets[s], 0), T) : 0, end = a.offsets ? min(max(a.offsets[s + 1], 0), T) : T;
+    const int b0 = (int)((uint32_t)begin / (uint32_t)a.rows), b1 = begin < end ? (int)((uint32_t)(end - 1) / (uint32_t)a.rows) : b0 - 1;
     float v[3] = {};
-    if (col < a.D) {
-        const float* p = a.sums + (b0 + wave + s) * 3 * a.D + col;
+    const float* p = a.sums + (int64_t)(b0 + slice + s) * 3 * D + col;
 #pragma unroll 4
-        for (int64_t b = b0 + wave; b <= b1; b += kReduceWaves, p += kReduceWaves * 3 * a.D) {
+    for (int b = b0 + slice; b <= b1; b += kReduceSlices, p += (int64_t)kReduceSlices * 3 * D)
 #pragma unroll
-            for (int k = 0; k < 3; ++k) v[k] += p[k * a.D];
-        }
-    }
+        for (int k = 0; k < 3; ++k) v[k] += p[k * D];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) part[k][wave][lane] = v[k];
+    for (int k = 0; k < 3; ++k) part[k][slice][lane] = v[k];
     __syncthreads();
-    if (wave != 0 || col >= a.D) return;
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-        for (int w = 1; w < kReduceWaves; ++w) v[k] += part[k][w][lane];
-    auto one = [](const uint16_t* p, int64_t at) { return p ? __uint_as_float((uint32_t)p[at] << 16) : 1.0f; };
-    if (a.dgate) a.dgate[s * a.D + col] = v[0] * one(a.w_post, col);
-    if (a.dscale) a.dscale[s * a.D + col] = v[1] * one(a.w_pre, col);
-    if (a.dshift) a.dshift[s * a.D + col] = v[2];
-    if (a.S == 1) {
-        if (a.dw_post) a.dw_post[col] = v[0] * one(a.gate, col);
-        if (a.dw_pre) a.dw_pre[col] = v[1] * (a.scale ? 1.0f + one(a.scale, col) : 1.0f);
-    } else {
-        if (a.dw_post) a.totals[s * 2 * a.D + col] = v[0];
-        if (a.dw_pre) a.totals[(s * 2 + 1) * a.D + col] = v[1];
+    if (slice >= 3 || col0 + lane >= D) return;                  // the first three rows of threads finish one sum each
+    float sum = part[slice][0][lane];
+    for (int w = 1; w < kReduceSlices; ++w) sum += part[slice][w][lane];
+    const int64_t at = (int64_t)s * D + col;
+    if (slice == 0) {
+        if (a.dgate) a.dgate[at] = sum * bf16_or(a.w_post, col, 1.0f);
+        if (a.dw_post && a.S == 1) a.dw_post[col] = sum * bf16_or(a.gate, col, 1.0f);
+        else if (a.dw_post) a.totals[(int64_t)s * 2 * D + col] = sum;
+    } else if (slice == 1) {
+        if (a.dscale) a.dscale[at] = sum * bf16_or(a.w_pre, col, 1.0f);
+        if (a.dw_pre && a.S == 1) a.dw_pre[col] = sum * (1.0f + bf16_or(a.scale, col, 0.0f));
+        else if (a.dw_pre) a.totals[((int64_t)s * 2 + 1) * D + col] = sum;
+    } else if (a.dshift) {
+        a.dshift[at] = sum;
     }
 }
 
-// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s, the sequences dealt to the waves as the slots above.
-__global__ __launch_bounds__(kReduceWaves * 64) void norm_weights_kernel(const NormGradArgs a) {
-    __shared__ float part[2][kReduceWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s, the sequences dealt as the slots above.
+__global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_weights_kernel(const NormGradArgs a) {
+    __shared__ float part[2][kReduceSlices][kReduceCols];
+    const int lane = threadIdx.x % kReduceCols, slice = threadIdx.x / kReduceCols, D = (int)a.D;
+    const int col0 = blockIdx.x * kReduceCols, col = min(col0 + lane, D - 1);
     float v[2] = {};
-    if (col < a.D)
-        for (int64_t s = wave; s < a.S; s += kReduceWaves) {
-            if (a.dw_post) v[0] += a.totals[s * 2 * a.D + col] * (a.gate ? __uint_as_float((uint32_t)a.gate[s * a.ld_gate + col] << 16) : 1.0f);
-            if (a.dw_pre) v[1] += a.totals[(s * 2 + 1) * a.D + col] * (1.0f + (a.scale ? __uint_as_float((uint32_t)a.scale[s * a.ld_mod + col] << 16) : 0.0f));
-        }
-    part[0][wave][lane] = v[0];
-    part[1][wave][lane] = v[1];
+    for (int64_t s = slice; s < a.S; s += kReduceSlices) {
+        if (a.dw_post) v[0] += a.totals[s * 2 * D + col] * bf16_or(a.gate, s * a.ld_gate + col, 1.0f);
+        if (a.dw_pre) v[1] += a.totals[(s * 2 + 1) * D + col] * (1.0f + bf16_or(a.scale, s * a.ld_mod + col, 0.0f));
+    }
+    part[0][slice][lane] = v[0];
+    part[1][slice][lane] = v[1];
     __syncthreads();
-    if (wave != 0 || col >= a.D) return;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        for (int w = 1; w < kReduceWaves; ++w) v[k] += part[k][w][lane];
-    if (a.dw_post) a.dw_post[col] = v[0];
-    if (a.dw_pre) a.dw_pre[col] = v[1];
+    if (slice >= 2 || col0 + lane >= D) return;
+    float sum = part[slice][0][lane];
+    for (int w = 1; w < kReduceSlices; ++w) sum += part[slice][w][lane];
+    float* const to = slice ? a.dw_pre : a.dw_post;
+    if (to) to[col] = sum;
 }
 
 // f(waves of a team, chunks of a lane) for rows of D values.
@@ -547,10 +528,14 @@ hipError_t with_team(int64_t D, F f) {
     return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
 }
 
-// Backward pass: waves of a team, and rows of one: the rows dealt once over the teams that the chip holds, 16 waves to a compute unit.
+constexpr unsigned kFewGroups = 512;         // workgroups of the forward pass up to which vectors are loaded early
+
+// Backward pass: waves of a team, and rows of one: the rows dealt once over teams of eight waves to a compute unit. Sixteen read at the same rate and leave
+// twice the sums: [16896, 3840] 175 -> 167 us, [16896, 2048] 104 -> 97, [8192, 3840] 90 -> 85, [16896, 512] 40 -> 34, fp32 [2111, 2048] 28.7 -> 27.4.
 int team_waves(int64_t D) { return (int)((D + 511) / 512); }
 int64_t team_rows(int64_t T, int64_t D) {
-    const int64_t teams = 256 * (16 / team_waves(D));
+    const int waves = team_waves(D);
+    const int64_t teams = 256 * (waves < 8 ? 8 / waves : 1);
     return T > teams ? (T + teams - 1) / teams : 1;
 }
 
@@ -561,8 +546,13 @@ hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream) {
         constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
         const int64_t teams = team_threads(W) / (W * 64);
         const dim3 grid((unsigned)((a.T + teams - 1) / teams));
-        if (a.x_f32) hipLaunchKernelGGL((norm_kernel<W, C, true>), grid, dim3(team_threads(W)), 0, stream, a);
-        else hipLaunchKernelGGL((norm_kernel<W, C, false>), grid, dim3(team_threads(W)), 0, stream, a);
+        auto go = [&](auto f32, auto early) {
+            hipLaunchKernelGGL((norm_kernel<W, C, decltype(f32)::value, decltype(early)::value>), grid, dim3(team_threads(W)), 0, stream, a);
+        };
+        using T = std::true_type;
+        using F = std::false_type;
+        if (grid.x <= kFewGroups) a.x_f32 ? go(T{}, T{}) : go(F{}, T{});
+        else a.x_f32 ? go(T{}, F{}) : go(F{}, F{});
         return hipGetLastError();
     });
 }
@@ -595,14 +585,15 @@ hipError_t launch_residual_norm_backward(const NormGradArgs& a_in, hipStream_t s
         }
         e = hipGetLastError();
     }
-    const unsigned cols = (unsigned)((a.D + 63) / 64);
+    const unsigned cols = (unsigned)((a.D + kReduceCols - 1) / kReduceCols), threads = kReduceCols * kReduceSlices;
     const bool weights = a.dw_post || a.dw_pre;
-    if (e == hipSuccess && a.S > 0 && (weights || a.dgate || a.dscale || a.dshift)) {
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3(cols, (unsigned)a.S), dim3(kReduceWaves * 64), 0, stream, a);
+    if (e != hipSuccess || !(weights || a.dgate || a.dscale || a.dshift)) return e;
+    if (a.S > 0) {
+        hipLaunchKernelGGL(norm_reduce_kernel, dim3(cols, (unsigned)a.S), dim3(threads), 0, stream, a);
         e = hipGetLastError();
     }
     if (e == hipSuccess && weights && a.S != 1) {
-        hipLaunchKernelGGL(norm_weights_kernel, dim3(cols), dim3(kReduceWaves * 64), 0, stream, a);
+        hipLaunchKernelGGL(norm_weights_kernel, dim3(cols), dim3(threads), 0, stream, a);
         e = hipGetLastError();
     }
     return e;
@@ -610,7 +601,7 @@ hipError_t launch_residual_norm_backward(const NormGradArgs& a_in, hipStream_t s
 
 hipError_t prepare_norm_kernels() {
     hipFuncAttributes f;
-    hipError_t e = hipFuncGetAttributes(&f, reinterpret_cast<const void*>(norm_reduce_kernel));        // loads the code object
+    hipError_t e = hipFuncGetAttributes(&f, reinterpret_cast<const void*>(norm_weights_kernel));        // loads the code object
     return e;
 }
 
