@@ -62,20 +62,22 @@ struct GatedMixed {
 // Up to sixteen rows of X: reading W is all there is, and it goes straight from memory into the registers that the matrix instruction takes (few_rows.hip has
 // the layout). A workgroup owns sixteen columns of H, so sixteen gate rows and the sixteen up rows; its waves divide the contraction in lines of 128
 // bytes, neighbouring waves on neighbouring lines, four lines of a row in flight, and their sums meet in LDS in a fixed order.
-constexpr int kFewRows = 16, kFewWaves = 4, kFewLines = 4;
-__global__ __launch_bounds__(kFewWaves * 64) void gated_few_rows_kernel(const GemmArgs a) {
-    __shared__ __align__(16) float sums[kFewWaves][2][64][4];
+constexpr int kFewRows = 16, kFewLines = 4;
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 4) void gated_few_rows_kernel(const GemmArgs a) {
+    __shared__ __align__(16) float sums[WAVES][2][64][4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, kb = lane >> 4;
     const int units = (int)(a.K / 64);
     const int64_t n0 = (int64_t)blockIdx.x * 16, n = min(n0 + li, a.N - 1);
     const uint16_t* const w_row[2] = {static_cast<const uint16_t*>(a.W) + n * a.ldw + kb * 16, static_cast<const uint16_t*>(a.W) + (a.N + n) * a.ldw + kb * 16};
     const uint16_t* const x_row = static_cast<const uint16_t*>(a.A) + min((int64_t)li, a.M - 1) * a.lda + kb * 16;     // (rows behind the last repeat it, never stored)
     f32x4 acc[2] = {};
-    for (int u0 = wave; u0 < units; u0 += kFewWaves * kFewLines) {
+    for (int u0 = wave; u0 < units; u0 += WAVES * kFewLines) {
         Frag8 w[kFewLines][2][2], x[kFewLines][2];
 #pragma unroll
         for (int u = 0; u < kFewLines; ++u) {
-            const int64_t at = (int64_t)min(u0 + u * kFewWaves, units - 1) * 64;                  // (behind the end: loaded again, not used)
+            if (u0 + u * WAVES >= units) break;
+            const int64_t at = (int64_t)(u0 + u * WAVES) * 64;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
 #pragma unroll
@@ -86,21 +88,28 @@ __global__ __launch_bounds__(kFewWaves * 64) void gated_few_rows_kernel(const Ge
         __builtin_amdgcn_sched_barrier(0);                                                       // all the loads first
 #pragma unroll
         for (int u = 0; u < kFewLines; ++u) {
-            if (u0 + u * kFewWaves >= units) break;
+            if (u0 + u * WAVES >= units) break;
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int f = 0; f < 2; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][f][c].v, x[u][c].v, acc[f], 0, 0, 0);
         }
     }
-#pragma unroll
-    for (int f = 0; f < 2; ++f) *reinterpret_cast<f32x4*>(sums[wave][f][lane]) = acc[f];
-    __syncthreads();
-    if (wave != 0) return;
     // row li of X, columns 4 kb .. of the sixteen
     const int64_t col = n0 + 4 * kb;
     const int valid = (int)min((int64_t)4, a.N - col);
-    if (li >= a.M || valid <= 0) return;
+    float bias[2][4] = {};
+    if (wave == 0 && a.bias && valid > 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t at = col + min(e, valid - 1);
+            bias[0][e] = __uint_as_float((uint32_t)a.bias[at] << 16);
+            bias[1][e] = __uint_as_float((uint32_t)a.bias[a.N + at] << 16);
+        }
+#pragma unroll
+    for (int f = 0; f < 2; ++f) *reinterpret_cast<f32x4*>(sums[wave][f][lane]) = acc[f];
+    __syncthreads();
+    if (wave != 0 || li >= a.M || valid <= 0) return;
     const GateForm form = gate_form(a.act);
     uint16_t out[3][4];
     f32x4 s[2];
@@ -108,13 +117,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void gated_few_rows_kernel(const Ge
     for (int f = 0; f < 2; ++f) {
         s[f] = *reinterpret_cast<const f32x4*>(sums[0][f][lane]);
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) s[f] += *reinterpret_cast<const f32x4*>(sums[w][f][lane]);
+        for (int w = 1; w < WAVES; ++w) s[f] += *reinterpret_cast<const f32x4*>(sums[w][f][lane]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int64_t at = col + min(e, valid - 1);
-        const float g = s[0][e] + (a.bias ? __uint_as_float((uint32_t)a.bias[at] << 16) : 0.f);
-        const float u = s[1][e] + (a.bias ? __uint_as_float((uint32_t)a.bias[a.N + at] << 16) : 0.f);
+        const float g = s[0][e] + bias[0][e], u = s[1][e] + bias[1][e];
         out[0][e] = (uint16_t)f32_to_bf16_rne((a.act == RTL_ACT_GELU ? gate_value<true>(g, form) : gate_value<false>(g, form)) * u);
         out[1][e] = (uint16_t)f32_to_bf16_rne(g);
         out[2][e] = (uint16_t)f32_to_bf16_rne(u);
@@ -193,8 +200,12 @@ using Gated192 = GatedMixed<192, 4, 2>;
 hipError_t launch_gated(const GemmArgs& a_in, hipStream_t stream) {
     GemmArgs a = a_in;
     if (a.M <= kFewRows && a.N < (int64_t)1 << 27) {               // (a launch takes fewer than 2^32 threads)
-        hipLaunchKernelGGL(gated_few_rows_kernel, dim3((unsigned)((a.N + 15) / 16)), dim3(kFewWaves * 64), 0, stream, a);
-        return hipGetLastError();
+        const int64_t groups = (a.N + 15) / 16;
+        auto go = [&](auto waves) {
+            hipLaunchKernelGGL(gated_few_rows_kernel<decltype(waves)::value>, dim3((unsigned)groups), dim3(decltype(waves)::value * 64), 0, stream, a);
+            return hipGetLastError();
+        };
+        return groups <= 128 && a.K > 1024 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 4>{});
     }
     const GatedForm form = gated_form(a.M, a.N, a.K);
     if (form.shape >= 0) return with_gated(form.shape, [&](auto k) { return decltype(k)::launch(a, stream); });

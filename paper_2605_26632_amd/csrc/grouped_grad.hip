@@ -15,6 +15,7 @@
 // 8192 rows, [4096, 2048], eight experts, inputs that change: input gradient 122 us with 1024 rows each, 161 with 484 to 1997 (216 tall and 104 half
 // tiles: the units are active 65 % of the launch); weight gradient 141 and 143. Matrix cores busy 42 and 43 % at 2.18 GHz, uneven.
 #include <cmath>
+#include <mutex>
 #include "groups.h"
 
 namespace rtl {
@@ -435,89 +436,155 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
 
 // Both gradients of one linear in one launch: the tiles of the longer contraction first, then the others, each workgroup to the unit that frees first. One
 // after the other, each of the two would end with units idle: a gated linear's [4096, 2 x 8192, 2048] has 128 tiles of 256 x 256 in dX, of 256 stages
-// each, and 512 in dW, of 64; 128 units with a tile of dX each and four of dW on each of the others end together.
+// each, and 512 in dW, of 64; 128 units with a tile of dX each and four of dW on each of the others end together. Where there are few tiles the
+// contractions are cut into parts, whose fp32 planes pair_reduce_kernel adds up.
 struct PairArgs {
     GradArgs d, w;           // input and weight gradient
-    int nd, nw, parts;       // tiles of each, those of dW in each of `parts` parts of its contraction
-    int64_t w_plane, sums_plane;      // elements between the parts' planes
+    int nd, nw, d_parts, w_parts;      // tiles of each, in that many parts of their contraction
+    int64_t d_plane, w_plane, sums_plane;      // elements between the parts' planes
     bool w_first;
 };
-template <bool F32, int DM, int WM, int BN, int THREADS>
+// D_F32, W_F32: fp32 results (planes).
+template <bool D_F32, bool W_F32, int DM, int WM, int BN, int THREADS, int RING>
 __global__ __launch_bounds__(THREADS) void grad_pair_kernel(const PairArgs a) {
     constexpr bool BIG = THREADS == 512;
-    const int all_w = a.nw * a.parts, pad_d = (a.nd + 7) / 8 * 8, pad_w = (all_w + 7) / 8 * 8;
+    const int all_d = a.nd * a.d_parts, all_w = a.nw * a.w_parts, pad_d = (all_d + 7) / 8 * 8, pad_w = (all_w + 7) / 8 * 8;
     int id = (int)blockIdx.x;
     const int lead = a.w_first ? pad_w : pad_d;
     const bool is_w = (id < lead) == a.w_first;
     if (id >= lead) id -= lead;
-    const int n = is_w ? all_w : a.nd, xcd = id % 8, t = xcd_share_start(n, xcd) + id / 8;       // an XCD's share: neighbouring tiles
+    const int n = is_w ? all_w : all_d, xcd = id % 8, t = xcd_share_start(n, xcd) + id / 8;       // an XCD's share: neighbouring tiles
     if (t >= xcd_share_start(n, xcd + 1)) return;
     int pm, pn;
     if (is_w) {
         const int part = t / a.nw;
         GradArgs g = a.w;
-        if constexpr (F32) {
+        if constexpr (W_F32) {
             g.C = static_cast<float*>(g.C) + part * a.w_plane;
             if (g.row_sums) g.row_sums = static_cast<float*>(g.row_sums) + part * a.sums_plane;
         }
         tile_walk<8>(t % a.nw, (int)((g.m + WM - 1) / WM), (int)((g.n + BN - 1) / BN), pm, pn);
-        if constexpr (!BIG) grad_tile<true, F32, WM, BN, 2, 2, 4>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.parts);
-        else grad_tile<true, F32, WM, BN, 2, 4, WM == 256 ? 2 : 3>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.parts);
+        if constexpr (!BIG) grad_tile<true, W_F32, WM, BN, 2, 2, RING>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.w_parts);
+        else grad_tile<true, W_F32, WM, BN, 2, 4, WM == 256 ? 2 : 3>(g, (int64_t)pm * WM, (int64_t)pn * BN, part, a.w_parts);
     } else {
-        tile_walk<(DM >= 256 ? 8 : 16)>(t, (int)((a.d.m + DM - 1) / DM), (int)((a.d.n + BN - 1) / BN), pm, pn);
-        if constexpr (!BIG) grad_tile<false, false, DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, 4>(a.d, (int64_t)pm * DM, (int64_t)pn * BN);
-        else grad_tile<false, false, DM, BN, 2, 4, DM == 256 ? 2 : 3>(a.d, (int64_t)pm * DM, (int64_t)pn * BN);
+        const int part = t / a.nd;
+        GradArgs g = a.d;
+        if constexpr (D_F32) g.C = static_cast<float*>(g.C) + part * a.d_plane;
+        tile_walk<(DM >= 256 ? 8 : 16)>(t % a.nd, (int)((g.m + DM - 1) / DM), (int)((g.n + BN - 1) / BN), pm, pn);
+        if constexpr (!BIG) grad_tile<false, D_F32, DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, RING>(g, (int64_t)pm * DM, (int64_t)pn * BN, part, a.d_parts);
+        else grad_tile<false, D_F32, DM, BN, 2, 4, DM == 256 ? 2 : 3>(g, (int64_t)pm * DM, (int64_t)pn * BN, part, a.d_parts);
     }
 }
 
-template <int DM, int WM, int BN, int THREADS>
-struct Pair {
-    static constexpr bool kBig = THREADS == 512;
-    using LD = std::conditional_t<kBig, GradSmem<DM, BN, 2, 4, DM == 256 ? 2 : 3>, GradSmem<DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, 4>>;
-    using LW = std::conditional_t<kBig, GradSmem<WM, BN, 2, 4, WM == 256 ? 2 : 3>, GradSmem<WM, BN, 2, 2, 4>>;
-    static constexpr int kLds = LD::kTotal > LW::kTotal ? LD::kTotal : LW::kTotal;
-    static hipError_t prepare() {
-        auto limit = [](const void* k) { return hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kLds); };
-        const hipError_t e = limit(reinterpret_cast<const void*>(grad_pair_kernel<false, DM, WM, BN, THREADS>));
-        return e != hipSuccess ? e : limit(reinterpret_cast<const void*>(grad_pair_kernel<true, DM, WM, BN, THREADS>));
+// Adds the parts' planes up in order: four columns of dW to a thread, behind them one of the bias gradient, behind those four columns of dX.
+struct PairReduceArgs {
+    const float *w, *sums, *d;       // planes; NULL: that result is there already
+    void *dw, *dbias;
+    uint16_t* dx;
+    int64_t N, K, M, lddw, lddx;
+    int w_parts, d_parts;
+    bool f32;
+};
+__global__ __launch_bounds__(256) void pair_reduce_kernel(const PairReduceArgs a) {
+    int64_t q = blockIdx.x * (int64_t)256 + threadIdx.x;
+    const int64_t K4 = a.K / 4, all_w = a.w ? a.N * K4 : 0, all_s = a.sums ? a.N : 0;
+    auto four = [](const float* p, int64_t plane, int parts) {
+        float4 s = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+        for (int i = 1; i < parts; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(p + i * plane);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        return s;
+    };
+    auto rounded = [](const float4& s) {
+        return make_uint2(f32_to_bf16_rne(s.x) | f32_to_bf16_rne(s.y) << 16, f32_to_bf16_rne(s.z) | f32_to_bf16_rne(s.w) << 16);
+    };
+    if (q < all_w) {
+        const int64_t row = q / K4, col = q % K4 * 4, at = row * a.lddw + col;
+        const float4 s = four(a.w + row * a.K + col, a.N * a.K, a.w_parts);
+        if (a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at) = s;
+        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.dw) + at) = rounded(s);
+        return;
     }
-    static hipError_t launch(const PairArgs& a, bool f32, hipStream_t stream) {
-        const dim3 grid((unsigned)((a.nd + 7) / 8 * 8 + (a.nw * a.parts + 7) / 8 * 8)), block(THREADS);
-        if (f32) hipLaunchKernelGGL((grad_pair_kernel<true, DM, WM, BN, THREADS>), grid, block, kLds, stream, a);
-        else hipLaunchKernelGGL((grad_pair_kernel<false, DM, WM, BN, THREADS>), grid, block, kLds, stream, a);
-        return hipGetLastError();
+    q -= all_w;
+    if (q < all_s) {
+        float s = a.sums[q];
+        for (int i = 1; i < a.w_parts; ++i) s += a.sums[i * a.N + q];
+        if (a.f32) static_cast<float*>(a.dbias)[q] = s;
+        else static_cast<uint16_t*>(a.dbias)[q] = (uint16_t)f32_to_bf16_rne(s);
+        return;
+    }
+    q -= all_s;
+    if (!a.d || q >= a.M * K4) return;
+    const int64_t row = q / K4, col = q % K4 * 4;
+    *reinterpret_cast<uint2*>(a.dx + row * a.lddx + col) = rounded(four(a.d + row * a.K + col, a.M * a.K, a.d_parts));
+}
+
+template <int DM, int WM, int BN, int THREADS, int RING>
+struct Pair {
+    static constexpr bool kBig = THREADS == 512, kDParts = DM < 256;       // (tall tiles of dX are never cut into parts)
+    using LD = std::conditional_t<kBig, GradSmem<DM, BN, 2, 4, DM == 256 ? 2 : 3>, GradSmem<DM, BN, DM == 64 ? 1 : 2, DM == 64 ? 4 : 2, RING>>;
+    using LW = std::conditional_t<kBig, GradSmem<WM, BN, 2, 4, WM == 256 ? 2 : 3>, GradSmem<WM, BN, 2, 2, RING>>;
+    static constexpr int kLds = LD::kTotal > LW::kTotal ? LD::kTotal : LW::kTotal;
+    template <class F>
+    static hipError_t kernels(F f) {
+        hipError_t e = f(std::false_type{}, std::false_type{});
+        if (e == hipSuccess) e = f(std::false_type{}, std::true_type{});
+        if constexpr (kDParts) {
+            if (e == hipSuccess) e = f(std::true_type{}, std::false_type{});
+            if (e == hipSuccess) e = f(std::true_type{}, std::true_type{});
+        }
+        return e;
+    }
+    static hipError_t prepare() {
+        return kernels([](auto d, auto w) {
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(grad_pair_kernel<decltype(d)::value, decltype(w)::value, DM, WM, BN, THREADS, RING>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        });
+    }
+    static hipError_t launch(const PairArgs& a, bool d_f32, bool w_f32, hipStream_t stream) {
+        const dim3 grid((unsigned)((a.nd * a.d_parts + 7) / 8 * 8 + (a.nw * a.w_parts + 7) / 8 * 8));
+        return kernels([&](auto d, auto w) {
+            if (decltype(d)::value != d_f32 || decltype(w)::value != w_f32) return hipSuccess;
+            hipLaunchKernelGGL((grad_pair_kernel<decltype(d)::value, decltype(w)::value, DM, WM, BN, THREADS, RING>), grid, dim3(THREADS), kLds, stream, a);
+            return hipGetLastError();
+        });
     }
 };
 template <class Op>
 hipError_t with_pair(int form, Op op) {
     switch (form) {
-        case 0: return op(Pair<64, 128, 128, 256>{});
-        case 1: return op(Pair<128, 128, 128, 256>{});
-        case 2: return op(Pair<128, 128, 256, 512>{});
-        case 3: return op(Pair<128, 256, 256, 512>{});
-        case 4: return op(Pair<256, 128, 256, 512>{});
-        default: return op(Pair<256, 256, 256, 512>{});
+        case 0: return op(Pair<64, 128, 128, 256, 4>{});
+        case 1: return op(Pair<128, 128, 128, 256, 4>{});
+        case 2: return op(Pair<64, 128, 128, 256, 2>{});
+        case 3: return op(Pair<128, 128, 256, 512, 0>{});
+        case 4: return op(Pair<128, 256, 256, 512, 0>{});
+        case 5: return op(Pair<256, 128, 256, 512, 0>{});
+        default: return op(Pair<256, 256, 256, 512, 0>{});
     }
 }
-constexpr int kPairForms = 6;
+constexpr int kPairForms = 7;
 struct PairShape {
-    int dm, wm, bn;
+    int dm, wm, bn, units;                           // units: workgroups that run at a time
     double d_fixed, d_stage, w_fixed, w_stage;       // us of a tile with every unit at work (dgrad_shape, wgrad_plan)
 };
-constexpr PairShape kPairShapes[kPairForms] = {{64, 128, 128, 3.8, 0.305, 4.8, 0.53}, {128, 128, 128, 4.8, 0.53, 4.8, 0.53}, {128, 128, 256, 8, 0.78, 8, 0.78},
-                                               {128, 256, 256, 8, 0.78, 9, 1.5},      {256, 128, 256, 8, 1.5, 8, 0.78},      {256, 256, 256, 8, 1.5, 9, 1.5}};
+// A ring of two leaves room for two workgroups a unit, which hide each other's beginnings and ends and take twice as long for a stage.
+constexpr PairShape kPairShapes[kPairForms] = {
+    {64, 128, 128, 256, 3.8, 0.305, 4.8, 0.53}, {128, 128, 128, 256, 4.8, 0.53, 4.8, 0.53}, {64, 128, 128, 512, 5.0, 0.65, 6.0, 1.06},
+    {128, 128, 256, 256, 8, 0.78, 8, 0.78},     {128, 256, 256, 256, 8, 0.78, 9, 1.5},      {256, 128, 256, 256, 8, 1.5, 8, 0.78}, {256, 256, 256, 256, 8, 1.5, 9, 1.5}};
 
-// End of n1 tiles of t1 and then n2 of t2, each to the unit that frees first (as mixed_time; t1 >= t2).
-double pair_time(int64_t n1, double t1, int64_t n2, double t2) {
-    const int64_t x = n1 % kUnits;
-    const double a = (double)(n1 / kUnits) * t1, b = x ? a + t1 : a;                 // when the units are done with the first, x of them at b
+// End of n1 tiles of t1 and then n2 of t2 on `units`, each to the one that frees first (as mixed_time; t1 >= t2).
+double pair_time(int units, int64_t n1, double t1, int64_t n2, double t2) {
+    const int64_t x = n1 % units;
+    const double a = (double)(n1 / units) * t1, b = x ? a + t1 : a;                 // when the units are done with the first, x of them at b
     if (n2 == 0) return b;
-    const double least = (a * (double)(kUnits - x) + b * (double)x + (double)n2 * t2) / kUnits;
+    const double least = (a * (double)(units - x) + b * (double)x + (double)n2 * t2) / units;
     double best = 1e30;
     for (int k = 0; k < 3; ++k)
         for (double from : {a, b}) {
             const double rounds = ceil((least - from) / t2 - 0.001) + k, end = from + (rounds > 0 ? rounds : 0) * t2;
-            const double held = (double)(kUnits - x) * floor((end - a) / t2 + 0.001) + (end >= b ? (double)x * floor((end - b) / t2 + 0.001) : 0.0);
+            const double held = (double)(units - x) * floor((end - a) / t2 + 0.001) + (end >= b ? (double)x * floor((end - b) / t2 + 0.001) : 0.0);
             if (held >= (double)n2 && end < best) best = end;
         }
     return best > b ? best : b;
@@ -676,48 +743,67 @@ int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room) {
 }
 
 struct PairPlan {
-    int form, parts;
+    int form, d_parts, w_parts;
     int64_t nd, nw;
     bool w_first;
+    size_t w_bytes, d_bytes;         // planes
 };
-// The tiles of both gradients, and in how many parts the rows of the weight gradient are cut (wgrad_plan), by the end of the launch.
-static PairPlan pair_plan(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
-    PairPlan plan{0, 1, 0, 0, false};
+// The tiles of both gradients, and in how many parts their contractions are cut, by the end of the launch and, with parts, of the second one that adds the planes
+// up (3.5 us and the planes' way there and back at 3.5 TB/s).
+static PairPlan make_pair_plan(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
+    PairPlan plan{0, 1, 1, 0, 0, false, 0, 0};
     double best = 1e30;
+    const double d_stages = (double)((N + 63) / 64), w_stages = (double)((M + 63) / 64);
     for (int i = 0; i < kPairForms; ++i) {
         const PairShape& s = kPairShapes[i];
         const int64_t across = (K + s.bn - 1) / s.bn, nd = dx ? (M + s.dm - 1) / s.dm * across : 0, nw = dw ? (N + s.wm - 1) / s.wm * across : 0;
-        const double td = s.d_fixed + s.d_stage * (double)((N + 63) / 64), stages = (double)((M + 63) / 64);
-        for (int parts = 1; parts == 1 || (dw && parts <= 64 && (double)(parts * 2) <= stages); parts *= 2) {
-            const double bytes = parts > 1 ? (double)parts * (double)wgrad_plane(1, N, K) : 0.0;
-            if (bytes > (double)room) break;
-            const double tw = s.w_fixed + s.w_stage * stages / parts;
-            double us = tw > td ? pair_time(nw * parts, tw, nd, td) : pair_time(nd, td, nw * parts, tw);
-            if (parts > 1) us = (us + 3.5 + bytes * 2 / 3.5e6) / 0.95;
-            if (us < best) {
-                best = us;
-                plan = PairPlan{i, parts, nd, nw, tw > td};
+        for (int dp = 1; dp == 1 || (dx && s.dm < 256 && dp <= 64 && (double)(dp * 2) <= d_stages && nd * dp <= 2 * s.units); dp *= 2)
+            for (int wp = 1; wp == 1 || (dw && wp <= 64 && (double)(wp * 2) <= w_stages && nw * wp <= 2 * s.units); wp *= 2) {
+                const size_t w_bytes = wp > 1 ? (size_t)wp * wgrad_plane(1, N, K) : 0, d_bytes = dp > 1 ? (size_t)dp * (size_t)M * (size_t)K * 4 : 0;
+                if (w_bytes + d_bytes > room) continue;
+                const double td = s.d_fixed + s.d_stage * d_stages / dp, tw = s.w_fixed + s.w_stage * w_stages / wp;
+                double us = tw > td ? pair_time(s.units, nw * wp, tw, nd * dp, td) : pair_time(s.units, nd * dp, td, nw * wp, tw);
+                if (w_bytes + d_bytes) us = (us + 3.5 + (double)(w_bytes + d_bytes) * 2 / 3.5e6) / 0.95;
+                if (us < best) {
+                    best = us;
+                    plan = PairPlan{i, dp, wp, nd, nw, tw > td, w_bytes, d_bytes};
+                }
             }
-        }
     }
     return plan;
 }
-void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[2]) {
+// (several microseconds of host time: kept per problem, the last one of each place of a table)
+static PairPlan pair_plan(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
+    struct Entry {
+        int64_t M, N, K;
+        size_t room;
+        bool dx, dw, set;
+        PairPlan plan;
+    };
+    static Entry table[256];
+    static std::mutex mu;
+    Entry& e = table[((uint64_t)(M * 31 + N * 7 + K) * 2654435761u + room / 256 * 40503u + dx * 2 + dw) % 256];
+    std::lock_guard<std::mutex> lock(mu);
+    if (!e.set || e.M != M || e.N != N || e.K != K || e.dx != dx || e.dw != dw || e.room != room) e = Entry{M, N, K, room, dx, dw, true, make_pair_plan(M, N, K, dx, dw, room)};
+    return e.plan;
+}
+void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[3]) {
     const PairPlan plan = pair_plan(M, N, K, dx, dw, room);
     out[0] = plan.form;
-    out[1] = plan.parts;
+    out[1] = plan.d_parts;
+    out[2] = plan.w_parts;
 }
 size_t grad_pair_workspace(int64_t M, int64_t N, int64_t K, size_t room) {
     size_t most = 0;
-    for (bool dx : {false, true}) {
-        const int parts = pair_plan(M, N, K, dx, true, room).parts;
-        if (parts > 1 && (size_t)parts * wgrad_plane(1, N, K) > most) most = (size_t)parts * wgrad_plane(1, N, K);
+    for (int i = 1; i < 4; ++i) {
+        const PairPlan plan = pair_plan(M, N, K, (i & 1) != 0, (i & 2) != 0, room);
+        if (plan.w_bytes + plan.d_bytes > most) most = plan.w_bytes + plan.d_bytes;
     }
     return most;
 }
 int64_t grad_pair_grid(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room) {
     const PairPlan plan = pair_plan(M, N, K, dx, dw, room);
-    return (plan.nd + plan.nw * plan.parts + 16) * (plan.form >= 2 ? 2 : 1);
+    return (plan.nd * plan.d_parts + plan.nw * plan.w_parts + 16) * (plan.form >= 3 ? 2 : 1);
 }
 
 hipError_t launch_grad_pair(const GroupedGradArgs& a, void* dx, int64_t lddx, void* workspace, size_t room, hipStream_t stream) {
@@ -727,24 +813,35 @@ hipError_t launch_grad_pair(const GroupedGradArgs& a, void* dx, int64_t lddx, vo
     if (a.out) p.w = GradArgs{a.dY, a.X, a.out, a.bias_out, a.lddy, a.ldx, a.ldo, a.N, a.K, a.T};
     p.nd = (int)plan.nd;
     p.nw = (int)plan.nw;
-    p.parts = plan.parts;
+    p.d_parts = plan.d_parts;
+    p.w_parts = plan.w_parts;
     p.w_first = plan.w_first;
-    float* const planes = static_cast<float*>(workspace);
-    float* const bias_planes = planes + (size_t)plan.parts * a.N * a.K;
-    if (plan.parts > 1) {
-        p.w.C = planes;
-        p.w.row_sums = a.bias_out ? bias_planes : nullptr;
+    // workspace: [planes of dW | of the bias gradient | of dX]
+    PairReduceArgs r{nullptr, nullptr, nullptr, a.out, a.bias_out, static_cast<uint16_t*>(dx), a.N, a.K, a.T, a.ldo, lddx, plan.w_parts, plan.d_parts, a.f32};
+    float* at = static_cast<float*>(workspace);
+    if (plan.w_parts > 1) {
+        p.w.C = at;
         p.w.ldc = a.K;
         p.w_plane = a.N * a.K;
-        p.sums_plane = a.N;
+        r.w = at;
+        at += (size_t)plan.w_parts * a.N * a.K;
+        if (a.bias_out) {
+            p.w.row_sums = at;
+            p.sums_plane = a.N;
+            r.sums = at;
+        }
+        at += (size_t)plan.w_parts * a.N;
     }
-    const hipError_t e = with_pair(plan.form, [&](auto k) { return decltype(k)::launch(p, a.f32 || plan.parts > 1, stream); });
-    if (e != hipSuccess || plan.parts == 1) return e;
-    GroupedGradArgs r = a;
-    r.parts = plan.parts;
-    r.o_stride = 0;
-    const int64_t work = a.N * (a.K / 4) + (a.bias_out ? a.N : 0);
-    hipLaunchKernelGGL(wgrad_reduce_kernel, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, stream, r, planes, bias_planes);
+    if (plan.d_parts > 1) {
+        p.d.C = at;
+        p.d.ldc = a.K;
+        p.d_plane = a.T * a.K;
+        r.d = at;
+    }
+    const hipError_t e = with_pair(plan.form, [&](auto k) { return decltype(k)::launch(p, plan.d_parts > 1, a.f32 || plan.w_parts > 1, stream); });
+    if (e != hipSuccess || (!r.w && !r.d)) return e;
+    const int64_t work = (r.w ? a.N * (a.K / 4) : 0) + (r.sums ? a.N : 0) + (r.d ? a.T * (a.K / 4) : 0);
+    hipLaunchKernelGGL(pair_reduce_kernel, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, stream, r);
     return hipGetLastError();
 }
 

@@ -204,10 +204,10 @@ int64_t wgrad_grid(int64_t T, int64_t E, int64_t N, int64_t K, size_t room);
 hipError_t launch_grouped_wgrad(const GroupedGradArgs& a, void* workspace, size_t room, hipStream_t stream);
 
 // Both gradients of one linear in one launch (a second one where the rows are cut into parts): a as for the weight gradient, with W, ldw for dX [T,K] (lddx);
-// dx or a.out may be NULL. room: bytes of the workspace for partial planes, of which grad_pair_workspace would be used. pair_choice: the form, parts (tests).
+// dx or a.out may be NULL. room: bytes of the workspace for partial planes, of which grad_pair_workspace would be used. pair_choice: the form, parts of dX's and dW's contraction (tests).
 size_t grad_pair_workspace(int64_t M, int64_t N, int64_t K, size_t room);
 int64_t grad_pair_grid(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room);
-void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[2]);
+void pair_choice(int64_t M, int64_t N, int64_t K, bool dx, bool dw, size_t room, int out[3]);
 hipError_t launch_grad_pair(const GroupedGradArgs& a, void* dx, int64_t lddx, void* workspace, size_t room, hipStream_t stream);
 
 // ---- gated linears (gated.hip) -------------------------------------------------------------------
