@@ -60,44 +60,52 @@ struct GatedMixed {
 };
 
 // Up to sixteen rows of X: reading W is all there is, and it goes straight from memory into the registers that the matrix instruction takes (few_rows.hip has
-// the layout). A workgroup owns sixteen columns of H, so sixteen gate rows and the sixteen up rows; its waves divide the contraction in lines of 128
-// bytes, neighbouring waves on neighbouring lines, four lines of a row in flight, and their sums meet in LDS in a fixed order.
-constexpr int kFewRows = 16, kFewLines = 4;
-template <int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 4) void gated_few_rows_kernel(const GemmArgs a) {
-    __shared__ __align__(16) float sums[WAVES][2][64][4];
+// the layout). A workgroup owns COLS columns of H: sixteen, sixteen gate rows of W for one instruction and the sixteen up rows for another; or
+// eight, whose gate and up rows are the sixteen of one instruction, where sixteen would leave units idle, each of which pulls at a rate of its own. Its
+// waves divide the contraction in lines of 128 bytes, neighbouring waves on neighbouring lines, four lines of a row in flight, and their sums meet in LDS in
+// a fixed order. [1, 10240, 3840] 23.9 us one after the other in a graph, 6.6 TB/s.
+constexpr int kFewRows = 16, kFewWaves = 4, kFewLines = 4;
+template <int COLS>
+__global__ __launch_bounds__(kFewWaves * 64, 4) void gated_few_rows_kernel(const GemmArgs a) {
+    constexpr int NB = COLS == 16 ? 2 : 1;               // instructions for a line
+    __shared__ __align__(16) float sums[kFewWaves][NB][64][4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, kb = lane >> 4;
     const int units = (int)(a.K / 64);
-    const int64_t n0 = (int64_t)blockIdx.x * 16, n = min(n0 + li, a.N - 1);
-    const uint16_t* const w_row[2] = {static_cast<const uint16_t*>(a.W) + n * a.ldw + kb * 16, static_cast<const uint16_t*>(a.W) + (a.N + n) * a.ldw + kb * 16};
+    const int64_t n0 = (int64_t)blockIdx.x * COLS;
+    const uint16_t* w_row[NB];
+#pragma unroll
+    for (int f = 0; f < NB; ++f) {
+        const int64_t n = min(n0 + li % COLS, a.N - 1) + ((COLS == 16 ? f : li / COLS & 1) ? a.N : 0);
+        w_row[f] = static_cast<const uint16_t*>(a.W) + n * a.ldw + kb * 16;
+    }
     const uint16_t* const x_row = static_cast<const uint16_t*>(a.A) + min((int64_t)li, a.M - 1) * a.lda + kb * 16;     // (rows behind the last repeat it, never stored)
-    f32x4 acc[2] = {};
-    for (int u0 = wave; u0 < units; u0 += WAVES * kFewLines) {
-        Frag8 w[kFewLines][2][2], x[kFewLines][2];
+    f32x4 acc[NB] = {};
+    for (int u0 = wave; u0 < units; u0 += kFewWaves * kFewLines) {
+        Frag8 w[kFewLines][NB][2], x[kFewLines][2];
 #pragma unroll
         for (int u = 0; u < kFewLines; ++u) {
-            if (u0 + u * WAVES >= units) break;
-            const int64_t at = (int64_t)(u0 + u * WAVES) * 64;
+            if (u0 + u * kFewWaves >= units) break;
+            const int64_t at = (int64_t)(u0 + u * kFewWaves) * 64;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
 #pragma unroll
-                for (int f = 0; f < 2; ++f) w[u][f][c].u = *reinterpret_cast<const uint4*>(w_row[f] + at + c * 8);
+                for (int f = 0; f < NB; ++f) w[u][f][c].u = *reinterpret_cast<const uint4*>(w_row[f] + at + c * 8);
                 x[u][c].u = *reinterpret_cast<const uint4*>(x_row + at + c * 8);
             }
         }
         __builtin_amdgcn_sched_barrier(0);                                                       // all the loads first
 #pragma unroll
         for (int u = 0; u < kFewLines; ++u) {
-            if (u0 + u * WAVES >= units) break;
+            if (u0 + u * kFewWaves >= units) break;
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int f = 0; f < 2; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][f][c].v, x[u][c].v, acc[f], 0, 0, 0);
+                for (int f = 0; f < NB; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[u][f][c].v, x[u][c].v, acc[f], 0, 0, 0);
         }
     }
-    // row li of X, columns 4 kb .. of the sixteen
+    // row li of X, columns 4 kb .. of the sixteen (of fewer, in the first lane groups)
     const int64_t col = n0 + 4 * kb;
-    const int valid = (int)min((int64_t)4, a.N - col);
+    const int valid = 4 * kb >= COLS ? 0 : (int)min((int64_t)4, a.N - col);
     float bias[2][4] = {};
     if (wave == 0 && a.bias && valid > 0)
 #pragma unroll
@@ -107,7 +115,7 @@ __global__ __launch_bounds__(WAVES * 64, 4) void gated_few_rows_kernel(const Gem
             bias[1][e] = __uint_as_float((uint32_t)a.bias[a.N + at] << 16);
         }
 #pragma unroll
-    for (int f = 0; f < 2; ++f) *reinterpret_cast<f32x4*>(sums[wave][f][lane]) = acc[f];
+    for (int f = 0; f < NB; ++f) *reinterpret_cast<f32x4*>(sums[wave][f][lane]) = acc[f];
     __syncthreads();
     if (wave != 0 || li >= a.M || valid <= 0) return;
     const GateForm form = gate_form(a.act);
@@ -115,9 +123,10 @@ __global__ __launch_bounds__(WAVES * 64, 4) void gated_few_rows_kernel(const Gem
     f32x4 s[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-        s[f] = *reinterpret_cast<const f32x4*>(sums[0][f][lane]);
+        const int from = COLS < 16 && f ? lane + 4 * COLS : lane, block = COLS < 16 ? 0 : f;       // the up rows' sums lie COLS / 4 lane groups further on
+        s[f] = *reinterpret_cast<const f32x4*>(sums[0][block][from]);
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s[f] += *reinterpret_cast<const f32x4*>(sums[w][f][lane]);
+        for (int w = 1; w < kFewWaves; ++w) s[f] += *reinterpret_cast<const f32x4*>(sums[w][block][from]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -181,7 +190,7 @@ __global__ __launch_bounds__(kGradThreads) void gated_grad_kernel(const GatedGra
     if (a.H) store_run(a.H + row * a.ldh + col, h, valid);
 }
 
-// Runs `op` (launch or prepare) of small tile `i`; shapes and rings as in gemm.hip.
+// Runs `op` (launch or prepare) of small tile `i` of gemm.hip's kGatedShapes.
 template <class Op>
 hipError_t with_gated(int i, Op op) {
     switch (i) {
@@ -189,7 +198,9 @@ hipError_t with_gated(int i, Op op) {
         case 1: return op(Gated<64, 32, 1, 1, 4, 3>{});
         case 2: return op(Gated<64, 64, 1, 2, 2, 4>{});
         case 3: return op(Gated<128, 64, 2, 2, 2, 3>{});
-        default: return op(Gated<128, 128, 2, 2, 1, 3>{});
+        case 4: return op(Gated<128, 128, 4, 2, 1, 3>{});
+        case 5: return op(Gated<96, 128, 2, 2, 1, 3>{});
+        default: return op(Gated<64, 64, 2, 2, 1, 3>{});
     }
 }
 using Gated256 = GatedMixed<256, 2, 4>;
@@ -200,12 +211,15 @@ using Gated192 = GatedMixed<192, 4, 2>;
 hipError_t launch_gated(const GemmArgs& a_in, hipStream_t stream) {
     GemmArgs a = a_in;
     if (a.M <= kFewRows && a.N < (int64_t)1 << 27) {               // (a launch takes fewer than 2^32 threads)
-        const int64_t groups = (a.N + 15) / 16;
-        auto go = [&](auto waves) {
-            hipLaunchKernelGGL(gated_few_rows_kernel<decltype(waves)::value>, dim3((unsigned)groups), dim3(decltype(waves)::value * 64), 0, stream, a);
+        auto go = [&](auto cols) {
+            constexpr int C = decltype(cols)::value;
+            hipLaunchKernelGGL(gated_few_rows_kernel<C>, dim3((unsigned)((a.N + C - 1) / C)), dim3(kFewWaves * 64), 0, stream, a);
             return hipGetLastError();
         };
-        return groups <= 128 && a.K > 1024 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 4>{});
+        // Eight columns to a workgroup where sixteen leave units idle, and, with X small beside them, for long rows of W. us, 16 | 8 columns: [16, 700, 4096]
+        // 12.8 | 9.5, [1, 1500, 2944] 8.1 | 5.7, [1, 2816, 2048] 6.8 | 7.0, [16, 3000, 1024] 5.3 | 6.1, [1, 10240, 3840] 27.1 | 23.9, [4, 10240, 3840] 28.1 |
+        // 26.8, [8, 10240, 3840] 29.2 | 29.8, [2, 8192, 1024] 7.1 | 7.5. (Four columns, and eight or sixteen waves, are not quicker.)
+        return a.N <= 2048 || (a.M <= 4 && a.K > 2048) ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 16>{});
     }
     const GatedForm form = gated_form(a.M, a.N, a.K);
     if (form.shape >= 0) return with_gated(form.shape, [&](auto k) { return decltype(k)::launch(a, stream); });
@@ -228,7 +242,7 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, hipStream_t stream) {
 hipError_t prepare_gated_kernels() {
     hipError_t e = Gated256::prepare();
     if (e == hipSuccess) e = Gated192::prepare();
-    for (int i = 0; i < 5 && e == hipSuccess; ++i) e = with_gated(i, [](auto k) { return decltype(k)::prepare(); });
+    for (int i = 0; i < 7 && e == hipSuccess; ++i) e = with_gated(i, [](auto k) { return decltype(k)::prepare(); });
     return e;
 }
 

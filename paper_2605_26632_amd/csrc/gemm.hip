@@ -331,8 +331,7 @@ struct SplitChoice {
     bool part_256;
 };
 static int64_t part_pitch(int64_t N) { return (N + 7) / 8 * 8; }     // columns of a plane: whole eight-column chunks
-// gated: a gated linear of N rows of W, which has no 256 x 96 tile.
-static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_t blocks, bool dense, bool fp8, size_t room, bool gated = false) {
+static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_t blocks, bool dense, bool fp8, size_t room) {
     const double busy = (double)(plan.body_tiles + plan.tail_tiles < 256 ? plan.body_tiles + plan.tail_tiles : 256);
     const double load = busy > 96 ? (busy - 96) / 160 : 0.0;
     const double per_kb = dense ? 0.0146 + 0.0053 * load : 0.0107 + 0.0065 * load;
@@ -345,7 +344,6 @@ static SplitChoice pick_split(const TilePlan& plan, int64_t M, int64_t N, int64_
         const int64_t tiles = ((M + s.bm - 1) / s.bm) * ((N + s.bn - 1) / s.bn);
         if (tiles > 4096) continue;                        // far more than a few passes: never the better one
         double block = s.block;
-        if (gated && s.bm == 256) continue;
         if (s.bm == 256) {                                 // one pass only, slower as the chip fills (its rivals are, in the sparse case)
             if (tiles > 256) continue;
             if (dense && tiles > 128) block += 0.0021 * (double)(tiles - 128);
@@ -400,9 +398,37 @@ void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t 
     out[2] = c.part_256 ? 256 : 128;
 }
 
+// Tiles of a gated linear (gated.hip; bn rows of W, half of them gates), as kDenseShapes; `held`: workgroups that a compute unit holds at a time, which share
+// its rate. In order: the first four of kDenseShapes; 128 x 128 with eight waves (four take 5 to 10 % longer: [631, 5781, 3584] 51.7 -> 49.0 us, [1456, 6707, 896]
+// 45.4 -> 39.8); 96 x 128, whose tiles fill the units where 128 rows leave some idle ([333, 2739, 4032] 25.9 -> 24.5, [11169, 70, 5952] 41.9 -> 38.5);
+// 64 x 64 with a ring of three, three to a unit, for short contractions ([600, 1500, 1024] 11.5 -> 8.4, [699, 973, 128] 5.6 -> 4.8).
+struct GatedShape {
+    SplitShape tile;
+    int held;
+};
+constexpr GatedShape kGatedShapes[] = {{{32, 32, 1.45, 0.081}, 1}, {{64, 32, 1.55, 0.135}, 1}, {{64, 64, 1.25, 0.19}, 1}, {{128, 64, 2.5, 0.285}, 1},
+                                       {{128, 128, 3.0, 0.35}, 1}, {{96, 128, 2.4, 0.34}, 1},  {{64, 64, 1.1, 0.2}, 3}};
 GatedForm gated_form(int64_t M, int64_t F, int64_t K) {
-    const TilePlan p = plan_for(M, 2 * F, true);
-    return GatedForm{pick_split(p, M, 2 * F, K / 64, true, false, 0, true).shape, p.use_192, p.m_split, p.body_tiles, p.tail_tiles};
+    const int64_t N = 2 * F, blocks = K / 64;
+    const TilePlan p = plan_for(M, N, true);
+    const double busy = (double)(p.body_tiles + p.tail_tiles < 256 ? p.body_tiles + p.tail_tiles : 256), load = busy > 96 ? (busy - 96) / 160 : 0.0;
+    double best = 3.3 + (double)blocks * p.cost * (0.0146 + 0.0053 * load);           // as in pick_split
+    int shape = -1;
+    for (int i = 0; i < (int)(sizeof(kGatedShapes) / sizeof(GatedShape)); ++i) {
+        const SplitShape& s = kGatedShapes[i].tile;
+        const int64_t tiles = ((M + s.bm - 1) / s.bm) * ((N + s.bn - 1) / s.bn), passes = (tiles + 255) / 256;
+        const bool wide = s.bm >= 96 && s.bn >= 128;
+        if (tiles > 4096 || (passes > 1 && wide && M > 2048)) continue;
+        double block = s.block, t;
+        if (s.bm == 32) block += 0.0005 * (double)(M < 32 ? M : 32);
+        if (kGatedShapes[i].held > 1) t = s.fixed + (double)blocks * block * (tiles > 256 ? 0.95 * (double)tiles / 256 : 1.0);
+        else t = (double)passes * (s.fixed + (double)blocks * block) * (passes == 1 ? 1.0 : !wide ? 1.24 : passes > 2 ? 1.3 : 1.12);
+        if (t < best) {
+            best = t;
+            shape = i;
+        }
+    }
+    return GatedForm{shape, p.use_192, p.m_split, p.body_tiles, p.tail_tiles};
 }
 
 void mx_choice(int64_t M, int64_t N, int64_t K, size_t room, int out[3]) {
