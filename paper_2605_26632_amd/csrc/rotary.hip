@@ -306,9 +306,10 @@ void deal(HeadSide& side, int64_t T, int step, int64_t waves) {
 
 constexpr int64_t kGroups = 1024;            // workgroups that the chip holds at a time, and of the backward pass at most
 
-// One side's share of them.
-int64_t share(const RotaryArgs& a, int i) {
-    const int64_t n = kGroups * a.side[i].H / (a.side[0].H + a.side[1].H);
+// One side's share of them, by the iterations that its tasks of whole tokens take.
+int64_t share(const RotaryArgs& a, int i, int step) {
+    auto work = [&](int k) { return a.side[k].H > 0 ? (double)((a.side[k].H + step - 1) / step) + 0.7 : 0.0; };
+    const int64_t n = (int64_t)((double)kGroups * work(i) / (work(0) + work(1)));
     return n > 0 ? n : 1;
 }
 
@@ -323,7 +324,7 @@ hipError_t launch_rotary(const RotaryArgs& a_in, hipStream_t stream) {
         for (int i = 0; i < 2; ++i) {
             HeadSide& side = a.side[i];
             side.splits = 1;
-            if (side.H > 0) deal(side, a.T, 64 / L, share(a, i) * kHeadWaves);
+            if (side.H > 0) deal(side, a.T, 64 / L, share(a, i, 64 / L) * kHeadWaves);
             side.groups = side.H > 0 ? (unsigned)((a.T * side.splits + kHeadWaves - 1) / kHeadWaves) : 0;
         }
         const dim3 grid(a.side[0].groups + a.side[1].groups), block(kHeadWaves * 64);
@@ -342,7 +343,7 @@ hipError_t launch_rotary_backward(const RotaryArgs& a_in, float* sums, hipStream
             side.groups = 0;
             side.splits = 1;
             if (side.H > 0 && a.T > 0) {
-                const int64_t most = share(a, i);
+                const int64_t most = share(a, i, 64 / L);
                 deal(side, a.T, 64 / L, most * kHeadWaves);
                 const int64_t groups = (a.T * side.splits + kHeadWaves - 1) / kHeadWaves;
                 side.groups = (unsigned)(groups < most ? groups : most);
