@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import block_plan as plan
 import block_ref as ref
 from paper_2605_26632_amd import binding as rtl
 
@@ -41,7 +42,18 @@ def untouched(full, cols, first=0, fill=3.0):
 
 # M, F, K: one row to several tiles, odd widths, one to many stages of the contraction
 SIZES = [(1, 1, 64), (1, 704, 512), (2, 17, 128), (16, 200, 192), (17, 65, 64), (31, 130, 320), (37, 1000, 128), (64, 64, 64), (100, 333, 1088), (129, 129, 192),
-         (200, 2739, 576), (257, 264, 448), (300, 1100, 64), (513, 520, 256), (700, 1536, 640), (1030, 1029, 128), (2100, 1800, 192)]
+         (200, 2739, 576), (257, 264, 448), (300, 1100, 64), (513, 520, 256), (700, 1536, 640), (1030, 1029, 128), (2100, 1800, 192),
+         (3, 2100, 128), (16, 2049, 64), (4553, 24, 640), (180, 1399, 1088), (3182, 297, 1088), (1286, 1434, 448), (643, 2173, 576), (5014, 1302, 128),
+         (2370, 1199, 448), (4741, 2304, 64), (2746, 1943, 192), (4027, 2142, 64)]
+
+
+def test_sizes_reach_every_form():
+    assert {plan.gated_form(*s) for s in SIZES} == {"few", 0, 1, 2, 3, 4, 5, 6, "256", "tails", "256 tails", "192", "192 tails"}
+    got = {plan.pair_form(*s) for s in BACK_SIZES}
+    assert {g[0] for g in got} == {0, 1, 2, 3, 4, 5, 6}
+    # dX in parts, dW in parts, both, in each kind of kernel that has them
+    assert {(g[0], g[1] > 1, g[2] > 1) for g in got} >= {(0, True, False), (0, False, True), (0, True, True), (1, False, True), (2, True, False), (4, True, False),
+                                                        (5, False, True)}
 
 
 @pytest.mark.parametrize("M,F,K", SIZES)
@@ -118,7 +130,9 @@ def test_weight_beyond_32_bits():
         assert bool((H[:, 256:F - 256] == 0).all())
 
 
-BACK_SIZES = [(1, 4, 8), (1, 704, 512), (5, 20, 72), (37, 60, 64), (64, 128, 256), (129, 132, 200), (300, 704, 512), (701, 260, 136), (1500, 520, 640)]
+BACK_SIZES = [(1, 4, 8), (1, 704, 512), (5, 20, 72), (37, 60, 64), (64, 128, 256), (129, 132, 200), (300, 704, 512), (701, 260, 136), (1500, 520, 640),
+              (714, 64, 64), (271, 760, 64), (400, 68, 3824), (1080, 20, 1392), (259, 400, 3320), (284, 2852, 392), (1, 812, 2472), (519, 204, 4024), (73, 3648, 1472),
+              (513, 724, 4016), (1, 1392, 2872), (1416, 292, 3928), (2577, 68, 1688), (1607, 708, 3408)]
 
 
 @pytest.mark.parametrize("M,F,K", BACK_SIZES)
@@ -141,9 +155,11 @@ def test_backward_in_parts():
     want = ref.gated_backward(dH, X, W, P, "silu")
     full = rtl.gated_linear_backward(dH, X, W, P, with_bias=True, with_hidden=True)
     dX, dW, db, H = rtl.gated_linear_backward(dH, None, W, P)
-    assert dW is None and db is None and H is None and torch.equal(dX, full[0])
+    assert dW is None and db is None and H is None
+    ref.close(dX, *want["dX"])
     dX, dW, db, H = rtl.gated_linear_backward(dH, X, None, P)
-    assert dX is None and db is None and H is None and torch.equal(dW, full[1])
+    assert dX is None and db is None and H is None
+    ref.close(dW, *want["dW"])
     place, around = room(M, F, F + 9, first=1)
     dX, dW, db, H = rtl.gated_linear_backward(dH, X, W, P, out=(None, None, None, place))
     assert dX is None and dW is None and db is None and H is place
@@ -178,6 +194,22 @@ def test_backward_exact():
     dp = torch.cat([dh * u * torch.where(g > 0, 1.0, 0.5), dh * g], 1)
     assert torch.equal(dW.double(), dp.t() @ X.double()) and torch.equal(db.double(), dp.sum(0)) and torch.equal(H.double(), g * u)
     ref.close(dX, dp @ W.double(), torch.zeros(M, K, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("M,F,K", [(31, 2000, 64), (700, 48, 136), (300, 700, 72)])
+@pytest.mark.parametrize("share", [0.0, 0.5, 1.0])
+def test_backward_with_less_room(M, F, K, share):
+    """Any part of the optional room: fewer parts, other groupings of the sums, and nothing behind the workspace is written."""
+    gen = generator(M)
+    X, W, P, dH = bf16(gen, M, K), bf16(gen, 2 * F, K, std=K ** -0.5), bf16(gen, M, 2 * F), bf16(gen, M, F)
+    whole, least = rtl.gated_linear_backward_workspace(M, F, K), (4 * M * F + 255) // 256 * 256
+    assert whole > least                                           # there is optional room
+    size = least + int((whole - least) * share)
+    full = torch.full((size + 4096,), 7, dtype=torch.uint8, device=DEV)
+    got = dict(zip(("dX", "dW", "db", "H"), rtl.gated_linear_backward(dH, X, W, P, with_bias=True, with_hidden=True, ws=full[:size])))
+    for name, (value, err) in ref.gated_backward(dH, X, W, P, "silu").items():
+        ref.close(got[name], value, err, name)
+    assert bool((full[size:] == 7).all())
 
 
 @pytest.mark.parametrize("kind", ACTS)
