@@ -371,7 +371,7 @@ rtl_status rtl_grouped_mxfp4_linear(const void* X, const int32_t* offsets, const
  *   act  RTL_ACT_SILU g / (1 + e^-g), RTL_ACT_GELU g Phi(g), RTL_ACT_GELU_TANH its tanh form. fp32, H rounded once.
  *   X    [M, K] bf16 (ldx); W [2F, K] bf16 (ldw), the F rows of Wg first; bias NULL or bf16 [2F], those of Wg first.
  *   H    [M, F] bf16 (ldh); P NULL or [M, 2F] bf16 (ldp): G in its first F columns, U behind them, for the backward pass.
- *   K % 64 == 0, sizes, X and W as for rtl_dense_linear (F for N, F <= 2^29; a result of 2^23 and more tiles of 256 x 128 is RTL_ERR_SHAPE); H, P and
+ *   K % 64 == 0, sizes, X and W as for rtl_dense_linear (F for N, F <= 2^29; a result of 2^23 and more tiles of 256 x 96 is RTL_ERR_SHAPE); H, P and
  *   bias 2-byte aligned, any row stride.
  *
  * rtl_gated_linear_backward: from dH and the P of the forward call

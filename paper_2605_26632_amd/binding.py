@@ -869,8 +869,8 @@ def _rotation(pos, freq, axis, T):
     if freq is None:
         return 0, 1
     pairs = freq.numel()
-    if pos.dim() != 2:
-        raise ValueError("pos: shape (T, axes) expected")
+    if pos is None or axis is None or pos.dim() != 2:
+        raise ValueError("pos of shape (T, axes) and axis expected with freq")
     _whole(pos, (T, pos.shape[1]), torch.float32, "pos")
     _whole(freq, (pairs,), torch.float32, "freq")
     _whole(axis, (pairs,), torch.int32, "axis")

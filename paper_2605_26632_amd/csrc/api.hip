@@ -832,7 +832,7 @@ rtl_status rtl_gated_linear(const void* X, const void* W, const void* bias, void
     const rtl_status st = check_linear(X, W, H, M, F, K, ldx, ldw, ldh, K);
     if (st != RTL_OK && st != RTL_ERR_NULL && st != RTL_ERR_ALIGN) return st;
     if (M == 0 || F == 0) return st;
-    if (((M + 255) / 256) * ((F + 127) / 128) >= (int64_t)1 << 23) return RTL_ERR_SHAPE;
+    if (((M + 255) / 256) * ((F + 95) / 96) >= (int64_t)1 << 23) return RTL_ERR_SHAPE;       // workgroups of 512 threads
     if (st != RTL_OK) return st;
     if ((P && !aligned(P, 2)) || (bias && !aligned(bias, 2))) return RTL_ERR_ALIGN;
     RTL_REQUIRE_DEVICE();

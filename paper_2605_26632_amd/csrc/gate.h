@@ -35,13 +35,16 @@ __device__ __forceinline__ float gate_phi(float g, float& e) {
     return g < 0.0f ? half : 1.0f - half;
 }
 
+// g^2, cut where it no longer matters: a factor of zero (silu), and the slope's 1 - s, stay zero beside it for gates up to infinity.
+__device__ __forceinline__ float gate_square(float g) { return fminf(g * g, 1e30f); }
+
 template <bool ERF>
 __device__ __forceinline__ float gate_value(float g, GateForm f) {
     if constexpr (ERF) {
         float e;
         return g * gate_phi(g, e);
     } else {
-        return g * gate_sigmoid(g * (f.a + f.b * g * g));
+        return g * gate_sigmoid(g * (f.a + f.b * gate_square(g)));
     }
 }
 
@@ -54,7 +57,7 @@ __device__ __forceinline__ void gate_both(float g, GateForm f, float& value, flo
         value = g * phi;
         slope = phi + 0.39894228f * g * e;
     } else {
-        const float g2 = g * g, s = gate_sigmoid(g * (f.a + f.b * g2));
+        const float g2 = gate_square(g), s = gate_sigmoid(g * (f.a + f.b * g2));
         value = g * s;
         slope = s + value * (1.0f - s) * (f.a + 3.0f * f.b * g2);
     }

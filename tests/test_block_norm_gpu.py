@@ -203,6 +203,25 @@ def test_no_rows_and_empty_sequences():
     assert xo.shape == ho.shape == (0, 64)
 
 
+def test_most_sequences():
+    """A sequence for every row but the last ones, as many as are taken."""
+    S, D = 65535, 8
+    c = Case(S + 4, D, list(range(S + 1)), 15)
+    (x, ex), (h, eh) = c.want("none", "rms", 1.0)
+    xo, ho = c.forward("none", "rms", 1.0)
+    ref.close(xo, x, ex, "x")
+    ref.close(ho, h, eh, "h")
+    got = dict(zip(NAMES, c.backward("none", "rms", 1.0)))
+    seq = slice(0, S)
+    n, _, _ = ref.normed(c.x[seq].double(), "rms", EPS)
+    dh = c.dh[seq].double()
+    ref.close(got["dshift"], dh, torch.zeros_like(dh))
+    want = dh * n * c.w_pre.double()
+    ref.close(got["dscale"], want, 128 * ref.U * (want.abs() + (dh * c.w_pre.double()).abs() * n.abs()))
+    total = (1 + c.scale.double()) * dh * n
+    ref.close(got["dw_pre"], total.sum(0), (S + 200) * ref.U * total.abs().sum(0))
+
+
 def test_in_place():
     c = Case(100, 520, [3, 60, 98], 11)
     xo, ho = c.forward("rms", "layer", 0.5)

@@ -114,6 +114,30 @@ def test_large_gates():
         ref.close(rtl.gated_linear(X, W, act=kind), h, eh, kind)
 
 
+@pytest.mark.parametrize("kind", ACTS)
+def test_gates_up_to_infinity(kind):
+    """Gates whose square overflows, and infinite ones: g or nothing, slopes of one and zero; NaN where the formula has it."""
+    big = torch.tensor([1e18, 1e20, 3e38, -1e18, -1e20, -3e38, 2.0, -2.0], dtype=torch.bfloat16, device=DEV)
+    P = torch.ones(4, 16, dtype=torch.bfloat16, device=DEV)
+    P[:, :8] = big
+    eye, dH = torch.eye(16, dtype=torch.bfloat16, device=DEV), torch.ones(4, 8, dtype=torch.bfloat16, device=DEV)
+    dP, _, _, H = rtl.gated_linear_backward(dH, None, eye, P, act=kind, with_hidden=True)
+    want = torch.where(big > 1e3, big, torch.zeros_like(big))
+    assert torch.equal(H[:, :6], want[:6].expand(4, 6)) and torch.equal(dP[:, 8:14], want[:6].expand(4, 6))
+    assert torch.equal(dP[:, :6], (big > 1e3).to(torch.bfloat16)[:6].expand(4, 6))
+    assert bool(torch.isfinite(dP).all()) and bool(torch.isfinite(H).all())
+    for M in (1, 40):
+        X = torch.zeros(M, 64, dtype=torch.bfloat16, device=DEV)
+        X[:, 0] = 1.0
+        W = torch.zeros(16, 64, dtype=torch.bfloat16, device=DEV)
+        W[:8, 0], W[8:, 0] = big, 1.0
+        assert torch.equal(rtl.gated_linear(X, W, act=kind)[:, :6], want[:6].expand(M, 6))
+        W[0, 0], W[1, 0], W[2, 0] = float("inf"), float("-inf"), float("nan")
+        H = rtl.gated_linear(X, W, act=kind)
+        # (products with the zeros of X make every infinite weight's column of sums its own: inf, and -inf times nothing)
+        assert bool((H[:, 0] == float("inf")).all()) and bool(torch.isnan(H[:, 1:3]).all()) and torch.equal(H[:, 3:6], want[3:6].expand(M, 3))
+
+
 def test_weight_beyond_32_bits():
     """More than 2^32 bytes of gate rows: the up rows lie behind them."""
     F, K = 1 << 18, 8192 + 64
