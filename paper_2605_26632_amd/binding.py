@@ -392,20 +392,6 @@ def _here(*ts):
     return dev
 
 
-def _places(*ts):
-    """(number of the current device, which has to hold all of the tensors, their addresses)."""
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
-    at = []
-    for t in ts:
-        if t is None:
-            at.append(None)
-        elif t.get_device() != dev or dev < 0:
-            raise ValueError("librtlynx takes tensors of the current device (%d) only, not of %s" % (dev, t.device))
-        else:
-            at.append(t.data_ptr())
-    return dev, at
-
-
 def _matrix(t, dtype, name):
     """(rows, columns, row stride). torch leaves any stride there for a single row."""
     stride = t.stride()
@@ -653,7 +639,33 @@ def grouped_mxfp4_linear(X, offsets, Wq, Ws, bias=None, out=None, ws=None):
     return Y
 
 
-# ---- gated linears --------------------------------------------------------------------------------
+# ---- what a transformer block does between its linears ------------------------------------------------
+# The arguments of these are looked over, and their results allocated, by a compiled module (csrc/block_binding.cpp): in Python that took 6 to 20 us of
+# calls that keep the GPU busy for 3 to 10. `out` of the row-wise results: rows of no sequence keep what they held; without `out` they are zeros.
+
+_block = None
+
+
+def block():
+    """The compiled module. Raises if it has not been built."""
+    global _block
+    if _block is None:
+        lib()
+        try:
+            from . import _block as compiled
+        except ImportError as e:
+            raise RuntimeError("_block.so is not built (run python -m paper_2605_26632_amd.build): %s" % e) from e
+        _block = compiled
+    return _block
+
+
+def _place():
+    """(number of the current device, its current stream)."""
+    if not torch.cuda.is_initialized():
+        raise ValueError("librtlynx takes tensors of the current device only, and no device is in use")
+    dev = torch._C._cuda_getDevice()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
+
 
 def _choice(table, name, what):
     try:
@@ -665,22 +677,9 @@ def _choice(table, name, what):
 def gated_linear(X, W, bias=None, act="silu", with_pre=False, out=None, pre=None):
     """rtl_gated_linear: H = act(X W[:F]^T + bias[:F]) (X W[F:]^T + bias[F:]), X bf16 [M,K], W bf16 [2F,K], bias [2F]; act "silu", "gelu" or
     "gelu_tanh". H bf16 [M,F], or (H, P) with_pre or with a tensor `pre` for it: P bf16 [M,2F], what gated_linear_backward needs."""
-    dev, at = _places(X, W, bias)
-    _here(out, pre)
-    kind = _choice(ACT, act, "act")
-    M, K, ldx = _matrix(X, torch.bfloat16, "X")
-    rows, K_w, ldw = _matrix(W, torch.bfloat16, "W")
-    if K_w != K or rows % 2:
-        raise ValueError("W: shape (2F, %d) expected" % K)
-    F = rows // 2
-    _whole(bias, (rows,), torch.bfloat16, "bias")
-    H, ldh = _output(out, M, F, torch.bfloat16, X)
-    ldp = 0
-    if with_pre or pre is not None:
-        pre, ldp = _output(pre, M, rows, torch.bfloat16, X)
-    st = lib().rtl_gated_linear(*at, H.data_ptr(), _p(pre), kind, M, F, K, ldx, ldw, ldh, ldp, _on(dev))
-    _check(st, "rtl_gated_linear")
-    return H if pre is None else (H, pre)
+    status, H, P = block().gated_linear(*_place(), X, W, bias, _choice(ACT, act, "act"), with_pre, (out, pre))
+    _check(status, "rtl_gated_linear")
+    return H if P is None else (H, P)
 
 
 def gated_linear_backward_workspace(M, F, K):
@@ -691,93 +690,11 @@ def gated_linear_backward(dH, X, W, P, act="silu", with_bias=False, with_hidden=
     """rtl_gated_linear_backward: (dX, dW, db, H) of gated_linear from dH [M,F] and its P; db only with_bias, H (computed again, for the
     gradient of the layer behind) only with_hidden, else None. X None: no dW and db, W None: no dX. dW and db in `dtype` (bf16 or float32).
     `out`: the four tensors, None for what is not wanted; they then settle with_bias, with_hidden and dtype."""
-    dX, dW, db, H = out if out is not None else (None,) * 4
-    dev, at = _places(dH, X, W, P)
-    _here(dX, dW, db, H, ws)
-    kind = _choice(ACT, act, "act")
-    M, F, lddh = _matrix(dH, torch.bfloat16, "dH")
-    m, f2, ldp = _matrix(P, torch.bfloat16, "P")
-    if m != M or f2 != 2 * F:
-        raise ValueError("P: shape (%d, %d) expected" % (M, 2 * F))
-    bf, device = torch.bfloat16, dH.device
-    K = ldx = ldw = lddx = lddw = ldh = 0
-    if X is not None:
-        m, K, ldx = _matrix(X, bf, "X")
-        if m != M:
-            raise ValueError("dH and X differ in rows")
-    if W is not None:
-        n, k, ldw = _matrix(W, bf, "W")
-        if n != f2 or (X is not None and k != K):
-            raise ValueError("W: shape (%d, K) expected, K as in X" % f2)
-        K = k
-    if out is None:
-        if W is not None:
-            dX = torch.empty((M, K), dtype=bf, device=device)
-        if X is not None:
-            dW = torch.empty((f2, K), dtype=dtype, device=device)
-            db = torch.empty((f2,), dtype=dtype, device=device) if with_bias else None
-        if with_hidden:
-            H = torch.empty((M, F), dtype=bf, device=device)
-    if dX is not None:
-        if W is None:
-            raise ValueError("dX needs W")
-        lddx = _output(dX, M, K, bf, dH)[1]
-    if dW is not None:
-        if X is None:
-            raise ValueError("dW needs X")
-        dtype = dW.dtype
-        if dtype is not bf and dtype is not torch.float32:
-            raise ValueError("gradients in bf16 or float32")
-        lddw = _output(dW, f2, K, dtype, dH)[1]
-        _whole(db, (f2,), dtype, "db")
-    elif db is not None:
-        raise ValueError("db comes with dW")
-    if H is not None:
-        ldh = _output(H, M, F, bf, dH)[1]
-    L = lib()
-    if ws is None:
-        ws = _ws(L.rtl_gated_linear_backward_workspace(M, F, max(K, 1)), device)
-    st = L.rtl_gated_linear_backward(*at, _p(dX), _p(dW), _p(db), _p(H), kind, 1 if dtype is torch.float32 else 0, M, F, K,
-                                     lddh, ldx, ldw, ldp, lddx, lddw, ldh, _p(ws), _bytes(ws), _on(dev))
-    _check(st, "rtl_gated_linear_backward")
-    return dX, dW, db, H
-
-
-# ---- norms of a block with gate, residual and modulation ---------------------------------------------
-# `out` of the row-wise results: rows of no sequence keep what they held; without `out` they are zeros.
-
-def _residual_type(t, name):
-    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
-        raise ValueError("%s: bf16 or float32 expected" % name)
-    return t.dtype
-
-
-def _rows_of(t, shape, dtype, name):
-    """Row stride of a matrix of this shape; 0 for None."""
-    if t is None:
-        return 0
-    if t.shape != shape or t.dtype is not dtype:
-        raise ValueError("%s: %s matrix of shape %s expected" % (name, dtype, tuple(shape)))
-    ld, one = t.stride()
-    if one != 1 and shape[1] > 1:
-        raise ValueError("%s: contiguous rows expected" % name)
-    return ld if shape[0] > 1 else shape[1]
-
-
-def _sequences(offsets):
-    if offsets is None:
-        return 1
-    if offsets.numel() < 1:
-        raise ValueError("offsets: at least one number expected")
-    _whole(offsets, (offsets.numel(),), torch.int32, "offsets")
-    return offsets.numel() - 1
-
-
-def _modulation(scale, shift, shape):
-    a, b = _rows_of(scale, shape, torch.bfloat16, "scale"), _rows_of(shift, shape, torch.bfloat16, "shift")
-    if scale is not None and shift is not None and a != b:
-        raise ValueError("scale and shift differ in their row stride")
-    return a or b
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError("gradients in bf16 or float32")
+    got = block().gated_linear_backward(*_place(), dH, X, W, P, _choice(ACT, act, "act"), with_bias, with_hidden, dtype is torch.float32, out, ws)
+    _check(got[0], "rtl_gated_linear_backward")
+    return got[1:]
 
 
 def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shift=None, offsets=None, post="none", pre="layer", alpha=1.0, eps=1e-6,
@@ -786,22 +703,10 @@ def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shi
     shift bf16 [S,D] for the S sequences that offsets (int32 [S+1] on the device; None: one sequence) cut the rows into, weights bf16 [D]; norms
     `post` of y and `pre` of x': "none", "rms", "layer". Returns (x' of x's type, h bf16), None for what is not wanted. `out`: the two tensors, None for what
     is not wanted; it then settles with_x and with_h."""
-    xo, h = out if out is not None else (None, None)
-    dev, at = _places(x, y, gate, w_post, w_pre, scale, shift, offsets)
-    _here(xo, h)
-    kind, S = _residual_type(x, "x"), _sequences(offsets)
-    T, D, ldx = _matrix(x, kind, "x")
-    bf, rows, vectors = torch.bfloat16, (T, D), (S, D)
-    ldy, ld_gate, ld_mod = _rows_of(y, rows, bf, "y"), _rows_of(gate, vectors, bf, "gate"), _modulation(scale, shift, vectors)
-    _whole(w_post, (D,), bf, "w_post")
-    _whole(w_pre, (D,), bf, "w_pre")
-    if out is None:
-        xo = torch.empty(rows, dtype=kind, device=x.device) if with_x else None
-        h = torch.empty(rows, dtype=bf, device=x.device) if with_h else None
-    st = lib().rtl_residual_norm(*at, _p(xo), _p(h), kind is torch.float32, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps, out is None,
-                                 T, S, D, ldx, ldy, ld_gate, ld_mod, _rows_of(xo, rows, kind, "x'"), _rows_of(h, rows, bf, "h"), _on(dev))
-    _check(st, "rtl_residual_norm")
-    return xo, h
+    got = block().residual_norm(*_place(), x, y, gate, w_post, w_pre, scale, shift, offsets, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps,
+                                with_x, with_h, out)
+    _check(got[0], "rtl_residual_norm")
+    return got[1:]
 
 
 def residual_norm_backward_workspace(T, S, D):
@@ -813,96 +718,19 @@ def residual_norm_backward(dx_out, dh, x_out, y=None, gate=None, w_post=None, w_
     """rtl_residual_norm_backward: (dx, dy, dgate, dscale, dshift, dw_post, dw_pre) of residual_norm from the gradients of its results (either None:
     none), its x' and y. Gradients of what is not passed are None; dshift comes with scale's unless with_shift says otherwise. The last five are float32.
     `out`: the seven tensors, None for what is not wanted."""
-    got = list(out) if out is not None else [None] * 7
-    dev, at = _places(dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets)
-    _here(*got, ws)
-    like = x_out if x_out is not None else dx_out
-    if like is None:
-        raise ValueError("x' or its gradient expected")
-    kind, S = _residual_type(like, "x'"), _sequences(offsets)
-    T, D, _ = _matrix(like, kind, "x'")
-    bf, f32, rows, vectors = torch.bfloat16, torch.float32, (T, D), (S, D)
-    lds = (_rows_of(dx_out, rows, kind, "dx_out"), _rows_of(dh, rows, bf, "dh"), _rows_of(x_out, rows, kind, "x'"), _rows_of(y, rows, bf, "y"),
-           _rows_of(gate, vectors, bf, "gate"), _rows_of(scale, vectors, bf, "scale"))
-    _whole(w_post, (D,), bf, "w_post")
-    _whole(w_pre, (D,), bf, "w_pre")
-    if out is None:
-        def new(wanted, dtype, shape):
-            return torch.empty(shape, dtype=dtype, device=like.device) if wanted else None
-        shift = scale is not None if with_shift is None else with_shift
-        got = [new(True, kind, rows), new(y is not None, bf, rows), new(y is not None and gate is not None, f32, vectors), new(scale is not None, f32, vectors),
-               new(shift, f32, vectors), new(y is not None and w_post is not None, f32, (D,)), new(w_pre is not None, f32, (D,))]
-    dx, dy, dgate, dscale, dshift, dw_post, dw_pre = got
-    if out is not None:
-        for t, shape, name in ((dgate, vectors, "dgate"), (dscale, vectors, "dscale"), (dshift, vectors, "dshift"), (dw_post, (D,), "dw_post"),
-                               (dw_pre, (D,), "dw_pre")):
-            _whole(t, shape, f32, name)
-    L = lib()
-    if ws is None:
-        ws = _ws(L.rtl_residual_norm_backward_workspace(T, S, D), like.device)
-    st = L.rtl_residual_norm_backward(*at, *map(_p, got), kind is f32, _choice(NORM, post, "post"),
-                                      _choice(NORM, pre, "pre"), alpha, eps, out is None, T, S, D, *lds, _rows_of(dx, rows, kind, "dx"),
-                                      _rows_of(dy, rows, bf, "dy"), _p(ws), _bytes(ws), _on(dev))
-    _check(st, "rtl_residual_norm_backward")
-    return tuple(got)
-
-
-# ---- head norm and rotary positions ---------------------------------------------------------------------
-
-def _heads(t, T, D, name, H=None):
-    """(heads, stride between tokens, between heads) of a [T, H, D] tensor; zeros for None."""
-    if t is None:
-        return 0, 0, 0
-    stride = t.stride()
-    if len(stride) != 3 or t.dtype is not torch.bfloat16:
-        raise ValueError("%s: bf16 tensor of shape [T, heads, D] expected" % name)
-    shape = t.shape
-    if shape[0] != T or shape[2] != D or (H is not None and shape[1] != H):
-        raise ValueError("%s: shape (%d, %s, %d) expected" % (name, T, "heads" if H is None else H, D))
-    if stride[2] != 1:
-        raise ValueError("%s: contiguous heads expected" % name)
-    return shape[1], stride[0], stride[1]
-
-
-def _rotation(pos, freq, axis, T):
-    """(pairs, axes)"""
-    if freq is None:
-        return 0, 1
-    pairs = freq.numel()
-    if pos is None or axis is None or pos.dim() != 2:
-        raise ValueError("pos of shape (T, axes) and axis expected with freq")
-    _whole(pos, (T, pos.shape[1]), torch.float32, "pos")
-    _whole(freq, (pairs,), torch.float32, "freq")
-    _whole(axis, (pairs,), torch.int32, "axis")
-    return pairs, pos.shape[1]
+    got = block().residual_norm_backward(*_place(), dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets, _choice(NORM, post, "post"),
+                                         _choice(NORM, pre, "pre"), alpha, eps, -1 if with_shift is None else int(with_shift), out, ws)
+    _check(got[0], "rtl_residual_norm_backward")
+    return got[1:]
 
 
 def norm_rotary(q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, interleaved=True, out=None):
     """rtl_norm_rotary: the heads of q bf16 [T,Hq,D] and k [T,Hk,D] (k or q None: without) normed (norm "rms", weights wq, wk bf16 [D] or None, or "none")
     and their pairs (2j, 2j+1), or (j, j + pairs) if not interleaved, turned by pos[t, axis[j]] freq[j]: pos float32 [T,axes], freq float32 [pairs], axis int32
     [pairs]; freq None: no rotation. Any strides with contiguous heads. Returns (q', k'), new dense tensors or those of `out`, which may be q and k themselves."""
-    qo, ko = out if out is not None else (None, None)
-    dev, at = _places(q, k, pos, freq, axis, wq, wk)
-    _here(qo, ko)
-    like = q if q is not None else k
-    if like is None:
-        raise ValueError("q or k expected")
-    T, D = like.shape[0], like.shape[-1]
-    Hq, ldq, sq = _heads(q, T, D, "q")
-    Hk, ldk, sk = _heads(k, T, D, "k")
-    pairs, axes = _rotation(pos, freq, axis, T)
-    _whole(wq, (D,), torch.bfloat16, "wq")
-    _whole(wk, (D,), torch.bfloat16, "wk")
-    if out is None:
-        qo = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=like.device) if q is not None else None
-        ko = torch.empty((T, Hk, D), dtype=torch.bfloat16, device=like.device) if k is not None else None
-    if (q is None) != (qo is None) or (k is None) != (ko is None):
-        raise ValueError("out: tensors for what is passed expected")
-    st = lib().rtl_norm_rotary(*at, _p(qo), _p(ko), _choice(NORM, norm, "norm"), eps,
-                               int(interleaved), T, Hq, Hk, D, pairs, axes, ldq, sq, ldk, sk, *_heads(qo, T, D, "q'", Hq)[1:],
-                               *_heads(ko, T, D, "k'", Hk)[1:], _on(dev))
-    _check(st, "rtl_norm_rotary")
-    return qo, ko
+    got = block().norm_rotary(*_place(), q, k, pos, freq, axis, wq, wk, _choice(NORM, norm, "norm"), eps, interleaved, out)
+    _check(got[0], "rtl_norm_rotary")
+    return got[1:]
 
 
 def norm_rotary_backward_workspace(D):
@@ -912,35 +740,9 @@ def norm_rotary_backward_workspace(D):
 def norm_rotary_backward(dq_out, dk_out, q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, interleaved=True, out=None, ws=None):
     """rtl_norm_rotary_backward: (dq, dk, dwq, dwk) of norm_rotary from the gradients of its results; q and k are needed with the norm only (else None will
     do), dwq and dwk (float32 [D]) come with wq and wk. `out`: the four tensors, None for what is not passed or not wanted."""
-    dq, dk, dwq, dwk = out if out is not None else (None,) * 4
-    dev, at = _places(dq_out, dk_out, q, k, pos, freq, axis, wq, wk)
-    _here(dq, dk, dwq, dwk, ws)
-    like = dq_out if dq_out is not None else dk_out
-    if like is None:
-        raise ValueError("a gradient expected")
-    T, D = like.shape[0], like.shape[-1]
-    bf = torch.bfloat16
-    Hq, lddqo, sdqo = _heads(dq_out, T, D, "dq_out")
-    Hk, lddko, sdko = _heads(dk_out, T, D, "dk_out")
-    pairs, axes = _rotation(pos, freq, axis, T)
-    _whole(wq, (D,), bf, "wq")
-    _whole(wk, (D,), bf, "wk")
-    if out is None:
-        dq = torch.empty((T, Hq, D), dtype=bf, device=like.device) if Hq else None
-        dk = torch.empty((T, Hk, D), dtype=bf, device=like.device) if Hk else None
-        dwq = torch.empty((D,), dtype=torch.float32, device=like.device) if wq is not None else None
-        dwk = torch.empty((D,), dtype=torch.float32, device=like.device) if wk is not None else None
-    _whole(dwq, (D,), torch.float32, "dwq")
-    _whole(dwk, (D,), torch.float32, "dwk")
-    L = lib()
-    if ws is None and (dwq is not None or dwk is not None):
-        ws = _ws(L.rtl_norm_rotary_backward_workspace(D), like.device)
-    st = L.rtl_norm_rotary_backward(*at, _p(dq), _p(dk), _p(dwq), _p(dwk),
-                                    _choice(NORM, norm, "norm"), eps, int(interleaved), T, Hq, Hk, D, pairs, axes, lddqo, sdqo, lddko, sdko,
-                                    *_heads(q, T, D, "q", Hq if q is not None else None)[1:], *_heads(k, T, D, "k", Hk if k is not None else None)[1:],
-                                    *_heads(dq, T, D, "dq", Hq)[1:], *_heads(dk, T, D, "dk", Hk)[1:], _p(ws), _bytes(ws) if ws is not None else 0, _on(dev))
-    _check(st, "rtl_norm_rotary_backward")
-    return dq, dk, dwq, dwk
+    got = block().norm_rotary_backward(*_place(), dq_out, dk_out, q, k, pos, freq, axis, wq, wk, _choice(NORM, norm, "norm"), eps, interleaved, out, ws)
+    _check(got[0], "rtl_norm_rotary_backward")
+    return got[1:]
 
 
 # ---- diagnostics ------------------------------------------------------------------------------
