@@ -14,8 +14,8 @@
 namespace rtl {
 namespace {
 
-// A row's team is a wave or a workgroup; workgroups of 256 threads, or of the team's where that is more.
-constexpr int team_threads(int waves) { return waves > 4 ? waves * 64 : 256; }
+// A row's team is a wave, four of which make a workgroup, or a workgroup.
+constexpr int team_threads(int waves) { return waves > 1 ? waves * 64 : 256; }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -150,11 +150,10 @@ __device__ __forceinline__ Stats row_stats(const float (&v)[NCH][8], int kind, i
     return s;
 }
 
-// EARLY: the vectors of the sequence are loaded beside the rows, not behind the sums: for few rows, where a launch is as long as the loads that wait for each
-// other. With many rows the registers are worth more.
-template <int WAVES, int NCH, bool F32, bool EARLY>
+// A lane has NCH chunks of eight columns. [16896, 3840] with everything 101 us, 5.1 TB/s, what a copy reaches.
+template <int WAVES, int NCH, bool F32>
 __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArgs a) {
-    __shared__ float slots[4 * WAVES];
+    __shared__ float slots[2 * WAVES];
     constexpr int TEAM = WAVES * 64, TEAMS = team_threads(WAVES) / TEAM;
     const int tl = threadIdx.x % TEAM;
     const int64_t row = (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
@@ -174,20 +173,14 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
         return;
     }
     TeamSum<WAVES> sum{slots};
-    constexpr uint32_t kOnes = 0x3F803F80u;
     // a chunk of a vector, `none` where there is no vector
-    auto vector = [&](const uint16_t* p, int64_t at, int c, uint32_t none) {
+    constexpr uint32_t kOnes = 0x3F803F80u;
+    auto vector = [&](const uint16_t* p, int64_t at, int c, uint32_t none, float (&f)[8]) {
         uint4 v = make_uint4(none, none, none, none);
         if (p && column(c) < (uint32_t)D) v = *reinterpret_cast<const uint4*>(p + at + column(c));
-        return v;
+        unpack8(v, f);
     };
-    auto post_weight = [&](int c) { return vector(a.w_post, 0, c, kOnes); };
-    auto gates = [&](int c) { return vector(a.gate, s * a.ld_gate, c, kOnes); };
-    auto pre_weight = [&](int c) { return vector(a.w_pre, 0, c, kOnes); };
-    auto scales = [&](int c) { return vector(a.scale, s * a.ld_mod, c, 0); };
-    auto shifts = [&](int c) { return vector(a.shift, s * a.ld_mod, c, 0); };
     float x[NCH][8], y[NCH][8];
-    uint4 early[EARLY ? NCH : 1][5];
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
 #pragma unroll
@@ -196,20 +189,13 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
             load8_as<F32>(a.x, row * a.ldx, column(c), x[c]);
             if (a.y) load8(a.y + row * a.ldy, column(c), y[c]);
         }
-        if constexpr (EARLY) {
-            early[c][0] = post_weight(c);
-            early[c][1] = gates(c);
-            early[c][2] = pre_weight(c);
-            early[c][3] = scales(c);
-            early[c][4] = shifts(c);
-        }
     }
     const Stats sy = row_stats<WAVES, NCH>(y, a.y ? a.post : RTL_NORM_NONE, tl, D, a.eps, sum);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
         float w[8], g[8];
-        unpack8(EARLY ? early[EARLY ? c : 0][0] : post_weight(c), w);
-        unpack8(EARLY ? early[EARLY ? c : 0][1] : gates(c), g);
+        vector(a.w_post, 0, c, kOnes, w);
+        vector(a.gate, s * a.ld_gate, c, kOnes, g);
         if (column(c) < (uint32_t)D) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
@@ -221,9 +207,9 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
         float w[8], g[8], b[8], h[8];
-        unpack8(EARLY ? early[EARLY ? c : 0][2] : pre_weight(c), w);
-        unpack8(EARLY ? early[EARLY ? c : 0][3] : scales(c), g);
-        unpack8(EARLY ? early[EARLY ? c : 0][4] : shifts(c), b);
+        vector(a.w_pre, 0, c, kOnes, w);
+        vector(a.scale, s * a.ld_mod, c, 0, g);
+        vector(a.shift, s * a.ld_mod, c, 0, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] = w[e] * ((x[c][e] - sx.mean) * sx.scale) * (1.0f + g[e]) + b[e];
         if (column(c) < (uint32_t)D) store8_as<false>(a.h, row * a.ldh, column(c), h);
@@ -292,6 +278,7 @@ struct Raw8 {
 // team one after the other, and the few teams that a compute unit holds would not hide the loads behind them.
 // Lanes behind the end of the row work on the row's first columns and are left out of the sums and stores only: branches around the arithmetic made the
 // compiler keep two copies of what lives across them, and spill.
+// [16896, 3840], one of the norms, 74 to 78 us, 386 MB at 5.0 TB/s, and 4.5 for the reduction; fp32 [2111, 2048] with both norms and five sequences 20 + 4.5 + 3.5.
 // SOLO: a wave to a team, four teams to a workgroup. POST: norm(y) is not y.
 template <bool F32, bool SOLO, bool POST>
 __global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(const NormGradArgs a) {
@@ -375,81 +362,81 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(con
             for (int e = 0; e < 8; ++e) f_post[e] *= v[e];
         }
 #pragma unroll 1
-      for (; row < run_end; ++row) {
-        float x[8], y[8], dh[8], dt[8];
-        rx.get(x);
-        ry.get(y);
-        rh.get(dh);
-        rd.get(dt);
-        if (row + 1 < run_end) fetch(row + 1);
-        float mx = 0.f, rsx = 1.0f, my = 0.f, rsy = 1.0f;
-        if (layer_pre || layer_post) {
-            float u = 0.f, v = 0.f;
+        for (; row < run_end; ++row) {
+            float x[8], y[8], dh[8], dt[8];
+            rx.get(x);
+            ry.get(y);
+            rh.get(dh);
+            rd.get(dt);
+            if (row + 1 < run_end) fetch(row + 1);
+            float mx = 0.f, rsx = 1.0f, my = 0.f, rsy = 1.0f;
+            if (layer_pre || layer_post) {
+                float u = 0.f, v = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                u += x[e];
-                v += y[e];
+                for (int e = 0; e < 8; ++e) {
+                    u += x[e];
+                    v += y[e];
+                }
+                sum(u, v);
+                if (layer_pre) mx = u * inv;
+                if (layer_post) my = v * inv;
             }
-            sum(u, v);
-            if (layer_pre) mx = u * inv;
-            if (layer_post) my = v * inv;
-        }
-        if (norm_pre || POST) {
-            float u = 0.f, v = 0.f;
+            if (norm_pre || POST) {
+                float u = 0.f, v = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] -= mx;
+                    u += x[e] * x[e];
+                    if constexpr (POST) {
+                        y[e] -= my;
+                        v += y[e] * y[e];
+                    }
+                }
+                sum(u, v);
+                if (norm_pre) rsx = 1.0f / sqrtf(u * inv + a.eps);
+                if constexpr (POST) rsy = 1.0f / sqrtf(v * inv + a.eps);
+            }
+            // n in x's place, norm(y) in y's; the columns' sums; dn in dh's place
+            float m = 0.f, mn = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] -= mx;
-                u += x[e] * x[e];
+                x[e] *= rsx;
+                if constexpr (POST) y[e] *= rsy;
+                of_scale[e] += dh[e] * x[e];
+                of_shift[e] += dh[e];
+                dh[e] *= f_pre[e];
+                m += dh[e];
+                mn += dh[e] * x[e];
+            }
+            if (norm_pre) {
+                sum(m, mn);
+                m = layer_pre ? m * inv : 0.f;
+                mn *= inv;
+            } else {
+                m = mn = 0.f;
+            }
+            float p = 0.f, pn = 0.f, out[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                dt[e] += rsx * (dh[e] - m - x[e] * mn);
+                out[e] = a.alpha * dt[e];
+                of_gate[e] += dt[e] * y[e];
+                dt[e] *= f_post[e];
                 if constexpr (POST) {
-                    y[e] -= my;
-                    v += y[e] * y[e];
+                    p += dt[e];
+                    pn += dt[e] * y[e];
                 }
             }
-            sum(u, v);
-            if (norm_pre) rsx = 1.0f / sqrtf(u * inv + a.eps);
-            if constexpr (POST) rsy = 1.0f / sqrtf(v * inv + a.eps);
-        }
-        // n in x's place, norm(y) in y's; the columns' sums; dn in dh's place
-        float m = 0.f, mn = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] *= rsx;
-            if constexpr (POST) y[e] *= rsy;
-            of_scale[e] += dh[e] * x[e];
-            of_shift[e] += dh[e];
-            dh[e] *= f_pre[e];
-            m += dh[e];
-            mn += dh[e] * x[e];
-        }
-        if (norm_pre) {
-            sum(m, mn);
-            m = layer_pre ? m * inv : 0.f;
-            mn *= inv;
-        } else {
-            m = mn = 0.f;
-        }
-        float p = 0.f, pn = 0.f, out[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            dt[e] += rsx * (dh[e] - m - x[e] * mn);
-            out[e] = a.alpha * dt[e];
-            of_gate[e] += dt[e] * y[e];
-            dt[e] *= f_post[e];
+            if (a.dx && mine) store8_as<F32>(a.dx, (int64_t)row * a.lddx, column(), out);
             if constexpr (POST) {
-                p += dt[e];
-                pn += dt[e] * y[e];
-            }
-        }
-        if (a.dx && mine) store8_as<F32>(a.dx, (int64_t)row * a.lddx, column(), out);
-        if constexpr (POST) {
-            sum(p, pn);
-            p = layer_post ? p * inv : 0.f;
-            pn *= inv;
+                sum(p, pn);
+                p = layer_post ? p * inv : 0.f;
+                pn *= inv;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dt[e] = rsy * (dt[e] - p - y[e] * pn);
+                for (int e = 0; e < 8; ++e) dt[e] = rsy * (dt[e] - p - y[e] * pn);
+            }
+            if (a.dy && mine) store8_as<false>(a.dy, (int64_t)row * a.lddy, column(), dt);
         }
-        if (a.dy && mine) store8_as<false>(a.dy, (int64_t)row * a.lddy, column(), dt);
-      }
         if (a.sums && mine) {
             float* to = a.sums + (int64_t)(team + s) * 3 * a.D;
             const uint32_t at = column();
@@ -517,18 +504,21 @@ __global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_weights_kern
     if (to) to[col] = sum;
 }
 
-// f(waves of a team, chunks of a lane) for rows of D values.
+// f(waves of a team, chunks of a lane) for T rows of D values. With few rows a launch is as long as a row, and one chunk to a lane is soonest through it; with
+// many, half the waves at two chunks spare barriers and workgroups. us, one | two chunks: [4, 1024] 3.3 | 4.4, [4, 3840] 3.6 | 4.8, [512, 3840] 5.5 | 6.0,
+// [4, 8192] 4.1 | 4.9, [2048, 1024] 5.5 | 5.9, [2048, 3840] 14.2 | 14.4; [33792, 1024] 51.9 | 51.0, [16896, 3840] 106.3 | 105.3, [4096, 8192] 45.0 | 44.1.
+// (One wave: [33792, 512] 24.7, two of one row 30.3. Four of one chunk: [16896, 2048] 51.9, two of two 51.6, one of four 53.8.)
+constexpr int64_t kFewNormRows = 2048;
 template <class F>
-hipError_t with_team(int64_t D, F f) {
+hipError_t with_team(int64_t T, int64_t D, F f) {
     using std::integral_constant;
+    const bool few = T <= kFewNormRows;
     if (D <= 512) return f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    if (D <= 1024) return f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+    if (D <= 1024) return few ? f(integral_constant<int, 2>{}, integral_constant<int, 1>{}) : f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
     if (D <= 2048) return f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    if (D <= 4096) return f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+    if (D <= 4096) return few ? f(integral_constant<int, 8>{}, integral_constant<int, 1>{}) : f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    return few ? f(integral_constant<int, 16>{}, integral_constant<int, 1>{}) : f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
 }
-
-constexpr unsigned kFewGroups = 512;         // workgroups of the forward pass up to which vectors are loaded early
 
 // Backward pass: waves of a team, and rows of one: the rows dealt once over teams of eight waves to a compute unit. Sixteen read at the same rate and leave
 // twice the sums: [16896, 3840] 175 -> 167 us, [16896, 2048] 104 -> 97, [8192, 3840] 90 -> 85, [16896, 512] 40 -> 34, fp32 [2111, 2048] 28.7 -> 27.4.
@@ -542,17 +532,12 @@ int64_t team_rows(int64_t T, int64_t D) {
 }  // namespace
 
 hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream) {
-    return with_team(a.D, [&](auto waves, auto chunks) {
+    return with_team(a.T, a.D, [&](auto waves, auto chunks) {
         constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
         const int64_t teams = team_threads(W) / (W * 64);
-        const dim3 grid((unsigned)((a.T + teams - 1) / teams));
-        auto go = [&](auto f32, auto early) {
-            hipLaunchKernelGGL((norm_kernel<W, C, decltype(f32)::value, decltype(early)::value>), grid, dim3(team_threads(W)), 0, stream, a);
-        };
-        using T = std::true_type;
-        using F = std::false_type;
-        if (grid.x <= kFewGroups) a.x_f32 ? go(T{}, T{}) : go(F{}, T{});
-        else a.x_f32 ? go(T{}, F{}) : go(F{}, F{});
+        const dim3 grid((unsigned)((a.T + teams - 1) / teams)), block(team_threads(W));
+        if (a.x_f32) hipLaunchKernelGGL((norm_kernel<W, C, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((norm_kernel<W, C, false>), grid, block, 0, stream, a);
         return hipGetLastError();
     });
 }

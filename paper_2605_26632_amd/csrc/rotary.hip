@@ -154,7 +154,10 @@ __device__ __forceinline__ float square_sum(const float (&v)[2][8]) {
     return s;
 }
 
-// A wave takes one token and side.per heads of it, 64 / L at a time. The first side[0].groups workgroups have the heads of q, the others those of k.
+// A wave takes one token and side.per heads of it, 64 / L at a time: one time only, unless the launch would be too large. Then the four waves of a workgroup work on
+// neighbouring heads, and memory gives more than to waves that go through a token each, though every wave takes the token's sines anew (us, a token to a wave |
+// one time): [16896, 30 + 30, 128] 105 | 96, [16896, 40 + 40, 128] 139 | 123, [5000, 64 + 8, 128] 32.8 | 29.0, [1, 30 + 30, 128] 4.3 | 3.2;
+// [4096, 24 + 24, 128] 17.7 | 18.1, [16896, 12 + 12, 256] 82.7 | 84.3. The first side[0].groups workgroups have the heads of q, the others those of k.
 template <int L, bool HALVES>
 __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArgs a) {
     __shared__ float lds[kHeadWaves][2][kMostPairs];
@@ -186,7 +189,8 @@ __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArg
 }
 
 // The same walk for the gradients; a wave goes on to further tokens, and what it has of the weight's gradient goes to the workspace at the end, a
-// workgroup's four waves and a wave's 64 / L heads added up in order.
+// workgroup's four waves and a wave's 64 / L heads added up in order. [4433, 30 + 30, 128] 36 us, 204 MB (some of them in the cache behind L2), and 5
+// for the reduction.
 template <int L, bool HALVES>
 __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(const RotaryArgs a) {
     __shared__ float lds[kHeadWaves][2][kMostPairs];
@@ -286,15 +290,19 @@ hipError_t with_lanes(int D, F f) {
     return f(integral_constant<int, 32>{});
 }
 
-// Deals the heads of a side to waves: a task is a token and `per` of its heads. `waves` run at a time; a task costs about .7 of an iteration over 64 / L heads
-// besides its iterations, and the last round of tasks counts in full.
+constexpr int64_t kMostTasks = (int64_t)1 << 23;         // of a side, where a task can be more than an iteration (a launch takes fewer than 2^32 threads)
+
+// Deals the heads of a side to the waves of the backward pass: a task is a token and `per` of its heads. `waves` run at a time; a task costs about .7 of an
+// iteration over 64 / L heads besides its iterations, and the last round of tasks counts in full. us, tokens as tasks | so | an iteration to a task:
+// [1, 30 + 30, 128] 9.6 | 7.6 | 7.6, [5000, 64 + 8, 128] 62.7 | 56.1 | 59.6, [4096, 30 + 30, 128] 37.3 | 37.5 | 38.6, [16896, 12 + 12, 256] 129 | 129 | 141,
+// [16896, 40 + 40, 128] 206 | 206 | 203.
 void deal(HeadSide& side, int64_t T, int step, int64_t waves) {
     const int most = (side.H + step - 1) / step;
     double best = 0;
     for (int splits = 1; splits <= most; splits += 1 + splits / 16) {
         const int per = (most + splits - 1) / splits;
         const int64_t n = (most + per - 1) / per, rounds = (T * n + waves - 1) / waves;
-        if (splits > 1 && T * n > (int64_t)1 << 25) break;             // (a launch takes fewer than 2^32 threads)
+        if (splits > 1 && T * n > kMostTasks) break;
         const double time = (double)rounds * (per + 0.7);
         if (splits == 1 || time < best) {
             best = time;
@@ -304,9 +312,9 @@ void deal(HeadSide& side, int64_t T, int step, int64_t waves) {
     }
 }
 
-constexpr int64_t kGroups = 1024;            // workgroups that the chip holds at a time, and of the backward pass at most
+constexpr int64_t kGroups = 1024;            // workgroups of the backward pass, as many as the chip holds at a time
 
-// One side's share of them, by the iterations that its tasks of whole tokens take.
+// One side's share of them, by the iterations that its tasks of whole tokens take. (Halves: [1024, 24 + 8] alike, [300, 48 + 2, 64] 9.4 -> 9.6.)
 int64_t share(const RotaryArgs& a, int i, int step) {
     auto work = [&](int k) { return a.side[k].H > 0 ? (double)((a.side[k].H + step - 1) / step) + 0.7 : 0.0; };
     const int64_t n = (int64_t)((double)kGroups * work(i) / (work(0) + work(1)));
@@ -324,7 +332,11 @@ hipError_t launch_rotary(const RotaryArgs& a_in, hipStream_t stream) {
         for (int i = 0; i < 2; ++i) {
             HeadSide& side = a.side[i];
             side.splits = 1;
-            if (side.H > 0) deal(side, a.T, 64 / L, share(a, i, 64 / L) * kHeadWaves);
+            if (side.H > 0) {
+                const int64_t most = (side.H + 64 / L - 1) / (64 / L), times = (a.T * most + kMostTasks - 1) / kMostTasks;
+                side.per = (int)(times > 1 ? times : 1) * (64 / L);
+                side.splits = (side.H + side.per - 1) / side.per;
+            }
             side.groups = side.H > 0 ? (unsigned)((a.T * side.splits + kHeadWaves - 1) / kHeadWaves) : 0;
         }
         const dim3 grid(a.side[0].groups + a.side[1].groups), block(kHeadWaves * 64);
