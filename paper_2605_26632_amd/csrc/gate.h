@@ -5,7 +5,7 @@
 //              silu with another argument, so that the two share one path
 //   gelu       g Phi(g), Phi(g) = .5 erfc(-g / sqrt 2) by the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook: erfc(x) = (a1 t + ..
 //              + a5 t^5) e^-x^2, t = 1 / (1 + p x), x >= 0, off by at most 1.5e-7. As a product it keeps its relative accuracy where Phi is small.
-// e^x and 1 / x are the hardware's (an fp32 unit or two); all of it is rounded to bf16 afterwards, whose half step is 2^-9 of the value.
+// e^x and 1 / x are the hardware's (an fp32 unit or two); all of it is rounded to bf16 afterwards, whose half step is up to 2^-8 of the value.
 #pragma once
 #include <hip/hip_runtime.h>
 #include "rtlynx.h"
