@@ -166,6 +166,25 @@ def test_large_mean_and_empty_rows(post, pre):
     ref.close(ho, h, eh, "h")
 
 
+@pytest.mark.parametrize("D", [512, 520, 1024, 1032, 2048, 2056, 3840, 4096, 4104, 8192])
+@pytest.mark.parametrize("wide", [False, True])
+def test_many_rows(D, wide):
+    """Either side of the number of rows from which fewer waves take a row, and the same rows on both."""
+    c = Case(2049, D, [1, 1000, 2047], D, wide)
+    (x, ex), (h, eh) = c.want("rms", "layer", 0.75)
+    xo, ho = c.forward("rms", "layer", 0.75)
+    mine = slice(1, 2047)
+    ref.close(xo[mine], x[mine], ex[mine], "x")
+    ref.close(ho[mine], h[mine], eh[mine], "h")
+    for t in (xo, ho):
+        assert bool((t[:1] == 0).all()) and bool((t[2047:] == 0).all())
+    c.x, c.y = c.x[:2048], c.y[:2048]
+    xo, ho = c.forward("rms", "layer", 0.75)
+    ref.close(xo[mine], x[mine], ex[mine], "x")
+    ref.close(ho[mine], h[mine], eh[mine], "h")
+    assert bool((xo[2047:] == 0).all())
+
+
 def test_rows_do_not_meet():
     c = Case(50, 264, [0, 25, 50], 8)
     (x, ex), (h, eh) = c.want("rms", "layer", 1.0)

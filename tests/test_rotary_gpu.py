@@ -160,6 +160,21 @@ def test_turning_back():
     ref.close(back, q.double(), (2 ** 0.5 * ref.HALF[torch.bfloat16] + 64 * ref.U + 1e-8) * length)
 
 
+def test_more_tokens_than_waves_are_launched_for():
+    """So many that a wave goes over a token's heads twice; rows across the tensor against the formula, all of them against a call on the last ones."""
+    gen = generator(8)
+    T, H, D = (1 << 22) + 5, 17, 8
+    q = normal(gen, T, H, D)
+    w = normal(gen, D, std=0.1, mean=1.0)
+    pos, freq, axis = rotation(gen, T, 4, 2)
+    out = rtl.norm_rotary(q, None, pos, freq, axis, w)[0]
+    some = torch.cat([torch.arange(0, T, 40009, device=DEV), torch.arange(T - 9, T, device=DEV)])
+    ref.close(out[some], *ref.norm_rotary(q[some], pos[some], freq, axis, w, "rms", EPS, True), "forward")
+    half = T // 2
+    assert torch.equal(out[:half], rtl.norm_rotary(q[:half], None, pos[:half], freq, axis, w)[0])
+    assert torch.equal(out[half:], rtl.norm_rotary(q[half:], None, pos[half:], freq, axis, w)[0])
+
+
 def test_captured_and_replayed():
     gen = generator(6)
     q, k = normal(gen, 200, 6, 64), normal(gen, 200, 2, 64)
