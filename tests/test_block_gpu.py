@@ -126,3 +126,81 @@ def test_two_streams_at_once():
     for g, w in zip(got, want):
         for name in w:
             assert torch.equal(g[name], w[name]), name
+
+
+@pytest.fixture
+def large():
+    """Gives the memory of large tensors back."""
+    yield
+    torch.cuda.empty_cache()
+
+
+def far(t, ld=(1 << 23) + 8):
+    """The same values in rows so far apart that the last ones lie more than 2^32 bytes behind the first."""
+    assert (t.shape[0] - 1) * ld * t.element_size() > 1 << 32
+    wide = torch.empty(t.shape[0] * ld, dtype=t.dtype, device=DEV).as_strided(t.shape, (ld,) + tuple(t.stride()[1:]))
+    wide.copy_(t)
+    return wide
+
+
+def same(got, want):
+    assert all((g is None and w is None) or torch.equal(g, w) for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("M,F", [(300, 100), (1030, 4), (2080, 516)])
+def test_gated_rows_far_apart(M, F, large):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(M)
+    X, W, dH = (torch.randn(*s, generator=gen, device=DEV).to(torch.bfloat16) for s in ((M, 64), (2 * F, 64), (M, F)))
+    H, P = rtl.gated_linear(X, W, with_pre=True)
+    ld = (1 << 33) // M // 8 * 8                                  # (X and dX up to 2^22)
+    ldx = min(ld, 1 << 22)
+    big = [far(torch.zeros_like(H), ld), far(torch.zeros_like(P), ld)]
+    wide_x = far(X, ldx) if (M - 1) * ldx * 2 > 1 << 32 else X
+    rtl.gated_linear(wide_x, W, out=big[0], pre=big[1])
+    same(big, (H, P))
+    want = rtl.gated_linear_backward(dH, X, W, P, with_hidden=True)
+    big[0].zero_()
+    wide_dx = torch.zeros_like(X) if wide_x is X else far(torch.zeros_like(X), ldx)
+    got = rtl.gated_linear_backward(far(dH, ld), wide_x, W, big[1], out=[wide_dx, torch.zeros_like(W), None, big[0]])
+    same(got, want)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+def test_norm_rows_far_apart(kind, large):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    T, D = 300, 264
+    x, dx = (torch.randn(T, D, generator=gen, device=DEV).to(kind) for _ in range(2))
+    y, dh = (torch.randn(T, D, generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    gate, scale, shift = (torch.randn(2, D, generator=gen, device=DEV).to(torch.bfloat16) for _ in range(3))
+    offsets = torch.tensor([1, 100, 298], dtype=torch.int32, device=DEV)
+    how = dict(offsets=offsets, post="rms", pre="layer")
+    want = rtl.residual_norm(x, y, gate=gate, scale=scale, shift=shift, **how)
+    fx, fy = far(x), far(y)
+    big = [far(torch.zeros_like(w)) for w in want]
+    same(rtl.residual_norm(fx, fy, gate=gate, scale=scale, shift=shift, out=big, **how), want)
+    want = rtl.residual_norm_backward(dx, dh, x, y, gate=gate, scale=scale, **how)
+    for t in big:
+        t.zero_()
+    same(rtl.residual_norm_backward(far(dx), far(dh), fx, fy, gate=gate, scale=scale, out=big + [None if w is None else torch.empty_like(w) for w in want[2:]], **how),
+         want)
+
+
+@pytest.mark.parametrize("interleaved", [True, False])
+def test_tokens_and_heads_far_apart(interleaved, large):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(4)
+    T, H, D = 9, 300, 32
+    q, k = (torch.randn(T, H, D, generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    w = torch.randn(D, generator=gen, device=DEV).to(torch.bfloat16)
+    pos, freq = torch.randn(T, 2, generator=gen, device=DEV), torch.rand(16, generator=gen, device=DEV)
+    axis = torch.arange(16, dtype=torch.int32, device=DEV) % 2
+    fq, fk = far(q, (1 << 28) + 8), far(k.transpose(0, 1)).transpose(0, 1)             # tokens, and heads
+    want = rtl.norm_rotary(q, k, pos, freq, axis, w, w, interleaved=interleaved)
+    out = [far(torch.zeros_like(q), (1 << 28) + 8), far(torch.zeros_like(k).transpose(0, 1)).transpose(0, 1)]
+    same(rtl.norm_rotary(fq, fk, pos, freq, axis, w, w, interleaved=interleaved, out=out), want)
+    want = rtl.norm_rotary_backward(k, q, q, k, pos, freq, axis, w, w, interleaved=interleaved)
+    gq, gk = far(k, (1 << 28) + 8), far(q.transpose(0, 1)).transpose(0, 1)
+    same(rtl.norm_rotary_backward(gq, gk, fq, fk, pos, freq, axis, w, w, interleaved=interleaved, out=out + [torch.empty(D, device=DEV), torch.empty(D, device=DEV)]),
+         want)

@@ -173,6 +173,8 @@ def test_more_tokens_than_waves_are_launched_for():
     half = T // 2
     assert torch.equal(out[:half], rtl.norm_rotary(q[:half], None, pos[:half], freq, axis, w)[0])
     assert torch.equal(out[half:], rtl.norm_rotary(q[half:], None, pos[half:], freq, axis, w)[0])
+    del q, out, pos
+    torch.cuda.empty_cache()
 
 
 def test_captured_and_replayed():
