@@ -52,8 +52,8 @@ def test_sizes_reach_every_form():
     got = {plan.pair_form(*s) for s in BACK_SIZES}
     assert {g[0] for g in got} == {0, 1, 2, 3, 4, 5, 6}
     # dX in parts, dW in parts, both, in each kind of kernel that has them
-    assert {(g[0], g[1] > 1, g[2] > 1) for g in got} >= {(0, True, False), (0, False, True), (0, True, True), (1, False, True), (2, True, False), (4, True, False),
-                                                        (5, False, True)}
+    assert {(g[0], g[1] > 1, g[2] > 1) for g in got} >= {(i, d, w) for i in range(4) for d in (False, True) for w in (False, True)} | {
+        (4, True, False), (5, False, True), (6, False, True)}
 
 
 @pytest.mark.parametrize("M,F,K", SIZES)
@@ -156,7 +156,8 @@ def test_weight_beyond_32_bits():
 
 BACK_SIZES = [(1, 4, 8), (1, 704, 512), (5, 20, 72), (37, 60, 64), (64, 128, 256), (129, 132, 200), (300, 704, 512), (701, 260, 136), (1500, 520, 640),
               (714, 64, 64), (271, 760, 64), (400, 68, 3824), (1080, 20, 1392), (259, 400, 3320), (284, 2852, 392), (1, 812, 2472), (519, 204, 4024), (73, 3648, 1472),
-              (513, 724, 4016), (1, 1392, 2872), (1416, 292, 3928), (2577, 68, 1688), (1607, 708, 3408)]
+              (513, 724, 4016), (1, 1392, 2872), (1416, 292, 3928), (2577, 68, 1688), (1607, 708, 3408), (65, 512, 8), (503, 104, 8), (4121, 488, 8),
+              (3596, 16, 1192), (4704, 920, 136), (6008, 16, 776), (5832, 72, 3856)]
 
 
 @pytest.mark.parametrize("M,F,K", BACK_SIZES)
