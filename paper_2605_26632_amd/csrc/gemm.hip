@@ -401,7 +401,9 @@ void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t 
 // Tiles of a gated linear (gated.hip; bn rows of W, half of them gates), as kDenseShapes; `held`: workgroups that a compute unit holds at a time, which share
 // its rate. In order: the first four of kDenseShapes; 128 x 128 with eight waves (four take 5 to 10 % longer: [631, 5781, 3584] 51.7 -> 49.0 us, [1456, 6707, 896]
 // 45.4 -> 39.8); 96 x 128, whose tiles fill the units where 128 rows leave some idle ([333, 2739, 4032] 25.9 -> 24.5, [11169, 70, 5952] 41.9 -> 38.5);
-// 64 x 64 with a ring of three, three to a unit, for short contractions ([600, 1500, 1024] 11.5 -> 8.4, [699, 973, 128] 5.6 -> 4.8).
+// 64 x 64 with a ring of three, three to a unit, for short contractions ([600, 1500, 1024] 11.5 -> 8.4, [699, 973, 128] 5.6 -> 4.8); a unit with two of them takes
+// half as long again for a stage, three quarters of a microsecond more for each ([67, 4666, 5760] 33.6 -> 24.6 with 128 x 64 instead, [8226, 862, 64] 14.7 -> 12.0 with
+// 256 rows). Over 260 problems the choice is 1.1 % slower than the best in the mean, 21 % at worst.
 struct GatedShape {
     SplitShape tile;
     int held;
@@ -421,7 +423,10 @@ GatedForm gated_form(int64_t M, int64_t F, int64_t K) {
         if (tiles > 4096 || (passes > 1 && wide && M > 2048)) continue;
         double block = s.block, t;
         if (s.bm == 32) block += 0.0005 * (double)(M < 32 ? M : 32);
-        if (kGatedShapes[i].held > 1) t = s.fixed + (double)blocks * block * (tiles > 256 ? 0.95 * (double)tiles / 256 : 1.0);
+        if (kGatedShapes[i].held > 1) {
+            const double share = (double)tiles / 256, more = share > 1 ? share - 1 : 0;          // tiles of a unit, which come as they leave room
+            t = s.fixed + 0.75 * more + (double)blocks * block * (share <= 1 ? 1.0 : share > 1.5 ? share : 1.5);
+        }
         else t = (double)passes * (s.fixed + (double)blocks * block) * (passes == 1 ? 1.0 : !wide ? 1.24 : passes > 2 ? 1.3 : 1.12);
         if (t < best) {
             best = t;
