@@ -265,14 +265,22 @@ __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(con
     }
 }
 
-// The workgroups' sums of a side (blockIdx.y), 16 columns to a workgroup, dealt to its 64 groups of 16 lanes in turn and those added in order.
+// The workgroups' sums of a side (blockIdx.y), 16 columns to a workgroup, dealt to its 64 groups of 16 lanes in turn and those added in order. Eight loads of a lane
+// are under way at a time: one after the other they were most of the launch ([4433, 30 + 30, 128], both kernels, 40.5 -> 38.8 us).
+constexpr int kAtOnce = 8;
 __global__ __launch_bounds__(1024) void rotary_reduce_kernel(const RotaryArgs a) {
     __shared__ float part[64][16];
     const HeadSide& side = a.side[blockIdx.y];
     const int i = blockIdx.x * 16 + (threadIdx.x & 15), g = threadIdx.x >> 4;
     float s = 0.f;
     if (i < a.D && side.dw)
-        for (uint32_t b = g; b < side.groups; b += 64) s += side.sums[(int64_t)b * a.D + i];
+        for (uint32_t b = g; b < side.groups; b += 64 * kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) v[u] = side.sums[(int64_t)min(b + 64 * u, side.groups - 1) * a.D + i];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) s += b + 64 * u < side.groups ? v[u] : 0.f;
+        }
     part[g][threadIdx.x & 15] = s;
     __syncthreads();
     if (g != 0 || i >= a.D || !side.dw) return;
