@@ -14,8 +14,6 @@ LIB_PATH = os.path.join(_HERE, "librtlynx.so")
 
 COMP_NONE, COMP_GROUP, COMP_ROW, COMP_TENSOR = 0, 1, 2, 3
 COMP = {"none": COMP_NONE, "group": COMP_GROUP, "row": COMP_ROW, "tensor": COMP_TENSOR}
-ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2}             # rtl_act
-NORM = {"none": 0, "rms": 1, "layer": 2}                 # rtl_norm
 
 SYMBOLS = ["rtl_sparsify_pack_workspace", "rtl_sparsify_pack", "rtl_packed_linear_workspace",
            "rtl_packed_linear", "rtl_sparse_linear_workspace", "rtl_sparse_linear", "rtl_sparse_linear_static",
@@ -659,27 +657,13 @@ def block():
     return _block
 
 
-def _place():
-    """(number of the current device, its current stream)."""
-    if not torch.cuda.is_initialized():
-        raise ValueError("librtlynx takes tensors of the current device only, and no device is in use")
-    dev = torch._C._cuda_getDevice()
-    return dev, torch._C._cuda_getCurrentRawStream(dev)
-
-
-def _choice(table, name, what):
-    try:
-        return table[name]
-    except KeyError:
-        raise ValueError("%s: one of %s" % (what, ", ".join(table))) from None
-
-
 def gated_linear(X, W, bias=None, act="silu", with_pre=False, out=None, pre=None):
     """rtl_gated_linear: H = act(X W[:F]^T + bias[:F]) (X W[F:]^T + bias[F:]), X bf16 [M,K], W bf16 [2F,K], bias [2F]; act "silu", "gelu" or
     "gelu_tanh". H bf16 [M,F], or (H, P) with_pre or with a tensor `pre` for it: P bf16 [M,2F], what gated_linear_backward needs."""
-    status, H, P = block().gated_linear(*_place(), X, W, bias, _choice(ACT, act, "act"), with_pre, (out, pre))
-    _check(status, "rtl_gated_linear")
-    return H if P is None else (H, P)
+    got = block().gated_linear(X, W, bias, act, with_pre, (out, pre))
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_gated_linear")
+    return got[0] if got[1] is None else got
 
 
 def gated_linear_backward_workspace(M, F, K):
@@ -692,9 +676,10 @@ def gated_linear_backward(dH, X, W, P, act="silu", with_bias=False, with_hidden=
     `out`: the four tensors, None for what is not wanted; they then settle with_bias, with_hidden and dtype."""
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("gradients in bf16 or float32")
-    got = block().gated_linear_backward(*_place(), dH, X, W, P, _choice(ACT, act, "act"), with_bias, with_hidden, dtype is torch.float32, out, ws)
-    _check(got[0], "rtl_gated_linear_backward")
-    return got[1:]
+    got = block().gated_linear_backward(dH, X, W, P, act, with_bias, with_hidden, dtype is torch.float32, out, ws)
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_gated_linear_backward")
+    return got
 
 
 def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shift=None, offsets=None, post="none", pre="layer", alpha=1.0, eps=1e-6,
@@ -703,10 +688,10 @@ def residual_norm(x, y=None, gate=None, w_post=None, w_pre=None, scale=None, shi
     shift bf16 [S,D] for the S sequences that offsets (int32 [S+1] on the device; None: one sequence) cut the rows into, weights bf16 [D]; norms
     `post` of y and `pre` of x': "none", "rms", "layer". Returns (x' of x's type, h bf16), None for what is not wanted. `out`: the two tensors, None for what
     is not wanted; it then settles with_x and with_h."""
-    got = block().residual_norm(*_place(), x, y, gate, w_post, w_pre, scale, shift, offsets, _choice(NORM, post, "post"), _choice(NORM, pre, "pre"), alpha, eps,
-                                with_x, with_h, out)
-    _check(got[0], "rtl_residual_norm")
-    return got[1:]
+    got = block().residual_norm(x, y, gate, w_post, w_pre, scale, shift, offsets, post, pre, alpha, eps, with_x, with_h, out)
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_residual_norm")
+    return got
 
 
 def residual_norm_backward_workspace(T, S, D):
@@ -718,19 +703,21 @@ def residual_norm_backward(dx_out, dh, x_out, y=None, gate=None, w_post=None, w_
     """rtl_residual_norm_backward: (dx, dy, dgate, dscale, dshift, dw_post, dw_pre) of residual_norm from the gradients of its results (either None:
     none), its x' and y. Gradients of what is not passed are None; dshift comes with scale's unless with_shift says otherwise. The last five are float32.
     `out`: the seven tensors, None for what is not wanted."""
-    got = block().residual_norm_backward(*_place(), dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets, _choice(NORM, post, "post"),
-                                         _choice(NORM, pre, "pre"), alpha, eps, -1 if with_shift is None else int(with_shift), out, ws)
-    _check(got[0], "rtl_residual_norm_backward")
-    return got[1:]
+    got = block().residual_norm_backward(dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets, post, pre, alpha, eps,
+                                         -1 if with_shift is None else int(with_shift), out, ws)
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_residual_norm_backward")
+    return got
 
 
 def norm_rotary(q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, interleaved=True, out=None):
     """rtl_norm_rotary: the heads of q bf16 [T,Hq,D] and k [T,Hk,D] (k or q None: without) normed (norm "rms", weights wq, wk bf16 [D] or None, or "none")
     and their pairs (2j, 2j+1), or (j, j + pairs) if not interleaved, turned by pos[t, axis[j]] freq[j]: pos float32 [T,axes], freq float32 [pairs], axis int32
     [pairs]; freq None: no rotation. Any strides with contiguous heads. Returns (q', k'), new dense tensors or those of `out`, which may be q and k themselves."""
-    got = block().norm_rotary(*_place(), q, k, pos, freq, axis, wq, wk, _choice(NORM, norm, "norm"), eps, interleaved, out)
-    _check(got[0], "rtl_norm_rotary")
-    return got[1:]
+    got = block().norm_rotary(q, k, pos, freq, axis, wq, wk, norm, eps, interleaved, out)
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_norm_rotary")
+    return got
 
 
 def norm_rotary_backward_workspace(D):
@@ -740,9 +727,10 @@ def norm_rotary_backward_workspace(D):
 def norm_rotary_backward(dq_out, dk_out, q, k, pos, freq, axis, wq=None, wk=None, norm="rms", eps=1e-6, interleaved=True, out=None, ws=None):
     """rtl_norm_rotary_backward: (dq, dk, dwq, dwk) of norm_rotary from the gradients of its results; q and k are needed with the norm only (else None will
     do), dwq and dwk (float32 [D]) come with wq and wk. `out`: the four tensors, None for what is not passed or not wanted."""
-    got = block().norm_rotary_backward(*_place(), dq_out, dk_out, q, k, pos, freq, axis, wq, wk, _choice(NORM, norm, "norm"), eps, interleaved, out, ws)
-    _check(got[0], "rtl_norm_rotary_backward")
-    return got[1:]
+    got = block().norm_rotary_backward(dq_out, dk_out, q, k, pos, freq, axis, wq, wk, norm, eps, interleaved, out, ws)
+    if got.__class__ is not tuple:
+        raise RtlError(got, "rtl_norm_rotary_backward")
+    return got
 
 
 # ---- diagnostics ------------------------------------------------------------------------------

@@ -1,9 +1,9 @@
 // Argument marshalling of the block operators (gated linears, norms of a block, rotary positions), compiled: their smallest calls keep the GPU busy for 3 to 10 us,
 // and looking a dozen tensors over in Python, allocating the results and calling through ctypes took 6 to 20. Nothing is computed here; the functions of
-// binding.py wrap these, which are called with all arguments in place, the number of the current device and its stream in front, and return
-// (status, results ...).
+// binding.py wrap these, which are called with all arguments in place and return their results in a tuple, or the number of an error.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
 #include <ATen/ops/empty.h>
 #include "rtlynx.h"
 
@@ -22,17 +22,39 @@ struct Result {
     const Tensor* t = nullptr;
 };
 
+PyObject *current_device = nullptr, *current_stream = nullptr;        // torch's functions: the number of the current device, and the stream of one
+
+constexpr const char* kActs[] = {"silu", "gelu", "gelu_tanh"};          // rtl_act
+constexpr const char* kNorms[] = {"none", "rms", "layer"};              // rtl_norm
+
 struct Call {
     PyObject* const* args;
-    Py_ssize_t count, next = 0;
-    int64_t dev;
-    void* stream;
+    Py_ssize_t next = 0;
+    int64_t dev = -1;
+    void* stream = nullptr;
 
-    Call(PyObject* const* a, Py_ssize_t n, Py_ssize_t expected) : args(a), count(n) {
-        TORCH_CHECK(n == expected, "block binding: ", expected, " arguments expected");
-        dev = integer();
-        stream = reinterpret_cast<void*>(static_cast<uintptr_t>(PyLong_AsUnsignedLongLong(args[next++])));
+    Call(PyObject* const* a, Py_ssize_t n, Py_ssize_t expected) : args(a) { TORCH_CHECK(n == expected, "block binding: ", expected, " arguments expected"); }
+    // the current device and its stream; asked for by the first tensor of a device, since there is none to ask about before
+    void place() {
+        THPObjectPtr d(PyObject_CallNoArgs(current_device));
+        if (!d) throw python_error();
+        THPObjectPtr s(PyObject_CallOneArg(current_stream, d.get()));
+        if (!s) throw python_error();
+        dev = PyLong_AsLongLong(d.get());
+        stream = reinterpret_cast<void*>(static_cast<uintptr_t>(PyLong_AsUnsignedLongLong(s.get())));
+        if (PyErr_Occurred()) throw python_error();
     }
+    template <int N>
+    int choice(const char* const (&names)[N], const char* what) {
+        PyObject* o = args[next++];
+        for (int i = 0; PyUnicode_Check(o) && i < N; ++i)
+            if (PyUnicode_CompareWithASCIIString(o, names[i]) == 0) return i;
+        std::string all;
+        for (const char* n : names) all += (all.empty() ? "" : ", ") + std::string(n);
+        TORCH_CHECK_VALUE(false, what, ": one of ", all);
+    }
+    rtl_act act() { return static_cast<rtl_act>(choice(kActs, "act")); }
+    rtl_norm norm(const char* what) { return static_cast<rtl_norm>(choice(kNorms, what)); }
     int64_t integer() {
         const long long v = PyLong_AsLongLong(args[next++]);
         if (v == -1 && PyErr_Occurred()) throw python_error();
@@ -49,11 +71,13 @@ struct Call {
         return v != 0;
     }
     // the next tensor, which has to lie on the current device; NULL for None
-    const Tensor* tensor(PyObject* o) const {
+    const Tensor* tensor(PyObject* o) {
         if (o == Py_None) return nullptr;
         TORCH_CHECK_VALUE(THPVariable_Check(o), "tensor or None expected, not ", Py_TYPE(o)->tp_name);
         const Tensor& t = THPVariable_Unpack(o);
-        TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == dev, "librtlynx takes tensors of the current device (", dev, ") only, not of ", t.device());
+        TORCH_CHECK_VALUE(t.is_cuda(), "librtlynx takes tensors of the current device only, not of ", t.device());
+        if (dev < 0) place();
+        TORCH_CHECK_VALUE(t.get_device() == dev, "librtlynx takes tensors of the current device (", dev, ") only, not of ", t.device());
         return &t;
     }
     const Tensor* tensor() { return tensor(args[next++]); }
@@ -123,15 +147,15 @@ struct Workspace {
 
 template <int N>
 PyObject* answer(rtl_status status, Result (&r)[N]) {
-    PyObject* out = PyTuple_New(N + 1);
+    PyObject* out = status == RTL_OK ? PyTuple_New(N) : PyLong_FromLong(status);
     if (!out) throw python_error();
-    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(status));
+    if (status != RTL_OK) return out;
     for (int i = 0; i < N; ++i) {
         PyObject* o = Py_None;
         if (r[i].given) o = r[i].given;
         else if (r[i].t) o = THPVariable_Wrap(std::move(r[i].fresh));
         if (o == Py_None || r[i].given) Py_INCREF(o);
-        PyTuple_SET_ITEM(out, i + 1, o);
+        PyTuple_SET_ITEM(out, i, o);
     }
     return out;
 }
@@ -145,10 +169,10 @@ PyObject* answer(rtl_status status, Result (&r)[N]) {
 // X, W, bias, act, with_pre, (H, P) or None
 PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 8);
+    Call c(args, n, 6);
     const Tensor *X = c.tensor(), *W = c.tensor(), *bias = c.tensor();
     TORCH_CHECK_VALUE(X && W, "X and W expected");
-    const auto act = static_cast<rtl_act>(c.integer());
+    const rtl_act act = c.act();
     const bool with_pre = c.truth();
     Result r[2];
     c.results(r);
@@ -166,10 +190,10 @@ PyObject* gated_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // dH, X, W, P, act, with_bias, with_hidden, float32, (dX, dW, db, H) or None, workspace
 PyObject* gated_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 12);
+    Call c(args, n, 10);
     const Tensor *dH = c.tensor(), *X = c.tensor(), *W = c.tensor(), *P = c.tensor();
     TORCH_CHECK_VALUE(dH && P, "dH and P expected");
-    const auto act = static_cast<rtl_act>(c.integer());
+    const rtl_act act = c.act();
     const bool with_bias = c.truth(), with_hidden = c.truth();
     at::ScalarType type = c.truth() ? kF32 : kBf16;
     Result r[4];
@@ -220,10 +244,10 @@ int64_t sequences(const Tensor* offsets) {
 // x, y, gate, w_post, w_pre, scale, shift, offsets, post, pre, alpha, eps, with_x, with_h, (x', h) or None
 PyObject* residual_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 17);
+    Call c(args, n, 15);
     const Tensor *x = c.tensor(), *y = c.tensor(), *gate = c.tensor(), *w_post = c.tensor(), *w_pre = c.tensor(), *scale = c.tensor(), *shift = c.tensor(),
                  *offsets = c.tensor();
-    const auto post = static_cast<rtl_norm>(c.integer()), pre = static_cast<rtl_norm>(c.integer());
+    const rtl_norm post = c.norm("post"), pre = c.norm("pre");
     const float alpha = c.real(), eps = c.real();
     const bool with_x = c.truth(), with_h = c.truth();
     Result r[2];
@@ -252,10 +276,10 @@ PyObject* residual_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // dx_out, dh, x_out, y, gate, w_post, w_pre, scale, offsets, post, pre, alpha, eps, with_shift (-1: with scale), seven results or None, workspace
 PyObject* residual_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 18);
+    Call c(args, n, 16);
     const Tensor *dx_out = c.tensor(), *dh = c.tensor(), *x_out = c.tensor(), *y = c.tensor(), *gate = c.tensor(), *w_post = c.tensor(), *w_pre = c.tensor(),
                  *scale = c.tensor(), *offsets = c.tensor();
-    const auto post = static_cast<rtl_norm>(c.integer()), pre = static_cast<rtl_norm>(c.integer());
+    const rtl_norm post = c.norm("post"), pre = c.norm("pre");
     const float alpha = c.real(), eps = c.real();
     const int64_t with_shift = c.integer();
     Result r[7];
@@ -328,9 +352,9 @@ struct Rotation {
 // q, k, pos, freq, axis, wq, wk, norm, eps, interleaved, (q', k') or None
 PyObject* norm_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 13);
+    Call c(args, n, 11);
     const Tensor *q = c.tensor(), *k = c.tensor(), *pos = c.tensor(), *freq = c.tensor(), *axis = c.tensor(), *wq = c.tensor(), *wk = c.tensor();
-    const auto norm = static_cast<rtl_norm>(c.integer());
+    const rtl_norm norm = c.norm("norm");
     const float eps = c.real();
     const bool interleaved = c.truth();
     Result r[2];
@@ -357,10 +381,10 @@ PyObject* norm_rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
 // dq_out, dk_out, q, k, pos, freq, axis, wq, wk, norm, eps, interleaved, (dq, dk, dwq, dwk) or None, workspace
 PyObject* norm_rotary_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    Call c(args, n, 16);
+    Call c(args, n, 14);
     const Tensor *dq_out = c.tensor(), *dk_out = c.tensor(), *q = c.tensor(), *k = c.tensor(), *pos = c.tensor(), *freq = c.tensor(), *axis = c.tensor(),
                  *wq = c.tensor(), *wk = c.tensor();
-    const auto norm = static_cast<rtl_norm>(c.integer());
+    const rtl_norm norm = c.norm("norm");
     const float eps = c.real();
     const bool interleaved = c.truth();
     Result r[4];
@@ -400,4 +424,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_block", "Argument marshalling of 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__block() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__block() {
+    PyObject* torch = PyImport_ImportModule("torch._C");
+    if (!torch) return nullptr;
+    current_device = PyObject_GetAttrString(torch, "_cuda_getDevice");
+    current_stream = current_device ? PyObject_GetAttrString(torch, "_cuda_getCurrentRawStream") : nullptr;
+    Py_DECREF(torch);
+    return current_stream ? PyModule_Create(&module) : nullptr;
+}

@@ -189,3 +189,15 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
                  lambda: rtl.norm_rotary_backward(x.view(4, 1, 64), None, None, None, None, None, None)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_names_what_it_takes():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for call, where in ((lambda: rtl.residual_norm(None), "x expected"), (lambda: rtl.norm_rotary(None, None, None, None, None), "q or k"),
+                        (lambda: rtl.residual_norm(None, post="l2"), "post: one of none, rms, layer"), (lambda: rtl.residual_norm(None, pre=1), "pre: one of none, rms, layer"),
+                        (lambda: rtl.gated_linear(None, None, act="relu"), "X and W|act: one of silu, gelu, gelu_tanh"),
+                        (lambda: rtl.norm_rotary(None, None, None, None, None, norm="rms "), "norm: one of none, rms, layer"),
+                        (lambda: rtl.residual_norm(x), "current device only"), (lambda: rtl.residual_norm([1.0]), "tensor or None"),
+                        (lambda: rtl.residual_norm(None, out=(None,)), "out: 2 tensors")):
+        with pytest.raises(ValueError, match=where):
+            call()
