@@ -15,9 +15,9 @@ constexpr auto kF32 = at::kFloat;
 
 const char* name_of(at::ScalarType t) { return t == kBf16 ? "torch.bfloat16" : t == kF32 ? "torch.float32" : t == at::kInt ? "torch.int32" : "torch.uint8"; }
 
-// A result: the caller's tensor, a new one, or none.
+// A result: the caller's tensor, held while the call runs without the interpreter's lock, a new one, or none.
 struct Result {
-    PyObject* given = nullptr;
+    THPObjectPtr given;
     Tensor fresh;
     const Tensor* t = nullptr;
 };
@@ -88,9 +88,11 @@ struct Call {
         if (o == Py_None) return false;
         TORCH_CHECK_VALUE((PyTuple_Check(o) || PyList_Check(o)) && PySequence_Fast_GET_SIZE(o) == N, "out: ", N, " tensors or None expected");
         for (int i = 0; i < N; ++i) {
-            r[i].given = PySequence_Fast_GET_ITEM(o, i);
-            r[i].t = tensor(r[i].given);
-            if (!r[i].t) r[i].given = nullptr;
+            PyObject* item = PySequence_Fast_GET_ITEM(o, i);
+            r[i].t = tensor(item);
+            if (!r[i].t) continue;
+            Py_INCREF(item);
+            r[i].given = item;
         }
         return true;
     }
@@ -151,10 +153,8 @@ PyObject* answer(rtl_status status, Result (&r)[N]) {
     if (!out) throw python_error();
     if (status != RTL_OK) return out;
     for (int i = 0; i < N; ++i) {
-        PyObject* o = Py_None;
-        if (r[i].given) o = r[i].given;
-        else if (r[i].t) o = THPVariable_Wrap(std::move(r[i].fresh));
-        if (o == Py_None || r[i].given) Py_INCREF(o);
+        PyObject* o = r[i].given ? r[i].given.release() : r[i].t ? THPVariable_Wrap(std::move(r[i].fresh)) : Py_None;
+        if (o == Py_None) Py_INCREF(o);
         PyTuple_SET_ITEM(out, i, o);
     }
     return out;
