@@ -156,7 +156,7 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
     __shared__ float slots[2 * WAVES];
     constexpr int TEAM = WAVES * 64, TEAMS = team_threads(WAVES) / TEAM;
     const int tl = threadIdx.x % TEAM;
-    const int64_t row = (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
+    const int64_t row = a.first + (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
     if (row >= a.T) return;
     const int D = (int)a.D;
     auto column = [&](int c) { return (uint32_t)((c * TEAM + tl) * 8); };
@@ -531,14 +531,23 @@ int64_t team_rows(int64_t T, int64_t D) {
 
 }  // namespace
 
-hipError_t launch_residual_norm(const NormArgs& a, hipStream_t stream) {
+// Workgroups of one launch, which takes fewer than 2^32 threads: 2^23 rows of more than 4096 columns, 512 threads each, would have as many.
+constexpr int64_t kMostNormGroups = (int64_t)1 << 22;
+
+hipError_t launch_residual_norm(const NormArgs& a_in, hipStream_t stream) {
+    NormArgs a = a_in;
     return with_team(a.T, a.D, [&](auto waves, auto chunks) {
         constexpr int W = decltype(waves)::value, C = decltype(chunks)::value;
-        const int64_t teams = team_threads(W) / (W * 64);
-        const dim3 grid((unsigned)((a.T + teams - 1) / teams)), block(team_threads(W));
-        if (a.x_f32) hipLaunchKernelGGL((norm_kernel<W, C, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((norm_kernel<W, C, false>), grid, block, 0, stream, a);
-        return hipGetLastError();
+        constexpr int64_t teams = team_threads(W) / (W * 64), most = kMostNormGroups * teams;
+        hipError_t e = hipSuccess;
+        for (a.first = 0; a.first < a.T && e == hipSuccess; a.first += most) {
+            const int64_t rows = a.T - a.first < most ? a.T - a.first : most;
+            const dim3 grid((unsigned)((rows + teams - 1) / teams)), block(team_threads(W));
+            if (a.x_f32) hipLaunchKernelGGL((norm_kernel<W, C, true>), grid, block, 0, stream, a);
+            else hipLaunchKernelGGL((norm_kernel<W, C, false>), grid, block, 0, stream, a);
+            e = hipGetLastError();
+        }
+        return e;
     });
 }
 

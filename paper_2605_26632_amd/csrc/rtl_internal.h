@@ -242,6 +242,7 @@ struct NormArgs {
     int post, pre;          // rtl_norm
     float alpha, eps;
     bool x_f32, clear;
+    int64_t first;          // first row of the launch, filled in there
 };
 struct NormGradArgs {
     const void *dx_out, *x;                                          // x: x' of the forward pass; dx_out nullable
