@@ -194,11 +194,13 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
         float w[8], g[8];
-        vector(a.w_post, 0, c, kOnes, w);
-        vector(a.gate, s * a.ld_gate, c, kOnes, g);
+        if (a.y) {                           // (without y neither vector is looked at: what it holds need not be finite)
+            vector(a.w_post, 0, c, kOnes, w);
+            vector(a.gate, s * a.ld_gate, c, kOnes, g);
+        }
         if (column(c) < (uint32_t)D) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
+            for (int e = 0; e < 8; ++e) x[c][e] = a.y ? a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale)) : a.alpha * x[c][e];
             if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, column(c), x[c]);
         }
     }
