@@ -349,9 +349,9 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(con
             f_pre[e] = f_post[e] = 1.0f;
         }
         const uint32_t col = column();
-        if (a.w_pre) load8(a.w_pre, col, f_pre);
+        if (a.w_pre && a.dh) load8(a.w_pre, col, f_pre);          // (without dh neither is looked at: zeros times them need not be zeros)
         if (a.w_post) load8(a.w_post, col, f_post);
-        if (a.scale) {
+        if (a.scale && a.dh) {
             float v[8];
             load8(a.scale + s * a.ld_mod, col, v);
 #pragma unroll
@@ -478,8 +478,8 @@ __global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_reduce_kerne
         if (a.dw_post && a.S == 1) a.dw_post[col] = sum * bf16_or(a.gate, col, 1.0f);
         else if (a.dw_post) a.totals[(int64_t)s * 2 * D + col] = sum;
     } else if (slice == 1) {
-        if (a.dscale) a.dscale[at] = sum * bf16_or(a.w_pre, col, 1.0f);
-        if (a.dw_pre && a.S == 1) a.dw_pre[col] = sum * (1.0f + bf16_or(a.scale, col, 0.0f));
+        if (a.dscale) a.dscale[at] = a.dh ? sum * bf16_or(a.w_pre, col, 1.0f) : 0.f;
+        if (a.dw_pre && a.S == 1) a.dw_pre[col] = a.dh ? sum * (1.0f + bf16_or(a.scale, col, 0.0f)) : 0.f;
         else if (a.dw_pre) a.totals[((int64_t)s * 2 + 1) * D + col] = sum;
     } else if (a.dshift) {
         a.dshift[at] = sum;
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_weights_kern
     float v[2] = {};
     for (int64_t s = slice; s < a.S; s += kReduceSlices) {
         if (a.dw_post) v[0] += a.totals[s * 2 * D + col] * bf16_or(a.gate, s * a.ld_gate + col, 1.0f);
-        if (a.dw_pre) v[1] += a.totals[(s * 2 + 1) * D + col] * (1.0f + bf16_or(a.scale, s * a.ld_mod + col, 0.0f));
+        if (a.dw_pre && a.dh) v[1] += a.totals[(s * 2 + 1) * D + col] * (1.0f + bf16_or(a.scale, s * a.ld_mod + col, 0.0f));
     }
     part[0][slice][lane] = v[0];
     part[1][slice][lane] = v[1];

@@ -8,6 +8,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 EPS = 1e-6
 BAD = [float("inf"), float("-inf"), float("nan")]
+NAMES = ("dx", "dy", "dgate", "dscale", "dshift", "dw_post", "dw_pre")
 
 
 def normal(seed, *shape, dtype=torch.bfloat16, std=1.0, mean=0.0):
@@ -40,6 +41,26 @@ def test_no_branch_no_gate(D, bad, wide):
     got = rtl.residual_norm(x, gate=spoilt(2, 3, D, bad=bad), w_post=spoilt(3, D, bad=bad), **how)
     assert torch.equal(got[0], x * 0.5) and bool(torch.signbit(got[0][3]).all())
     assert torch.equal(got[1], want[1]) and bool(torch.isfinite(got[1]).all())
+
+
+@pytest.mark.parametrize("D", [64, 1032])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("post,pre", [("none", "layer"), ("rms", "rms")])
+def test_no_gradient_no_modulation(D, bad, post, pre):
+    """With dh None nothing passes through the second norm, whatever w_pre and scale hold: their gradients are zeros, the others those of ordinary ones."""
+    dx, x, y = (normal(i, 20, D) for i in (4, 5, 6))
+    offsets = torch.tensor(OFFSETS, dtype=torch.int32, device=DEV)
+    how = dict(gate=normal(7, 3, D), w_post=normal(8, D), offsets=offsets, post=post, pre=pre, alpha=0.5, eps=EPS)
+    want = rtl.residual_norm_backward(dx, None, x, y, w_pre=normal(9, D), scale=normal(10, 3, D), **how)
+    got = rtl.residual_norm_backward(dx, None, x, y, w_pre=spoilt(9, D, bad=bad), scale=spoilt(10, 3, D, bad=bad), **how)
+    for name, g, w in zip(NAMES, got, want):
+        assert torch.equal(g, w) and bool(torch.isfinite(g).all()), name
+    for i in (3, 4, 6):
+        assert bool((got[i] == 0).all())
+    one = dict(how, gate=how["gate"][:1], offsets=None)             # (a single sequence has its sums from another kernel)
+    got = dict(zip(NAMES, rtl.residual_norm_backward(dx, None, x, y, w_pre=spoilt(9, D, bad=bad), scale=spoilt(10, 1, D, bad=bad), **one)))
+    for name in ("dscale", "dshift", "dw_pre"):
+        assert bool((got[name] == 0).all()), name
 
 
 def test_zz_most_rows_of_wide_norms():
