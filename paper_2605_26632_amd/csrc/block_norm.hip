@@ -473,28 +473,37 @@ __global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_reduce_kerne
     float sum = part[slice][0][lane];
     for (int w = 1; w < kReduceSlices; ++w) sum += part[slice][w][lane];
     const int64_t at = (int64_t)s * D + col;
+    // Zero where there is nothing to sum up, whatever the vectors of a sequence without rows, or of a gradient that is not there, hold.
+    const bool any = begin < end, any_h = any && a.dh;
     if (slice == 0) {
-        if (a.dgate) a.dgate[at] = sum * bf16_or(a.w_post, col, 1.0f);
-        if (a.dw_post && a.S == 1) a.dw_post[col] = sum * bf16_or(a.gate, col, 1.0f);
+        if (a.dgate) a.dgate[at] = any ? sum * bf16_or(a.w_post, col, 1.0f) : 0.f;
+        if (a.dw_post && a.S == 1) a.dw_post[col] = any ? sum * bf16_or(a.gate, col, 1.0f) : 0.f;
         else if (a.dw_post) a.totals[(int64_t)s * 2 * D + col] = sum;
     } else if (slice == 1) {
-        if (a.dscale) a.dscale[at] = a.dh ? sum * bf16_or(a.w_pre, col, 1.0f) : 0.f;
-        if (a.dw_pre && a.S == 1) a.dw_pre[col] = a.dh ? sum * (1.0f + bf16_or(a.scale, col, 0.0f)) : 0.f;
+        if (a.dscale) a.dscale[at] = any_h ? sum * bf16_or(a.w_pre, col, 1.0f) : 0.f;
+        if (a.dw_pre && a.S == 1) a.dw_pre[col] = any_h ? sum * (1.0f + bf16_or(a.scale, col, 0.0f)) : 0.f;
         else if (a.dw_pre) a.totals[((int64_t)s * 2 + 1) * D + col] = sum;
     } else if (a.dshift) {
         a.dshift[at] = sum;
     }
 }
 
-// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s, the sequences dealt as the slots above.
+// dw_post = sum_s gate_s totals_s, dw_pre = sum_s (1 + scale_s) totals_s over the sequences that have rows, dealt as the slots above.
 __global__ __launch_bounds__(kReduceCols * kReduceSlices) void norm_weights_kernel(const NormGradArgs a) {
     __shared__ float part[2][kReduceSlices][kReduceCols];
     const int lane = threadIdx.x % kReduceCols, slice = threadIdx.x / kReduceCols, D = (int)a.D;
     const int col0 = blockIdx.x * kReduceCols, col = min(col0 + lane, D - 1);
     float v[2] = {};
     for (int64_t s = slice; s < a.S; s += kReduceSlices) {
-        if (a.dw_post) v[0] += a.totals[s * 2 * D + col] * bf16_or(a.gate, s * a.ld_gate + col, 1.0f);
-        if (a.dw_pre && a.dh) v[1] += a.totals[(s * 2 + 1) * D + col] * (1.0f + bf16_or(a.scale, s * a.ld_mod + col, 0.0f));
+        const bool any = min(max(a.offsets[s], 0), (int)a.T) < min(max(a.offsets[s + 1], 0), (int)a.T);       // (several sequences or none: there are offsets)
+        if (a.dw_post) {
+            const float total = a.totals[s * 2 * D + col], factor = bf16_or(a.gate, s * a.ld_gate + col, 1.0f);
+            v[0] = any ? v[0] + total * factor : v[0];
+        }
+        if (a.dw_pre && a.dh) {
+            const float total = a.totals[(s * 2 + 1) * D + col], factor = 1.0f + bf16_or(a.scale, s * a.ld_mod + col, 0.0f);
+            v[1] = any ? v[1] + total * factor : v[1];
+        }
     }
     part[0][slice][lane] = v[0];
     part[1][slice][lane] = v[1];

@@ -63,6 +63,32 @@ def test_no_gradient_no_modulation(D, bad, post, pre):
         assert bool((got[name] == 0).all()), name
 
 
+@pytest.mark.parametrize("D", [64, 1032])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("behind", [0, 5])
+def test_vectors_of_empty_sequences(D, bad, behind):
+    """What gate and scale hold for a sequence without rows reaches no weight's gradient; its own gradients are zeros, whatever the weights hold."""
+    dx, dh, x, y = (normal(i, 20, D) for i in (11, 12, 13, 14))
+    offsets = torch.tensor([o if i < 3 else 20 - behind for i, o in enumerate(OFFSETS + [20])], dtype=torch.int32, device=DEV)      # the last one empty too
+    gate, scale = normal(15, 4, D), normal(16, 4, D)
+    how = dict(w_post=normal(17, D), w_pre=normal(18, D), offsets=offsets, post="rms", pre="layer", eps=EPS)
+    want = rtl.residual_norm_backward(dx, dh, x, y, gate=gate, scale=scale, **how)
+    gate[1], gate[3], scale[1], scale[3] = bad, bad, bad, bad
+    got = rtl.residual_norm_backward(dx, dh, x, y, gate=gate, scale=scale, **how)
+    for name, g, w in zip(NAMES, got, want):
+        assert torch.equal(g, w) and bool(torch.isfinite(g).all()), name
+    got = dict(zip(NAMES, rtl.residual_norm_backward(dx, dh, x, y, gate=gate, scale=scale, **dict(how, w_post=spoilt(17, D, bad=bad), w_pre=spoilt(18, D, bad=bad)))))
+    for name in ("dgate", "dscale", "dshift"):
+        assert bool((got[name][1] == 0).all()) and bool((got[name][3] == 0).all()), name
+    # a single sequence without rows, and no rows at all
+    none = torch.tensor([4, 4], dtype=torch.int32, device=DEV)
+    for rows, off in ((20, none), (0, None)):
+        got = rtl.residual_norm_backward(dx[:rows], dh[:rows], x[:rows], y[:rows], gate=gate[1:2], scale=scale[1:2],
+                                         **dict(how, offsets=off, w_post=spoilt(17, D, bad=bad), w_pre=spoilt(18, D, bad=bad)))
+        for name, g in zip(NAMES, got):
+            assert bool((g == 0).all()), name
+
+
 def test_zz_most_rows_of_wide_norms():
     """So many rows of more than 4096 columns that one launch would have 2^32 threads and more: each row is taken once."""
     T, D, step = (1 << 23) + 3, 4104, 1 << 20
