@@ -200,7 +200,7 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
         }
         if (column(c) < (uint32_t)D) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] = a.y ? a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale)) : a.alpha * x[c][e];
+            for (int e = 0; e < 8; ++e) x[c][e] = a.y ? fmaf(a.alpha, x[c][e], g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale))) : a.alpha * x[c][e];
             if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, column(c), x[c]);
         }
     }
