@@ -65,21 +65,23 @@ __device__ __forceinline__ void turn(float pos, float freq, float& sn, float& cs
 }
 
 // What a lane does in every head: its two chunks of eight values (first value, or -1 for none) and its eight pairs. HALVES: element e of the first chunk and
-// of the second are pair e; else a chunk holds four pairs, of which the lane has the two chunks' eight. Pairs from `pairs` on are turned by nothing.
+// of the second are pair e; else a chunk holds four pairs, of which the lane has the two chunks' eight.
+// Chunks that only pass are left alone: turned by zero, a value that is not finite would reach the other of its pair.
 constexpr int kMostPairs = 256 + 8;
 struct LanePlan {
     int at[2], pair0;
+    bool turned[2];          // of each chunk (HALVES: of both)
 };
 template <bool HALVES>
 __device__ __forceinline__ LanePlan lane_plan(int c, int D, int pairs) {
     const int chunks = D / 8, none = (pairs + 7) / 8 * 8;
     if constexpr (HALVES) {
         const int half = pairs / 8, rest = 2 * half + 2 * (c - half);
-        if (c < half) return LanePlan{{c * 8, (c + half) * 8}, c * 8};
-        return LanePlan{{rest < chunks ? rest * 8 : -1, rest + 1 < chunks ? (rest + 1) * 8 : -1}, none};
+        if (c < half) return LanePlan{{c * 8, (c + half) * 8}, c * 8, {true, true}};
+        return LanePlan{{rest < chunks ? rest * 8 : -1, rest + 1 < chunks ? (rest + 1) * 8 : -1}, none, {false, false}};
     } else {
         const int i = 2 * c;
-        return LanePlan{{i < chunks ? i * 8 : -1, i + 1 < chunks ? (i + 1) * 8 : -1}, min(c * 8, none)};
+        return LanePlan{{i < chunks ? i * 8 : -1, i + 1 < chunks ? (i + 1) * 8 : -1}, min(c * 8, none), {i * 4 < pairs, i * 4 + 4 < pairs}};
     }
 }
 
@@ -111,14 +113,15 @@ __device__ __forceinline__ Turns token_turns(const RotaryArgs& a, const LanePlan
 
 // Both chunks turned; BACK: by the negative angle.
 template <bool HALVES, bool BACK>
-__device__ __forceinline__ void apply_turns(float (&v)[2][8], const Turns& t) {
+__device__ __forceinline__ void apply_turns(float (&v)[2][8], const Turns& t, const LanePlan& plan) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float& x = HALVES ? v[0][e] : v[e / 4][2 * (e % 4)];
         float& y = HALVES ? v[1][e] : v[e / 4][2 * (e % 4) + 1];
         const float s = BACK ? -t.sn[e] : t.sn[e], p = x * t.cs[e] - y * s, q = x * s + y * t.cs[e];
-        x = p;
-        y = q;
+        const bool turned = plan.turned[HALVES ? 0 : e / 4];
+        x = turned ? p : x;
+        y = turned ? q : y;
     }
 }
 
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArg
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[c][e] *= r * w[c][e];
         }
-        apply_turns<HALVES, false>(v, turns);
+        apply_turns<HALVES, false>(v, turns, plan);
         store_chunks(out + h * side.so, plan, v);
     }
 }
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(con
             if (a.norm) {
                 float v[2][8];
                 load_chunks(in + h * side.s, plan, v);
-                apply_turns<HALVES, true>(d, turns);
+                apply_turns<HALVES, true>(d, turns, plan);
                 const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) * inv + a.eps);
                 float m = 0.f;
 #pragma unroll
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(con
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[c][e] = r * (d[c][e] - v[c][e] * m);
             } else {
-                apply_turns<HALVES, true>(d, turns);
+                apply_turns<HALVES, true>(d, turns, plan);
             }
             store_chunks(out + h * side.so, plan, d);
         }

@@ -89,6 +89,30 @@ def test_vectors_of_empty_sequences(D, bad, behind):
             assert bool((g == 0).all()), name
 
 
+@pytest.mark.parametrize("interleaved", [True, False])
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("D,pairs", [(64, 8), (72, 24), (128, 48), (96, 0), (264, 8), (24, 8)])
+def test_values_behind_the_pairs_pass(interleaved, bad, D, pairs):
+    """Each by itself: one that is not finite leaves the others as they are, and a negative zero keeps its sign."""
+    T, H = 9, 3
+    pos, freq = normal(21, T, 2, dtype=torch.float32), normal(22, pairs, dtype=torch.float32)
+    axis = torch.arange(pairs, dtype=torch.int32, device=DEV) % 2
+    v = normal(23, T, H, D)
+    v[:, 1, 2 * pairs:] = -0.0
+    for at in range(2 * pairs, D):
+        v[at % T, 2, at] = bad                                     # in each place once, several in a head where there are more places than tokens
+    how = dict(norm="none", interleaved=interleaved)
+    turned = rtl.norm_rotary(v, None, pos, freq, axis, **how)[0]
+    back = rtl.norm_rotary_backward(v, None, None, None, pos, freq, axis, **how)[0]
+    plain = v.clone()
+    plain[..., 2 * pairs:] = 0
+    want = rtl.norm_rotary(plain, None, pos, freq, axis, **how)[0], rtl.norm_rotary_backward(plain, None, None, None, pos, freq, axis, **how)[0]
+    for got, w in zip((turned, back), want):
+        assert torch.equal(got[..., :2 * pairs], w[..., :2 * pairs])
+        a, b = got[..., 2 * pairs:], v[..., 2 * pairs:]
+        assert bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all()) and bool(torch.signbit(a[:, 1]).all())
+
+
 def test_zz_most_rows_of_wide_norms():
     """So many rows of more than 4096 columns that one launch would have 2^32 threads and more: each row is taken once."""
     T, D, step = (1 << 23) + 3, 4104, 1 << 20
