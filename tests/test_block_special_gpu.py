@@ -1,7 +1,11 @@
 """The block operators on the GPU where care is called for: vectors that should not matter and are not finite, gates far below zero, launches of the largest size."""
+import math
+
 import pytest
 import torch
 
+import block_plan as plan
+import block_ref as ref
 from paper_2605_26632_amd import binding as rtl
 
 pytestmark = pytest.mark.gpu
@@ -111,6 +115,52 @@ def test_values_behind_the_pairs_pass(interleaved, bad, D, pairs):
         assert torch.equal(got[..., :2 * pairs], w[..., :2 * pairs])
         a, b = got[..., 2 * pairs:], v[..., 2 * pairs:]
         assert bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all()) and bool(torch.signbit(a[:, 1]).all())
+
+
+def far_gates():
+    return torch.linspace(-12.5, -0.5, 400).to(torch.bfloat16).to(DEV)
+
+
+def gelu_below_zero(g):
+    """Value and slope of g < 0 in 64 bits and how far they may be off. U = 2^-24; Phi(g) = .5 P(t) e, e = exp(-x), x = g^2 / 2. P is off by 2e-7 of itself as a formula;
+    t by 4 U, which P magnifies at most 3.4 times; its evaluation has eight steps of two roundings, each of at most twice P: 14 + 32 U. e: 4 x U from its
+    argument's roundings and 4 U. Two products: 2 U. In all (4 x + 52) U + 2e-7 of Phi itself, so that nothing is forgiven where Phi is small."""
+    g = g.double()
+    x, phi = g * g / 2, 0.5 * torch.special.erfc(-g / math.sqrt(2))
+    rel = (4 * x + 52) * ref.U + 2e-7
+    bell = g * torch.exp(-x) / math.sqrt(2 * math.pi)
+    return g * phi, (g * phi).abs() * (rel + ref.U), phi + bell, phi * rel + bell.abs() * (4 * x + 10) * ref.U + ref.U * (phi + bell).abs()
+
+
+# rows and contractions that reach each form of the launch at 400 columns
+GELU_SIZES = [(1, 64), (20, 256), (400, 512), (800, 1024), (2100, 2048), (4000, 64), (3000, 128), (20, 64), (6000, 64), (12000, 64)]
+
+
+def test_gelu_sizes_reach_their_forms():
+    assert [plan.gated_form(M, 400, K) for M, K in GELU_SIZES] == ["few", 0, 1, 2, 3, 4, 5, 6, "tails", "192"]
+
+
+@pytest.mark.parametrize("M,K", GELU_SIZES)
+def test_gelu_far_below_zero(M, K):
+    """H at gates whose Phi is down to 4e-36: right to a rounding."""
+    g = far_gates()
+    F = g.numel()
+    X, W = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV), torch.zeros(2 * F, K, dtype=torch.bfloat16, device=DEV)
+    X[:, 0], W[:F, 0], W[F:, 0] = 1.0, g, 1.0
+    value, err, _, _ = gelu_below_zero(g)
+    ref.close(rtl.gated_linear(X, W, act="gelu"), value.expand(M, F), err.expand(M, F), "H")
+
+
+def test_gelu_gradients_far_below_zero():
+    g = far_gates()
+    M, F = 3, g.numel()
+    P = torch.cat([g, torch.ones_like(g)]).expand(M, 2 * F).contiguous()
+    eye, dH = torch.eye(2 * F, dtype=torch.bfloat16, device=DEV), torch.ones(M, F, dtype=torch.bfloat16, device=DEV)
+    dP, _, _, H = rtl.gated_linear_backward(dH, None, eye, P, act="gelu", with_hidden=True)        # (weights of the identity: dX is [dG dU])
+    value, err, slope, err_slope = gelu_below_zero(g)
+    ref.close(H, value.expand(M, F), err.expand(M, F), "H")
+    ref.close(dP[:, F:], value.expand(M, F), err.expand(M, F), "dU")
+    ref.close(dP[:, :F], slope.expand(M, F), err_slope.expand(M, F), "dG")
 
 
 def test_zz_most_rows_of_wide_norms():
