@@ -192,7 +192,8 @@ def prepare(case, seed):
             st["dx"] = _normal(gen, T, D, dtype=kind)
             st["dh"] = _normal(gen, T, D)
         elif own:
-            st["out"] = (torch.zeros(T, D, dtype=kind, device=DEV), torch.zeros(T, D, dtype=bf, device=DEV))
+            # a program keeps its results; where rows belong to nobody it takes new ones, in which the call writes those rows as zeros
+            st["out"] = None if case["spare"] else (torch.empty(T, D, dtype=kind, device=DEV), torch.empty(T, D, dtype=bf, device=DEV))
         if own and op == "norm_backward":
             from paper_2605_26632_amd import binding as rtl
             st["room"] = torch.empty(rtl.residual_norm_backward_workspace(T, S, D), dtype=torch.uint8, device=DEV)
