@@ -180,11 +180,17 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
         if (p && column(c) < (uint32_t)D) v = *reinterpret_cast<const uint4*>(p + at + column(c));
         unpack8(v, f);
     };
+    // Without y its vectors count as ones, whatever they hold, and its values as -0: alpha x plus that is alpha x, the sign of a zero too.
+    // (Branches around the vectors took 3 to 4 % longer, [16896, 3840] 102 -> 105 us.)
+    const float none = a.y ? 0.f : -0.f;
     float x[NCH][8], y[NCH][8];
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[c][e] = y[c][e] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            x[c][e] = 0.f;
+            y[c][e] = none;
+        }
         if (column(c) < (uint32_t)D) {
             load8_as<F32>(a.x, row * a.ldx, column(c), x[c]);
             if (a.y) load8(a.y + row * a.ldy, column(c), y[c]);
@@ -194,13 +200,11 @@ __global__ __launch_bounds__(team_threads(WAVES)) void norm_kernel(const NormArg
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
         float w[8], g[8];
-        if (a.y) {                           // (without y neither vector is looked at: what it holds need not be finite)
-            vector(a.w_post, 0, c, kOnes, w);
-            vector(a.gate, s * a.ld_gate, c, kOnes, g);
-        }
+        vector(a.y ? a.w_post : nullptr, 0, c, kOnes, w);
+        vector(a.y ? a.gate : nullptr, s * a.ld_gate, c, kOnes, g);
         if (column(c) < (uint32_t)D) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[c][e] = a.y ? fmaf(a.alpha, x[c][e], g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale))) : a.alpha * x[c][e];
+            for (int e = 0; e < 8; ++e) x[c][e] = a.alpha * x[c][e] + g[e] * (w[e] * ((y[c][e] - sy.mean) * sy.scale));
             if (a.x_out) store8_as<F32>(a.x_out, row * a.ldxo, column(c), x[c]);
         }
     }
