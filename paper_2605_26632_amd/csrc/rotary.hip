@@ -111,15 +111,16 @@ __device__ __forceinline__ Turns token_turns(const RotaryArgs& a, const LanePlan
     return t;
 }
 
-// Both chunks turned; BACK: by the negative angle.
-template <bool HALVES, bool BACK>
+// Both chunks turned; BACK: by the negative angle. PART: there are values behind the pairs. (Selections in place of the template took heads that are turned
+// whole 1 % longer, [16896, 30 + 30, 128] 102 -> 103 us, branches 2 to 5 %.)
+template <bool HALVES, bool BACK, bool PART>
 __device__ __forceinline__ void apply_turns(float (&v)[2][8], const Turns& t, const LanePlan& plan) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float& x = HALVES ? v[0][e] : v[e / 4][2 * (e % 4)];
         float& y = HALVES ? v[1][e] : v[e / 4][2 * (e % 4) + 1];
         const float s = BACK ? -t.sn[e] : t.sn[e], p = x * t.cs[e] - y * s, q = x * s + y * t.cs[e];
-        const bool turned = plan.turned[HALVES ? 0 : e / 4];
+        const bool turned = !PART || plan.turned[HALVES ? 0 : e / 4];
         x = turned ? p : x;
         y = turned ? q : y;
     }
@@ -161,7 +162,7 @@ __device__ __forceinline__ float square_sum(const float (&v)[2][8]) {
 // neighbouring heads, and memory gives more than to waves that go through a token each, though every wave takes the token's sines anew (us, a token to a wave |
 // one time): [16896, 30 + 30, 128] 105 | 96, [16896, 40 + 40, 128] 139 | 123, [5000, 64 + 8, 128] 32.8 | 29.0, [1, 30 + 30, 128] 4.3 | 3.2;
 // [4096, 24 + 24, 128] 17.7 | 18.1, [16896, 12 + 12, 256] 82.7 | 84.3. The first side[0].groups workgroups have the heads of q, the others those of k.
-template <int L, bool HALVES>
+template <int L, bool HALVES, bool PART>
 __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArgs a) {
     __shared__ float lds[kHeadWaves][2][kMostPairs];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArg
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[c][e] *= r * w[c][e];
         }
-        apply_turns<HALVES, false>(v, turns, plan);
+        apply_turns<HALVES, false, PART>(v, turns, plan);
         store_chunks(out + h * side.so, plan, v);
     }
 }
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArg
 // The same walk for the gradients; a wave goes on to further tokens, and what it has of the weight's gradient goes to the workspace at the end, a
 // workgroup's four waves and a wave's 64 / L heads added up in order. [4433, 30 + 30, 128] 36 us, 204 MB (some of them in the cache behind L2), and 5
 // for the reduction.
-template <int L, bool HALVES>
+template <int L, bool HALVES, bool PART>
 __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(const RotaryArgs a) {
     __shared__ float lds[kHeadWaves][2][kMostPairs];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(con
             if (a.norm) {
                 float v[2][8];
                 load_chunks(in + h * side.s, plan, v);
-                apply_turns<HALVES, true>(d, turns, plan);
+                apply_turns<HALVES, true, PART>(d, turns, plan);
                 const float r = 1.0f / sqrtf(head_sum<L>(square_sum(v)) * inv + a.eps);
                 float m = 0.f;
 #pragma unroll
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(con
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[c][e] = r * (d[c][e] - v[c][e] * m);
             } else {
-                apply_turns<HALVES, true>(d, turns, plan);
+                apply_turns<HALVES, true, PART>(d, turns, plan);
             }
             store_chunks(out + h * side.so, plan, d);
         }
@@ -291,14 +292,21 @@ __global__ __launch_bounds__(1024) void rotary_reduce_kernel(const RotaryArgs a)
     side.dw[i] = s;
 }
 
-// f(lanes of a head)
+// f(lanes of a head, pairs in halves, values behind the pairs)
 template <class F>
-hipError_t with_lanes(int D, F f) {
+hipError_t with_form(const RotaryArgs& a, F f) {
     using std::integral_constant;
-    if (D <= 64) return f(integral_constant<int, 4>{});
-    if (D <= 128) return f(integral_constant<int, 8>{});
-    if (D <= 256) return f(integral_constant<int, 16>{});
-    return f(integral_constant<int, 32>{});
+    auto go = [&](auto lanes) {
+        using T = std::true_type;
+        using N = std::false_type;
+        const bool part = 2 * a.pairs < a.D;
+        if (a.interleaved) return part ? f(lanes, N{}, T{}) : f(lanes, N{}, N{});
+        return part ? f(lanes, T{}, T{}) : f(lanes, T{}, N{});
+    };
+    if (a.D <= 64) return go(integral_constant<int, 4>{});
+    if (a.D <= 128) return go(integral_constant<int, 8>{});
+    if (a.D <= 256) return go(integral_constant<int, 16>{});
+    return go(integral_constant<int, 32>{});
 }
 
 constexpr int64_t kMostTasks = (int64_t)1 << 23;         // of a side, where a task can be more than an iteration (a launch takes fewer than 2^32 threads)
@@ -337,8 +345,9 @@ int64_t share(const RotaryArgs& a, int i, int step) {
 size_t rotary_backward_scratch(int64_t D) { return (size_t)(kGroups + 2) * (size_t)D * sizeof(float); }
 
 hipError_t launch_rotary(const RotaryArgs& a_in, hipStream_t stream) {
-    return with_lanes(a_in.D, [&](auto lanes) {
+    return with_form(a_in, [&](auto lanes, auto halves, auto part) {
         constexpr int L = decltype(lanes)::value;
+        constexpr bool HALVES = decltype(halves)::value, PART = decltype(part)::value;
         RotaryArgs a = a_in;
         for (int i = 0; i < 2; ++i) {
             HeadSide& side = a.side[i];
@@ -351,15 +360,15 @@ hipError_t launch_rotary(const RotaryArgs& a_in, hipStream_t stream) {
             side.groups = side.H > 0 ? (unsigned)((a.T * side.splits + kHeadWaves - 1) / kHeadWaves) : 0;
         }
         const dim3 grid(a.side[0].groups + a.side[1].groups), block(kHeadWaves * 64);
-        if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<L, false>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((rotary_kernel<L, true>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((rotary_kernel<L, HALVES, PART>), grid, block, 0, stream, a);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_rotary_backward(const RotaryArgs& a_in, float* sums, hipStream_t stream) {
-    return with_lanes(a_in.D, [&](auto lanes) {
+    return with_form(a_in, [&](auto lanes, auto halves, auto part) {
         constexpr int L = decltype(lanes)::value;
+        constexpr bool HALVES = decltype(halves)::value, PART = decltype(part)::value;
         RotaryArgs a = a_in;
         for (int i = 0; i < 2; ++i) {
             HeadSide& side = a.side[i];
@@ -375,8 +384,7 @@ hipError_t launch_rotary_backward(const RotaryArgs& a_in, float* sums, hipStream
         }
         const unsigned groups = a.side[0].groups + a.side[1].groups;
         if (groups > 0) {
-            if (a.interleaved) hipLaunchKernelGGL((rotary_backward_kernel<L, false>), dim3(groups), dim3(kHeadWaves * 64), 0, stream, a);
-            else hipLaunchKernelGGL((rotary_backward_kernel<L, true>), dim3(groups), dim3(kHeadWaves * 64), 0, stream, a);
+            hipLaunchKernelGGL((rotary_backward_kernel<L, HALVES, PART>), dim3(groups), dim3(kHeadWaves * 64), 0, stream, a);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
