@@ -397,19 +397,20 @@ rtl_status rtl_gated_linear_backward(const void* dH, const void* X, const void* 
  * them, in one pass: for the rows of sequence s
  *     x' = alpha x + gate_s (w_post norm_post(y)),     h = w_pre norm_pre(x') (1 + scale_s) + shift_s.
  *   norms    RTL_NORM_NONE v, RTL_NORM_RMS v / sqrt(mean v^2 + eps), RTL_NORM_LAYER (v - mean v) / sqrt(mean (v - mean v)^2 + eps), along D.
- *   x, x_out [T, D] of x_type, RTL_BF16 or RTL_F32 (ldx, ldxo); y, h [T, D] bf16 (ldy, ldh). y NULL: x' = alpha x. x_out or h may be NULL. x_out may be x,
- *            and h may be y, in place (same rows, same stride). h is made of the x' that is not rounded yet.
+ *   x, x_out [T, D] of x_type, RTL_BF16 or RTL_F32 (ldx, ldxo); y, h [T, D] bf16 (ldy, ldh). y NULL: x' = alpha x, whatever gate and w_post hold.
+ *            x_out or h may be NULL. x_out may be x, and h may be y, in place (same rows, same stride). h is made of the x' that is not rounded yet.
  *   gate     bf16 [S, D] (ld_gate); scale, shift bf16 [S, D] (ld_mod, one for both); w_post, w_pre bf16 [D]. Any may be NULL: a gate or weight of ones,
  *            a scale or shift of zeros.
- *   offsets  device int32 [S + 1], ascending, read by the kernels alone: rows o_s up to o_{s+1} are sequence s, which may be empty. Rows in front of
- *            o_0 and from o_S on belong to nobody: they are not read, and left as they were in the results, or written as zeros with `clear`.
+ *   offsets  device int32 [S + 1], ascending, read by the kernels alone: rows o_s up to o_{s+1} are sequence s, which may be empty (its vectors are not looked
+ *            at). Rows in front of o_0 and from o_S on belong to nobody: they are not read, and left as they were in the results, or written as zeros with `clear`.
  *            NULL: all rows are one sequence (S must be 1). Whatever they hold, nothing outside of the tensors is touched; results of
  *            offsets that do not ascend are unspecified.
  *   T < 2^24, S <= 65535, D % 8 == 0, D <= 8192 (RTL_ERR_SHAPE); all rows 16-byte aligned (strides % 8 == 0 bf16, % 4 == 0 fp32).
  *
  * rtl_residual_norm_backward: from the gradients dx_out (of x_type) and dh, either of which may be NULL (none), x' as the forward call gave it, and y:
  *   dx [T, D] of x_type, dy [T, D] bf16 and the sums over rows, fp32: dgate, dscale, dshift [S, D], dw_post, dw_pre [D], all dense. Any result may be
- *   NULL; the gradient of a vector that is NULL can be asked for. dy, dgate and dw_post need y, x' is needed with dh. An empty sequence has zeros. The
+ *   NULL; the gradient of a vector that is NULL can be asked for. dy, dgate and dw_post need y, x' is needed with dh. An empty sequence has zeros and
+ *   adds nothing to dw_post and dw_pre, whatever its vectors hold; with dh NULL dscale, dshift and dw_pre are zeros, whatever w_pre and scale hold. The
  *   sums are formed in a fixed order. dx may be dx_out, dy may be dh or y, in place. S * ceil(D / 32) < 2^22.
  *   workspace  rtl_residual_norm_backward_workspace(T, S, D) bytes, 256-byte aligned; needed for the sums only.
  * ------------------------------------------------------------------------------------------- */
@@ -430,7 +431,7 @@ rtl_status rtl_residual_norm_backward(const void* dx_out, const void* dh, const 
  * Norm and rotary positions of several axes (time, height, width) for the heads of q and k, in one pass over both:
  *     n = w v / sqrt(mean v^2 + eps) along a head of D values (norm == RTL_NORM_RMS; v itself with RTL_NORM_NONE), and pair j of n turned by the angle
  *     pos[t, axis[j]] freq[j]:  (a, b) -> (a cos - b sin, a sin + b cos),  j < pairs.
- *   Pairs are values (2j, 2j + 1) of a head (interleaved != 0) or (j, j + pairs); values behind 2 pairs pass (normed).
+ *   Pairs are values (2j, 2j + 1) of a head (interleaved != 0) or (j, j + pairs); values behind 2 pairs pass (normed), each by itself.
  *   q, k     [T, Hq, D], [T, Hk, D] bf16; ldq, ldk elements between tokens, sq, sk between heads (so that heads in front of tokens, and the
  *            parts of one product that makes q, k and v, are taken as they are). Results likewise; they may be the inputs, in place (same strides).
  *            Hq or Hk of 0: without q or k.

@@ -284,7 +284,7 @@ struct Raw8 {
 // team one after the other, and the few teams that a compute unit holds would not hide the loads behind them.
 // Lanes behind the end of the row work on the row's first columns and are left out of the sums and stores only: branches around the arithmetic made the
 // compiler keep two copies of what lives across them, and spill.
-// [16896, 3840], one of the norms, 74 to 78 us, 386 MB at 5.0 TB/s, and 4.5 for the reduction; fp32 [2111, 2048] with both norms and five sequences 20 + 4.5 + 3.5.
+// [8192, 3840], one of the norms, 74 to 78 us, 386 MB at 5.0 TB/s, and 4.5 for the reduction; fp32 [2111, 2048] with both norms and five sequences 19 to 20, 4.5 to 5 and 3.5.
 // SOLO: a wave to a team, four teams to a workgroup. POST: norm(y) is not y.
 template <bool F32, bool SOLO, bool POST>
 __global__ __launch_bounds__(SOLO ? 256 : 1024, 4) void norm_backward_kernel(const NormGradArgs a) {

@@ -403,7 +403,8 @@ void gemm_choice(bool sparse, bool fp8, int64_t M, int64_t N, int64_t K, size_t 
 // 45.4 -> 39.8); 96 x 128, whose tiles fill the units where 128 rows leave some idle ([333, 2739, 4032] 25.9 -> 24.5, [11169, 70, 5952] 41.9 -> 38.5);
 // 64 x 64 with a ring of three, three to a unit, for short contractions ([600, 1500, 1024] 11.5 -> 8.4, [699, 973, 128] 5.6 -> 4.8); a unit with two of them takes
 // half as long again for a stage, three quarters of a microsecond more for each ([67, 4666, 5760] 33.6 -> 24.6 with 128 x 64 instead, [8226, 862, 64] 14.7 -> 12.0 with
-// 256 rows). Over 260 problems the choice is 1.1 % slower than the best in the mean, 21 % at worst.
+// 256 rows). Over 260 problems the choice is 1.1 % slower than the best in the mean; at worst 21 % ([144, 6103, 256] 8.4 us, 6.9 with three 64 x 64 to a unit) and 20 %
+// ([1909, 1956, 6016] 94.5, 78.9 with 256 rows).
 struct GatedShape {
     SplitShape tile;
     int held;

@@ -193,8 +193,8 @@ __global__ __launch_bounds__(kHeadWaves * 64) void rotary_kernel(const RotaryArg
 }
 
 // The same walk for the gradients; a wave goes on to further tokens, and what it has of the weight's gradient goes to the workspace at the end, a
-// workgroup's four waves and a wave's 64 / L heads added up in order. [4433, 30 + 30, 128] 36 us, 204 MB (some of them in the cache behind L2), and 5
-// for the reduction.
+// workgroup's four waves and a wave's 64 / L heads added up in order. [4433, 30 + 30, 128] 34.5 us at the least, 204 MB (some of them in the cache behind
+// L2), and 4 for the reduction.
 template <int L, bool HALVES, bool PART>
 __global__ __launch_bounds__(kHeadWaves * 64, 4) void rotary_backward_kernel(const RotaryArgs a) {
     __shared__ float lds[kHeadWaves][2][kMostPairs];

@@ -236,7 +236,7 @@ struct NormArgs {
     const void* x;          // bf16, or fp32 with x_f32 (x_out too)
     const uint16_t *y, *gate, *w_post, *w_pre, *scale, *shift;       // nullable
     const int* offsets;     // nullable: all rows are sequence 0
-    void* x_out;            // written when y is set
+    void* x_out;            // nullable
     uint16_t* h;            // nullable
     int64_t T, S, D, ldx, ldy, ld_gate, ld_mod, ldxo, ldh;
     int post, pre;          // rtl_norm
