@@ -100,8 +100,9 @@ def gated_backward(dH, X, W, P, kind):
 # ---- norms with gate, residual and modulation --------------------------------------------------------
 
 def normed(v, kind, eps):
-    """(norm(v), factor, error). Sums along a row are taken by 256 threads at most 16 values each and then over at most 16 waves: chains of 16 + 6 + 16 additions,
-    so that mean, mean square and with them the factor are off by 64 U of their magnitudes; a difference to the mean by that of the mean and its own."""
+    """(norm(v), factor, error). Sums along a row: 8 values of a thread (16 where a row has at most 8 waves), the lanes of a wave, at most 16 waves: chains of at
+    most 16 + 6 + 16 additions, so that mean, mean square and with them the factor are off by 64 U of their magnitudes; a difference to the mean by that of the
+    mean and its own."""
     if kind == "none":
         return v, torch.ones_like(v[:, :1]), torch.zeros_like(v)
     m = v.mean(1, keepdim=True) if kind == "layer" else torch.zeros_like(v[:, :1])
